@@ -258,6 +258,142 @@ int sdtw_normalized_backward(const sdtw_desc *desc, const float *x, const float 
                              size_t workspace_bytes, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------
+ * Operators of a model that is trained with Soft-DTW: a learned position prior on the costs and the
+ * loss on what the model answers at the positions the alignment names.
+ *
+ * Element types of their tensors (SDTW_INPUT_F16 and SDTW_INPUT_BF16 name the same types above).  All
+ * sums, maxima and exponentials are carried in 32 bits or more; results are rounded once, on store.
+ * Pointers need the alignment of one element only; rows may start anywhere.
+ */
+enum { SDTW_TYPE_F32 = 0, SDTW_TYPE_F16 = 1, SDTW_TYPE_BF16 = 2 };
+enum { SDTW_ID_I32 = 0, SDTW_ID_I64 = 1 };
+
+/*
+ * Distillation from a teacher's top logits.
+ * Row t of the student, logits z [vocab], is taught by row r of the teacher (r = teacher_row[t], or t), of which
+ * only `top` logits t_k and their tokens id_k are kept.  With a = z / temperature, p = softmax(a):
+ *   SDTW_DISTILL_RENORMALIZED  q_k = exp(t_k / temperature) / (the sum of these over the row's slots)
+ *   SDTW_DISTILL_TAIL          q_k = exp(t_k / temperature - teacher_lse[r]), where teacher_lse is the log-sum-exp of
+ *                              ALL the teacher's logits over the temperature; what is left, q_r = max(0, 1 - sum q_k), is
+ *                              held against the student's mass outside the kept tokens, p_r
+ *   loss[t] = sum_k q_k (log q_k - log p[id_k])  (+ q_r (log q_r - log p_r))
+ *   dlogits[t,v] = g[t] / temperature * (Q p_v - sum of q_k with id_k = v)     for a kept token, Q = sum q_k + q_r
+ *                  g[t] / temperature * p_v (Q - q_r / p_r)                    for the others
+ *   - A slot with a negative id is unused.  Slots of one id add up.  A row without a used slot, whose kept
+ *     teacher logits are all -inf (renormalised), or whose teacher_row is negative, has no target: loss 0,
+ *     gradient 0, whatever its logits are.
+ *   - A term with q = 0 is 0.  q > 0 on a token (or tail) to which the student gives no mass (logits -inf)
+ *     is a loss of +inf.  If the kept tokens are the whole vocabulary there is no tail term.
+ *   - An id >= vocab or a teacher_row >= teacher_rows cannot be seen on the host: loss and gradient of such a
+ *     row are NaN.  So are those of a row whose logits hold a NaN or +inf, or nothing but -inf.
+ * Any rows >= 0 (0: nothing is done).
+ */
+enum { SDTW_DISTILL_RENORMALIZED = 0, SDTW_DISTILL_TAIL = 1 };
+typedef struct sdtw_distill_desc {
+    int32_t rows;            /* rows of the student, >= 0 */
+    int32_t vocab;           /* >= 1, < 2^30 */
+    int32_t top;             /* slots per row of the teacher, 1..1024 */
+    int32_t teacher_rows;    /* rows of the teacher's arrays, >= 1 (>= rows without teacher_row) */
+    float temperature;       /* > 0, finite */
+    int32_t target;          /* SDTW_DISTILL_RENORMALIZED or SDTW_DISTILL_TAIL */
+    int32_t logit_type;      /* SDTW_TYPE_*: logits and dlogits */
+    int32_t teacher_type;    /* SDTW_TYPE_*: teacher_logits */
+    int32_t id_type;         /* SDTW_ID_*: teacher_ids */
+    uint32_t flags;          /* 0 */
+    int64_t logit_stride;    /* elements from one row of logits to the next, >= vocab */
+    int64_t grad_stride;     /* the same of dlogits */
+    int64_t teacher_stride;  /* the same of teacher_logits, >= top */
+    int64_t id_stride;       /* the same of teacher_ids, >= top */
+} sdtw_distill_desc;
+
+/* Floats per row that the forward call leaves for the backward call. */
+#define SDTW_DISTILL_STATS 8
+
+/* Bytes of workspace of sdtw_distill_forward and sdtw_distill_step; 0 if the descriptor is invalid.  Host only. */
+size_t sdtw_distill_workspace_bytes(const sdtw_distill_desc *desc);
+
+/*
+ *   logits [rows, vocab], teacher_logits [teacher_rows, top], teacher_ids [teacher_rows, top]: device, read only.
+ *   teacher_lse [teacher_rows]: device, float32, read only; NULL exactly when target is SDTW_DISTILL_RENORMALIZED.
+ *   teacher_row [rows]: device, int32, read only, or NULL (row t goes with the teacher's row t).
+ *   loss [rows]: device, float32, out.
+ *   stats [rows, SDTW_DISTILL_STATS]: device, float32, out: what sdtw_distill_backward needs of the forward pass.
+ */
+int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits,
+                         const void *teacher_ids, const float *teacher_lse, const int32_t *teacher_row, float *loss,
+                         float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Must follow sdtw_distill_forward with the same descriptor and inputs.
+ *   grad_loss [rows]: device, float32, upstream gradient of each row's loss, or NULL for ones.
+ *   dlogits [rows, vocab]: device, out, of logit_type.  It may be `logits` itself (with the same stride).
+ */
+int sdtw_distill_backward(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits,
+                          const void *teacher_ids, const float *teacher_lse, const int32_t *teacher_row,
+                          const float *grad_loss, const float *stats, void *dlogits, void *stream);
+
+/*
+ * Both in one call, for a caller who knows every row's upstream gradient beforehand (a mean over the rows):
+ * a row is read from memory once instead of twice where it fits on the chip.  Arguments as above.
+ */
+int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits,
+                      const void *teacher_ids, const float *teacher_lse, const int32_t *teacher_row,
+                      const float *grad_loss, float *loss, void *dlogits, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
+/*
+ * A learned relative position bias by buckets, on planes of scores or costs [B, H, N, M].
+ * Row i of sequence b stands at position i + offset_b, column j at position j; r = j - i - offset_b.
+ *   two-sided: d = |r|; the first half of the buckets serves r <= 0, the second r > 0 (n = buckets / 2 each)
+ *   one-sided: d = max(0, -r), n = buckets
+ * With e = n / 2 (rounded down), m = n - e: distances below e have a bucket each; bucket e + k (k < m) begins at the
+ * smallest d with d^m >= e^(m-k) max_distance^k - equal steps of the logarithm, in whole numbers - and the
+ * last one has no end.
+ *   forward   out[b,h,i,j] = in[b,h,i,j] + table[h, bucket(r)]
+ *   backward  dtable[h,u] = sum over b, i, j with bucket(r) = u of scale[b] * grad[b,h,i,j]
+ * With length vectors only the cells i < row_len[b], j < col_len[b] take part: the others are copied from `in`
+ * (0 without one) by the forward call and not looked at by the backward call.
+ * Any B, H, N, M >= 0.  A scalar or per-sequence offset serves rows that continue a cached sequence (N = 1: one new token).
+ */
+typedef struct sdtw_bias_desc {
+    int32_t B, H, N, M;          /* >= 0 */
+    int32_t buckets;             /* 2..256; two-sided: even, 4..256 */
+    int32_t max_distance;        /* > e, <= 2^24 */
+    int32_t two_sided;           /* 0 or 1 */
+    int32_t plane_type;          /* SDTW_TYPE_*: in, out, grad */
+    int32_t table_type;          /* SDTW_TYPE_*: table */
+    uint32_t flags;              /* 0 */
+    int64_t offset;              /* offset_b of every sequence, |offset| < 2^62; not used with `offsets` */
+    int64_t in_stride[3];        /* elements between sequences, heads, rows of in (forward) or grad (backward); >= 0 and
+                                    0 where all share one; columns are contiguous */
+    int64_t out_stride[3];       /* the same of out (forward only); different cells may not share memory */
+    int64_t table_stride[2];     /* elements between heads and between buckets of the table (forward only) */
+} sdtw_bias_desc;
+
+/* First distance of each of the n buckets of a side (host memory, n values); host only. */
+int sdtw_position_bias_starts(const sdtw_bias_desc *desc, int32_t *starts);
+
+/*
+ *   table [H, buckets]: device, read only.  in [B,H,N,M]: device, read only, or NULL for zeros.
+ *   offsets [B], row_len [B], col_len [B]: device, int32, read only, or NULL.  Lengths are clamped to [0, N], [0, M].
+ *   out [B,H,N,M]: device, out; it may be `in` itself (with the same strides).
+ */
+int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, const void *in, const int32_t *offsets,
+                               const int32_t *row_len, const int32_t *col_len, void *out, void *stream);
+
+/* Bytes of workspace of sdtw_position_bias_backward; 0 if the descriptor is invalid.  Host only. */
+size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc);
+
+/*
+ *   grad [B,H,N,M]: device, read only (in_stride).  scale [B]: device, float32, or NULL for ones.
+ *   dtable [H, buckets]: device, float32, contiguous, out.  The same inputs give the same bits: no atomics.
+ */
+int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, const float *scale, const int32_t *offsets,
+                                const int32_t *row_len, const int32_t *col_len, float *dtable, void *workspace,
+                                size_t workspace_bytes, void *stream);
+
+/*
  * Reads the device-side status word of a workspace: waits for `stream`, copies 4 bytes to the
  * host.  *device_status receives SDTW_OK, SDTW_ERR_STATE or SDTW_ERR_TIMEOUT.  When a backward
  * call found SDTW_ERR_STATE its dx, dy and E outputs are filled with NaN.

@@ -6,6 +6,8 @@ Importing the package does not load the library; the first call does, and it rai
 the library has not been built.
 """
 from .binding import (  # noqa: F401
+    DISTILL_RENORMALIZED,
+    DISTILL_TAIL,
     FLAG_DENSE_E,
     FLAG_MIN_MEMORY,
     FLAG_VALUE_ONLY,
@@ -20,12 +22,19 @@ from .binding import (  # noqa: F401
     sdtw_backward_ragged,
     sdtw_barycenter_step,
     sdtw_barycenter_workspace_bytes,
+    sdtw_distill_backward,
+    sdtw_distill_forward,
+    sdtw_distill_step,
+    sdtw_distill_workspace_bytes,
     sdtw_forward,
     sdtw_forward_half,
     sdtw_forward_ragged,
     sdtw_normalized_backward,
     sdtw_normalized_forward,
     sdtw_normalized_workspace_bytes,
+    sdtw_position_bias_backward,
+    sdtw_position_bias_forward,
+    sdtw_position_bias_starts,
     sdtw_status_string,
     sdtw_version,
     sdtw_workspace_bytes,

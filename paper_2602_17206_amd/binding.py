@@ -52,6 +52,27 @@ class BaryDesc(ctypes.Structure):
     ]
 
 
+class DistillDesc(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("top", ctypes.c_int32), ("teacher_rows", ctypes.c_int32),
+        ("temperature", ctypes.c_float), ("target", ctypes.c_int32),
+        ("logit_type", ctypes.c_int32), ("teacher_type", ctypes.c_int32), ("id_type", ctypes.c_int32),
+        ("flags", ctypes.c_uint32),
+        ("logit_stride", ctypes.c_int64), ("grad_stride", ctypes.c_int64), ("teacher_stride", ctypes.c_int64),
+        ("id_stride", ctypes.c_int64),
+    ]
+
+
+class BiasDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("N", ctypes.c_int32), ("M", ctypes.c_int32),
+        ("buckets", ctypes.c_int32), ("max_distance", ctypes.c_int32), ("two_sided", ctypes.c_int32),
+        ("plane_type", ctypes.c_int32), ("table_type", ctypes.c_int32), ("flags", ctypes.c_uint32),
+        ("offset", ctypes.c_int64), ("in_stride", ctypes.c_int64 * 3), ("out_stride", ctypes.c_int64 * 3),
+        ("table_stride", ctypes.c_int64 * 2),
+    ]
+
+
 EXPORTED_SYMBOLS = (
     "sdtw_version", "sdtw_status_string", "sdtw_workspace_bytes", "sdtw_forward", "sdtw_backward",
     "sdtw_barycenter_workspace_bytes", "sdtw_barycenter_step", "sdtw_workspace_status",
@@ -61,6 +82,9 @@ EXPORTED_SYMBOLS = (
     "sdtw_debug_profile", "sdtw_debug_profile_read", "sdtw_debug_force_workgroup_shape",
     "sdtw_debug_rate_probe", "sdtw_forward_static_scratch", "sdtw_debug_set_pool_blocks",
     "sdtw_half_workspace_bytes", "sdtw_forward_half", "sdtw_backward_half",
+    "sdtw_distill_workspace_bytes", "sdtw_distill_forward", "sdtw_distill_backward", "sdtw_distill_step",
+    "sdtw_position_bias_starts", "sdtw_position_bias_forward", "sdtw_position_bias_workspace_bytes",
+    "sdtw_position_bias_backward",
 )
 
 
@@ -134,6 +158,23 @@ def load_library():
     lib.sdtw_debug_set_pool_blocks.argtypes = [ctypes.c_longlong]
     lib.sdtw_debug_rate_probe.restype = i32
     lib.sdtw_debug_rate_probe.argtypes = [i32, i32, i32, i32, vp, sz, ctypes.POINTER(ctypes.c_float), vp]
+    pd, pb = ctypes.POINTER(DistillDesc), ctypes.POINTER(BiasDesc)
+    lib.sdtw_distill_workspace_bytes.restype = sz
+    lib.sdtw_distill_workspace_bytes.argtypes = [pd]
+    lib.sdtw_distill_forward.restype = i32
+    lib.sdtw_distill_forward.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sdtw_distill_backward.restype = i32
+    lib.sdtw_distill_backward.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    lib.sdtw_distill_step.restype = i32
+    lib.sdtw_distill_step.argtypes = [pd, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sdtw_position_bias_starts.restype = i32
+    lib.sdtw_position_bias_starts.argtypes = [pb, vp]
+    lib.sdtw_position_bias_forward.restype = i32
+    lib.sdtw_position_bias_forward.argtypes = [pb, vp, vp, vp, vp, vp, vp, vp]
+    lib.sdtw_position_bias_workspace_bytes.restype = sz
+    lib.sdtw_position_bias_workspace_bytes.argtypes = [pb]
+    lib.sdtw_position_bias_backward.restype = i32
+    lib.sdtw_position_bias_backward.argtypes = [pb, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -558,3 +599,224 @@ def sdtw_backward_half(desc, workspace, grad_value=None, want_dx=True, want_dy=T
     if rc != 0:
         raise SdtwError(rc, "sdtw_backward_half")
     return dx, dy, E
+
+
+# ---------------------------------------------------------------- operators of a model trained with Soft-DTW
+
+TYPE_F32, TYPE_F16, TYPE_BF16 = 0, 1, 2
+ID_I32, ID_I64 = 0, 1
+DISTILL_RENORMALIZED, DISTILL_TAIL = 0, 1
+DISTILL_STATS = 8
+
+
+def _type_of(t, name):
+    import torch
+
+    kind = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}.get(t.dtype)
+    if kind is None:
+        raise ValueError("%s must be float32, float16 or bfloat16" % name)
+    return kind
+
+
+def _rows_ptr(t, shape, device, name, dtype=None):
+    """Device pointer and row stride of a matrix whose rows are contiguous."""
+    if t.device != device or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
+        raise ValueError("%s must be%s [%s] on %s" % (name, " %s" % dtype if dtype else "", ", ".join(map(str, shape)), device))
+    if (t.stride(1) != 1 and shape[1] > 1) or (t.stride(0) < shape[1] and shape[0] > 1):
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return t.data_ptr(), max(t.stride(0), shape[1])
+
+
+def _vector_ptr(t, n, device, dtype, name):
+    if t is None:
+        return None
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s [%d] on %s" % (name, dtype, n, device))
+    return t.data_ptr()
+
+
+def _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row):
+    """(descriptor, the pointers every distillation call begins with)"""
+    import torch
+
+    if logits.dim() != 2 or teacher_logits.dim() != 2 or not logits.is_cuda:
+        raise ValueError("logits [T, V] and teacher_logits [R, K] must be device matrices")
+    dev, (T, V), (R, K) = logits.device, logits.shape, teacher_logits.shape
+    if teacher_ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError("teacher_ids must be int32 or int64")
+    zp, zs = _rows_ptr(logits, (T, V), dev, "logits")
+    tp, ts = _rows_ptr(teacher_logits, (R, K), dev, "teacher_logits")
+    ip, ids = _rows_ptr(teacher_ids, (R, K), dev, "teacher_ids")
+    desc = DistillDesc(T, V, K, R, float(temperature), DISTILL_RENORMALIZED if teacher_lse is None else DISTILL_TAIL,
+                       _type_of(logits, "logits"), _type_of(teacher_logits, "teacher_logits"),
+                       ID_I64 if teacher_ids.dtype == torch.int64 else ID_I32, 0, zs, V, ts, ids)
+    return desc, (zp, tp, ip, _vector_ptr(teacher_lse, R, dev, torch.float32, "teacher_lse"),
+                  _vector_ptr(teacher_row, T, dev, torch.int32, "teacher_row"))
+
+
+def _distill_grad_out(desc, logits, dlogits):
+    """(dlogits, its pointer), with its row stride in the descriptor"""
+    import torch
+
+    if dlogits is None:
+        dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    ptr, desc.grad_stride = _rows_ptr(dlogits, logits.shape, logits.device, "dlogits", logits.dtype)
+    return dlogits, ptr
+
+
+def _operator_workspace(nbytes, workspace, device, where):
+    if workspace is None:
+        if nbytes == 0:
+            raise SdtwError(STATUS_INVALID_ARG, where)
+        workspace = Workspace(nbytes, device)
+    return workspace
+
+
+def sdtw_distill_workspace_bytes(desc):
+    return int(load_library().sdtw_distill_workspace_bytes(ctypes.byref(desc)))
+
+
+def sdtw_distill_forward(logits, teacher_logits, teacher_ids, temperature=1.0, teacher_lse=None, teacher_row=None,
+                         loss=None, stats=None, workspace=None, stream=None):
+    """Divergence of every row of ``logits`` [T, V] from the teacher's top logits [R, K] at the tokens ``teacher_ids``
+    [R, K] (negative: unused).  Row t goes with the teacher's row ``teacher_row[t]`` (int32; negative: no target), or t.
+    The teacher's probabilities are renormalised over the kept tokens, or, with ``teacher_lse`` [R] (float32, the log-sum-exp
+    of all of its logits over the temperature), the rest of its mass is held against the student's outside the kept tokens.
+    Returns (loss [T] float32, stats); keep stats for :func:`sdtw_distill_backward`."""
+    import torch
+
+    lib = load_library()
+    desc, args = _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row)
+    dev = logits.device
+    workspace = _operator_workspace(lib.sdtw_distill_workspace_bytes(ctypes.byref(desc)), workspace, dev, "sdtw_distill_forward")
+    if loss is None:
+        loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
+    if stats is None:
+        stats = torch.empty((desc.rows, DISTILL_STATS), dtype=torch.float32, device=dev)
+    rc = lib.sdtw_distill_forward(ctypes.byref(desc), *args, _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"),
+                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), workspace.ptr,
+                                  workspace.nbytes, _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_distill_forward")
+    return loss, stats
+
+
+def sdtw_distill_backward(logits, teacher_logits, teacher_ids, stats, grad_loss=None, temperature=1.0, teacher_lse=None,
+                          teacher_row=None, dlogits=None, stream=None):
+    """Gradient [T, V] (of the logits' type) of the losses :func:`sdtw_distill_forward` produced, weighted by ``grad_loss``
+    [T] (float32; None: ones).  ``dlogits`` may be ``logits`` itself."""
+    import torch
+
+    lib = load_library()
+    desc, args = _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row)
+    dev = logits.device
+    dlogits, dp = _distill_grad_out(desc, logits, dlogits)
+    rc = lib.sdtw_distill_backward(ctypes.byref(desc), *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
+                                   _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), dp, _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_distill_backward")
+    return dlogits
+
+
+def sdtw_distill_step(logits, teacher_logits, teacher_ids, grad_loss=None, temperature=1.0, teacher_lse=None,
+                      teacher_row=None, loss=None, dlogits=None, workspace=None, stream=None):
+    """Loss and gradient in one call, for a caller who knows ``grad_loss`` beforehand.  Returns (loss [T], dlogits [T, V])."""
+    import torch
+
+    lib = load_library()
+    desc, args = _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row)
+    dev = logits.device
+    workspace = _operator_workspace(lib.sdtw_distill_workspace_bytes(ctypes.byref(desc)), workspace, dev, "sdtw_distill_step")
+    if loss is None:
+        loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
+    dlogits, dp = _distill_grad_out(desc, logits, dlogits)
+    rc = lib.sdtw_distill_step(ctypes.byref(desc), *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
+                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, workspace.ptr, workspace.nbytes,
+                               _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_distill_step")
+    return loss, dlogits
+
+
+def _bias_args(plane, shape, dtype, device, buckets, max_distance, two_sided, offset, row_len, col_len, name):
+    """(descriptor without output and table, pointers of offsets, row_len, col_len)"""
+    import torch
+
+    B, H, N, M = shape
+    desc = BiasDesc(B, H, N, M, int(buckets), int(max_distance), 1 if two_sided else 0, 0, 0, 0)
+    if plane is not None:
+        if plane.dim() != 4 or not plane.is_cuda:
+            raise ValueError("%s must be a device tensor [B, H, N, M]" % name)
+        if M > 1 and plane.stride(3) != 1:
+            raise ValueError("%s must have contiguous rows" % name)
+        desc.in_stride[:] = [plane.stride(0), plane.stride(1), plane.stride(2)]
+    offsets = None
+    if torch.is_tensor(offset):
+        offsets = _vector_ptr(offset, B, device, torch.int32, "offset")
+    else:
+        desc.offset = int(offset)
+    return desc, (offsets, _vector_ptr(row_len, B, device, torch.int32, "row_len"),
+                  _vector_ptr(col_len, B, device, torch.int32, "col_len"))
+
+
+def sdtw_position_bias_starts(buckets, max_distance=128, two_sided=True):
+    """First distance of each bucket of a side (host)."""
+    desc = BiasDesc(1, 1, 1, 1, int(buckets), int(max_distance), 1 if two_sided else 0, 0, 0, 0)
+    starts = (ctypes.c_int32 * max(1, int(buckets)))()
+    rc = load_library().sdtw_position_bias_starts(ctypes.byref(desc), starts)
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_position_bias_starts")
+    return list(starts)[:buckets // 2 if two_sided else buckets]
+
+
+def sdtw_position_bias_forward(table, plane=None, max_distance=128, two_sided=True, offset=0, row_len=None, col_len=None,
+                               out=None, stream=None):
+    """plane [B, H, N, M] + table[h, bucket(j - i - offset)], ``table`` [H, buckets] of any strides (an embedding's transpose).
+    ``offset``: a number, or int32 [B]: where every sequence's row 0 stands.  ``row_len``, ``col_len`` [B] int32: cells beyond
+    keep what ``plane`` holds.  Without ``plane`` the bias alone goes to ``out``.  ``out`` may be ``plane`` itself."""
+    import torch
+
+    lib = load_library()
+    if plane is None and out is None:
+        raise ValueError("one of plane and out is needed")
+    like = plane if plane is not None else out
+    if like.dim() != 4 or table.dim() != 2 or not like.is_cuda or table.device != like.device or table.shape[0] != like.shape[1]:
+        raise ValueError("plane [B, H, N, M] and table [H, buckets] must be on one device")
+    if out is None:
+        out = torch.empty(plane.shape, dtype=plane.dtype, device=plane.device)
+    elif out.shape != like.shape or out.dtype != like.dtype or out.device != like.device or (out.shape[3] > 1 and out.stride(3) != 1):
+        raise ValueError("out must have the shape and type of plane and contiguous rows")
+    desc, args = _bias_args(plane, like.shape, like.dtype, like.device, table.shape[1], max_distance, two_sided, offset, row_len,
+                            col_len, "plane")
+    desc.plane_type, desc.table_type = _type_of(like, "plane"), _type_of(table, "table")
+    desc.out_stride[:] = [out.stride(0), out.stride(1), out.stride(2)]
+    desc.table_stride[:] = [table.stride(0), table.stride(1)]
+    rc = lib.sdtw_position_bias_forward(ctypes.byref(desc), table.data_ptr(), None if plane is None else plane.data_ptr(), *args,
+                                        out.data_ptr(), _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_position_bias_forward")
+    return out
+
+
+def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True, offset=0, row_len=None, col_len=None, scale=None,
+                                dtable=None, workspace=None, stream=None):
+    """Gradient [H, buckets] (float32) of the table from ``grad`` [B, H, N, M] of the planes (any strides, broadcast ones too),
+    each sequence's times ``scale[b]`` (float32 [B]; None: ones)."""
+    import torch
+
+    lib = load_library()
+    if grad.dim() != 4 or not grad.is_cuda:
+        raise ValueError("grad must be a device tensor [B, H, N, M]")
+    dev = grad.device
+    desc, args = _bias_args(grad, grad.shape, grad.dtype, dev, buckets, max_distance, two_sided, offset, row_len, col_len, "grad")
+    desc.plane_type = _type_of(grad, "grad")
+    workspace = _operator_workspace(lib.sdtw_position_bias_workspace_bytes(ctypes.byref(desc)), workspace, dev,
+                                    "sdtw_position_bias_backward")
+    if dtable is None:
+        dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
+    rc = lib.sdtw_position_bias_backward(ctypes.byref(desc), grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"),
+                                         *args, _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable"), workspace.ptr,
+                                         workspace.nbytes, _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_position_bias_backward")
+    return dtable

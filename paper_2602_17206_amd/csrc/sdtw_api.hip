@@ -15,8 +15,29 @@
 #include "../../include/sdtw.h"
 #include "kernels.h"
 #include "dp_kernels.h"
+#include "host_common.h"
 #include "layout.h"
 #include "rate_probe.h"
+
+namespace sdtw {
+
+struct ProfEntry { const char *name; hipEvent_t a, b; };
+static bool g_profile = false;
+static std::vector<ProfEntry> g_prof;
+
+bool profile_begin(const char *name, hipStream_t st)
+{
+    if (!g_profile) return false;
+    ProfEntry e{name, nullptr, nullptr};
+    if (hipEventCreate(&e.a) != hipSuccess || hipEventCreate(&e.b) != hipSuccess) return false;
+    (void)hipEventRecord(e.a, st);
+    g_prof.push_back(e);
+    return true;
+}
+
+void profile_end(hipStream_t st) { (void)hipEventRecord(g_prof.back().b, st); }
+
+}  // namespace sdtw
 
 namespace {
 
@@ -27,26 +48,6 @@ using namespace sdtw;
 std::atomic<uint32_t> g_spin_limit{1u << 23};  // ~10 s of polling before a band gives up
 std::atomic<int> g_force_slots{0};             // 0 = choose by problem size, 1, 2 or 4 = force that workgroup shape
 std::atomic<long long> g_pool_blocks{-1};      // >= 0: capacity of the compact-E block pool (at most the layout's), to force an overflow
-
-// Optional per-kernel timing (test/benchmark hook): when switched on, every kernel launch of the
-// library is bracketed by two HIP events on the caller's stream.
-struct ProfEntry { const char *name; hipEvent_t a, b; };
-bool g_profile = false;
-std::vector<ProfEntry> g_prof;
-
-struct ProfScope {
-    hipStream_t st;
-    bool on;
-    ProfScope(const char *name, hipStream_t s) : st(s), on(g_profile)
-    {
-        if (!on) return;
-        ProfEntry e{name, nullptr, nullptr};
-        if (hipEventCreate(&e.a) != hipSuccess || hipEventCreate(&e.b) != hipSuccess) { on = false; return; }
-        (void)hipEventRecord(e.a, st);
-        g_prof.push_back(e);
-    }
-    ~ProfScope() { if (on) (void)hipEventRecord(g_prof.back().b, st); }
-};
 
 bool desc_ok(const sdtw_desc *d, int *why)
 {
@@ -255,14 +256,6 @@ void launch_dp(const sdtw_desc *d, const Layout &L, const Params &p, float *valu
         default: return launch_dp_kch<FWD, 0>(d, L, p, value, st, grad);
     }
 }
-
-int check_ws(const void *ws, size_t bytes, size_t need)
-{
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0 || bytes < need) return SDTW_ERR_WORKSPACE;
-    return SDTW_OK;
-}
-
-inline int hip_ok() { return hipGetLastError() == hipSuccess ? SDTW_OK : SDTW_ERR_HIP; }
 
 unsigned fill_grid(size_t n) { size_t g = (n + 255) / 256; return (unsigned)(g < 1 ? 1 : (g > 4096 ? 4096 : g)); }
 

@@ -1,0 +1,415 @@
+// C entry points of the operators beside Soft-DTW (declared in include/sdtw.h): distillation from a teacher's top
+// logits and the learned relative position bias.  Argument checks, workspace carving and kernel launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "distill_kernels.h"
+#include "host_common.h"
+#include "layout.h"
+#include "position_bias_kernels.h"
+
+namespace {
+
+using namespace sdtw;
+
+bool type_ok(int t) { return t == SDTW_TYPE_F32 || t == SDTW_TYPE_F16 || t == SDTW_TYPE_BF16; }
+
+// Calls f with a value of the element type.
+template <typename F> void with_type(int type, F f)
+{
+    if (type == SDTW_TYPE_F32)
+        f(float{});
+    else if (type == SDTW_TYPE_F16)
+        f(_Float16{});
+    else
+        f(Bf16{});
+}
+
+// ---------------------------------------------------------------- distillation
+
+struct DistillPlan {
+    int32_t slices, slice_cols, threads;       // forward
+    int32_t back_slices, back_cols;            // backward
+    size_t off_stats, off_partial, total;
+};
+
+bool distill_ok(const sdtw_distill_desc *d)
+{
+    if (!d) return false;
+    if (d->rows < 0 || d->vocab < 1 || d->vocab >= 1 << 30 || d->top < 1 || d->top > kMaxTop || d->teacher_rows < 1) return false;
+    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(1.0f / d->temperature)) return false;
+    if (d->target != SDTW_DISTILL_RENORMALIZED && d->target != SDTW_DISTILL_TAIL) return false;
+    if (!type_ok(d->logit_type) || !type_ok(d->teacher_type)) return false;
+    if (d->id_type != SDTW_ID_I32 && d->id_type != SDTW_ID_I64) return false;
+    if (d->flags != 0) return false;
+    if (d->logit_stride < d->vocab || d->grad_stride < d->vocab || d->teacher_stride < d->top || d->id_stride < d->top) return false;
+    const int64_t most = (int64_t)1 << 60;  // no address overflows 64 bits
+    const int64_t rows = std::max<int64_t>(1, std::max(d->rows, d->teacher_rows));
+    return d->logit_stride <= most / rows && d->grad_stride <= most / rows && d->teacher_stride <= most / rows && d->id_stride <= most / rows;
+}
+
+// Columns of a slice when `rows` rows are shared by about `want` workgroups, none with fewer than `least` columns.
+int32_t slice_columns(int64_t rows, int64_t vocab, int64_t want, int64_t least, int64_t most)
+{
+    const int64_t per_row = std::max<int64_t>(1, (want + rows - 1) / rows);
+    int64_t cols = (vocab + per_row - 1) / per_row;
+    cols = std::min(std::max(cols, least), most);
+    return (int32_t)((cols + 7) / 8 * 8);
+}
+
+DistillPlan distill_plan(const sdtw_distill_desc *d)
+{
+    DistillPlan P{};
+    const int64_t rows = std::max(d->rows, 1);
+    // (a slice's marks are one bit a column in LDS: at most 32 KB)
+    P.slice_cols = slice_columns(rows, d->vocab, 512, 4096, 1 << 18);
+    P.slices = (d->vocab + P.slice_cols - 1) / P.slice_cols;
+    P.threads = P.slice_cols >= 16384 ? 512 : 256;
+    P.back_cols = slice_columns(rows, d->vocab, 1024, 4096, 1 << 18);
+    P.back_slices = (d->vocab + P.back_cols - 1) / P.back_cols;
+    size_t o = 0;
+    P.off_stats = o;
+    o = align_up(o + (size_t)rows * sizeof(RowStats), 256);
+    P.off_partial = o;
+    if (P.slices > 1) o = align_up(o + (size_t)rows * P.slices * sizeof(float4), 256);
+    P.total = o;
+    return P;
+}
+
+bool distill_args_ok(const sdtw_distill_desc *d, const void *logits, const void *teacher_logits, const void *teacher_ids,
+                     const float *teacher_lse, const int32_t *teacher_row)
+{
+    if (!logits || !teacher_logits || !teacher_ids) return false;
+    if ((d->target == SDTW_DISTILL_TAIL) != (teacher_lse != nullptr)) return false;
+    return teacher_row || d->teacher_rows >= d->rows;
+}
+
+DistillParams distill_params(const sdtw_distill_desc *d, const void *logits, const void *teacher_logits, const void *teacher_ids,
+                             const float *teacher_lse, const int32_t *teacher_row)
+{
+    DistillParams p{};
+    p.rows = d->rows; p.vocab = d->vocab; p.top = d->top; p.teacher_rows = d->teacher_rows;
+    p.teacher_type = d->teacher_type; p.id64 = d->id_type == SDTW_ID_I64; p.tail = d->target == SDTW_DISTILL_TAIL;
+    p.inv_temperature_d = 1.0 / (double)d->temperature;
+    p.inv_temperature = (float)p.inv_temperature_d;
+    p.scale2 = (float)(1.4426950408889634 * p.inv_temperature_d);
+    p.logit_stride = d->logit_stride; p.grad_stride = d->grad_stride;
+    p.teacher_stride = d->teacher_stride; p.id_stride = d->id_stride;
+    p.logits = logits; p.teacher_logits = teacher_logits; p.teacher_ids = teacher_ids;
+    p.teacher_lse = teacher_lse; p.teacher_row = teacher_row;
+    return p;
+}
+
+void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, hipStream_t st)
+{
+    p.slices = P.slices;
+    p.slice_cols = P.slice_cols;
+    const size_t slots = (size_t)p.top * 12;
+    const size_t marks = ((size_t)std::min(p.vocab, P.slice_cols) + 31) / 32 * 4;
+    {
+        ProfScope ps("distill_forward", st);
+        with_type(type, [&](auto t) {
+            distill_forward_kernel<decltype(t)><<<(unsigned)(p.rows * (int64_t)P.slices), P.threads, slots + marks, st>>>(p);
+        });
+    }
+    if (P.slices > 1) {
+        ProfScope ps("distill_join", st);
+        with_type(type, [&](auto t) { distill_join_kernel<decltype(t)><<<(unsigned)p.rows, 64, slots, st>>>(p); });
+    }
+}
+
+void launch_distill_backward(const DistillPlan &P, DistillParams p, int type, hipStream_t st)
+{
+    p.slices = P.back_slices;
+    p.slice_cols = P.back_cols;
+    ProfScope ps("distill_backward", st);
+    with_type(type, [&](auto t) {
+        distill_backward_kernel<decltype(t)><<<(unsigned)(p.rows * (int64_t)P.back_slices), 256, 0, st>>>(p);
+    });
+}
+
+bool distill_grid_ok(const sdtw_distill_desc *d, const DistillPlan &P)
+{
+    return (int64_t)d->rows * std::max(P.slices, P.back_slices) <= 0x7fffffff;
+}
+
+// ---------------------------------------------------------------- position bias
+
+bool power_at_least(int d, int m, int e, int k, int D);
+
+// First distances of the buckets from e on: the smallest d with d^m >= e^(m-k) D^k.
+void bucket_starts(int e, int m, int D, int32_t *start)
+{
+    for (int k = 0; k < m; ++k) {
+        const double x = (double)e * std::pow((double)D / e, (double)k / m);
+        const double near = std::nearbyint(x);
+        // The power is good to about 1e-13 of itself; nearer than that to a whole number the whole numbers decide.
+        if (std::fabs(x - near) < 1e-9 * x)
+            start[k] = (int32_t)near + (power_at_least((int)near, m, e, k, D) ? 0 : 1);
+        else
+            start[k] = (int32_t)std::ceil(x);
+    }
+}
+
+// d^m >= e^(m-k) D^k in whole numbers of as many 32-bit digits as it takes (m <= 128 factors below 2^25).
+bool power_at_least(int d, int m, int e, int k, int D)
+{
+    constexpr int kDigits = 128;
+    uint32_t a[kDigits] = {1}, b[kDigits] = {1};
+    auto times = [](uint32_t *x, uint32_t f) {
+        uint64_t carry = 0;
+        for (int i = 0; i < kDigits; ++i) {
+            carry += (uint64_t)x[i] * f;
+            x[i] = (uint32_t)carry;
+            carry >>= 32;
+        }
+    };
+    for (int i = 0; i < m; ++i) {
+        times(a, (uint32_t)d);
+        times(b, (uint32_t)(i < k ? D : e));
+    }
+    for (int i = kDigits - 1; i >= 0; --i)
+        if (a[i] != b[i]) return a[i] > b[i];
+    return true;
+}
+
+bool bias_ok(const sdtw_bias_desc *d)
+{
+    if (!d) return false;
+    if (d->B < 0 || d->H < 0 || d->N < 0 || d->M < 0) return false;
+    if (d->two_sided != 0 && d->two_sided != 1) return false;
+    if (d->buckets < (d->two_sided ? 4 : 2) || d->buckets > kMaxBuckets || (d->two_sided && d->buckets % 2 != 0)) return false;
+    const int n = d->two_sided ? d->buckets / 2 : d->buckets;
+    if (d->max_distance <= n / 2 || d->max_distance > 1 << 24) return false;
+    if (!type_ok(d->plane_type) || !type_ok(d->table_type) || d->flags != 0) return false;
+    if (d->N >= 1 << 30 || d->M >= 1 << 30) return false;
+    if (d->offset >= (int64_t)1 << 62 || d->offset <= -((int64_t)1 << 62)) return false;
+    const int64_t most = (int64_t)1 << 59, size[3] = {d->B, d->H, d->N};
+    for (int i = 0; i < 3; ++i)
+        if (d->in_stride[i] < 0 || d->out_stride[i] < 0 || d->in_stride[i] > most / std::max<int64_t>(1, size[i]) ||
+            d->out_stride[i] > most / std::max<int64_t>(1, size[i]))
+            return false;
+    return true;
+}
+
+// Whether different cells of `out` have different places: sorted by stride, each dimension steps over the ones inside it.
+bool disjoint(const sdtw_bias_desc *d)
+{
+    struct Dim { int64_t size, stride; } dim[3] = {{d->B, d->out_stride[0]}, {d->H, d->out_stride[1]}, {d->N, d->out_stride[2]}};
+    std::sort(dim, dim + 3, [](const Dim &a, const Dim &b) { return a.stride < b.stride; });
+    int64_t span = d->M;  // elements from the first cell of what lies inside to behind its last one
+    for (const Dim &x : dim) {
+        if (x.size <= 1) continue;
+        if (x.stride < span) return false;
+        span += (x.size - 1) * x.stride;
+    }
+    return true;
+}
+
+BucketRule bucket_rule(const sdtw_bias_desc *d)
+{
+    BucketRule r{};
+    r.two_sided = d->two_sided;
+    r.n = d->two_sided ? d->buckets / 2 : d->buckets;
+    r.e = r.n / 2;
+    r.m = r.n - r.e;
+    bucket_starts(r.e, r.m, d->max_distance, r.start);
+    return r;
+}
+
+BiasParams bias_params(const sdtw_bias_desc *d, const void *in, const int32_t *offsets, const int32_t *row_len, const int32_t *col_len)
+{
+    BiasParams p{};
+    p.B = d->B; p.H = d->H; p.N = d->N; p.M = d->M;
+    p.buckets = d->buckets; p.table_type = d->table_type;
+    p.offset = d->offset;
+    for (int i = 0; i < 3; ++i) { p.in_stride[i] = d->in_stride[i]; p.out_stride[i] = d->out_stride[i]; }
+    p.table_stride[0] = d->table_stride[0]; p.table_stride[1] = d->table_stride[1];
+    p.in = in;
+    p.offsets = offsets; p.row_len = row_len; p.col_len = col_len;
+    return p;
+}
+
+int width_of(int type) { return type == SDTW_TYPE_F32 ? 4 : 8; }
+
+// How the backward pass is split: strips of diagonals, then the batch, then the way down a strip.
+struct BiasPlan { int64_t strips, first_col, batch_per_part, batch_parts, steps_per_part, step_parts, parts; };
+
+BiasPlan bias_plan(const sdtw_bias_desc *d)
+{
+    BiasPlan P{};
+    if (d->B == 0 || d->H == 0 || d->N == 0 || d->M == 0) return P;
+    const int64_t steps = (d->N + 7) / 8, width = 64 * width_of(d->plane_type), want = 2048;
+    P.first_col = -8 * (steps - 1);
+    P.strips = (d->M - P.first_col + width - 1) / width;
+    const int64_t units = P.strips * d->H;
+    P.batch_parts = std::min<int64_t>(d->B, (want + units - 1) / units);
+    P.batch_per_part = (d->B + P.batch_parts - 1) / P.batch_parts;
+    P.batch_parts = (d->B + P.batch_per_part - 1) / P.batch_per_part;
+    P.step_parts = std::max<int64_t>(1, std::min<int64_t>(steps / 16, (want + units * P.batch_parts - 1) / (units * P.batch_parts)));
+    P.steps_per_part = (steps + P.step_parts - 1) / P.step_parts;
+    P.step_parts = (steps + P.steps_per_part - 1) / P.steps_per_part;
+    P.parts = P.strips * P.batch_parts * P.step_parts;
+    return P;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdtw_distill_workspace_bytes(const sdtw_distill_desc *desc)
+{
+    if (!distill_ok(desc)) return 0;
+    return distill_plan(desc).total;
+}
+
+int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits, const void *teacher_ids,
+                         const float *teacher_lse, const int32_t *teacher_row, float *loss, float *stats, void *workspace,
+                         size_t workspace_bytes, void *stream)
+{
+    if (!distill_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->rows == 0) return SDTW_OK;
+    if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !loss || !stats) return SDTW_ERR_INVALID_ARG;
+    const DistillPlan P = distill_plan(desc);
+    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    (void)hipGetLastError();  // what an earlier, unrelated call left behind is not this call's error
+    DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
+    p.loss = loss;
+    p.stats = reinterpret_cast<RowStats *>(stats);
+    p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
+    launch_distill_forward(P, p, desc->logit_type, static_cast<hipStream_t>(stream));
+    return hip_ok();
+}
+
+int sdtw_distill_backward(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits, const void *teacher_ids,
+                          const float *teacher_lse, const int32_t *teacher_row, const float *grad_loss, const float *stats,
+                          void *dlogits, void *stream)
+{
+    if (!distill_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->rows == 0) return SDTW_OK;
+    if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !stats || !dlogits) return SDTW_ERR_INVALID_ARG;
+    if (dlogits == logits && desc->grad_stride != desc->logit_stride) return SDTW_ERR_INVALID_ARG;
+    const DistillPlan P = distill_plan(desc);
+    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
+    p.grad_loss = grad_loss;
+    p.stats = reinterpret_cast<RowStats *>(const_cast<float *>(stats));
+    p.dlogits = dlogits;
+    launch_distill_backward(P, p, desc->logit_type, static_cast<hipStream_t>(stream));
+    return hip_ok();
+}
+
+int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const void *teacher_logits, const void *teacher_ids,
+                      const float *teacher_lse, const int32_t *teacher_row, const float *grad_loss, float *loss, void *dlogits,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!distill_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->rows == 0) return SDTW_OK;
+    if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !loss || !dlogits) return SDTW_ERR_INVALID_ARG;
+    if (dlogits == logits && desc->grad_stride != desc->logit_stride) return SDTW_ERR_INVALID_ARG;
+    const DistillPlan P = distill_plan(desc);
+    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    (void)hipGetLastError();
+    DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
+    p.loss = loss;
+    p.grad_loss = grad_loss;
+    p.dlogits = dlogits;
+    p.stats = reinterpret_cast<RowStats *>(static_cast<char *>(workspace) + P.off_stats);
+    p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    launch_distill_forward(P, p, desc->logit_type, st);
+    launch_distill_backward(P, p, desc->logit_type, st);
+    return hip_ok();
+}
+
+int sdtw_position_bias_starts(const sdtw_bias_desc *desc, int32_t *starts)
+{
+    if (!bias_ok(desc) || !starts) return SDTW_ERR_INVALID_ARG;
+    const BucketRule r = bucket_rule(desc);
+    for (int u = 0; u < r.n; ++u) starts[u] = u < r.e ? u : r.start[u - r.e];
+    return SDTW_OK;
+}
+
+int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, const void *in, const int32_t *offsets,
+                               const int32_t *row_len, const int32_t *col_len, void *out, void *stream)
+{
+    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->B == 0 || desc->H == 0 || desc->N == 0 || desc->M == 0) return SDTW_OK;
+    if (!table || !out || !disjoint(desc)) return SDTW_ERR_INVALID_ARG;
+    if (in == out)  // in place: a thread reads exactly the cells that it writes
+        for (int i = 0; i < 3; ++i)
+            if (desc->in_stride[i] != desc->out_stride[i]) return SDTW_ERR_INVALID_ARG;
+    BiasParams p = bias_params(desc, in, offsets, row_len, col_len);
+    p.table = table;
+    p.out = out;
+    const int W = width_of(desc->plane_type);
+    p.tx = 1;
+    while (p.tx < 256 && p.tx * W < desc->M) p.tx *= 2;
+    const int rows = 256 / p.tx * kBiasRows, cols = p.tx * W;
+    p.col_tiles = (desc->M + cols - 1) / cols;
+    p.row_tiles = (desc->N + rows - 1) / rows;
+    const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, planes = (int64_t)desc->B * desc->H;
+    if (tiles > 0x7fffffff / planes) return SDTW_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const BucketRule rule = bucket_rule(desc);
+    {
+        ProfScope ps("position_bias_forward", st);
+        with_type(desc->plane_type, [&](auto t) {
+            position_bias_forward_kernel<decltype(t)><<<(unsigned)(tiles * planes), 256, (size_t)(rows + cols) * 4, st>>>(p, rule);
+        });
+    }
+    return hip_ok();
+}
+
+size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc)
+{
+    if (!bias_ok(desc)) return 0;
+    return std::max<size_t>(256, align_up((size_t)desc->H * desc->buckets * (size_t)bias_plan(desc).parts * sizeof(double), 256));
+}
+
+int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, const float *scale, const int32_t *offsets,
+                                const int32_t *row_len, const int32_t *col_len, float *dtable, void *workspace,
+                                size_t workspace_bytes, void *stream)
+{
+    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->H == 0) return SDTW_OK;
+    const BiasPlan P = bias_plan(desc);
+    if (!dtable || (!grad && P.parts > 0)) return SDTW_ERR_INVALID_ARG;
+    if (P.parts > 0x7fffffff / desc->H || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, sdtw_position_bias_workspace_bytes(desc))) return rc;
+    (void)hipGetLastError();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    BiasParams p = bias_params(desc, grad, offsets, row_len, col_len);
+    p.scale = scale;
+    p.dtable = dtable;
+    p.partial = static_cast<double *>(workspace);
+    p.strips = (int32_t)P.strips;
+    p.first_col = (int32_t)P.first_col;
+    p.batch_parts = (int32_t)P.batch_parts;
+    p.batch_per_part = (int32_t)P.batch_per_part;
+    p.step_parts = (int32_t)P.step_parts;
+    p.steps_per_part = (int32_t)P.steps_per_part;
+    p.parts = (int32_t)P.parts;
+    const BucketRule rule = bucket_rule(desc);
+    if (P.parts > 0) {
+        ProfScope ps("position_bias_backward", st);
+        with_type(desc->plane_type, [&](auto t) {
+            position_bias_backward_kernel<decltype(t)><<<(unsigned)(P.parts * desc->H), 256, 0, st>>>(p, rule);
+        });
+    }
+    {
+        ProfScope ps("position_bias_table", st);
+        position_bias_table_kernel<<<(unsigned)(desc->H * desc->buckets), 256, 0, st>>>(p);
+    }
+    return hip_ok();
+}
+
+}  // extern "C"
