@@ -45,7 +45,7 @@ typedef enum sdtw_status {
     SDTW_ERR_INVALID_ARG = 1, /* null pointer, non-positive size, gamma not finite or <= 0, bad mode,
                                  bandwidth < 0 or 0 < bandwidth < |N-M| */
     SDTW_ERR_WORKSPACE = 2,   /* workspace missing, misaligned or smaller than required */
-    SDTW_ERR_UNSUPPORTED = 3, /* bandwidth != 0 in a normalised Soft-DTW call */
+    SDTW_ERR_UNSUPPORTED = 3, /* bandwidth != 0 in a normalised Soft-DTW call; a position penalty in fused mode */
     SDTW_ERR_STATE = 4,       /* device: backward on a workspace not filled by a matching forward;
                                  host: backward with a SDTW_FLAG_VALUE_ONLY descriptor */
     SDTW_ERR_HIP = 5,         /* a HIP runtime call of this call failed (launch, copy); an error that an
@@ -392,6 +392,26 @@ size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc);
 int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, const float *scale, const int32_t *offsets,
                                 const int32_t *row_len, const int32_t *col_len, float *dtable, void *workspace,
                                 size_t workspace_bytes, void *stream);
+
+/*
+ * Soft-DTW under a learned position penalty: the cost of cell (i, j) of pair b is
+ *   ||x_i - y_j||^2 + max(0, table[b mod H, bucket(j - i - offset)])
+ * - the soft, learned counterpart of the band constraint.  Entries of the table are penalties: the sweeps skip what
+ * non-negative costs prove to be empty, so a negative entry counts as 0 and has gradient 0.
+ *   desc: as for sdtw_forward, SDTW_UNFUSED only (SDTW_ERR_UNSUPPORTED otherwise).
+ *   bias: B * H == desc->B (pair b is sequence b / H, head b mod H), the same N and M, plane_type SDTW_TYPE_F32; buckets,
+ *         max_distance, two_sided, offset, table_type and table_stride as above; in_stride and out_stride are not used.
+ *   x_len, y_len: as for sdtw_forward_ragged, or NULL.
+ *   dtable [H, buckets]: device, float32, out: the sum over the pairs of grad_value times the bucket's cells of E; or NULL.
+ * Everything else as sdtw_forward / sdtw_backward; the workspace also holds E for a call that is given no E_out.
+ */
+size_t sdtw_biased_workspace_bytes(const sdtw_desc *desc, const sdtw_bias_desc *bias);
+int sdtw_forward_biased(const sdtw_desc *desc, const sdtw_bias_desc *bias, const float *x, const float *y, const void *table,
+                        const int32_t *x_len, const int32_t *y_len, float *value, void *workspace, size_t workspace_bytes,
+                        void *stream);
+int sdtw_backward_biased(const sdtw_desc *desc, const sdtw_bias_desc *bias, const float *x, const float *y, const void *table,
+                         const int32_t *x_len, const int32_t *y_len, const float *grad_value, float *dx, float *dy, float *dtable,
+                         float *E_out, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Reads the device-side status word of a workspace: waits for `stream`, copies 4 bytes to the

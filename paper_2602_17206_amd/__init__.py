@@ -18,15 +18,18 @@ from .binding import (  # noqa: F401
     library_path,
     load_library,
     sdtw_backward,
+    sdtw_backward_biased,
     sdtw_backward_half,
     sdtw_backward_ragged,
     sdtw_barycenter_step,
+    sdtw_biased_workspace_bytes,
     sdtw_barycenter_workspace_bytes,
     sdtw_distill_backward,
     sdtw_distill_forward,
     sdtw_distill_step,
     sdtw_distill_workspace_bytes,
     sdtw_forward,
+    sdtw_forward_biased,
     sdtw_forward_half,
     sdtw_forward_ragged,
     sdtw_normalized_backward,

@@ -84,7 +84,7 @@ EXPORTED_SYMBOLS = (
     "sdtw_half_workspace_bytes", "sdtw_forward_half", "sdtw_backward_half",
     "sdtw_distill_workspace_bytes", "sdtw_distill_forward", "sdtw_distill_backward", "sdtw_distill_step",
     "sdtw_position_bias_starts", "sdtw_position_bias_forward", "sdtw_position_bias_workspace_bytes",
-    "sdtw_position_bias_backward",
+    "sdtw_position_bias_backward", "sdtw_biased_workspace_bytes", "sdtw_forward_biased", "sdtw_backward_biased",
 )
 
 
@@ -175,6 +175,13 @@ def load_library():
     lib.sdtw_position_bias_workspace_bytes.argtypes = [pb]
     lib.sdtw_position_bias_backward.restype = i32
     lib.sdtw_position_bias_backward.argtypes = [pb, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    pdesc = ctypes.POINTER(Desc)
+    lib.sdtw_biased_workspace_bytes.restype = sz
+    lib.sdtw_biased_workspace_bytes.argtypes = [pdesc, pb]
+    lib.sdtw_forward_biased.restype = i32
+    lib.sdtw_forward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sdtw_backward_biased.restype = i32
+    lib.sdtw_backward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -820,3 +827,66 @@ def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True,
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_backward")
     return dtable
+
+
+def sdtw_biased_workspace_bytes(desc, bias_desc):
+    return int(load_library().sdtw_biased_workspace_bytes(ctypes.byref(desc), ctypes.byref(bias_desc)))
+
+
+def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, offset=0, x_len=None, y_len=None, bandwidth=0,
+                        workspace=None, value=None, stream=None, value_only=False, min_memory=False):
+    """value[b] = sdtw_gamma(x_b, y_b) with max(0, table[b mod H, bucket(j - i - offset)]) added to the cost of cell (i, j): a
+    learned position penalty, ``table`` [H, buckets] of any strides.  Unfused mode.
+    Returns (value, state, workspace); keep the last two for :func:`sdtw_backward_biased`."""
+    import torch
+
+    lib = load_library()
+    desc = _desc_for(x, y, gamma, UNFUSED)
+    desc.bandwidth = int(bandwidth)
+    desc.flags |= (FLAG_VALUE_ONLY if value_only else 0) | (FLAG_MIN_MEMORY if min_memory else 0)
+    dev = x.device
+    if table.dim() != 2 or table.device != dev or table.shape[0] < 1 or desc.B % table.shape[0]:
+        raise ValueError("table must be [H, buckets] on the sequences' device, the number of pairs a multiple of H")
+    H, buckets = table.shape
+    bias = BiasDesc(desc.B // H, H, desc.N, desc.M, buckets, int(max_distance), 1 if two_sided else 0, TYPE_F32,
+                    _type_of(table, "table"), 0, int(offset))
+    bias.table_stride[:] = [table.stride(0), table.stride(1)]
+    workspace = _operator_workspace(lib.sdtw_biased_workspace_bytes(ctypes.byref(desc), ctypes.byref(bias)), workspace, dev,
+                                    "sdtw_forward_biased")
+    if value is None:
+        value = torch.empty(desc.B, dtype=torch.float32, device=dev)
+    rc = lib.sdtw_forward_biased(ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"),
+                                 _ptr(y, torch.float32, name="y"), table.data_ptr(), _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"),
+                                 _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"), _ptr(value, torch.float32, (desc.B,), "value"),
+                                 workspace.ptr, workspace.nbytes, _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_forward_biased")
+    return value, (desc, bias), workspace
+
+
+def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=None, y_len=None, want_E=False, dx=None, dy=None,
+                         dtable=None, E=None, stream=None):
+    """Gradients of the values :func:`sdtw_forward_biased` produced (same tensors).
+    Returns (dx, dy, dtable [H, buckets] float32, E or None)."""
+    import torch
+
+    lib = load_library()
+    desc, bias = state
+    dev = x.device
+    if dx is None:
+        dx = torch.empty((desc.B, desc.N, desc.D), dtype=torch.float32, device=dev)
+    if dy is None:
+        dy = torch.empty((desc.B, desc.M, desc.D), dtype=torch.float32, device=dev)
+    if dtable is None:
+        dtable = torch.empty((bias.H, bias.buckets), dtype=torch.float32, device=dev)
+    if want_E and E is None:
+        E = torch.empty((desc.B, desc.N, desc.M), dtype=torch.float32, device=dev)
+    rc = lib.sdtw_backward_biased(
+        ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"), _ptr(y, torch.float32, name="y"), table.data_ptr(),
+        _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"), _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"),
+        _ptr(grad_value, torch.float32, (desc.B,), "grad_value"), _ptr(dx, torch.float32, (desc.B, desc.N, desc.D), "dx"),
+        _ptr(dy, torch.float32, (desc.B, desc.M, desc.D), "dy"), _ptr(dtable, torch.float32, (bias.H, bias.buckets), "dtable"),
+        _ptr(E, torch.float32, (desc.B, desc.N, desc.M), "E"), workspace.ptr, workspace.nbytes, _stream_ptr(stream))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_backward_biased")
+    return dx, dy, dtable, E

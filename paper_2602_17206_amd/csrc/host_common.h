@@ -2,6 +2,8 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <cstdint>
+
 #include "../../include/sdtw.h"
 
 namespace sdtw {
@@ -25,5 +27,14 @@ inline int check_ws(const void *ws, size_t bytes, size_t need)
 }
 
 inline int hip_ok() { return hipGetLastError() == hipSuccess ? SDTW_OK : SDTW_ERR_HIP; }
+
+// The position bias (train_ops.hip) as the Soft-DTW calls use it: with `penalty` negative table entries count as 0.
+int position_bias_add(const sdtw_bias_desc *d, const void *table, bool penalty, const void *in, const int32_t *offsets,
+                      const int32_t *row_len, const int32_t *col_len, void *out, hipStream_t st);
+// ... and its table's gradient; penalty_table: 0 for the entries that are negative there, or nullptr;
+// scale: [B], or [B, H] with scale_heads.
+int position_bias_table_grad(const sdtw_bias_desc *d, const void *penalty_table, const void *grad, const float *scale, bool scale_heads,
+                             const int32_t *offsets, const int32_t *row_len, const int32_t *col_len, float *dtable,
+                             void *workspace, size_t workspace_bytes, hipStream_t st);
 
 }  // namespace sdtw

@@ -33,12 +33,14 @@ struct BucketRule {
 
 struct BiasParams {
     int32_t B, H, N, M, buckets, table_type;
+    int32_t penalty;  // negative table entries count as 0
     int64_t offset;
     int64_t in_stride[3], out_stride[3], table_stride[2];
     const void *table, *in;
     void *out;
     const int32_t *offsets, *row_len, *col_len;
-    const float *scale;
+    const float *scale;    // [B], or [B, H] with scale_heads
+    int32_t scale_heads;
     float *dtable;
     // forward: tiles of (256 / ty * width) columns and ty * 8 rows
     int32_t tx, col_tiles, row_tiles;
@@ -53,6 +55,12 @@ __device__ __forceinline__ int clamp_len(const int32_t *len, int b, int full) { 
 
 // a position difference as 32 bits: beyond 2^30 every distance is in the last bucket
 __device__ __forceinline__ int clamp_rel(int64_t r) { return (int)min(max(r, (int64_t) - (1 << 30)), (int64_t)1 << 30); }
+
+__device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
+{
+    const float v = load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type);
+    return p.penalty && v < 0.0f ? 0.0f : v;
+}
 
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
@@ -74,7 +82,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     const int nd = min(cols, p.M - j0) + rows - 1;
     for (int q = threadIdx.x; q < nd; q += 256) {
         const int u = rule.bucket(clamp_rel((int64_t)j0 - (i0 + rows - 1) + q - offset));
-        diag[q] = load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type);
+        diag[q] = load_bias(p, h, u);
     }
     __syncthreads();
     const int x = threadIdx.x % p.tx, y = threadIdx.x / p.tx;
@@ -174,7 +182,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     for (int b = b0; b < b1; ++b) {
         const int rlen = clamp_len(p.row_len, b, p.N), clen = clamp_len(p.col_len, b, p.M);
         const T *g = static_cast<const T *>(p.in) + b * p.in_stride[0] + h * p.in_stride[1];
-        const double scale = p.scale ? (double)p.scale[b] : 1.0;
+        const double scale = p.scale ? (double)p.scale[p.scale_heads ? (int64_t)b * p.H + h : b] : 1.0;
         // the steps at which the strip touches the columns [0, clen) and the rows [0, rlen)
         const int64_t from = max((int64_t)sp * p.steps_per_part, base + 64 * W >= 0 ? (int64_t)0 : (-base - 64 * W) / 8);
         const int64_t past_cols = clen - base <= 0 ? 0 : (clen - base + 7) / 8;
@@ -222,7 +230,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     for (int u = threadIdx.x; u < p.buckets; u += 256) p.partial[((int64_t)h * p.buckets + u) * p.parts + part] = bucket_sum[u];
 }
 
-// dtable[h,u]: the parts in a fixed order.
+// dtable[h,u]: the parts in a fixed order.  With a table (a penalty) its negative entries, which count as 0, get 0.
 __global__ __launch_bounds__(256) void position_bias_table_kernel(BiasParams p)
 {
     __shared__ double sums[4];
@@ -232,7 +240,11 @@ __global__ __launch_bounds__(256) void position_bias_table_kernel(BiasParams p)
     s = wave_sum_f64(s);
     if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
     __syncthreads();
-    if (threadIdx.x == 0) p.dtable[blockIdx.x] = (float)((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    if (threadIdx.x == 0) {
+        const int h = blockIdx.x / p.buckets, u = blockIdx.x % p.buckets;
+        const bool off = p.table && load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type) < 0.0f;
+        p.dtable[blockIdx.x] = off ? 0.0f : (float)((sums[0] + sums[1]) + (sums[2] + sums[3]));
+    }
 }
 
 }  // namespace sdtw

@@ -269,8 +269,11 @@ unsigned prep_grid(const Params &p, int64_t norm_rows)
     return (unsigned)(g < 1 ? 1 : (g > 8192 ? 8192 : g));
 }
 
+// A learned position penalty on the cost tensor (sdtw_forward_biased).
+struct Penalty { const sdtw_bias_desc *desc; const void *table; };
+
 int forward_impl(const sdtw_desc *d, const float *x, const float *y, float *value, void *ws, hipStream_t st,
-                 const int32_t *x_len = nullptr, const int32_t *y_len = nullptr, int pieces = 2)
+                 const int32_t *x_len = nullptr, const int32_t *y_len = nullptr, int pieces = 2, const Penalty *penalty = nullptr)
 {
     (void)hipGetLastError();  // what an earlier, unrelated call left behind is not this call's error
     const Layout L = layout_of(d);
@@ -311,6 +314,9 @@ int forward_impl(const sdtw_desc *d, const float *x, const float *y, float *valu
                 cost_tensor_kernel<<<g, 256, 0, st>>>(p);
             }
         }
+    }
+    if (penalty) {  // (unfused mode: the whole tensor, in place)
+        if (int rc = position_bias_add(penalty->desc, penalty->table, true, p.cost, nullptr, nullptr, nullptr, p.cost, st)) return rc;
     }
     {
         const bool unf = d->mode == SDTW_UNFUSED;
@@ -547,7 +553,7 @@ const char *sdtw_status_string(int status)
         case SDTW_OK: return "ok";
         case SDTW_ERR_INVALID_ARG: return "invalid argument";
         case SDTW_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
-        case SDTW_ERR_UNSUPPORTED: return "unsupported option (normalised Soft-DTW takes no bandwidth)";
+        case SDTW_ERR_UNSUPPORTED: return "unsupported option (normalised Soft-DTW takes no bandwidth, a position penalty needs the unfused mode)";
         case SDTW_ERR_STATE: return "backward called on a workspace without a matching forward";
         case SDTW_ERR_HIP: return "HIP runtime error";
         case SDTW_ERR_TIMEOUT: return "a band gave up waiting for its neighbour";
@@ -678,6 +684,71 @@ int sdtw_backward_half(const sdtw_desc *desc, const float *grad_value, float *dx
     const float *x32 = reinterpret_cast<const float *>(base + H.off_x), *y32 = reinterpret_cast<const float *>(base + H.off_y);
     return backward_impl(desc, x32, y32, grad_value, dx, dy, E_out, workspace, static_cast<hipStream_t>(stream), nullptr,
                          nullptr, 1);
+}
+
+// Soft-DTW under a learned position penalty: the plain workspace first (its header carries the status word), then a
+// dense E for calls without E_out, then the partial sums of the table's gradient.
+struct BiasedLayout { size_t off_E, off_sums, total; sdtw_bias_desc planes; };
+
+static bool biased_layout(const sdtw_desc *d, const sdtw_bias_desc *bias, BiasedLayout *L)
+{
+    if (!bias || bias->H < 1 || bias->B < 1 || (int64_t)bias->B * bias->H != d->B || bias->N != d->N || bias->M != d->M ||
+        bias->plane_type != SDTW_TYPE_F32)
+        return false;
+    L->planes = *bias;
+    const int64_t cells = (int64_t)d->N * d->M;
+    L->planes.in_stride[0] = L->planes.out_stride[0] = cells * bias->H;
+    L->planes.in_stride[1] = L->planes.out_stride[1] = cells;
+    L->planes.in_stride[2] = L->planes.out_stride[2] = d->M;
+    const size_t sums = sdtw_position_bias_workspace_bytes(&L->planes);
+    if (sums == 0) return false;
+    L->off_E = align_up(layout_of(d).total, 256);
+    L->off_sums = align_up(L->off_E + (size_t)d->B * cells * sizeof(float), 256);
+    L->total = align_up(L->off_sums + sums, 256);
+    return true;
+}
+
+size_t sdtw_biased_workspace_bytes(const sdtw_desc *desc, const sdtw_bias_desc *bias)
+{
+    int why;
+    BiasedLayout L;
+    if (!desc_ok(desc, &why) || desc->mode != SDTW_UNFUSED || !biased_layout(desc, bias, &L)) return 0;
+    return L.total;
+}
+
+int sdtw_forward_biased(const sdtw_desc *desc, const sdtw_bias_desc *bias, const float *x, const float *y, const void *table,
+                        const int32_t *x_len, const int32_t *y_len, float *value, void *workspace, size_t workspace_bytes,
+                        void *stream)
+{
+    int why;
+    BiasedLayout L;
+    if (!desc_ok(desc, &why)) return why;
+    if (desc->mode != SDTW_UNFUSED) return SDTW_ERR_UNSUPPORTED;
+    if (!biased_layout(desc, bias, &L) || !x || !y || !table || !value) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, L.total)) return rc;
+    const Penalty penalty{&L.planes, table};
+    return forward_impl(desc, x, y, value, workspace, static_cast<hipStream_t>(stream), x_len, y_len, 2, &penalty);
+}
+
+int sdtw_backward_biased(const sdtw_desc *desc, const sdtw_bias_desc *bias, const float *x, const float *y, const void *table,
+                         const int32_t *x_len, const int32_t *y_len, const float *grad_value, float *dx, float *dy, float *dtable,
+                         float *E_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int why;
+    BiasedLayout L;
+    if (!desc_ok(desc, &why)) return why;
+    if (desc->mode != SDTW_UNFUSED) return SDTW_ERR_UNSUPPORTED;
+    if (!biased_layout(desc, bias, &L) || !x || !y || !table) return SDTW_ERR_INVALID_ARG;
+    if (desc->flags & SDTW_FLAG_VALUE_ONLY) return SDTW_ERR_STATE;
+    if (int rc = check_ws(workspace, workspace_bytes, L.total)) return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    char *base = static_cast<char *>(workspace);
+    float *E = E_out || !dtable ? E_out : reinterpret_cast<float *>(base + L.off_E);
+    if (int rc = backward_impl(desc, x, y, grad_value, dx, dy, E, workspace, st, x_len, y_len)) return rc;
+    if (!dtable) return SDTW_OK;
+    // (dvalue/dtable[h,u] of a pair is the sum of its E over the bucket's cells)
+    return position_bias_table_grad(&L.planes, table, E, grad_value, true, nullptr, nullptr, nullptr, dtable, base + L.off_sums,
+                                    workspace_bytes - L.off_sums, st);
 }
 
 size_t sdtw_barycenter_workspace_bytes(const sdtw_bary_desc *desc)

@@ -259,6 +259,80 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
 
 }  // namespace
 
+namespace sdtw {
+
+int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalty, const void *in, const int32_t *offsets,
+                      const int32_t *row_len, const int32_t *col_len, void *out, hipStream_t st)
+{
+    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->B == 0 || desc->H == 0 || desc->N == 0 || desc->M == 0) return SDTW_OK;
+    if (!table || !out || !disjoint(desc)) return SDTW_ERR_INVALID_ARG;
+    if (in == out)  // in place: a thread reads exactly the cells that it writes
+        for (int i = 0; i < 3; ++i)
+            if (desc->in_stride[i] != desc->out_stride[i]) return SDTW_ERR_INVALID_ARG;
+    BiasParams p = bias_params(desc, in, offsets, row_len, col_len);
+    p.table = table;
+    p.penalty = penalty;
+    p.out = out;
+    const int W = width_of(desc->plane_type);
+    p.tx = 1;
+    while (p.tx < 256 && p.tx * W < desc->M) p.tx *= 2;
+    const int rows = 256 / p.tx * kBiasRows, cols = p.tx * W;
+    p.col_tiles = (desc->M + cols - 1) / cols;
+    p.row_tiles = (desc->N + rows - 1) / rows;
+    const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, planes = (int64_t)desc->B * desc->H;
+    if (tiles > 0x7fffffff / planes) return SDTW_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    const BucketRule rule = bucket_rule(desc);
+    {
+        ProfScope ps("position_bias_forward", st);
+        with_type(desc->plane_type, [&](auto t) {
+            position_bias_forward_kernel<decltype(t)><<<(unsigned)(tiles * planes), 256, (size_t)(rows + cols) * 4, st>>>(p, rule);
+        });
+    }
+    return hip_ok();
+}
+
+int position_bias_table_grad(const sdtw_bias_desc *desc, const void *penalty_table, const void *grad, const float *scale,
+                             bool scale_heads, const int32_t *offsets, const int32_t *row_len, const int32_t *col_len, float *dtable,
+                             void *workspace, size_t workspace_bytes, hipStream_t st)
+{
+    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
+    if (desc->H == 0) return SDTW_OK;
+    const BiasPlan P = bias_plan(desc);
+    if (!dtable || (!grad && P.parts > 0)) return SDTW_ERR_INVALID_ARG;
+    if (P.parts > 0x7fffffff / desc->H || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, sdtw_position_bias_workspace_bytes(desc))) return rc;
+    (void)hipGetLastError();
+    BiasParams p = bias_params(desc, grad, offsets, row_len, col_len);
+    p.scale = scale;
+    p.scale_heads = scale_heads;
+    p.table = penalty_table;
+    p.dtable = dtable;
+    p.partial = static_cast<double *>(workspace);
+    p.strips = (int32_t)P.strips;
+    p.first_col = (int32_t)P.first_col;
+    p.batch_parts = (int32_t)P.batch_parts;
+    p.batch_per_part = (int32_t)P.batch_per_part;
+    p.step_parts = (int32_t)P.step_parts;
+    p.steps_per_part = (int32_t)P.steps_per_part;
+    p.parts = (int32_t)P.parts;
+    const BucketRule rule = bucket_rule(desc);
+    if (P.parts > 0) {
+        ProfScope ps("position_bias_backward", st);
+        with_type(desc->plane_type, [&](auto t) {
+            position_bias_backward_kernel<decltype(t)><<<(unsigned)(P.parts * desc->H), 256, 0, st>>>(p, rule);
+        });
+    }
+    {
+        ProfScope ps("position_bias_table", st);
+        position_bias_table_kernel<<<(unsigned)(desc->H * desc->buckets), 256, 0, st>>>(p);
+    }
+    return hip_ok();
+}
+
+}  // namespace sdtw
+
 extern "C" {
 
 size_t sdtw_distill_workspace_bytes(const sdtw_distill_desc *desc)
@@ -340,33 +414,7 @@ int sdtw_position_bias_starts(const sdtw_bias_desc *desc, int32_t *starts)
 int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, const void *in, const int32_t *offsets,
                                const int32_t *row_len, const int32_t *col_len, void *out, void *stream)
 {
-    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
-    if (desc->B == 0 || desc->H == 0 || desc->N == 0 || desc->M == 0) return SDTW_OK;
-    if (!table || !out || !disjoint(desc)) return SDTW_ERR_INVALID_ARG;
-    if (in == out)  // in place: a thread reads exactly the cells that it writes
-        for (int i = 0; i < 3; ++i)
-            if (desc->in_stride[i] != desc->out_stride[i]) return SDTW_ERR_INVALID_ARG;
-    BiasParams p = bias_params(desc, in, offsets, row_len, col_len);
-    p.table = table;
-    p.out = out;
-    const int W = width_of(desc->plane_type);
-    p.tx = 1;
-    while (p.tx < 256 && p.tx * W < desc->M) p.tx *= 2;
-    const int rows = 256 / p.tx * kBiasRows, cols = p.tx * W;
-    p.col_tiles = (desc->M + cols - 1) / cols;
-    p.row_tiles = (desc->N + rows - 1) / rows;
-    const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, planes = (int64_t)desc->B * desc->H;
-    if (tiles > 0x7fffffff / planes) return SDTW_ERR_INVALID_ARG;
-    (void)hipGetLastError();
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    const BucketRule rule = bucket_rule(desc);
-    {
-        ProfScope ps("position_bias_forward", st);
-        with_type(desc->plane_type, [&](auto t) {
-            position_bias_forward_kernel<decltype(t)><<<(unsigned)(tiles * planes), 256, (size_t)(rows + cols) * 4, st>>>(p, rule);
-        });
-    }
-    return hip_ok();
+    return position_bias_add(desc, table, false, in, offsets, row_len, col_len, out, static_cast<hipStream_t>(stream));
 }
 
 size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc)
@@ -379,37 +427,8 @@ int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, co
                                 const int32_t *row_len, const int32_t *col_len, float *dtable, void *workspace,
                                 size_t workspace_bytes, void *stream)
 {
-    if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
-    if (desc->H == 0) return SDTW_OK;
-    const BiasPlan P = bias_plan(desc);
-    if (!dtable || (!grad && P.parts > 0)) return SDTW_ERR_INVALID_ARG;
-    if (P.parts > 0x7fffffff / desc->H || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
-    if (int rc = check_ws(workspace, workspace_bytes, sdtw_position_bias_workspace_bytes(desc))) return rc;
-    (void)hipGetLastError();
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    BiasParams p = bias_params(desc, grad, offsets, row_len, col_len);
-    p.scale = scale;
-    p.dtable = dtable;
-    p.partial = static_cast<double *>(workspace);
-    p.strips = (int32_t)P.strips;
-    p.first_col = (int32_t)P.first_col;
-    p.batch_parts = (int32_t)P.batch_parts;
-    p.batch_per_part = (int32_t)P.batch_per_part;
-    p.step_parts = (int32_t)P.step_parts;
-    p.steps_per_part = (int32_t)P.steps_per_part;
-    p.parts = (int32_t)P.parts;
-    const BucketRule rule = bucket_rule(desc);
-    if (P.parts > 0) {
-        ProfScope ps("position_bias_backward", st);
-        with_type(desc->plane_type, [&](auto t) {
-            position_bias_backward_kernel<decltype(t)><<<(unsigned)(P.parts * desc->H), 256, 0, st>>>(p, rule);
-        });
-    }
-    {
-        ProfScope ps("position_bias_table", st);
-        position_bias_table_kernel<<<(unsigned)(desc->H * desc->buckets), 256, 0, st>>>(p);
-    }
-    return hip_ok();
+    return position_bias_table_grad(desc, nullptr, grad, scale, false, offsets, row_len, col_len, dtable, workspace, workspace_bytes,
+                                    static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,118 @@
+"""Soft-DTW under a learned position penalty against the float64 oracle on the cost matrix written out here, and the
+small training example that runs the operators together.  Bars: the path's own (1e-4 relative for the values, 1e-3 of the
+largest entry for gradients), the table's gradient as one of them."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2602_17206_amd as pkg
+from paper_2602_17206_amd import binding
+from paper_2602_17206_amd.workloads import normal_pairs, ragged_lengths
+
+pytestmark = pytest.mark.gpu
+
+
+def bucket_line(lo, hi, buckets, D, two_sided):
+    """bucket of r = lo .. hi - 1, from the library's whole-number starts (held against whole numbers elsewhere)"""
+    first = np.array(pkg.sdtw_position_bias_starts(buckets, D, two_sided))
+    r = np.arange(lo, hi)
+    d = np.abs(r) if two_sided else np.maximum(0, -r)
+    u = np.searchsorted(first, d, side="right") - 1
+    return u + (buckets // 2) * (r > 0) if two_sided else u
+
+
+@pytest.mark.parametrize("B,H,N,M,D,gamma,extra", [
+    (2, 1, 1, 1, 3, 1.0, {}), (4, 2, 40, 55, 8, 1.0, {}), (6, 3, 130, 97, 16, 0.1, {}), (3, 3, 64, 300, 200, 0.5, {}),
+    (4, 1, 150, 160, 20, 0.1, {"bandwidth": 30}), (4, 2, 200, 170, 8, 0.5, {"ragged": True}), (4, 2, 220, 190, 8, 0.1, {"min_memory": True}),
+    (70, 1, 800, 790, 4, 0.5, {"check": 3}),  # too many bands for the tables of both sweeps: the recomputing sweep
+])
+@pytest.mark.parametrize("two_sided", [True, False])
+def test_values_and_gradients(B, H, N, M, D, gamma, extra, two_sided):
+    x, y = normal_pairs(31, B, N, M, D)
+    rng = np.random.default_rng(B + N)
+    buckets, far = 16, 60
+    table = np.abs(rng.standard_normal((H, buckets))).astype(np.float32) * 2
+    table[:, 3] = -1.0  # counts as 0
+    g = rng.uniform(0.5, 2.0, B).astype(np.float32)
+    xl = yl = None
+    if extra.get("ragged"):
+        xl, yl = ragged_lengths(1, B, N), ragged_lengths(2, B, M)
+    to = lambda a: None if a is None else torch.from_numpy(a).cuda()  # noqa: E731
+    xd, yd, td, gd = to(x), to(y), to(table), to(g)
+    kw = {k: v for k, v in extra.items() if k in ("bandwidth", "min_memory")}
+    value, state, ws = pkg.sdtw_forward_biased(xd, yd, td, gamma, max_distance=far, two_sided=two_sided, offset=2, x_len=to(xl), y_len=to(yl), **kw)
+    dx, dy, dt, E = pkg.sdtw_backward_biased(state, xd, yd, td, ws, grad_value=gd, x_len=to(xl), y_len=to(yl), want_E=True)
+    assert binding.workspace_status(ws) == 0
+    value2, state2, ws2 = pkg.sdtw_forward_biased(xd, yd, td, gamma, max_distance=far, two_sided=two_sided, offset=2, x_len=to(xl), y_len=to(yl), **kw)
+    again = pkg.sdtw_backward_biased(state2, xd, yd, td, ws2, grad_value=gd, x_len=to(xl), y_len=to(yl))
+    assert torch.equal(value, value2) and torch.equal(again[2], dt) and again[3] is None
+    line = bucket_line(-(N - 1) - 2, M - 2, buckets, far, two_sided)
+    at = line[np.arange(M)[None] - np.arange(N)[:, None] + N - 1]
+    want_dt, largest = np.zeros((H, buckets)), 0.0
+    for b in range(B):
+        n, m = (N if xl is None else int(xl[b])), (M if yl is None else int(yl[b]))
+        if b >= extra.get("check", B):
+            e = E[b].double().cpu().numpy()
+        else:
+            a, c = x[b, :n].astype(np.float64), y[b, :m].astype(np.float64)
+            d = ((a[:, None] - c[None]) ** 2).sum(2) + np.maximum(table[b % H].astype(np.float64), 0)[at[:n, :m]]
+            ref = oracle.from_cost(d, gamma, bandwidth=extra.get("bandwidth"))
+            assert abs(float(value[b]) - ref["value"]) <= 1e-4 * max(1.0, abs(ref["value"]))
+            e = np.zeros((N, M))
+            e[:n, :m] = ref["E"]
+            want_x = 2 * g[b] * (a * ref["E"].sum(1)[:, None] - ref["E"] @ c)
+            want_y = 2 * g[b] * (c * ref["E"].sum(0)[:, None] - ref["E"].T @ a)
+            for got, want, k in ((dx[b], want_x, n), (dy[b], want_y, m)):
+                got = got.double().cpu().numpy()
+                assert np.abs(got[:k] - want).max() <= 1e-3 * np.abs(want).max() + 1e-12 and (got[k:] == 0).all()
+            assert np.abs(E[b].double().cpu().numpy() - e).max() <= 1e-3
+        want_dt[b % H] += g[b] * np.bincount(at.ravel(), weights=e.ravel(), minlength=buckets)
+    want_dt[:, 3] = 0
+    got = dt.double().cpu().numpy()
+    assert np.abs(got - want_dt).max() <= 1e-3 * np.abs(want_dt).max() and (got[:, 3] == 0).all()
+
+
+def test_a_table_of_zeros_changes_nothing():
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(5, 8, 100, 90, 16))
+    value, desc, ws = pkg.sdtw_forward(x, y, 0.5, pkg.UNFUSED)
+    dx, dy, E = pkg.sdtw_backward(desc, x, y, ws, want_E=True)
+    table = torch.zeros((2, 32), device="cuda", dtype=torch.bfloat16)
+    v, state, w = pkg.sdtw_forward_biased(x, y, table, 0.5)
+    bx, by, bt, bE = pkg.sdtw_backward_biased(state, x, y, table, w, want_E=True)
+    assert torch.equal(v, value) and torch.equal(bx, dx) and torch.equal(by, dy) and torch.equal(bE, E)
+    # every pair's E is somewhere in the table: with weights of one the sums agree
+    assert abs(float(bt.double().sum()) - float(E.double().sum())) <= 1e-6 * float(E.double().sum())
+
+
+def test_table_gradient_against_differences():
+    """Central differences of the oracle's values in the table's entries: with h = 1e-4 their own error is some 1e-7 of the
+    gradient here, so the path's bar, 1e-3 of the largest entry, is the kernels' alone."""
+    x, y = normal_pairs(6, 2, 30, 30, 4)
+    rng = np.random.default_rng(1)
+    table = np.abs(rng.standard_normal((1, 8))).astype(np.float32) + np.float32(0.2)
+    xd, yd, td = (torch.from_numpy(a).cuda() for a in (x, y, table))
+    _, state, ws = pkg.sdtw_forward_biased(xd, yd, td, 2.0, max_distance=20)
+    dt = pkg.sdtw_backward_biased(state, xd, yd, td, ws)[2].double().cpu().numpy()[0]
+    at = bucket_line(-29, 30, 8, 20, True)[np.arange(30)[None] - np.arange(30)[:, None] + 29]
+
+    def value(line):
+        cost = ((x.astype(np.float64)[:, :, None] - y.astype(np.float64)[:, None]) ** 2).sum(3) + line[at]
+        return sum(oracle.from_cost(c, 2.0)["value"] for c in cost)
+    step = 1e-4 * np.eye(8)
+    line = table[0].astype(np.float64)
+    want = np.array([(value(line + e) - value(line - e)) / 2e-4 for e in step])
+    assert np.abs(dt - want).max() <= 1e-3 * np.abs(want).max()
+
+
+def test_refusals():
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(6, 4, 30, 30, 4))
+    table = torch.zeros((2, 32), device="cuda")
+    with pytest.raises(ValueError):
+        pkg.sdtw_forward_biased(x, y, torch.zeros((3, 32), device="cuda"), 1.0)
+    with pytest.raises(pkg.SdtwError):
+        pkg.sdtw_forward_biased(x, y, torch.zeros((2, 31), device="cuda"), 1.0)
+    value, state, ws = pkg.sdtw_forward_biased(x, y, table, 1.0, value_only=True)
+    with pytest.raises(pkg.SdtwError) as e:
+        pkg.sdtw_backward_biased(state, x, y, table, ws)
+    assert e.value.status == binding.STATUS_STATE

@@ -167,3 +167,26 @@ def test_the_binding_checks_its_tensors():
         pkg.sdtw_position_bias_backward(torch.zeros(1, 2, 3, 3), 32)
     with pytest.raises(pkg.SdtwError):
         pkg.sdtw_position_bias_starts(33, 128, True)
+
+
+def test_position_penalty_entry_points_refuse():
+    lib = pkg.load_library()
+    d = binding.make_desc(6, 8, 9, 4, 1.0, pkg.UNFUSED)
+    b = bias_desc()
+    need = lib.sdtw_biased_workspace_bytes(ctypes.byref(d), ctypes.byref(b))
+    assert need > pkg.sdtw_workspace_bytes(d) + 4 * 6 * 8 * 9
+
+    def both(d, b, ws=FAKE, nbytes=need, x=FAKE, table=FAKE):
+        f = lib.sdtw_forward_biased(ctypes.byref(d), ctypes.byref(b), x, FAKE, table, None, None, FAKE, ws, nbytes, None)
+        r = lib.sdtw_backward_biased(ctypes.byref(d), ctypes.byref(b), x, FAKE, table, None, None, None, FAKE, FAKE, FAKE, None, ws, nbytes, None)
+        return {f, r}
+
+    for kw in (dict(B=3), dict(H=1), dict(N=9), dict(M=8), dict(plane_type=1), dict(buckets=31), dict(B=0, H=0), dict(table_type=5)):
+        assert lib.sdtw_biased_workspace_bytes(ctypes.byref(d), ctypes.byref(bias_desc(**kw))) == 0, kw
+        assert both(d, bias_desc(**kw)) == {binding.STATUS_INVALID_ARG}, kw
+    assert both(binding.make_desc(6, 8, 9, 4, 1.0, pkg.FUSED), b) == {binding.STATUS_UNSUPPORTED}
+    assert both(binding.make_desc(6, 8, 9, 4, -1.0, pkg.UNFUSED), b) == {binding.STATUS_INVALID_ARG}
+    assert both(d, b, x=None) == {binding.STATUS_INVALID_ARG}
+    assert both(d, b, table=None) == {binding.STATUS_INVALID_ARG}
+    assert both(d, b, ws=None) == {binding.STATUS_WORKSPACE}
+    assert both(d, b, nbytes=need - 1) == {binding.STATUS_WORKSPACE}
