@@ -616,28 +616,43 @@ DISTILL_RENORMALIZED, DISTILL_TAIL = 0, 1
 DISTILL_STATS = 8
 
 
-def _type_of(t, name):
-    import torch
+_type_codes = {}
 
-    kind = {torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16}.get(t.dtype)
+
+def _type_of(t, name):
+    if not _type_codes:
+        import torch
+
+        _type_codes.update({torch.float32: TYPE_F32, torch.float16: TYPE_F16, torch.bfloat16: TYPE_BF16})
+    kind = _type_codes.get(t.dtype)
     if kind is None:
         raise ValueError("%s must be float32, float16 or bfloat16" % name)
     return kind
 
 
-def _rows_ptr(t, shape, device, name, dtype=None):
-    """Device pointer and row stride of a matrix whose rows are contiguous."""
-    if t.device != device or tuple(t.shape) != tuple(shape) or (dtype is not None and t.dtype != dtype):
-        raise ValueError("%s must be%s [%s] on %s" % (name, " %s" % dtype if dtype else "", ", ".join(map(str, shape)), device))
-    if (t.stride(1) != 1 and shape[1] > 1) or (t.stride(0) < shape[1] and shape[0] > 1):
+def _stream_of(stream, device):
+    """The given stream, or the current one of the tensors' device."""
+    if stream is not None:
+        return int(stream)
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _rows_ptr(t, T, K, device, name, dtype=None):
+    """Device pointer and row stride of a matrix [T, K] whose rows are contiguous."""
+    if t.device != device or t.shape != (T, K) or (dtype is not None and t.dtype != dtype):
+        raise ValueError("%s must be%s [%d, %d] on %s" % (name, " %s" % dtype if dtype else "", T, K, device))
+    step, along = t.stride()
+    if (along != 1 and K > 1) or (step < K and T > 1):
         raise ValueError("%s must have contiguous rows that do not overlap" % name)
-    return t.data_ptr(), max(t.stride(0), shape[1])
+    return t.data_ptr(), step if step > K else K
 
 
 def _vector_ptr(t, n, device, dtype, name):
     if t is None:
         return None
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+    if t.device != device or t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s [%d] on %s" % (name, dtype, n, device))
     return t.data_ptr()
 
@@ -649,14 +664,15 @@ def _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse,
     if logits.dim() != 2 or teacher_logits.dim() != 2 or not logits.is_cuda:
         raise ValueError("logits [T, V] and teacher_logits [R, K] must be device matrices")
     dev, (T, V), (R, K) = logits.device, logits.shape, teacher_logits.shape
-    if teacher_ids.dtype not in (torch.int32, torch.int64):
+    wide_ids = teacher_ids.dtype == torch.int64
+    if not wide_ids and teacher_ids.dtype != torch.int32:
         raise ValueError("teacher_ids must be int32 or int64")
-    zp, zs = _rows_ptr(logits, (T, V), dev, "logits")
-    tp, ts = _rows_ptr(teacher_logits, (R, K), dev, "teacher_logits")
-    ip, ids = _rows_ptr(teacher_ids, (R, K), dev, "teacher_ids")
-    desc = DistillDesc(T, V, K, R, float(temperature), DISTILL_RENORMALIZED if teacher_lse is None else DISTILL_TAIL,
-                       _type_of(logits, "logits"), _type_of(teacher_logits, "teacher_logits"),
-                       ID_I64 if teacher_ids.dtype == torch.int64 else ID_I32, 0, zs, V, ts, ids)
+    zp, zs = _rows_ptr(logits, T, V, dev, "logits")
+    tp, ts = _rows_ptr(teacher_logits, R, K, dev, "teacher_logits")
+    ip, ids = _rows_ptr(teacher_ids, R, K, dev, "teacher_ids")
+    desc = DistillDesc(T, V, K, R, temperature, DISTILL_RENORMALIZED if teacher_lse is None else DISTILL_TAIL,
+                       _type_of(logits, "logits"), _type_of(teacher_logits, "teacher_logits"), ID_I64 if wide_ids else ID_I32, 0,
+                       zs, V, ts, ids)
     return desc, (zp, tp, ip, _vector_ptr(teacher_lse, R, dev, torch.float32, "teacher_lse"),
                   _vector_ptr(teacher_row, T, dev, torch.int32, "teacher_row"))
 
@@ -667,16 +683,20 @@ def _distill_grad_out(desc, logits, dlogits):
 
     if dlogits is None:
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    ptr, desc.grad_stride = _rows_ptr(dlogits, logits.shape, logits.device, "dlogits", logits.dtype)
+    ptr, desc.grad_stride = _rows_ptr(dlogits, desc.rows, desc.vocab, logits.device, "dlogits", logits.dtype)
     return dlogits, ptr
 
 
 def _operator_workspace(nbytes, workspace, device, where):
-    if workspace is None:
-        if nbytes == 0:
-            raise SdtwError(STATUS_INVALID_ARG, where)
-        workspace = Workspace(nbytes, device)
-    return workspace
+    """(what keeps the workspace alive, its pointer, its size)"""
+    import torch
+
+    if workspace is not None:
+        return workspace, workspace.ptr, workspace.nbytes
+    if nbytes == 0:
+        raise SdtwError(STATUS_INVALID_ARG, where)
+    buffer = torch.empty(nbytes, dtype=torch.uint8, device=device)  # (aligned to 512 bytes by torch's allocator)
+    return buffer, buffer.data_ptr(), nbytes
 
 
 def sdtw_distill_workspace_bytes(desc):
@@ -695,14 +715,14 @@ def sdtw_distill_forward(logits, teacher_logits, teacher_ids, temperature=1.0, t
     lib = load_library()
     desc, args = _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row)
     dev = logits.device
-    workspace = _operator_workspace(lib.sdtw_distill_workspace_bytes(ctypes.byref(desc)), workspace, dev, "sdtw_distill_forward")
+    ref = ctypes.byref(desc)
+    keep, wp, wn = _operator_workspace(lib.sdtw_distill_workspace_bytes(ref), workspace, dev, "sdtw_distill_forward")
     if loss is None:
         loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
     if stats is None:
         stats = torch.empty((desc.rows, DISTILL_STATS), dtype=torch.float32, device=dev)
-    rc = lib.sdtw_distill_forward(ctypes.byref(desc), *args, _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"),
-                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), workspace.ptr,
-                                  workspace.nbytes, _stream_ptr(stream))
+    rc = lib.sdtw_distill_forward(ref, *args, _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"),
+                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), wp, wn, _stream_of(stream, dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_forward")
     return loss, stats
@@ -719,7 +739,7 @@ def sdtw_distill_backward(logits, teacher_logits, teacher_ids, stats, grad_loss=
     dev = logits.device
     dlogits, dp = _distill_grad_out(desc, logits, dlogits)
     rc = lib.sdtw_distill_backward(ctypes.byref(desc), *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
-                                   _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), dp, _stream_ptr(stream))
+                                   _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), dp, _stream_of(stream, dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_backward")
     return dlogits
@@ -733,13 +753,13 @@ def sdtw_distill_step(logits, teacher_logits, teacher_ids, grad_loss=None, tempe
     lib = load_library()
     desc, args = _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row)
     dev = logits.device
-    workspace = _operator_workspace(lib.sdtw_distill_workspace_bytes(ctypes.byref(desc)), workspace, dev, "sdtw_distill_step")
+    ref = ctypes.byref(desc)
+    keep, wp, wn = _operator_workspace(lib.sdtw_distill_workspace_bytes(ref), workspace, dev, "sdtw_distill_step")
     if loss is None:
         loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
     dlogits, dp = _distill_grad_out(desc, logits, dlogits)
-    rc = lib.sdtw_distill_step(ctypes.byref(desc), *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
-                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, workspace.ptr, workspace.nbytes,
-                               _stream_ptr(stream))
+    rc = lib.sdtw_distill_step(ref, *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
+                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, wp, wn, _stream_of(stream, dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_step")
     return loss, dlogits
@@ -799,7 +819,7 @@ def sdtw_position_bias_forward(table, plane=None, max_distance=128, two_sided=Tr
     desc.out_stride[:] = [out.stride(0), out.stride(1), out.stride(2)]
     desc.table_stride[:] = [table.stride(0), table.stride(1)]
     rc = lib.sdtw_position_bias_forward(ctypes.byref(desc), table.data_ptr(), None if plane is None else plane.data_ptr(), *args,
-                                        out.data_ptr(), _stream_ptr(stream))
+                                        out.data_ptr(), _stream_of(stream, like.device))
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_forward")
     return out
@@ -817,13 +837,13 @@ def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True,
     dev = grad.device
     desc, args = _bias_args(grad, grad.shape, grad.dtype, dev, buckets, max_distance, two_sided, offset, row_len, col_len, "grad")
     desc.plane_type = _type_of(grad, "grad")
-    workspace = _operator_workspace(lib.sdtw_position_bias_workspace_bytes(ctypes.byref(desc)), workspace, dev,
-                                    "sdtw_position_bias_backward")
+    ref = ctypes.byref(desc)
+    keep, wp, wn = _operator_workspace(lib.sdtw_position_bias_workspace_bytes(ref), workspace, dev, "sdtw_position_bias_backward")
     if dtable is None:
         dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
-    rc = lib.sdtw_position_bias_backward(ctypes.byref(desc), grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"),
-                                         *args, _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable"), workspace.ptr,
-                                         workspace.nbytes, _stream_ptr(stream))
+    rc = lib.sdtw_position_bias_backward(ref, grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"), *args,
+                                         _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable"), wp, wn,
+                                         _stream_of(stream, dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_backward")
     return dtable
@@ -851,8 +871,11 @@ def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, of
     bias = BiasDesc(desc.B // H, H, desc.N, desc.M, buckets, int(max_distance), 1 if two_sided else 0, TYPE_F32,
                     _type_of(table, "table"), 0, int(offset))
     bias.table_stride[:] = [table.stride(0), table.stride(1)]
-    workspace = _operator_workspace(lib.sdtw_biased_workspace_bytes(ctypes.byref(desc), ctypes.byref(bias)), workspace, dev,
-                                    "sdtw_forward_biased")
+    if workspace is None:
+        nbytes = sdtw_biased_workspace_bytes(desc, bias)
+        if nbytes == 0:
+            raise SdtwError(STATUS_INVALID_ARG, "sdtw_biased_workspace_bytes")
+        workspace = Workspace(nbytes, dev)
     if value is None:
         value = torch.empty(desc.B, dtype=torch.float32, device=dev)
     rc = lib.sdtw_forward_biased(ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"),

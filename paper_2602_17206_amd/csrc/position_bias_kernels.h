@@ -65,7 +65,7 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
 {
-    constexpr int W = Vec<T>::W, R = kBiasRows;
+    constexpr int W = Elem<T>::kWidth, R = kBiasRows;
     extern __shared__ __align__(16) unsigned char lds[];
     float *diag = reinterpret_cast<float *>(lds);  // [rows + cols - 1] of the tile
     int64_t id = blockIdx.x;
@@ -93,23 +93,26 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     const float *mine = diag + x * W + (rows - 1 - y * R);  // mine[w - k]: row i + k, column j + w
     const int nr = min(R, p.N - i);
     if (j + W <= p.M) {
-        Vec<T> v[R] = {};
+        Bits4 v[R] = {};
         if (in)
 #pragma unroll
-            for (int k = 0; k < R; ++k)
-                if (k < nr) v[k] = load_vec(in + (int64_t)(i + k) * p.in_stride[2] + j);
+            for (int k = 0; k < R; ++k) v[k] = load_vec<true>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + j);
         float d[W + R - 1];
 #pragma unroll
         for (int q = 0; q < W + R - 1; ++q) d[q] = mine[q - (R - 1)];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
             if (k >= nr) break;
+            float sum[W];
 #pragma unroll
-            for (int w = 0; w < W; ++w) {
-                const T sum = Elem<T>::down(Elem<T>::up(v[k].e[w]) + d[w - k + R - 1]);
-                if (i + k < rlen && j + w < clen) v[k].e[w] = sum;
+            for (int w = 0; w < W; ++w) sum[w] = Elem<T>::at(v[k], w) + d[w - k + R - 1];
+            Bits4 o = Elem<T>::pack(sum);
+            if (i + k >= rlen || j + W > clen) {
+#pragma unroll
+                for (int w = 0; w < W; ++w)
+                    if (i + k >= rlen || j + w >= clen) Elem<T>::copy(o, w, v[k]);
             }
-            store_vec(out + (int64_t)(i + k) * p.out_stride[2] + j, v[k]);
+            store_vec<false>(out + (int64_t)(i + k) * p.out_stride[2] + j, o);
         }
     } else {
         for (int k = 0; k < nr; ++k)
@@ -128,7 +131,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams p, BucketRule rule)
 {
-    constexpr int W = Vec<T>::W, R = kBiasRows, A = W + R - 1, Q = 64 * W + R - 1;
+    constexpr int W = Elem<T>::kWidth, R = kBiasRows, A = W + R - 1, Q = 64 * W + R - 1;
     __shared__ double diag[4][Q];
     __shared__ double bucket_sum[kMaxBuckets];
     int64_t id = blockIdx.x;
@@ -196,13 +199,13 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
             const int64_t j = base + 8 * s + W * lane;
             if (j + W > 0 && j < clen) {
                 if (j >= 0 && j + W <= clen && i + R <= rlen) {
-                    Vec<T> v[R];
+                    Bits4 v[R];
 #pragma unroll
-                    for (int a = 0; a < R; ++a) v[a] = load_vec(g + (int64_t)(i + a) * p.in_stride[2] + j);
+                    for (int a = 0; a < R; ++a) v[a] = load_vec<true>(g + (int64_t)(i + a) * p.in_stride[2] + j);
 #pragma unroll
                     for (int a = 0; a < R; ++a)
 #pragma unroll
-                        for (int w = 0; w < W; ++w) f[w - a + R - 1] += Elem<T>::up(v[a].e[w]);
+                        for (int w = 0; w < W; ++w) f[w - a + R - 1] += Elem<T>::at(v[a], w);
                 } else {
 #pragma unroll
                     for (int a = 0; a < R; ++a)

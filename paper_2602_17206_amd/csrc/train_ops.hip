@@ -29,11 +29,13 @@ template <typename F> void with_type(int type, F f)
         f(Bf16{});
 }
 
+int width_of(int type) { return type == SDTW_TYPE_F32 ? 4 : 8; }
+
 // ---------------------------------------------------------------- distillation
 
 struct DistillPlan {
-    int32_t slices, slice_cols, threads;       // forward
-    int32_t back_slices, back_cols;            // backward
+    int32_t slices, slice_vecs, threads;  // forward
+    int32_t back_slices, back_vecs;       // backward
     size_t off_stats, off_partial, total;
 };
 
@@ -52,25 +54,40 @@ bool distill_ok(const sdtw_distill_desc *d)
     return d->logit_stride <= most / rows && d->grad_stride <= most / rows && d->teacher_stride <= most / rows && d->id_stride <= most / rows;
 }
 
-// Columns of a slice when `rows` rows are shared by about `want` workgroups, none with fewer than `least` columns.
-int32_t slice_columns(int64_t rows, int64_t vocab, int64_t want, int64_t least, int64_t most)
+// Vectors of a slice when `rows` rows of `vecs` vectors are shared by about `want` workgroups, none with fewer than `least`.
+int32_t slice_vectors(int64_t rows, int64_t vecs, int64_t want, int64_t least, int64_t most)
 {
     const int64_t per_row = std::max<int64_t>(1, (want + rows - 1) / rows);
-    int64_t cols = (vocab + per_row - 1) / per_row;
-    cols = std::min(std::max(cols, least), most);
-    return (int32_t)((cols + 7) / 8 * 8);
+    const int64_t n = (vecs + per_row - 1) / per_row;
+    return (int32_t)((std::min(std::max(n, least), most) + 7) / 8 * 8);
 }
 
 DistillPlan distill_plan(const sdtw_distill_desc *d)
 {
     DistillPlan P{};
-    const int64_t rows = std::max(d->rows, 1);
-    // (a slice's marks are one bit a column in LDS: at most 32 KB)
-    P.slice_cols = slice_columns(rows, d->vocab, 512, 4096, 1 << 18);
-    P.slices = (d->vocab + P.slice_cols - 1) / P.slice_cols;
-    P.threads = P.slice_cols >= 16384 ? 512 : 256;
-    P.back_cols = slice_columns(rows, d->vocab, 1024, 4096, 1 << 18);
-    P.back_slices = (d->vocab + P.back_cols - 1) / P.back_cols;
+    const int W = width_of(d->logit_type);
+    const int64_t rows = std::max(d->rows, 1), vecs = (d->vocab + W - 1) / W + 1;  // (a row may begin inside a vector)
+    // Many rows: a workgroup each, of one streaming wavefront up to 2048 vectors, three up to 16384, then four, next to the
+    // one for the slots.  (One / three / four of them: 33 / 47 / 72 us at 16384 x 1000 float32, 55 / 54 / 56 at 4096 x 32768
+    // bfloat16, 452 / 350 / 338 at 8192 x 131072.)
+    // Fewer than 512: up to fifteen, so that a row is on its way at once: 8.8 us at 1 x 32768 bfloat16, 15.3 at 400 x 32768,
+    // 19.7 at 200 x 100000 float32; slices of a row and a second kernel that joins them took 13.7, 20.0 and 29.5.
+    // Slices are for the few long rows (1 x 131072 bfloat16 13.8 us against 15.6), and for those whose marks - one bit an
+    // element in LDS - would take more than 32 KB.
+    const int64_t most = (1 << 18) / W;
+    if (rows >= 512) {
+        P.slice_vecs = slice_vectors(1, vecs, 1, 1, most);
+        P.threads = 64 * (P.slice_vecs < 2048 ? 2 : P.slice_vecs < 16384 ? 4 : 5);
+    } else if (rows >= 64 || vecs < 16384) {
+        P.slice_vecs = slice_vectors(1, vecs, 1, 1, most);
+        P.threads = 64 * (int)std::min<int64_t>(16, 1 + (P.slice_vecs + 127) / 128);
+    } else {
+        P.slice_vecs = slice_vectors(rows, vecs, 512, 512, most);
+        P.threads = 64 * 2;
+    }
+    P.slices = (int32_t)((vecs + P.slice_vecs - 1) / P.slice_vecs);
+    P.back_vecs = slice_vectors(rows, vecs, 1024, 512, 1 << 20);
+    P.back_slices = (int32_t)((vecs + P.back_vecs - 1) / P.back_vecs);
     size_t o = 0;
     P.off_stats = o;
     o = align_up(o + (size_t)rows * sizeof(RowStats), 256);
@@ -97,6 +114,7 @@ DistillParams distill_params(const sdtw_distill_desc *d, const void *logits, con
     p.inv_temperature_d = 1.0 / (double)d->temperature;
     p.inv_temperature = (float)p.inv_temperature_d;
     p.scale2 = (float)(1.4426950408889634 * p.inv_temperature_d);
+    p.student_inv_temperature = (double)p.scale2 * kLn2;
     p.logit_stride = d->logit_stride; p.grad_stride = d->grad_stride;
     p.teacher_stride = d->teacher_stride; p.id_stride = d->id_stride;
     p.logits = logits; p.teacher_logits = teacher_logits; p.teacher_ids = teacher_ids;
@@ -104,16 +122,24 @@ DistillParams distill_params(const sdtw_distill_desc *d, const void *logits, con
     return p;
 }
 
-void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, hipStream_t st)
+void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, bool stream, hipStream_t st)
 {
     p.slices = P.slices;
-    p.slice_cols = P.slice_cols;
+    p.slice_vecs = P.slice_vecs;
     const size_t slots = (size_t)p.top * 12;
-    const size_t marks = ((size_t)std::min(p.vocab, P.slice_cols) + 31) / 32 * 4;
+    const int W = width_of(type);
+    const size_t marks = ((size_t)std::min((p.vocab + W - 1) / W + 1, P.slice_vecs) * W + 31) / 32 * 4;
+    const unsigned grid = (unsigned)(p.rows * (int64_t)P.slices);
     {
         ProfScope ps("distill_forward", st);
         with_type(type, [&](auto t) {
-            distill_forward_kernel<decltype(t)><<<(unsigned)(p.rows * (int64_t)P.slices), P.threads, slots + marks, st>>>(p);
+            using T = decltype(t);
+            if (P.threads > 320)  // (few rows)
+                distill_forward_kernel<T, true, 1024><<<grid, P.threads, slots + marks, st>>>(p);
+            else if (stream)
+                distill_forward_kernel<T, true, 320><<<grid, P.threads, slots + marks, st>>>(p);
+            else
+                distill_forward_kernel<T, false, 320><<<grid, P.threads, slots + marks, st>>>(p);
         });
     }
     if (P.slices > 1) {
@@ -125,10 +151,51 @@ void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, hip
 void launch_distill_backward(const DistillPlan &P, DistillParams p, int type, hipStream_t st)
 {
     p.slices = P.back_slices;
-    p.slice_cols = P.back_cols;
+    p.slice_vecs = P.back_vecs;
     ProfScope ps("distill_backward", st);
     with_type(type, [&](auto t) {
         distill_backward_kernel<decltype(t)><<<(unsigned)(p.rows * (int64_t)P.back_slices), 256, 0, st>>>(p);
+    });
+}
+
+// The shape of the one-read kernel: vectors a thread and wavefronts, or 0 for rows that are too long.  Four vectors a thread for
+// short rows, eight for others (4 / 8: 44 / 49 us at 16384 x 1000 float32, 77 / 63 at 8192 x 8000 bfloat16, 92 / 87 at
+// 4096 x 24000), and twelve where only they hold a row of float32.
+struct RowsShape { int vectors, waves, per_simd; };
+RowsShape rows_shape(const sdtw_distill_desc *d, const void *logits)
+{
+    const int W = width_of(d->logit_type), size = 16 / W;
+    // (rows that begin anywhere may take one vector more)
+    const bool aligned = (reinterpret_cast<uintptr_t>(logits) % 16 == 0) && d->logit_stride * size % 16 == 0;
+    const int64_t vecs = ((int64_t)d->vocab + (aligned ? W - 1 : 2 * W - 2)) / W;
+    auto waves = [&](int nv) { return 1 + (int)std::min<int64_t>(99, (vecs + 64 * nv - 1) / (64 * nv)); };
+    if (vecs <= 512) return {4, waves(4), 5};
+    if (waves(8) <= 16) return {8, waves(8), W == 4 ? 5 : 4};
+    if (W == 4 && waves(12) <= 16) return {12, waves(12), 4};
+    return {0, 0, 0};
+}
+
+// LDS of the one-read kernel for a row's slots and marks (one for every element that the workgroup holds)
+int rows_ring_bytes(const sdtw_distill_desc *d, RowsShape s)
+{
+    return (d->top * 12 + (s.waves - 1) * s.vectors * 8 * width_of(d->logit_type) + 15) / 16 * 16;
+}
+
+void launch_distill_rows(const sdtw_distill_desc *d, RowsShape s, const DistillParams &p, hipStream_t st)
+{
+    const int ring = rows_ring_bytes(d, s);
+    const int resident = 256 * std::max(1, s.per_simd * 4 / s.waves);
+    const unsigned grid = (unsigned)std::min(p.rows, resident), threads = 64 * s.waves;
+    ProfScope ps("distill_rows", st);
+    with_type(d->logit_type, [&](auto t) {
+        using T = decltype(t);
+        constexpr bool wide = sizeof(T) == 4;
+        if (s.vectors == 4)
+            distill_rows_kernel<T, 4, 5><<<grid, threads, 3 * ring, st>>>(p, ring);
+        else if (s.vectors == 8)
+            distill_rows_kernel<T, 8, wide ? 5 : 4><<<grid, threads, 3 * ring, st>>>(p, ring);
+        else if constexpr (wide)
+            distill_rows_kernel<T, 12, 4><<<grid, threads, 3 * ring, st>>>(p, ring);
     });
 }
 
@@ -233,8 +300,6 @@ BiasParams bias_params(const sdtw_bias_desc *d, const void *in, const int32_t *o
     p.offsets = offsets; p.row_len = row_len; p.col_len = col_len;
     return p;
 }
-
-int width_of(int type) { return type == SDTW_TYPE_F32 ? 4 : 8; }
 
 // How the backward pass is split: strips of diagonals, then the batch, then the way down a strip.
 struct BiasPlan { int64_t strips, first_col, batch_per_part, batch_parts, steps_per_part, step_parts, parts; };
@@ -356,7 +421,7 @@ int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, cons
     p.loss = loss;
     p.stats = reinterpret_cast<RowStats *>(stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
-    launch_distill_forward(P, p, desc->logit_type, static_cast<hipStream_t>(stream));
+    launch_distill_forward(P, p, desc->logit_type, true, static_cast<hipStream_t>(stream));
     return hip_ok();
 }
 
@@ -398,7 +463,15 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
     p.stats = reinterpret_cast<RowStats *>(static_cast<char *>(workspace) + P.off_stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    launch_distill_forward(P, p, desc->logit_type, st);
+    const RowsShape shape = rows_shape(desc, logits);
+    if (shape.vectors > 0 && desc->top <= kRowsTop) {
+        launch_distill_rows(desc, shape, p, st);
+        return hip_ok();
+    }
+    // Two passes.  Up to twice the memory-side cache of 256 MB the first one reads without the streaming hint, and the second
+    // finds part of it there: 140 against 151 us at 1024 x 131072 bfloat16; at 8192 x 65536 (1 GB) 609 against 576.
+    const int64_t bytes = (int64_t)desc->rows * desc->vocab * (16 / width_of(desc->logit_type));
+    launch_distill_forward(P, p, desc->logit_type, bytes > (int64_t)512 << 20, st);
     launch_distill_backward(P, p, desc->logit_type, st);
     return hip_ok();
 }
