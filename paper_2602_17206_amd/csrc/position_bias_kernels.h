@@ -1,9 +1,8 @@
 // A learned relative position bias by buckets on planes [B, H, N, M], and the gradient of its table.
 //
 // The bias depends on the diagonal j - i alone.  Forward: a tile's diagonals are looked up once, into LDS, and
-// every row of the tile reads the same values one place further left.  Backward: a wavefront walks down a strip of
-// neighbouring diagonals - 8 rows and 8 columns further with every step - so that a diagonal's sum stays in one
-// register the whole way and the memory is read in whole aligned-as-it-comes vectors; buckets come in at the end.
+// every row of the tile reads the same values one place further left.  Backward: the plane is read once in tiles of whole
+// cache lines and summed up by diagonals; buckets, which are runs of neighbouring diagonals, come in at the end.
 #pragma once
 #include "vector_io.h"
 
@@ -11,24 +10,28 @@ namespace sdtw {
 
 constexpr int kMaxBuckets = 256;
 
-// The buckets of a side: distances below e one by one, bucket e + k from start[k] on.
+// The buckets of a side: distances below e one by one, bucket e + k from start[k] on (start[m]: beyond every distance).
 struct BucketRule {
     int32_t n, e, m, two_sided;
-    int32_t start[kMaxBuckets / 2];
-    __device__ __forceinline__ int side(int d) const
-    {
-        if (d < e) return d;
-        int b = e - 1;
-        for (int k = 0; k < m; ++k) b += d >= start[k];
-        return b;
-    }
-    __device__ __forceinline__ int bucket(int r) const
-    {
-        if (two_sided) return side(r < 0 ? -r : r) + (r > 0 ? n : 0);
-        return side(r < 0 ? -r : 0);
-    }
+    float per_octave, shift;  // bucket e + k is about per_octave * log2(d) + shift
+    int32_t start[kMaxBuckets / 2 + 1];
     // first distance of bucket u of a side; of bucket n: beyond every distance
-    __device__ __forceinline__ int first(int u) const { return u < e ? u : (u < n ? start[u - e] : 0x7fffffff); }
+    __device__ __forceinline__ int first(int u) const { return u < e ? u : start[u - e]; }
+    // The bucket of j - i - offset = r; `starts`: start[] in LDS.  The logarithm is a guess that the whole numbers correct:
+    // it is off by less than a distance's rounding, so by one bucket at most where buckets are wider than that, and the
+    // loops end at the right one in any case.
+    __device__ __forceinline__ int bucket(int r, const int32_t *starts) const
+    {
+        const int d = two_sided ? (r < 0 ? -r : r) : (r < 0 ? -r : 0);
+        int u = d;
+        if (d >= e) {
+            int k = min(max((int)(__builtin_amdgcn_logf((float)d) * per_octave + shift), 0), m - 1);
+            while (d < starts[k]) --k;
+            while (d >= starts[k + 1]) ++k;
+            u = e + k;
+        }
+        return two_sided && r > 0 ? u + n : u;
+    }
 };
 
 struct BiasParams {
@@ -44,12 +47,16 @@ struct BiasParams {
     float *dtable;
     // forward: tiles of (256 / ty * width) columns and ty * 8 rows
     int32_t tx, col_tiles, row_tiles;
-    // backward: strips of diagonals, parts of the batch, parts of the way down
-    int32_t strips, first_col, batch_parts, batch_per_part, step_parts, steps_per_part, parts;
+    // backward: tiles of `across` times 64 * width columns and 4 / across times 64 rows (col_tiles as above), parts of the batch
+    int32_t tiles, across, batch_parts, batch_per_part, parts;
     double *partial;  // [H][buckets][parts]
 };
 
 constexpr int kBiasRows = 8;
+
+// A wavefront's accesses to LDS are carried out in the order of their issue.  Where one lane's place is another lane's before or
+// after, this keeps the compiler from changing that order.
+__device__ __forceinline__ void wavefront_order() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
 __device__ __forceinline__ int clamp_len(const int32_t *len, int b, int full) { return len ? min(max(len[b], 0), full) : full; }
 
@@ -62,11 +69,15 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
     return p.penalty && v < 0.0f ? 0.0f : v;
 }
 
+// Bound by reading and writing the plane: 8 x 16 x 1100 x 937 float16 takes 98 us (5.4 TB/s both ways together), 32 x 1 x 1024 x
+// 1024 float32 46 us (5.8 TB/s); a single row, 32 x 16 x 1 x 4097 bfloat16, 11 us, bound by the way from table to LDS to row.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
 {
     constexpr int W = Elem<T>::kWidth, R = kBiasRows;
     extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ int32_t starts[kMaxBuckets / 2 + 1];
+    __shared__ float values[kMaxBuckets];
     float *diag = reinterpret_cast<float *>(lds);  // [rows + cols - 1] of the tile
     int64_t id = blockIdx.x;
     const int ct = (int)(id % p.col_tiles);
@@ -78,12 +89,13 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     const int j0 = ct * cols, i0 = rt * rows;
     const int64_t offset = p.offsets ? (int64_t)p.offsets[b] : p.offset;
     const int rlen = clamp_len(p.row_len, b, p.N), clen = clamp_len(p.col_len, b, p.M);
+    for (int u = threadIdx.x; u < p.buckets; u += 256) values[u] = load_bias(p, h, u);
+    for (int k = threadIdx.x; k <= rule.m; k += 256) starts[k] = rule.start[k];
+    __syncthreads();
     // diag[q] is the bias at j - i = j0 - (i0 + rows - 1) + q
     const int nd = min(cols, p.M - j0) + rows - 1;
-    for (int q = threadIdx.x; q < nd; q += 256) {
-        const int u = rule.bucket(clamp_rel((int64_t)j0 - (i0 + rows - 1) + q - offset));
-        diag[q] = load_bias(p, h, u);
-    }
+    for (int q = rows - min(rows, p.N - i0) + threadIdx.x; q < nd; q += 256)
+        diag[q] = values[rule.bucket(clamp_rel((int64_t)j0 - (i0 + rows - 1) + q - offset), starts)];
     __syncthreads();
     const int x = threadIdx.x % p.tx, y = threadIdx.x / p.tx;
     const int j = j0 + x * W, i = i0 + y * R;
@@ -124,84 +136,107 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     }
 }
 
-// One strip of 64 * W + 7 diagonals, one part of the batch, one part of the way down, four wavefronts in turn.
-// Step s covers rows 8 s .. 8 s + 7; lane l reads W columns from base + 8 s + W l on, so that element (a, w) of its
-// patch lies on diagonal j - i = base + W l + w - a whatever s is: W + 7 sums per lane.  They are carried in float32 over
-// at most 16 steps (128 terms) and in float64 beyond.
+// One tile of the plane, for a part of the batch.  A wavefront takes 64 rows of 64 * W columns, 8 rows at a time: lane l reads W
+// columns of each (whole cache lines from row to row), and element (a, w) of its patch lies on diagonal w - a of it: W + 7 sums
+// in registers.  The next 8 rows move every diagonal 8 places on, so 8 of the sums are complete and go to the wavefront's diagonals
+// in LDS (different places in all lanes, W of them at a time), and the others stay.  Float32 up to there: at most 64 terms; what
+// a pass leaves there is added up in float64, scaled, and the buckets - neighbouring diagonals - are summed at the end.
+// Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.40 ms (6.1 TB/s), 4 x 16 x 2048 x 2048 bfloat16 100 us
+// (5.4 TB/s).  A walk along the diagonals, whose sums stay in registers the whole way, took 1.46 ms and 127 us: its rows'
+// loads begin one place further on from row to row, so hardly any of them is whole cache lines.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams p, BucketRule rule)
 {
-    constexpr int W = Elem<T>::kWidth, R = kBiasRows, A = W + R - 1, Q = 64 * W + R - 1;
+    constexpr int W = Elem<T>::kWidth, R = kBiasRows, A = W + R - 1, Z = 64 + R - W, Q = 64 * W + Z;
+    typedef float Float4 __attribute__((ext_vector_type(4)));
+    __shared__ __align__(16) float pass_sum[4][Q];  // each wavefront's own
     __shared__ double diag[4][Q];
     __shared__ double bucket_sum[kMaxBuckets];
     int64_t id = blockIdx.x;
-    const int strip = (int)(id % p.strips);
-    id /= p.strips;
-    const int sp = (int)(id % p.step_parts);
-    id /= p.step_parts;
+    const int tile = (int)(id % p.tiles);
+    id /= p.tiles;
     const int bp = (int)(id % p.batch_parts), h = (int)(id / p.batch_parts);
-    const int part = (bp * p.step_parts + sp) * p.strips + strip;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int64_t base = p.first_col + (int64_t)strip * (64 * W);
+    const int part = bp * p.tiles + tile;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    // the tile's four wavefronts: `across` side by side, the others below
+    const int across = p.across, down = 4 / across;
+    const auto row_of = [&](int w) { return (tile / p.col_tiles * down + w / across) * 64; };
+    const auto col_of = [&](int w) { return (tile % p.col_tiles * across + w % across) * (64 * W); };
+    const int i0 = row_of(wave), j0 = col_of(wave), j = j0 + W * lane;
     const int b0 = bp * p.batch_per_part, b1 = min(p.B, b0 + p.batch_per_part);
     for (int u = threadIdx.x; u < p.buckets; u += 256) bucket_sum[u] = 0.0;
-    double acc[A];
-#pragma unroll
-    for (int k = 0; k < A; ++k) acc[k] = 0.0;
+    for (int q = lane; q < Q; q += 64) {
+        diag[wave][q] = 0.0;
+        pass_sum[wave][q] = 0.0f;
+    }
+    wavefront_order();
+    // place q of a wavefront's diagonals is the difference j - i = col - row - Z + q
     auto to_buckets = [&](int64_t offset) {
-        // the lanes' sums by diagonal: W of them at a time, which are W different places in every lane
-        for (int q = lane; q < Q; q += 64) diag[wave][q] = 0.0;
         __syncthreads();
-#pragma unroll
-        for (int k0 = 0; k0 < A; k0 += W) {
-#pragma unroll
-            for (int k = k0; k < k0 + W && k < A; ++k) diag[wave][W * lane + k] += acc[k];
-            __syncthreads();
+        int64_t lowest = (int64_t)1 << 62, highest = -lowest;
+        for (int w = 0; w < 4; ++w) {
+            lowest = min(lowest, (int64_t)col_of(w) - row_of(w) - Z - offset);
+            highest = max(highest, (int64_t)col_of(w) - row_of(w) - Z - offset + Q - 1);
         }
-        // diagonal q is r = lowest + q; a bucket's are neighbours
-        const int64_t lowest = base - (R - 1) - offset;
-        for (int u = wave; u < p.buckets; u += 4) {
+        for (int u0 = 0; u0 < p.buckets; u0 += 64) {
+            // a bucket's differences lo .. hi are neighbours; lane l looks at bucket u0 + l
+            const int u = u0 + lane;
             const bool right = rule.two_sided && u >= rule.n;
-            const int64_t d0 = rule.first(right ? u - rule.n : u), d1 = (int64_t)rule.first((right ? u - rule.n : u) + 1) - 1;
-            int64_t lo, hi;
-            if (right) {
-                lo = max(d0, (int64_t)1);
-                hi = d1 >= 0x7ffffffe ? (int64_t)1 << 62 : d1;
-            } else {
-                hi = !rule.two_sided && u == 0 ? (int64_t)1 << 62 : -d0;
-                lo = d1 >= 0x7ffffffe ? -((int64_t)1 << 62) : -d1;
+            const int side = right ? u - rule.n : u;
+            int64_t lo = 1, hi = 0;
+            if (u < p.buckets) {
+                const int64_t d0 = rule.first(side), d1 = (int64_t)rule.first(side + 1) - 1, end = (int64_t)1 << 62;
+                const bool open = d1 >= 0x7ffffffe;
+                lo = right ? max(d0, (int64_t)1) : open ? -end : -d1;
+                hi = right ? (open ? end : d1) : !rule.two_sided && u == 0 ? end : -d0;
             }
-            const int64_t qa = max(lo - lowest, (int64_t)0), qb = min(hi - lowest, (int64_t)Q - 1);
-            if (qa > qb) continue;
-            double s = 0.0;
-            for (int q = (int)qa + lane; q <= (int)qb; q += 64) s += (diag[0][q] + diag[1][q]) + (diag[2][q] + diag[3][q]);
-            s = wave_sum_f64(s);
-            if (lane == 0) bucket_sum[u] += s;
+            lo = max(lo, lowest);
+            hi = min(hi, highest);
+            const int from = (int)(lo - lowest), to = (int)(hi - lowest);
+            unsigned long long some = __ballot(lo <= hi);
+            for (int turn = 0; some != 0; ++turn, some &= some - 1) {
+                if ((turn & 3) != wave) continue;
+                const int l = __builtin_ctzll(some);
+                const int qa = __builtin_amdgcn_readlane(from, l), qb = __builtin_amdgcn_readlane(to, l);
+                double s = 0.0;
+                for (int w = 0; w < 4; ++w) {
+                    const int shift = (int)((int64_t)col_of(w) - row_of(w) - Z - offset - lowest);
+                    for (int q = max(qa - shift, 0) + lane; q <= min(qb - shift, Q - 1); q += 64) s += diag[w][q];
+                }
+                s = wave_sum_f64(s);
+                if (lane == 0) bucket_sum[u0 + l] += s;
+            }
         }
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < A; ++k) acc[k] = 0.0;
     };
     for (int b = b0; b < b1; ++b) {
         const int rlen = clamp_len(p.row_len, b, p.N), clen = clamp_len(p.col_len, b, p.M);
         const T *g = static_cast<const T *>(p.in) + b * p.in_stride[0] + h * p.in_stride[1];
         const double scale = p.scale ? (double)p.scale[p.scale_heads ? (int64_t)b * p.H + h : b] : 1.0;
-        // the steps at which the strip touches the columns [0, clen) and the rows [0, rlen)
-        const int64_t from = max((int64_t)sp * p.steps_per_part, base + 64 * W >= 0 ? (int64_t)0 : (-base - 64 * W) / 8);
-        const int64_t past_cols = clen - base <= 0 ? 0 : (clen - base + 7) / 8;
-        const int64_t to = min(min((int64_t)(sp + 1) * p.steps_per_part, (int64_t)((rlen + 7) / 8)), past_cols);
+        const int steps = j0 < clen ? min((rlen - i0 + R - 1) / R, 64 / R) : 0;
+        // A vector that hangs over the row's end is read further in and shifted, zeros coming in (rows shorter than one: by element).
+        const int jc = min(j, clen - W);
         float f[A];
 #pragma unroll
         for (int k = 0; k < A; ++k) f[k] = 0.0f;
-        int held = 0;
-        for (int64_t s = from + wave; s < to; s += 4) {
-            const int i = (int)(8 * s);
-            const int64_t j = base + 8 * s + W * lane;
-            if (j + W > 0 && j < clen) {
-                if (j >= 0 && j + W <= clen && i + R <= rlen) {
-                    Bits4 v[R];
+        float *sums = pass_sum[wave] + W * lane + (Z - R + W);  // (the last step's are at W * lane: none lie before the first)
+        for (int s = 0; s <= steps; ++s, sums -= R) {
+            if (s < steps) {
+                const int i = i0 + R * s;
+                Bits4 v[R];
+                if (clen >= W) {
 #pragma unroll
-                    for (int a = 0; a < R; ++a) v[a] = load_vec<true>(g + (int64_t)(i + a) * p.in_stride[2] + j);
+                    for (int a = 0; a < R; ++a) v[a] = load_vec<true>(g + (int64_t)min(i + a, rlen - 1) * p.in_stride[2] + jc);
+                    if (j0 + 64 * W > clen) {
+                        const int shift = min(j - jc, W) * 8 * (int)sizeof(T);
+#pragma unroll
+                        for (int a = 0; a < R; ++a) v[a] = shift < 128 ? shift_vec(v[a], shift) : Bits4{};
+                    }
+                    if (i + R > rlen) {
+#pragma unroll
+                        for (int a = 0; a < R; ++a)
+                            if (i + a >= rlen) v[a] = Bits4{};
+                    }
 #pragma unroll
                     for (int a = 0; a < R; ++a)
 #pragma unroll
@@ -210,25 +245,38 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
 #pragma unroll
                     for (int a = 0; a < R; ++a)
 #pragma unroll
-                        for (int w = 0; w < W; ++w)
-                            if (i + a < rlen && j + w >= 0 && j + w < clen)
-                                f[w - a + R - 1] += Elem<T>::up(g[(int64_t)(i + a) * p.in_stride[2] + j + w]);
+                        for (int w = 0; w < W; ++w) {
+                            const float x = Elem<T>::up(g[(int64_t)min(i + a, rlen - 1) * p.in_stride[2] + min(j + w, clen - 1)]);
+                            f[w - a + R - 1] += i + a < rlen && j + w < clen ? x : 0.0f;
+                        }
                 }
             }
-            if (++held == 16) {
+            // sums W - 1 .. W + 6 are complete; those below are W - 1 .. of the next rows' patch
+            // (float4 at a time; with W = 4 the second four are the next lane's first ones, after it has stored them)
 #pragma unroll
-                for (int k = 0; k < A; ++k) {
-                    acc[k] += scale * (double)f[k];
-                    f[k] = 0.0f;
-                }
-                held = 0;
+            for (int k0 = 0; k0 < R; k0 += 4) {
+                Float4 *at = reinterpret_cast<Float4 *>(sums + k0);
+                Float4 x = *at;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[k] += f[W - 1 + k0 + k];
+                *at = x;
+                wavefront_order();
             }
+#pragma unroll
+            for (int k = A - 1; k >= R; --k) f[k] = f[k - R];
+#pragma unroll
+            for (int k = 0; k < R; ++k) f[k] = 0.0f;
         }
-#pragma unroll
-        for (int k = 0; k < A; ++k) acc[k] += scale * (double)f[k];
-        if (p.offsets) to_buckets((int64_t)p.offsets[b]);  // (every sequence has its own diagonals' buckets)
+        for (int q = lane; q < Q; q += 64) {
+            diag[wave][q] += scale * (double)pass_sum[wave][q];
+            pass_sum[wave][q] = 0.0f;
+        }
+        wavefront_order();
+        if (p.offsets) {  // (every sequence has its own diagonals' buckets)
+            to_buckets((int64_t)p.offsets[b]);
+            for (int q = lane; q < Q; q += 64) diag[wave][q] = 0.0;
+        }
     }
-    __syncthreads();
     if (!p.offsets) to_buckets(p.offset);
     for (int u = threadIdx.x; u < p.buckets; u += 256) p.partial[((int64_t)h * p.buckets + u) * p.parts + part] = bucket_sum[u];
 }

@@ -102,6 +102,14 @@ template <bool STREAM, typename T> __device__ __forceinline__ void store_vec(T *
         *q = b;
 }
 
+// The vector moved down (shift > 0) or up by a number of bits below 128, zeros coming in.
+__device__ __forceinline__ Bits4 shift_vec(const Bits4 &v, int shift)
+{
+    unsigned __int128 x = __builtin_bit_cast(unsigned __int128, v);
+    x = shift >= 0 ? x >> shift : x << -shift;
+    return __builtin_bit_cast(Bits4, x);
+}
+
 // The same at a byte offset from a row's start, for a row that all lanes share: its address goes into scalar registers, and the
 // offset alone takes a vector register.
 typedef __attribute__((address_space(1))) Bits4Any GlobalBits4;
