@@ -104,11 +104,18 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     T *out = static_cast<T *>(p.out) + b * p.out_stride[0] + h * p.out_stride[1];
     const float *mine = diag + x * W + (rows - 1 - y * R);  // mine[w - k]: row i + k, column j + w
     const int nr = min(R, p.N - i);
-    if (j + W <= p.M) {
+    if (p.M >= W) {
         Bits4 v[R] = {};
-        if (in)
+        if (in) {
+            // a vector that hangs over the row's end is read further in and shifted (what it saw of its neighbours goes out)
+            const int jc = min(j, p.M - W);
 #pragma unroll
-            for (int k = 0; k < R; ++k) v[k] = load_vec<true>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + j);
+            for (int k = 0; k < R; ++k) v[k] = load_vec<true>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + jc);
+            if (jc != j) {
+#pragma unroll
+                for (int k = 0; k < R; ++k) v[k] = shift_vec(v[k], (j - jc) * 8 * (int)sizeof(T));
+            }
+        }
         float d[W + R - 1];
 #pragma unroll
         for (int q = 0; q < W + R - 1; ++q) d[q] = mine[q - (R - 1)];
@@ -124,7 +131,14 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
                 for (int w = 0; w < W; ++w)
                     if (i + k >= rlen || j + w >= clen) Elem<T>::copy(o, w, v[k]);
             }
-            store_vec<false>(out + (int64_t)(i + k) * p.out_stride[2] + j, o);
+            T *to = out + (int64_t)(i + k) * p.out_stride[2] + j;
+            if (j + W <= p.M) {
+                store_vec<false>(to, o);
+            } else {
+#pragma unroll
+                for (int w = 0; w < W - 1; ++w)
+                    if (j + w < p.M) to[w] = element<T>(o, w);
+            }
         }
     } else {
         for (int k = 0; k < nr; ++k)

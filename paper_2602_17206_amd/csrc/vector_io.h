@@ -85,6 +85,14 @@ template <> struct Elem<Bf16> {
     static __device__ __forceinline__ void copy(Bits4 &b, int e, const Bits4 &from) { copy_half(b, e, from); }
 };
 
+// element e of a vector, as it is
+template <typename T> __device__ __forceinline__ T element(const Bits4 &b, int e)
+{
+    const uint32_t v = b[sizeof(T) == 4 ? e : e >> 1];  // (a bit cast of b[e] itself is taken of element 0 by this compiler)
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, v);
+    else return __builtin_bit_cast(T, (uint16_t)(e & 1 ? v >> 16 : v));
+}
+
 // STREAM: the non-temporal hint, for data that is used once.  Reading 4 GiB takes 7.1 TB/s with it and 6.2 without; copying
 // 5.6 and 5.4 from and to whole cache lines, but 4.6 and 5.2 where rows start at odd 2-byte elements (half-written lines).
 template <bool STREAM, typename T> __device__ __forceinline__ Bits4 load_vec(const T *p)
