@@ -519,6 +519,36 @@ def test_operators_in_a_graph(T):
         assert torch.equal(loss, want[0]) and torch.equal(dz, want[1]) and torch.equal(out, want_b) and torch.equal(dt, want_t), i
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+def test_bias_in_place_where_rows_end_inside_a_vector(kind):
+    """Every thread writes the cells that are its own, whatever it reads of its neighbours' for the row's end."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    table = torch.randn((2, 32), generator=gen, device="cuda")
+    for M in (3, 9, 257, 513, 937, 1026, 2049):
+        plane = torch.randn((3, 2, 67, M), generator=gen, device="cuda").to(TYPES[kind])
+        at = torch.from_numpy(bucket_matrix(67, M, 32, 128, True, 0)).cuda()
+        want = (plane.float() + table[:, at]).to(plane.dtype)
+        for _ in range(3):
+            room = plane.clone()
+            pkg.sdtw_position_bias_forward(table, room, out=room)
+            assert torch.equal(room, want), M
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+def test_the_same_inputs_give_the_same_bits(kind):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    plane = torch.randn((2, 2, 777, 2051), generator=gen, device="cuda").to(TYPES[kind])
+    s = problem(300, 20011, 40, kind, True, 1.3, 5)
+    first = None
+    for _ in range(5):
+        loss, dz = pkg.sdtw_distill_step(s["z"], s["t"], s["ids"], teacher_lse=s["lse"])
+        loss_f, stats = pkg.sdtw_distill_forward(s["z"], s["t"], s["ids"], teacher_lse=s["lse"])
+        dz_f = pkg.sdtw_distill_backward(s["z"], s["t"], s["ids"], stats, teacher_lse=s["lse"])
+        got = [loss, dz, loss_f, dz_f, pkg.sdtw_position_bias_backward(plane, 32)]
+        first = first or got
+        assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
 def test_refusals_of_the_binding():
     s = problem(4, 50, 5, "f32", False, 1.0, 1)
     z, t, ids = s["z"], s["t"], s["ids"]
