@@ -6,6 +6,8 @@
 #pragma once
 #include "vector_io.h"
 
+#include <type_traits>
+
 namespace sdtw {
 
 constexpr int kMaxBuckets = 256;
@@ -60,6 +62,14 @@ __device__ __forceinline__ void wavefront_order() { __builtin_amdgcn_fence(__ATO
 
 __device__ __forceinline__ int clamp_len(const int32_t *len, int b, int full) { return len ? min(max(len[b], 0), full) : full; }
 
+// The workgroup's number, renumbered so that neighbouring tiles are on one XCD (workgroups go round the eight of them).  Reading
+// 32 planes of 8192 x 8192 float32 in tiles of 64 x 1024 runs at 6.7 TB/s so, and at 6.3 with the tiles dealt out in turn.
+__device__ __forceinline__ int neighbours_together()
+{
+    const int id = blockIdx.x, n = gridDim.x / 8;
+    return id < 8 * n ? id % 8 * n + id / 8 : id;
+}
+
 // a position difference as 32 bits: beyond 2^30 every distance is in the last bucket
 __device__ __forceinline__ int clamp_rel(int64_t r) { return (int)min(max(r, (int64_t) - (1 << 30)), (int64_t)1 << 30); }
 
@@ -69,7 +79,8 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
     return p.penalty && v < 0.0f ? 0.0f : v;
 }
 
-// Bound by reading and writing the plane: 8 x 16 x 1100 x 937 float16 takes 98 us (5.4 TB/s both ways together), 32 x 1 x 1024 x
+// Bound by reading and writing the plane: 8 x 16 x 1100 x 936 float16 takes 96 us (5.5 TB/s both ways together), 937 columns,
+// whose rows begin and end inside vectors, 115 us, 32 x 1 x 1024 x
 // 1024 float32 46 us (5.8 TB/s); a single row, 32 x 16 x 1 x 4097 bfloat16, 11 us, bound by the way from table to LDS to row.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
@@ -104,14 +115,14 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     T *out = static_cast<T *>(p.out) + b * p.out_stride[0] + h * p.out_stride[1];
     const float *mine = diag + x * W + (rows - 1 - y * R);  // mine[w - k]: row i + k, column j + w
     const int nr = min(R, p.N - i);
-    if (p.M >= W) {
+    auto patch = [&](auto whole) {
         Bits4 v[R] = {};
         if (in) {
             // a vector that hangs over the row's end is read further in and shifted (what it saw of its neighbours goes out)
-            const int jc = min(j, p.M - W);
+            const int jc = whole ? j : p.M - W;
 #pragma unroll
             for (int k = 0; k < R; ++k) v[k] = load_vec<true>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + jc);
-            if (jc != j) {
+            if (!whole) {
 #pragma unroll
                 for (int k = 0; k < R; ++k) v[k] = shift_vec(v[k], (j - jc) * 8 * (int)sizeof(T));
             }
@@ -132,7 +143,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
                     if (i + k >= rlen || j + w >= clen) Elem<T>::copy(o, w, v[k]);
             }
             T *to = out + (int64_t)(i + k) * p.out_stride[2] + j;
-            if (j + W <= p.M) {
+            if (whole) {
                 store_vec<false>(to, o);
             } else {
 #pragma unroll
@@ -140,6 +151,11 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
                     if (j + w < p.M) to[w] = element<T>(o, w);
             }
         }
+    };
+    if (j + W <= p.M) {
+        patch(std::true_type{});
+    } else if (p.M >= W) {
+        patch(std::false_type{});
     } else {
         for (int k = 0; k < nr; ++k)
             for (int w = 0; j + w < p.M; ++w) {
@@ -155,7 +171,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
 // in registers.  The next 8 rows move every diagonal 8 places on, so 8 of the sums are complete and go to the wavefront's diagonals
 // in LDS (different places in all lanes, W of them at a time), and the others stay.  Float32 up to there: at most 64 terms; what
 // a pass leaves there is added up in float64, scaled, and the buckets - neighbouring diagonals - are summed at the end.
-// Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.40 ms (6.1 TB/s), 4 x 16 x 2048 x 2048 bfloat16 100 us
+// Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.31 ms (6.6 TB/s), 4 x 16 x 2048 x 2048 bfloat16 100 us
 // (5.4 TB/s).  A walk along the diagonals, whose sums stay in registers the whole way, took 1.46 ms and 127 us: its rows'
 // loads begin one place further on from row to row, so hardly any of them is whole cache lines.
 template <typename T>
@@ -166,7 +182,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     __shared__ __align__(16) float pass_sum[4][Q];  // each wavefront's own
     __shared__ double diag[4][Q];
     __shared__ double bucket_sum[kMaxBuckets];
-    int64_t id = blockIdx.x;
+    int64_t id = neighbours_together();
     const int tile = (int)(id % p.tiles);
     id /= p.tiles;
     const int bp = (int)(id % p.batch_parts), h = (int)(id / p.batch_parts);
