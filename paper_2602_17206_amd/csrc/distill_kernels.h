@@ -508,14 +508,27 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillParams p)
     }
 }
 
-// dlogits over a slice of a row: every element as one outside the kept ones, then the kept ones over it.
-template <typename T>
+// dlogits over a slice of a row: every element as one outside the kept ones, then the kept ones over it.  A workgroup a slice,
+// or a wavefront (TEAM 64, with at most TOP slots), where rows are short.
+template <typename T, int TEAM, int TOP>
 __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
 {
     constexpr int W = Elem<T>::kWidth, U = 4;
-    __shared__ int ids[kMaxTop];
-    __shared__ float qs[kMaxTop];
-    const int row = blockIdx.x / p.slices, slice = blockIdx.x % p.slices;
+    __shared__ int team_ids[256 / TEAM][TOP];
+    __shared__ float team_qs[256 / TEAM][TOP];
+    const int team = TEAM == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / 64) : 0, thread = threadIdx.x % TEAM;
+    int *ids = team_ids[team];
+    float *qs = team_qs[team];
+    const int64_t at_slice = (int64_t)blockIdx.x * (256 / TEAM) + team;
+    if (TEAM == 64 && at_slice >= (int64_t)p.rows * p.slices) return;
+    const int row = (int)(at_slice / p.slices), slice = (int)(at_slice % p.slices);
+    // all of the slice's threads have come this far
+    auto meet = [] {
+        if (TEAM == 64)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+        else
+            __syncthreads();
+    };
     const Row<T> z = logits_row<T>(p, row);
     const int v0 = slice * p.slice_vecs, v1 = min(z.vecs, v0 + p.slice_vecs);
     if (v0 >= v1) return;
@@ -525,18 +538,18 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
         float fill[W];
 #pragma unroll
         for (int e = 0; e < W; ++e) fill[e] = st.flags & kRowInvalid ? NAN : 0.0f;
-        for (int i = v0 + threadIdx.x; i < v1; i += 256) store_gradient(dz, z, i, fill, z.outside(i));
+        for (int i = v0 + thread; i < v1; i += TEAM) store_gradient(dz, z, i, fill, z.outside(i));
         return;
     }
     const int r = teacher_row_of(p, row);
     const float g = (p.grad_loss ? p.grad_loss[row] : 1.0f) * p.inv_temperature;
-    constexpr int kMine = kMaxTop / 256;
+    constexpr int kMine = TOP / TEAM;
     int id[kMine];
     float val[kMine];
     const double lq = (double)st.lq_hi + (double)st.lq_lo;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-        const int k = threadIdx.x + i * 256;
+        const int k = thread + i * TEAM;
         id[i] = -1;
         if (k >= p.top) continue;
         const RawSlot raw = fetch_slot(p, r, k);
@@ -545,7 +558,7 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
         ids[k] = id[i];
         qs[k] = val[i];
     }
-    __syncthreads();
+    meet();
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int at = mark_of(id[i], p.vocab, z.pre, v0 * W);
@@ -557,22 +570,22 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
         }
         val[i] = g * (st.top * exp_at(kept_logit(z, id[i]), st.m, p.scale2) - q);
     }
-    __syncthreads();  // dlogits may be the logits: the kept ones have been read
+    meet();  // dlogits may be the logits: the kept ones have been read
     const float out = g * st.out, sub = huge_ref(st.off) ? finite_ref(st.off) : 0.0f, ref = whole_ref(st.off, p.scale2);
-    for (int i0 = v0 + threadIdx.x; i0 < v1; i0 += U * 256) {
+    for (int i0 = v0 + thread; i0 < v1; i0 += U * TEAM) {
         Bits4 v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = load_vec<true>(z.base + (int64_t)min(i0 + u * 256, v1 - 1) * W);
+        for (int u = 0; u < U; ++u) v[u] = load_vec<true>(z.base + (int64_t)min(i0 + u * TEAM, v1 - 1) * W);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u * 256;
+            const int i = i0 + u * TEAM;
             float d[W];
 #pragma unroll
             for (int e = 0; e < W; ++e) d[e] = out * __builtin_amdgcn_exp2f(fmaf(Elem<T>::at(v[u], e) - sub, p.scale2, -ref));
             if (i < v1) store_gradient(dz, z, i, d, z.outside(i));
         }
     }
-    __syncthreads();
+    meet();
 #pragma unroll
     for (int i = 0; i < kMine; ++i)
         if (id[i] >= 0) dz[id[i]] = Elem<T>::down(val[i]);
