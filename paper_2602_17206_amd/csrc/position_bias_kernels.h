@@ -79,10 +79,10 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
     return p.penalty && v < 0.0f ? 0.0f : v;
 }
 
-// Bound by reading and writing the plane: 8 x 16 x 1100 x 936 float16 takes 96 us (5.5 TB/s both ways together), 937 columns,
-// whose rows begin and end inside vectors, 115 us, 32 x 1 x 1024 x
-// 1024 float32 46 us (5.8 TB/s); a single row, 32 x 16 x 1 x 4097 bfloat16, 11 us, bound by the way from table to LDS to row.
-template <typename T>
+// Bound by reading and writing the plane: 8 x 16 x 2048 x 2048 bfloat16 takes 357 us (6.0 TB/s both ways together), 8 x 16 x 1100 x
+// 936 float16 95, with 937 columns, whose rows begin and end inside vectors, 115; a single row, 32 x 16 x 1 x 4097 bfloat16,
+// 11 us, bound by the way from table to LDS to row.  STREAM: the result is written past the caches.
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
 {
     constexpr int W = Elem<T>::kWidth, R = kBiasRows;
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
             }
             T *to = out + (int64_t)(i + k) * p.out_stride[2] + j;
             if (whole) {
-                store_vec<false>(to, o);
+                store_vec<STREAM>(to, o);
             } else {
 #pragma unroll
                 for (int w = 0; w < W - 1; ++w)
