@@ -364,10 +364,10 @@ int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalt
     const BucketRule rule = bucket_rule(desc);
     {
         ProfScope ps("position_bias_forward", st);
-        // Planes of 128 MB or more - half of the memory-side cache - are written past it: 357 against 386 us at 8 x 16 x 2048 x 2048
-        // bfloat16, 50 against 52 at 32 x 1 x 1024 x 1024 float32.  Smaller ones stay there for the next kernel: 73 against
-        // 88 us with a softmax behind it at 8 x 4 x 1024 x 1024 bfloat16.
-        const bool stream = planes * desc->N * desc->M * (16 / W) >= (int64_t)128 << 20;
+        // Planes that the memory-side cache of 256 MB cannot hold are written past it: 357 against 386 us at 8 x 16 x 2048 x 2048
+        // bfloat16, 93 against 100 at 8 x 16 x 1100 x 960 float16.  Others stay there for the next kernel: 73 against 88 us with a
+        // softmax behind it at 8 x 4 x 1024 x 1024 bfloat16; alone 44 against 48 at 32 x 1 x 1024 x 1024 float32.
+        const bool stream = planes * desc->N * desc->M * (16 / W) >= (int64_t)256 << 20;
         with_type(desc->plane_type, [&](auto t) {
             const auto kernel = stream ? position_bias_forward_kernel<decltype(t), true> : position_bias_forward_kernel<decltype(t), false>;
             kernel<<<(unsigned)(tiles * planes), 256, (size_t)(rows + cols) * 4, st>>>(p, rule);
