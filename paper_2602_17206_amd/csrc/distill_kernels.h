@@ -797,4 +797,85 @@ __global__ __launch_bounds__(1024, WAVES_PER_SIMD) void distill_rows_kernel(Dist
     __syncthreads();
 }
 
+// Short rows: a wavefront each, four of them a workgroup that know nothing of each other.  The row stays in registers, NV vectors a
+// lane, from its one read on; with GRAD its gradient is written, else its stats.  All loads of the row are on their way before
+// the slots' chain of dependent ones begins.
+template <typename T, int NV, bool GRAD>
+__global__ __launch_bounds__(256) void distill_short_kernel(DistillParams p, int team_bytes)
+{
+    constexpr int W = Elem<T>::kWidth;
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * 4 + wave;
+    if (row >= p.rows) return;
+    // what lanes of this wavefront wrote is there for the others
+    auto meet = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup"); };
+    const Row<T> z = logits_row<T>(p, row);
+    T *dz = GRAD ? dlogits_row<T>(p, row) : nullptr;
+    Bits4 v[NV];
+#pragma unroll
+    for (int u = 0; u < NV; ++u) v[u] = load_vec<GRAD>(z.base + (int64_t)min(lane + 64 * u, z.vecs - 1) * W);
+    const int r = teacher_row_of(p, (int)row);
+    const Slots sl = carve_slots(lds + wave * team_bytes, p.top);
+    Kept kept{};
+    bool repeated = false;
+    const bool target = r >= 0 && r < p.teacher_rows;
+    if (target) {
+        for (int w = lane; w < (z.vecs * W + 31) / 32; w += 64) sl.bits[w] = 0;
+        meet();
+        load_slots(p, r, z.pre, 0, z.vecs * W, sl, &repeated);
+        meet();
+        load_kept(p, z, sl);
+    }
+    float e[NV * W];
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < NV; ++u) {
+        const int at = lane + 64 * u;
+        unsigned out = z.outside(at);
+        if (p.tail && target) out |= vector_marks<T>(sl.bits, min(at, z.vecs - 1));
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            e[u * W + w] = out >> w & 1 ? -INFINITY : Elem<T>::at(v[u], w);
+            m = fmaxf(m, e[u * W + w]);
+        }
+    }
+    m = wave_max_all_f32(m);
+    const float sub = huge_ref(m) ? finite_ref(m) : 0.0f, ref = whole_ref(m, p.scale2);
+    float s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < NV * W; ++q) {
+        e[q] = __builtin_amdgcn_exp2f(fmaf(e[q] - sub, p.scale2, -ref));
+        s += e[q];
+    }
+    const MaxSum sum{m, wave_sum_all_f32(s)};
+    if (target) {
+        meet();
+        kept = reduce_slots(p, r, sl, __any(repeated));
+    } else {
+        kept.flags = r < 0 ? kRowNoTarget : kRowInvalid;
+    }
+    const RowStats st = finish_row(p, kept, sum);
+    if (lane == 0) {
+        p.loss[row] = row_loss(p, kept, sum, st);
+        if (!GRAD) p.stats[row] = st;
+    }
+    if constexpr (GRAD) {
+        const float g = (p.grad_loss ? p.grad_loss[row] : 1.0f) * p.inv_temperature;
+        const bool fill = st.flags & (kRowNoTarget | kRowInvalid);  // 0 or NaN whatever the row held
+        const float filler = st.flags & kRowInvalid ? NAN : 0.0f, factor = g * st.out * move_ref(m, st.off, p.scale2);
+#pragma unroll
+        for (int u = 0; u < NV; ++u) {
+            const int at = lane + 64 * u;
+            float d[W];
+#pragma unroll
+            for (int w = 0; w < W; ++w) d[w] = fill ? filler : e[u * W + w] * factor;
+            if (at < z.vecs) store_gradient(dz, z, at, d, z.outside(at));
+        }
+        if (fill) return;
+        meet();
+        store_kept<T>(p, sl, kept.q_scale, st, g, dz, lane, 64);
+    }
+}
+
 }  // namespace sdtw

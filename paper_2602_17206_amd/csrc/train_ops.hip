@@ -167,21 +167,49 @@ void launch_distill_backward(const DistillPlan &P, DistillParams p, int type, hi
     });
 }
 
-// The shape of the one-read kernel: vectors a thread and wavefronts, or 0 for rows that are too long.  Four vectors a thread for
-// short rows, eight for others (4 / 8: 44 / 49 us at 16384 x 1000 float32, 77 / 63 at 8192 x 8000 bfloat16, 92 / 87 at
-// 4096 x 24000), and twelve where only they hold a row of float32.
+// 16-byte vectors of a row (rows that begin anywhere may take one more)
+int64_t row_vectors(const sdtw_distill_desc *d, const void *logits)
+{
+    const int W = width_of(d->logit_type), size = 16 / W;
+    const bool aligned = (reinterpret_cast<uintptr_t>(logits) % 16 == 0) && d->logit_stride * size % 16 == 0;
+    return ((int64_t)d->vocab + (aligned ? W - 1 : 2 * W - 2)) / W;
+}
+
+// Rows of up to 512 vectors are a wavefront's: its vectors a lane, 0 for longer rows.  Loss and gradient of 16384 x 1000 float32 take 35 us,
+// with a workgroup to a row (distill_rows_kernel) 44, of 16384 x 2000 59 and 64, of 256 x 1000 9 and 10; with more vectors a lane there are too few
+// wavefronts.  The loss alone only with many rows: 24 against 30 us at 16384 x 1000, 8.5 and 9.3 at 1024; 9.4 against 8.0 at 256 x 4000 bfloat16.
+int short_vectors(const sdtw_distill_desc *d, const void *logits, bool gradient)
+{
+    const int64_t vecs = row_vectors(d, logits);
+    if (d->top > kRowsTop || (!gradient && d->rows < 1024)) return 0;
+    return vecs <= 256 ? 4 : vecs <= 512 ? 8 : 0;
+}
+
+// The shape of the one-read kernel for longer rows: vectors a thread and wavefronts, or 0 for rows that are too long.  Eight vectors a
+// thread (4 / 8: 77 / 63 us at 8192 x 8000 bfloat16, 92 / 87 at 4096 x 24000), and twelve where only they hold a row of float32.
 struct RowsShape { int vectors, waves, per_simd; };
 RowsShape rows_shape(const sdtw_distill_desc *d, const void *logits)
 {
-    const int W = width_of(d->logit_type), size = 16 / W;
-    // (rows that begin anywhere may take one vector more)
-    const bool aligned = (reinterpret_cast<uintptr_t>(logits) % 16 == 0) && d->logit_stride * size % 16 == 0;
-    const int64_t vecs = ((int64_t)d->vocab + (aligned ? W - 1 : 2 * W - 2)) / W;
+    const int W = width_of(d->logit_type);
+    const int64_t vecs = row_vectors(d, logits);
     auto waves = [&](int nv) { return 1 + (int)std::min<int64_t>(99, (vecs + 64 * nv - 1) / (64 * nv)); };
-    if (vecs <= 512) return {4, waves(4), 5};
     if (waves(8) <= 16) return {8, waves(8), W == 4 ? 5 : 4};
     if (W == 4 && waves(12) <= 16) return {12, waves(12), 4};
     return {0, 0, 0};
+}
+
+template <bool GRAD> void launch_distill_short(const sdtw_distill_desc *d, int vectors, const DistillParams &p, hipStream_t st)
+{
+    const int team = (d->top * 12 + vectors * 8 * width_of(d->logit_type) + 15) / 16 * 16;
+    const unsigned grid = (unsigned)(((int64_t)d->rows + 3) / 4);
+    ProfScope ps(GRAD ? "distill_step" : "distill_forward", st);
+    with_type(d->logit_type, [&](auto t) {
+        using T = decltype(t);
+        if (vectors == 4)
+            distill_short_kernel<T, 4, GRAD><<<grid, 256, 4 * team, st>>>(p, team);
+        else
+            distill_short_kernel<T, 8, GRAD><<<grid, 256, 4 * team, st>>>(p, team);
+    });
 }
 
 // LDS of the one-read kernel for a row's slots and marks (one for every element that the workgroup holds)
@@ -199,9 +227,7 @@ void launch_distill_rows(const sdtw_distill_desc *d, RowsShape s, const DistillP
     with_type(d->logit_type, [&](auto t) {
         using T = decltype(t);
         constexpr bool wide = sizeof(T) == 4;
-        if (s.vectors == 4)
-            distill_rows_kernel<T, 4, 5><<<grid, threads, 3 * ring, st>>>(p, ring);
-        else if (s.vectors == 8)
+        if (s.vectors == 8)
             distill_rows_kernel<T, 8, wide ? 5 : 4><<<grid, threads, 3 * ring, st>>>(p, ring);
         else if constexpr (wide)
             distill_rows_kernel<T, 12, 4><<<grid, threads, 3 * ring, st>>>(p, ring);
@@ -438,7 +464,11 @@ int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, cons
     p.loss = loss;
     p.stats = reinterpret_cast<RowStats *>(stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
-    launch_distill_forward(P, p, desc->logit_type, true, static_cast<hipStream_t>(stream));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (const int vectors = short_vectors(desc, logits, false))
+        launch_distill_short<false>(desc, vectors, p, st);
+    else
+        launch_distill_forward(P, p, desc->logit_type, true, st);
     return hip_ok();
 }
 
@@ -480,6 +510,10 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
     p.stats = reinterpret_cast<RowStats *>(static_cast<char *>(workspace) + P.off_stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (const int vectors = short_vectors(desc, logits, true)) {
+        launch_distill_short<true>(desc, vectors, p, st);
+        return hip_ok();
+    }
     const RowsShape shape = rows_shape(desc, logits);
     if (shape.vectors > 0 && desc->top <= kRowsTop) {
         launch_distill_rows(desc, shape, p, st);

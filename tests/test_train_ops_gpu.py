@@ -305,6 +305,37 @@ def test_gradient_against_differences_of_the_loss(tail):
         assert float((slope - (dz.double() * u.double()).sum(1)).abs().max()) < 5e-4
 
 
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("T,V", [(1030, 1500), (1027, 700), (1025, 3), (1026, 2047), (3, 2048), (2, 4090)])
+def test_short_rows_many_and_few(T, V, kind, tail):
+    run_both(problem(T, V, 24, kind, tail, 1.3, T + V, mapped=True, ragged=True, pad=1), 1.3, kind)
+
+
+@pytest.mark.parametrize("copies", [1, 300])
+@pytest.mark.parametrize("width", [9, 1900, 2100, 9001, 60001])
+def test_masks_in_rows_of_every_length(width, copies):
+    """The masked rows above in rows that are padded with -inf, one of each and many of each."""
+    z = [[1.0, -INF, 2.0, 0.5, LOW, -1.0], [1.0, -INF, 2.0, 0.5, LOW, -1.0], [LOW] * 5 + [-INF], [1.0, -INF, 2.0, 0.5, 3.0, -INF],
+         [-INF] * 6, [NAN, 0.0, 1.0, 2.0, 0.0, 0.0]]
+    t, ids = [[1.0, 0.0], [0.0, 0.5], [1.0, 0.0], [1.0, 0.0], [1.0, 0.0], [1.0, 0.0]], [[0, 2], [3, -1], [0, 3], [1, 2], [0, 1], [1, 2]]
+    wide = torch.full((6, width), -INF)
+    wide[:, :6] = torch.tensor(z)
+    wide[:, [1, width - 1]] = wide[:, [width - 1, 1]]  # a kept place at the row's end
+    ids = [[width - 1 if i == 1 else i for i in row] for row in ids]
+    z_d, t_d, i_d = wide.cuda().repeat(copies, 1), torch.tensor(t, device="cuda").repeat(copies, 1), torch.tensor(ids, device="cuda").repeat(copies, 1)
+    for lse in (None, torch.full((6 * copies,), 1.9, device="cuda")):
+        want = reference(f64(z_d[:4]), f64(t_d[:4]), i_d[:4].cpu().numpy(), 1.0, None if lse is None else f64(lse[:4]))
+        loss, stats = pkg.sdtw_distill_forward(z_d, t_d, i_d, teacher_lse=lse)
+        dz = pkg.sdtw_distill_backward(z_d, t_d, i_d, stats, teacher_lse=lse)
+        for lo, d in ((loss, dz), pkg.sdtw_distill_step(z_d, t_d, i_d, teacher_lse=lse)):
+            for c in {0, 1 % copies, copies // 2, copies - 1}:
+                check_loss(lo[6 * c:6 * c + 4], want[0])
+                check_grad(d[6 * c:6 * c + 4], want[1], want[2], "f32")
+            assert torch.isnan(lo.view(copies, 6)[:, 4:]).all() and torch.isnan(d.view(copies, 6, width)[:, 4:]).all()
+            assert not torch.isnan(lo.view(copies, 6)[:, :4]).any() and not torch.isnan(d.view(copies, 6, width)[:, :4]).any()
+
+
 # ---------------------------------------------------------------- position bias
 
 def buckets_of(n, D):
