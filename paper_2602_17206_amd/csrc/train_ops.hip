@@ -68,8 +68,8 @@ DistillPlan distill_plan(const sdtw_distill_desc *d)
     const int W = width_of(d->logit_type);
     const int64_t rows = std::max(d->rows, 1), vecs = (d->vocab + W - 1) / W + 1;  // (a row may begin inside a vector)
     // Many rows: a workgroup each, of one streaming wavefront up to 2048 vectors, three up to 16384, then four, next to the
-    // one for the slots.  (One / three / four of them: 33 / 47 / 72 us at 16384 x 1000 float32, 55 / 54 / 56 at 4096 x 32768
-    // bfloat16, 452 / 350 / 338 at 8192 x 131072.)
+    // one for the slots.  (One / three / four of them: 35 / 38 / 45 us at 8192 x 8000 bfloat16, 51 / 52 / 52 at 4096 x 32768,
+    // 452 / 350 / 338 at 8192 x 131072; 44 / 26 / 26 at 1024 x 32000 float32.)
     // Fewer than 512: up to fifteen, so that a row is on its way at once: 8.8 us at 1 x 32768 bfloat16, 15.3 at 400 x 32768,
     // 19.7 at 200 x 100000 float32; slices of a row and a second kernel that joins them took 13.7, 20.0 and 29.5.
     // Slices are for the few long rows (1 x 131072 bfloat16 13.8 us against 15.6), and for those whose marks - one bit an
