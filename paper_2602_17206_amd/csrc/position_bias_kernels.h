@@ -49,8 +49,8 @@ struct BiasParams {
     float *dtable;
     // forward: tiles of (256 / ty * width) columns and ty * 8 rows
     int32_t tx, col_tiles, row_tiles;
-    // backward: tiles of `across` times 64 * width columns and 4 / across times 64 rows (col_tiles as above), parts of the batch
-    int32_t tiles, across, batch_parts, batch_per_part, parts;
+    // backward: tiles of `across` times 64 * width columns and 4 / across times wave_rows rows (col_tiles as above), parts of the batch
+    int32_t wave_rows, tiles, across, batch_parts, batch_per_part, parts;
     double *partial;  // [H][buckets][parts]
 };
 
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
     }
 }
 
-// One tile of the plane, for a part of the batch.  A wavefront takes 64 rows of 64 * W columns, 8 rows at a time: lane l reads W
+// One tile of the plane, for a part of the batch.  A wavefront takes wave_rows (at most 64) rows of 64 * W columns, 8 rows at a time: lane l reads W
 // columns of each (whole cache lines from row to row), and element (a, w) of its patch lies on diagonal w - a of it: W + 7 sums
 // in registers.  The next 8 rows move every diagonal 8 places on, so 8 of the sums are complete and go to the wavefront's diagonals
 // in LDS (different places in all lanes, W of them at a time), and the others stay.  Float32 up to there: at most 64 terms; what
@@ -190,7 +190,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     // the tile's four wavefronts: `across` side by side, the others below
     const int across = p.across, down = 4 / across;
-    const auto row_of = [&](int w) { return (tile / p.col_tiles * down + w / across) * 64; };
+    const auto row_of = [&](int w) { return (tile / p.col_tiles * down + w / across) * p.wave_rows; };
     const auto col_of = [&](int w) { return (tile % p.col_tiles * across + w % across) * (64 * W); };
     const int i0 = row_of(wave), j0 = col_of(wave), j = j0 + W * lane;
     const int b0 = bp * p.batch_per_part, b1 = min(p.B, b0 + p.batch_per_part);
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
         const int rlen = clamp_len(p.row_len, b, p.N), clen = clamp_len(p.col_len, b, p.M);
         const T *g = static_cast<const T *>(p.in) + b * p.in_stride[0] + h * p.in_stride[1];
         const double scale = p.scale ? (double)p.scale[p.scale_heads ? (int64_t)b * p.H + h : b] : 1.0;
-        const int steps = j0 < clen ? min((rlen - i0 + R - 1) / R, 64 / R) : 0;
+        const int steps = j0 < clen ? min((rlen - i0 + R - 1) / R, p.wave_rows / R) : 0;
         // A vector that hangs over the row's end is read further in and shifted, zeros coming in (rows shorter than one: by element).
         const int jc = min(j, clen - W);
         float f[A];

@@ -339,25 +339,37 @@ BiasParams bias_params(const sdtw_bias_desc *d, const void *in, const int32_t *o
     return p;
 }
 
-// How the backward pass is split: tiles of the plane, then the batch, into 2048 workgroups where it has them.
+// How the backward pass is split (`fits`: into workgroups that can be counted): tiles of the plane, then the batch, into 2048 workgroups where it has them.
 // Measured with 1024, 2048, 4096, 8192: 32 x 1 x 8192 x 8192 float32 1385, 1393, 1433, 1481 us,
 // 4 x 16 x 2048 x 2048 bfloat16 99, 100, 101, 101 us; smaller planes are equal within 1 us.
-struct BiasPlan { int64_t across, col_tiles, tiles, batch_per_part, batch_parts, parts; };
+struct BiasPlan { bool fits; int64_t wave_rows, across, col_tiles, tiles, batch_per_part, batch_parts, parts; };
 
 BiasPlan bias_plan(const sdtw_bias_desc *d)
 {
     BiasPlan P{};
+    P.fits = true;
     if (d->B == 0 || d->H == 0 || d->N == 0 || d->M == 0) return P;
     const int64_t width = 64 * width_of(d->plane_type), want = 2048;
     P.across = d->M > 2 * width ? 4 : d->M > width ? 2 : 1;
     P.col_tiles = (d->M + P.across * width - 1) / (P.across * width);
-    const int64_t rows = 64 * (4 / P.across);
-    P.tiles = P.col_tiles * ((d->N + rows - 1) / rows);
+    auto tile = [&](int64_t wave_rows) {
+        const int64_t rows = wave_rows * (4 / P.across);
+        P.wave_rows = wave_rows;
+        P.tiles = P.col_tiles * ((d->N + rows - 1) / rows);
+    };
+    // A wavefront goes down 64 rows, 8 a step - or 16, where that makes no more than a workgroup for each compute unit, and the steps' latency
+    // counts: 19.1 against 23.0 us at 4 x 1 x 64 x 64 float32, 24.7 and 28.6 at 16 x 8 x 300 x 300 bfloat16; but 42 against 36 at
+    // 32 x 1 x 1024 x 1024 float32.
+    tile(64);
+    P.fits = P.tiles <= 0x7fffffff / d->H;
+    if (!P.fits) return P;
+    if (P.tiles * d->H * d->B <= 256) tile(16);
     const int64_t units = P.tiles * d->H;
     P.batch_parts = std::min<int64_t>(d->B, (want + units - 1) / units);
     P.batch_per_part = (d->B + P.batch_parts - 1) / P.batch_parts;
     P.batch_parts = (d->B + P.batch_per_part - 1) / P.batch_per_part;
     P.parts = P.tiles * P.batch_parts;
+    P.fits = P.parts <= 0x7fffffff / d->H;
     return P;
 }
 
@@ -371,7 +383,7 @@ int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalt
     if (!bias_ok(desc)) return SDTW_ERR_INVALID_ARG;
     if (desc->B == 0 || desc->H == 0 || desc->N == 0 || desc->M == 0) return SDTW_OK;
     if (!table || !out || !disjoint(desc)) return SDTW_ERR_INVALID_ARG;
-    if (in == out)  // in place: a thread reads exactly the cells that it writes
+    if (in == out)  // in place: a thread uses of what it reads exactly the cells that it writes
         for (int i = 0; i < 3; ++i)
             if (desc->in_stride[i] != desc->out_stride[i]) return SDTW_ERR_INVALID_ARG;
     BiasParams p = bias_params(desc, in, offsets, row_len, col_len);
@@ -410,7 +422,7 @@ int position_bias_table_grad(const sdtw_bias_desc *desc, const void *penalty_tab
     if (desc->H == 0) return SDTW_OK;
     const BiasPlan P = bias_plan(desc);
     if (!dtable || (!grad && P.parts > 0)) return SDTW_ERR_INVALID_ARG;
-    if (P.parts > 0x7fffffff / desc->H || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
+    if (!P.fits || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, sdtw_position_bias_workspace_bytes(desc))) return rc;
     (void)hipGetLastError();
     BiasParams p = bias_params(desc, grad, offsets, row_len, col_len);
@@ -419,6 +431,7 @@ int position_bias_table_grad(const sdtw_bias_desc *desc, const void *penalty_tab
     p.table = penalty_table;
     p.dtable = dtable;
     p.partial = static_cast<double *>(workspace);
+    p.wave_rows = (int32_t)P.wave_rows;
     p.across = (int32_t)P.across;
     p.col_tiles = (int32_t)P.col_tiles;
     p.tiles = (int32_t)P.tiles;
@@ -544,7 +557,8 @@ int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, co
 size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc)
 {
     if (!bias_ok(desc)) return 0;
-    return std::max<size_t>(256, align_up((size_t)desc->H * desc->buckets * (size_t)bias_plan(desc).parts * sizeof(double), 256));
+    const BiasPlan P = bias_plan(desc);
+    return P.fits ? std::max<size_t>(256, align_up((size_t)desc->H * desc->buckets * (size_t)P.parts * sizeof(double), 256)) : 0;
 }
 
 int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, const float *scale, const int32_t *offsets,

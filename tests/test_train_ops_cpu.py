@@ -134,6 +134,15 @@ def test_bias_pointers_strides_and_workspace():
     assert backward(nbytes=need - 1) == binding.STATUS_WORKSPACE
 
 
+def test_planes_that_need_more_workgroups_than_there_are():
+    lib = pkg.load_library()
+    most = (1 << 31) - 1
+    for kw in (dict(B=1, H=1 << 20, N=(1 << 30) - 1, M=(1 << 30) - 1), dict(B=most, H=most, N=1 << 20, M=1 << 20), dict(B=1, H=1, N=(1 << 30) - 1, M=(1 << 30) - 1)):
+        d = bias_desc(in_stride=(0, 0, 0), out_stride=(0, 0, 0), **kw)
+        assert lib.sdtw_position_bias_workspace_bytes(ctypes.byref(d)) == 0
+        assert lib.sdtw_position_bias_backward(ctypes.byref(d), FAKE, None, None, None, None, FAKE, FAKE, 1 << 40, None) == binding.STATUS_INVALID_ARG
+
+
 def starts_in_whole_numbers(n, D):
     e = n // 2
     m = n - e
