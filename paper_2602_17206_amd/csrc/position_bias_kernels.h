@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     typedef float Float4 __attribute__((ext_vector_type(4)));
     __shared__ __align__(16) float pass_sum[4][Q];  // each wavefront's own
     __shared__ double diag[4][Q];
-    __shared__ double bucket_sum[kMaxBuckets];
+    __shared__ double bucket_sum[kMaxBuckets], narrow_sum[4][64];
     int64_t id = neighbours_together();
     const int tile = (int)(id % p.tiles);
     id /= p.tiles;
@@ -223,7 +223,22 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
             lo = max(lo, lowest);
             hi = min(hi, highest);
             const int from = (int)(lo - lowest), to = (int)(hi - lowest);
-            unsigned long long some = __ballot(lo <= hi);
+            // of up to 8 diagonals: all at once, a lane each, over this wavefront's own place among the diagonals
+            const bool narrow = lo <= hi && to - from < 8;
+            double own = 0.0;
+            if (__any(narrow)) {
+                const int shift = (int)((int64_t)col_of(wave) - row_of(wave) - Z - offset - lowest);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const int q = from + k - shift;
+                    const double x = diag[wave][max(0, min(q, Q - 1))];
+                    own += narrow && from + k <= to && q >= 0 && q < Q ? x : 0.0;
+                }
+                narrow_sum[wave][lane] = own;
+            }
+            __syncthreads();
+            if (wave == 0 && narrow) bucket_sum[u] += (own + narrow_sum[1][lane]) + (narrow_sum[2][lane] + narrow_sum[3][lane]);
+            unsigned long long some = __ballot(lo <= hi && !narrow);
             for (int turn = 0; some != 0; ++turn, some &= some - 1) {
                 if ((turn & 3) != wave) continue;
                 const int l = __builtin_ctzll(some);
@@ -236,6 +251,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
                 s = wave_sum_f64(s);
                 if (lane == 0) bucket_sum[u0 + l] += s;
             }
+            __syncthreads();
         }
         __syncthreads();
     };
