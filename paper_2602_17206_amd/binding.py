@@ -6,6 +6,7 @@ device memory and the current stream; nothing is computed in Python and there is
 fallback: if the library has not been built, the first call raises.
 """
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -630,12 +631,29 @@ def _type_of(t, name):
     return kind
 
 
-def _stream_of(stream, device):
-    """The given stream, or the current one of the tensors' device."""
-    if stream is not None:
-        return int(stream)
+def _on_given_stream(call):
+    """With ``stream`` (a raw handle) the call runs as on that stream: what it allocates belongs to it too, so that no other
+    stream is given the memory while the kernels are still at work."""
+    @functools.wraps(call)
+    def on_stream(*args, stream=None, **kw):
+        if stream is None:
+            return call(*args, **kw)
+        import torch
+
+        device = next((a.device for a in (*args, *kw.values()) if torch.is_tensor(a)), None)
+        handle = int(stream)
+        given = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+        with torch.cuda.stream(given):
+            return call(*args, **kw)
+    return on_stream
+
+
+def _stream_of(device):
+    """The current stream of the tensors' device, which has to be the current one."""
     import torch
 
+    if device.index != torch._C._cuda_getDevice():
+        raise ValueError("the tensors must be on the current device")
     return torch._C._cuda_getCurrentRawStream(device.index)
 
 
@@ -703,8 +721,9 @@ def sdtw_distill_workspace_bytes(desc):
     return int(load_library().sdtw_distill_workspace_bytes(ctypes.byref(desc)))
 
 
+@_on_given_stream
 def sdtw_distill_forward(logits, teacher_logits, teacher_ids, temperature=1.0, teacher_lse=None, teacher_row=None,
-                         loss=None, stats=None, workspace=None, stream=None):
+                         loss=None, stats=None, workspace=None):
     """Divergence of every row of ``logits`` [T, V] from the teacher's top logits [R, K] at the tokens ``teacher_ids``
     [R, K] (negative: unused).  Row t goes with the teacher's row ``teacher_row[t]`` (int32; negative: no target), or t.
     The teacher's probabilities are renormalised over the kept tokens, or, with ``teacher_lse`` [R] (float32, the log-sum-exp
@@ -722,14 +741,15 @@ def sdtw_distill_forward(logits, teacher_logits, teacher_ids, temperature=1.0, t
     if stats is None:
         stats = torch.empty((desc.rows, DISTILL_STATS), dtype=torch.float32, device=dev)
     rc = lib.sdtw_distill_forward(ref, *args, _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"),
-                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), wp, wn, _stream_of(stream, dev))
+                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_forward")
     return loss, stats
 
 
+@_on_given_stream
 def sdtw_distill_backward(logits, teacher_logits, teacher_ids, stats, grad_loss=None, temperature=1.0, teacher_lse=None,
-                          teacher_row=None, dlogits=None, stream=None):
+                          teacher_row=None, dlogits=None):
     """Gradient [T, V] (of the logits' type) of the losses :func:`sdtw_distill_forward` produced, weighted by ``grad_loss``
     [T] (float32; None: ones).  ``dlogits`` may be ``logits`` itself."""
     import torch
@@ -739,14 +759,15 @@ def sdtw_distill_backward(logits, teacher_logits, teacher_ids, stats, grad_loss=
     dev = logits.device
     dlogits, dp = _distill_grad_out(desc, logits, dlogits)
     rc = lib.sdtw_distill_backward(ctypes.byref(desc), *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
-                                   _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), dp, _stream_of(stream, dev))
+                                   _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), dp, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_backward")
     return dlogits
 
 
+@_on_given_stream
 def sdtw_distill_step(logits, teacher_logits, teacher_ids, grad_loss=None, temperature=1.0, teacher_lse=None,
-                      teacher_row=None, loss=None, dlogits=None, workspace=None, stream=None):
+                      teacher_row=None, loss=None, dlogits=None, workspace=None):
     """Loss and gradient in one call, for a caller who knows ``grad_loss`` beforehand.  Returns (loss [T], dlogits [T, V])."""
     import torch
 
@@ -759,7 +780,7 @@ def sdtw_distill_step(logits, teacher_logits, teacher_ids, grad_loss=None, tempe
         loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
     dlogits, dp = _distill_grad_out(desc, logits, dlogits)
     rc = lib.sdtw_distill_step(ref, *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
-                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, wp, wn, _stream_of(stream, dev))
+                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_step")
     return loss, dlogits
@@ -796,8 +817,9 @@ def sdtw_position_bias_starts(buckets, max_distance=128, two_sided=True):
     return list(starts)[:buckets // 2 if two_sided else buckets]
 
 
+@_on_given_stream
 def sdtw_position_bias_forward(table, plane=None, max_distance=128, two_sided=True, offset=0, row_len=None, col_len=None,
-                               out=None, stream=None):
+                               out=None):
     """plane [B, H, N, M] + table[h, bucket(j - i - offset)], ``table`` [H, buckets] of any strides (an embedding's transpose).
     ``offset``: a number, or int32 [B]: where every sequence's row 0 stands.  ``row_len``, ``col_len`` [B] int32: cells beyond
     keep what ``plane`` holds.  Without ``plane`` the bias alone goes to ``out``.  ``out`` may be ``plane`` itself."""
@@ -819,14 +841,15 @@ def sdtw_position_bias_forward(table, plane=None, max_distance=128, two_sided=Tr
     desc.out_stride[:] = [out.stride(0), out.stride(1), out.stride(2)]
     desc.table_stride[:] = [table.stride(0), table.stride(1)]
     rc = lib.sdtw_position_bias_forward(ctypes.byref(desc), table.data_ptr(), None if plane is None else plane.data_ptr(), *args,
-                                        out.data_ptr(), _stream_of(stream, like.device))
+                                        out.data_ptr(), _stream_of(like.device))
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_forward")
     return out
 
 
+@_on_given_stream
 def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True, offset=0, row_len=None, col_len=None, scale=None,
-                                dtable=None, workspace=None, stream=None):
+                                dtable=None, workspace=None):
     """Gradient [H, buckets] (float32) of the table from ``grad`` [B, H, N, M] of the planes (any strides, broadcast ones too),
     each sequence's times ``scale[b]`` (float32 [B]; None: ones)."""
     import torch
@@ -843,7 +866,7 @@ def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True,
         dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
     rc = lib.sdtw_position_bias_backward(ref, grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"), *args,
                                          _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable"), wp, wn,
-                                         _stream_of(stream, dev))
+                                         _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_backward")
     return dtable

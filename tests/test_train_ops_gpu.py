@@ -525,6 +525,33 @@ def test_operators_run_on_the_stream_they_are_given():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(got_b, want_b) and torch.equal(got_t, want_t)
 
 
+def test_memory_of_a_call_on_another_stream_is_not_given_away():
+    """A busy stream gets the calls by its handle; meanwhile the current one fills whatever memory it is given."""
+    s = problem(600, 70001, 20, "f32", True, 1.0, 3)
+    plane = torch.randn((8, 2, 300, 320), device="cuda")
+    want = pkg.sdtw_distill_step(s["z"], s["t"], s["ids"], teacher_lse=s["lse"])
+    want_f = pkg.sdtw_distill_forward(s["z"], s["t"], s["ids"], teacher_lse=s["lse"])
+    want_b, want_t = pkg.sdtw_position_bias_forward(plane[0, :, 0, :32], plane), pkg.sdtw_position_bias_backward(plane, 32)
+    busy = torch.randn((4096, 4096), device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                busy @ busy
+        h = side.cuda_stream
+        got = pkg.sdtw_distill_step(s["z"], s["t"], s["ids"], teacher_lse=s["lse"], stream=h)
+        got_f = pkg.sdtw_distill_forward(s["z"], s["t"], s["ids"], teacher_lse=s["lse"], stream=h)
+        got_b, got_t = pkg.sdtw_position_bias_forward(plane[0, :, 0, :32], plane, stream=h), pkg.sdtw_position_bias_backward(plane, 32, stream=h)
+        kept = [torch.full((n,), 7.0, device="cuda") for n in (600, 600 * 8, 4096, 2 * 32, 1 << 14, 1 << 16, 1 << 20) for _ in range(4)]
+        torch.cuda.synchronize()
+        pairs = [*zip(got, want), *zip(got_f, want_f), (got_b, want_b), (got_t, want_t)]
+        assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in pairs)
+        assert all((k == 7.0).all() for k in kept)
+    # the default stream by its handle
+    assert torch.equal(pkg.sdtw_position_bias_backward(plane, 32, stream=0), want_t)
+
+
 @pytest.mark.parametrize("T", [2, 400])
 def test_operators_in_a_graph(T):
     s = problem(T, 9000, 20, "bf16", True, 1.0, 3)
