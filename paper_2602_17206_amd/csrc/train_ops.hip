@@ -246,7 +246,8 @@ bool power_at_least(int d, int m, int e, int k, int D);
 // First distances of the buckets from e on: the smallest d with d^m >= e^(m-k) D^k.
 void bucket_starts(int e, int m, int D, int32_t *start)
 {
-    for (int k = 0; k < m; ++k) {
+    start[0] = e;
+    for (int k = 1; k < m; ++k) {
         const double x = (double)e * std::pow((double)D / e, (double)k / m);
         const double near = std::nearbyint(x);
         // The power is good to about 1e-13 of itself; nearer than that to a whole number the whole numbers decide.
@@ -262,9 +263,10 @@ bool power_at_least(int d, int m, int e, int k, int D)
 {
     constexpr int kDigits = 128;
     uint32_t a[kDigits] = {1}, b[kDigits] = {1};
-    auto times = [](uint32_t *x, uint32_t f) {
+    const int digits = (25 * m + 31) / 32;  // (no factor is beyond 2^24, and m at most 128)
+    auto times = [digits](uint32_t *x, uint32_t f) {
         uint64_t carry = 0;
-        for (int i = 0; i < kDigits; ++i) {
+        for (int i = 0; i < digits; ++i) {
             carry += (uint64_t)x[i] * f;
             x[i] = (uint32_t)carry;
             carry >>= 32;
@@ -274,7 +276,7 @@ bool power_at_least(int d, int m, int e, int k, int D)
         times(a, (uint32_t)d);
         times(b, (uint32_t)(i < k ? D : e));
     }
-    for (int i = kDigits - 1; i >= 0; --i)
+    for (int i = digits - 1; i >= 0; --i)
         if (a[i] != b[i]) return a[i] > b[i];
     return true;
 }
