@@ -699,10 +699,21 @@ def _distill_grad_out(desc, logits, dlogits):
     """(dlogits, its pointer), with its row stride in the descriptor"""
     import torch
 
-    if dlogits is None:
+    if dlogits is None:  # (the descriptor's stride is that of whole rows)
         dlogits = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        return dlogits, dlogits.data_ptr()
     ptr, desc.grad_stride = _rows_ptr(dlogits, desc.rows, desc.vocab, logits.device, "dlogits", logits.dtype)
     return dlogits, ptr
+
+
+def _loss_out(rows, loss, device):
+    """(loss, its pointer)"""
+    import torch
+
+    if loss is None:
+        loss = torch.empty(rows, dtype=torch.float32, device=device)
+        return loss, loss.data_ptr()
+    return loss, _vector_ptr(loss, rows, device, torch.float32, "loss")
 
 
 def _operator_workspace(nbytes, workspace, device, where):
@@ -736,12 +747,13 @@ def sdtw_distill_forward(logits, teacher_logits, teacher_ids, temperature=1.0, t
     dev = logits.device
     ref = ctypes.byref(desc)
     keep, wp, wn = _operator_workspace(lib.sdtw_distill_workspace_bytes(ref), workspace, dev, "sdtw_distill_forward")
-    if loss is None:
-        loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
+    loss, lp = _loss_out(desc.rows, loss, dev)
     if stats is None:
         stats = torch.empty((desc.rows, DISTILL_STATS), dtype=torch.float32, device=dev)
-    rc = lib.sdtw_distill_forward(ref, *args, _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"),
-                                  _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats"), wp, wn, _stream_of(dev))
+        sp = stats.data_ptr()
+    else:
+        sp = _ptr(stats, torch.float32, (desc.rows, DISTILL_STATS), "stats")
+    rc = lib.sdtw_distill_forward(ref, *args, lp, sp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_forward")
     return loss, stats
@@ -776,11 +788,10 @@ def sdtw_distill_step(logits, teacher_logits, teacher_ids, grad_loss=None, tempe
     dev = logits.device
     ref = ctypes.byref(desc)
     keep, wp, wn = _operator_workspace(lib.sdtw_distill_workspace_bytes(ref), workspace, dev, "sdtw_distill_step")
-    if loss is None:
-        loss = torch.empty(desc.rows, dtype=torch.float32, device=dev)
+    loss, lp = _loss_out(desc.rows, loss, dev)
     dlogits, dp = _distill_grad_out(desc, logits, dlogits)
-    rc = lib.sdtw_distill_step(ref, *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"),
-                               _vector_ptr(loss, desc.rows, dev, torch.float32, "loss"), dp, wp, wn, _stream_of(dev))
+    rc = lib.sdtw_distill_step(ref, *args, _vector_ptr(grad_loss, desc.rows, dev, torch.float32, "grad_loss"), lp, dp, wp, wn,
+                               _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_distill_step")
     return loss, dlogits
@@ -864,8 +875,10 @@ def sdtw_position_bias_backward(grad, buckets, max_distance=128, two_sided=True,
     keep, wp, wn = _operator_workspace(lib.sdtw_position_bias_workspace_bytes(ref), workspace, dev, "sdtw_position_bias_backward")
     if dtable is None:
         dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
-    rc = lib.sdtw_position_bias_backward(ref, grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"), *args,
-                                         _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable"), wp, wn,
+        dp = dtable.data_ptr()
+    else:
+        dp = _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable")
+    rc = lib.sdtw_position_bias_backward(ref, grad.data_ptr(), _vector_ptr(scale, desc.B, dev, torch.float32, "scale"), *args, dp, wp, wn,
                                          _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_backward")
