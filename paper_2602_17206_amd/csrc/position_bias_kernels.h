@@ -80,9 +80,9 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
 }
 
 // Bound by reading and writing the plane: 8 x 16 x 2048 x 2048 bfloat16 takes 357 us (6.0 TB/s both ways together), 8 x 16 x 1100 x
-// 936 float16 95, with 937 columns, whose rows begin and end inside vectors, 115; a single row, 32 x 16 x 1 x 4097 bfloat16,
-// 11 us, bound by the way from table to LDS to row.  STREAM: the result is written past the caches.
-template <typename T, bool STREAM>
+// 936 float16 96, with 937 columns, whose rows begin and end inside vectors, 108; a single row, 32 x 16 x 1 x 4097 bfloat16,
+// 10 us, bound by the way from table to LDS to row.  STREAM_IN, STREAM_OUT: past the caches.
+template <typename T, bool STREAM_IN, bool STREAM_OUT>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
 {
     constexpr int W = Elem<T>::kWidth, R = kBiasRows;
@@ -109,23 +109,21 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
         diag[q] = values[rule.bucket(clamp_rel((int64_t)j0 - (i0 + rows - 1) + q - offset), starts)];
     __syncthreads();
     const int x = threadIdx.x % p.tx, y = threadIdx.x / p.tx;
-    const int j = j0 + x * W, i = i0 + y * R;
+    const int j = j0 + x * W, i = i0 + y * R, nr = min(R, p.N - i);
     if (j >= p.M || i >= p.N) return;
     const T *in = p.in ? static_cast<const T *>(p.in) + b * p.in_stride[0] + h * p.in_stride[1] : nullptr;
+    // (a vector that hangs over the row's end is read further in, and shifted: what it saw of its neighbours goes out)
+    Bits4 v[R] = {};
+    const int jc = min(j, p.M - W);
+    if (in && jc >= 0)
+#pragma unroll
+        for (int k = 0; k < R; ++k) v[k] = load_vec<STREAM_IN>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + jc);
     T *out = static_cast<T *>(p.out) + b * p.out_stride[0] + h * p.out_stride[1];
     const float *mine = diag + x * W + (rows - 1 - y * R);  // mine[w - k]: row i + k, column j + w
-    const int nr = min(R, p.N - i);
     auto patch = [&](auto whole) {
-        Bits4 v[R] = {};
-        if (in) {
-            // a vector that hangs over the row's end is read further in and shifted (what it saw of its neighbours goes out)
-            const int jc = whole ? j : p.M - W;
+        if (!whole) {
 #pragma unroll
-            for (int k = 0; k < R; ++k) v[k] = load_vec<true>(in + (int64_t)(i + min(k, nr - 1)) * p.in_stride[2] + jc);
-            if (!whole) {
-#pragma unroll
-                for (int k = 0; k < R; ++k) v[k] = shift_vec(v[k], (j - jc) * 8 * (int)sizeof(T));
-            }
+            for (int k = 0; k < R; ++k) v[k] = shift_vec(v[k], (j - jc) * 8 * (int)sizeof(T));
         }
         float d[W + R - 1];
 #pragma unroll
@@ -144,7 +142,7 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
             }
             T *to = out + (int64_t)(i + k) * p.out_stride[2] + j;
             if (whole) {
-                store_vec<STREAM>(to, o);
+                store_vec<STREAM_OUT>(to, o);
             } else {
 #pragma unroll
                 for (int w = 0; w < W - 1; ++w)

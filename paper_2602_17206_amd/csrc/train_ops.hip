@@ -341,6 +341,11 @@ BiasParams bias_params(const sdtw_bias_desc *d, const void *in, const int32_t *o
     return p;
 }
 
+bool begins_on_vectors(const void *plane, const int64_t (&stride)[3], int W)
+{
+    return reinterpret_cast<uintptr_t>(plane) % 16 == 0 && stride[0] % W == 0 && stride[1] % W == 0 && stride[2] % W == 0;
+}
+
 // How the backward pass is split (`fits`: into workgroups that can be counted): tiles of the plane, then the batch, into 2048 workgroups where it has them.
 // Measured with 1024, 2048, 4096, 8192: 32 x 1 x 8192 x 8192 float32 1385, 1393, 1433, 1481 us,
 // 4 x 16 x 2048 x 2048 bfloat16 99, 100, 101, 101 us; smaller planes are equal within 1 us.
@@ -407,9 +412,15 @@ int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalt
         // Planes that the memory-side cache of 256 MB cannot hold are written past it: 357 against 386 us at 8 x 16 x 2048 x 2048
         // bfloat16, 93 against 100 at 8 x 16 x 1100 x 960 float16.  Others stay there for the next kernel: 73 against 88 us with a
         // softmax behind it at 8 x 4 x 1024 x 1024 bfloat16; alone 44 against 48 at 32 x 1 x 1024 x 1024 float32.
-        const bool stream = planes * desc->N * desc->M * (16 / W) >= (int64_t)256 << 20;
+        // Rows that begin inside vectors share lines with their neighbours and go through the caches both ways: 382 against 391 us
+        // (read past them) and 407 (both) at 8 x 16 x 2001 x 2003 bfloat16, 175, 186 and 172 at 4 x 16 x 1001 x 1501 float32.
+        const bool vectors = begins_on_vectors(in, desc->in_stride, W) && begins_on_vectors(out, desc->out_stride, W);
+        const bool stream = vectors && planes * desc->N * desc->M * (16 / W) >= (int64_t)256 << 20;
         with_type(desc->plane_type, [&](auto t) {
-            const auto kernel = stream ? position_bias_forward_kernel<decltype(t), true> : position_bias_forward_kernel<decltype(t), false>;
+            using T = decltype(t);
+            const auto kernel = stream    ? position_bias_forward_kernel<T, true, true>
+                                : vectors ? position_bias_forward_kernel<T, true, false>
+                                          : position_bias_forward_kernel<T, false, false>;
             kernel<<<(unsigned)(tiles * planes), 256, (size_t)(rows + cols) * 4, st>>>(p, rule);
         });
     }
