@@ -382,7 +382,7 @@ int sdtw_position_bias_starts(const sdtw_bias_desc *desc, int32_t *starts);
 int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, const void *in, const int32_t *offsets,
                                const int32_t *row_len, const int32_t *col_len, void *out, void *stream);
 
-/* Bytes of workspace of sdtw_position_bias_backward; 0 if the descriptor is invalid.  Host only. */
+/* Bytes of workspace of sdtw_position_bias_backward; 0 if the descriptor is invalid or takes more than 2^31 workgroups.  Host only. */
 size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc);
 
 /*
