@@ -169,8 +169,8 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
 // in registers.  The next 8 rows move every diagonal 8 places on, so 8 of the sums are complete and go to the wavefront's diagonals
 // in LDS (different places in all lanes, W of them at a time), and the others stay.  Float32 up to there: at most 64 terms; what
 // a pass leaves there is added up in float64, scaled, and the buckets - neighbouring diagonals - are summed at the end.
-// Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.31 ms (6.6 TB/s), 4 x 16 x 2048 x 2048 bfloat16 100 us
-// (5.4 TB/s).  A walk along the diagonals, whose sums stay in registers the whole way, took 1.46 ms and 127 us: its rows'
+// Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.28 ms (6.7 TB/s), 4 x 16 x 2048 x 2048 bfloat16 85 us
+// (6.3 TB/s).  4 x 1 x 64 x 64 float32 takes 9 us: a wavefront's steps, then its buckets.  A walk along the diagonals, whose sums stay in registers the whole way, took 1.46 ms and 127 us: its rows'
 // loads begin one place further on from row to row, so hardly any of them is whole cache lines.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams p, BucketRule rule)
@@ -325,7 +325,7 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
     for (int u = threadIdx.x; u < p.buckets; u += 256) p.partial[((int64_t)h * p.buckets + u) * p.parts + part] = bucket_sum[u];
 }
 
-// dtable[h,u]: the parts in a fixed order.  With a table (a penalty) its negative entries, which count as 0, get 0.
+// dtable[h,u]: the parts in a fixed order; 2 to 5 us.  With a table (a penalty) its negative entries, which count as 0, get 0.
 __global__ __launch_bounds__(256) void position_bias_table_kernel(BiasParams p)
 {
     __shared__ double sums[4];

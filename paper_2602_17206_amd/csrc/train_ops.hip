@@ -346,9 +346,9 @@ bool begins_on_vectors(const void *plane, const int64_t (&stride)[3], int W)
     return reinterpret_cast<uintptr_t>(plane) % 16 == 0 && stride[0] % W == 0 && stride[1] % W == 0 && stride[2] % W == 0;
 }
 
-// How the backward pass is split (`fits`: into workgroups that can be counted): tiles of the plane, then the batch, into 2048 workgroups where it has them.
-// Measured with 1024, 2048, 4096, 8192: 32 x 1 x 8192 x 8192 float32 1385, 1393, 1433, 1481 us,
-// 4 x 16 x 2048 x 2048 bfloat16 99, 100, 101, 101 us; smaller planes are equal within 1 us.
+// How the backward pass is split (`fits`: into workgroups that can be counted): tiles of the plane, then the batch, into 2048
+// workgroups where it has them.  Measured with 1024, 2048, 8192: 32 x 1 x 8192 x 8192 float32 1330, 1315, 1324 us,
+// 4 x 16 x 2048 x 2048 bfloat16 101, 99, 98 us; smaller planes are equal within 1 us.
 struct BiasPlan { bool fits; int64_t wave_rows, across, col_tiles, tiles, batch_per_part, batch_parts, parts; };
 
 BiasPlan bias_plan(const sdtw_bias_desc *d)
@@ -365,7 +365,7 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
         P.tiles = P.col_tiles * ((d->N + rows - 1) / rows);
     };
     // A wavefront goes down 64 rows, 8 a step - or 16, where that makes no more than a workgroup for each compute unit, and the steps' latency
-    // counts: 19.1 against 23.0 us at 4 x 1 x 64 x 64 float32, 24.7 and 28.6 at 16 x 8 x 300 x 300 bfloat16; but 42 against 36 at
+    // counts: 17.1 against 21.2 us at 4 x 1 x 64 x 64 float32, 22.5 and 26.4 at 16 x 8 x 300 x 300 bfloat16; but 38.3 against 34.5 at
     // 32 x 1 x 1024 x 1024 float32.
     tile(64);
     P.fits = P.tiles <= 0x7fffffff / d->H;
