@@ -78,24 +78,27 @@ __device__ __forceinline__ float slot_logit(const DistillParams &p, const RawSlo
 }
 
 // Exponentials are powers of two: exp(x / temperature) = 2^(c x), c = log2(e) / temperature in float32 (`scale2`; what that rounds c
-// by is a change of the temperature, the same for every term).  They are taken relative to a whole power R(m) of two near the
-// maximum m: 2^fma(x, c, -R) rounds its exponent once, and moving a sum to another maximum is exact.  Beyond 1e30 (a row of masks
-// of the type's lowest value) c m may overflow: there the reference is m itself.
-constexpr float kHuge = 1e30f;
-__device__ __forceinline__ bool huge_ref(float m) { return !(fabsf(m) <= kHuge); }
-__device__ __forceinline__ float whole_ref(float m, float c) { return huge_ref(m) ? 0.0f : rintf(m * c); }
+// by is a change of the temperature, the same for every term).  They are taken relative to a reference near the maximum m.  As long as
+// |c m| is at most 2^22, where float32 still holds quarters, that is the whole power R(m) = 2^rint(c m), off by less than one octave:
+// 2^fma(x, c, -R) rounds its exponent once, and moving a sum to another maximum is exact.  Beyond (masks of -1e9, -1e30, the type's
+// lowest value) rounding c m would cost octaves, and the reference is m itself, subtracted from x before the scaling: what lies within
+// a factor of 2 of m is subtracted exactly, and everything else is more than 2^21 octaves away.
+constexpr float kWhole = 4194304.0f;
+__device__ __forceinline__ bool huge_ref(float m, float c) { return !(fabsf(m * c) <= kWhole); }
+__device__ __forceinline__ float whole_ref(float m, float c) { return huge_ref(m, c) ? 0.0f : rintf(m * c); }
 __device__ __forceinline__ float finite_ref(float m) { return m == -INFINITY ? 0.0f : m; }
+// what is subtracted from x before the scaling
+__device__ __forceinline__ float sub_ref(float m, float c) { return huge_ref(m, c) ? finite_ref(m) : 0.0f; }
 // 2^(c x) relative to the reference of m; what the hot loops spell out
 __device__ __forceinline__ float exp_at(float x, float m, float c)
 {
-    const float sub = huge_ref(m) ? finite_ref(m) : 0.0f;
-    return __builtin_amdgcn_exp2f(fmaf(x - sub, c, -whole_ref(m, c)));
+    return __builtin_amdgcn_exp2f(fmaf(x - sub_ref(m, c), c, -whole_ref(m, c)));
 }
-// from the reference of a to that of m >= a (a maximum of -inf: nothing was summed)
+// from the reference of a to that of m >= a (a maximum of -inf: nothing was summed), whichever kinds they are
 __device__ __forceinline__ float move_ref(float a, float m, float c)
 {
     if (a == -INFINITY) return 0.0f;
-    return __builtin_amdgcn_exp2f(huge_ref(a) || huge_ref(m) ? (a - m) * c : whole_ref(a, c) - whole_ref(m, c));
+    return __builtin_amdgcn_exp2f(fmaf(sub_ref(a, c) - sub_ref(m, c), c, whole_ref(a, c) - whole_ref(m, c)));
 }
 
 // Maximum m of some logits and sum s of their exponentials relative to its reference.
@@ -350,7 +353,8 @@ __device__ __forceinline__ RowStats finish_row(const DistillParams &p, const Kep
 __device__ __forceinline__ double log_ref(const DistillParams &p, float m, float x)
 {
     const double sub = (double)x * p.student_inv_temperature;
-    return huge_ref(m) ? ((double)finite_ref(m) - (double)x) * p.student_inv_temperature : (double)whole_ref(m, p.scale2) * kLn2 - sub;
+    return huge_ref(m, p.scale2) ? ((double)finite_ref(m) - (double)x) * p.student_inv_temperature
+                                 : (double)whole_ref(m, p.scale2) * kLn2 - sub;
 }
 __device__ __forceinline__ float row_loss(const DistillParams &p, const Kept &kept, MaxSum sum, const RowStats &st)
 {
@@ -386,6 +390,7 @@ template <typename T, int U, bool STREAM> struct RowStream {
     template <bool MARKED> __device__ __forceinline__ MaxSum run(const uint32_t *bits, float scale2)
     {
         MaxSum acc{-INFINITY, 0.0f};
+        float acc_ref = 0.0f, acc_sub = 0.0f;  // the reference of acc.m
         for (int i0 = v0 + tid; i0 < v1; i0 += U * n) {
             Bits4 next[U];
             fetch(next, i0 + U * n);
@@ -405,15 +410,19 @@ template <typename T, int U, bool STREAM> struct RowStream {
             float m = acc.m;
 #pragma unroll
             for (int e = 0; e < W * U; ++e) m = fmaxf(m, x[e]);
-            const float ref = whole_ref(m, scale2);
-            if (huge_ref(m) && m != -INFINITY) {
+            const float ref = whole_ref(m, scale2), sub = sub_ref(m, scale2);
+            if (sub != 0.0f) {
 #pragma unroll
-                for (int e = 0; e < W * U; ++e) x[e] -= m;
+                for (int e = 0; e < W * U; ++e) x[e] -= sub;
             }
-            float s2[2] = {moved(acc, m, scale2), 0.0f};  // (two sums side by side)
+            // (move_ref with the references at hand; two sums side by side)
+            const float move = __builtin_amdgcn_exp2f(fmaf(acc_sub - sub, scale2, acc_ref - ref));
+            float s2[2] = {acc.m == -INFINITY ? acc.s : acc.s * move, 0.0f};
 #pragma unroll
             for (int e = 0; e < W * U; ++e) s2[e & 1] += __builtin_amdgcn_exp2f(fmaf(x[e], scale2, -ref));
             acc = {m, s2[0] + s2[1]};
+            acc_ref = ref;
+            acc_sub = sub;
 #pragma unroll
             for (int u = 0; u < U; ++u) v[u] = next[u];
         }
@@ -574,7 +583,7 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
         val[i] = g * (st.top * exp_at(kept_logit(z, id[i]), st.m, p.scale2) - q);
     }
     meet();  // dlogits may be the logits: the kept ones have been read
-    const float out = g * st.out, sub = huge_ref(st.off) ? finite_ref(st.off) : 0.0f, ref = whole_ref(st.off, p.scale2);
+    const float out = g * st.out, sub = sub_ref(st.off, p.scale2), ref = whole_ref(st.off, p.scale2);
     for (int i0 = v0 + thread; i0 < v1; i0 += U * TEAM) {
         Bits4 v[U];
 #pragma unroll
@@ -751,7 +760,7 @@ __global__ __launch_bounds__(1024, WAVES_PER_SIMD) void distill_rows_kernel(Dist
 #pragma unroll
             for (int w = 0; w < W; ++w) own.m = fmaxf(own.m, e[u * W + w]);
         }
-        if (huge_ref(own.m) && own.m != -INFINITY) {
+        if (huge_ref(own.m, p.scale2) && own.m != -INFINITY) {
 #pragma unroll
             for (int q = 0; q < NV * W; ++q) e[q] -= own.m;
         }
@@ -845,7 +854,7 @@ __global__ __launch_bounds__(256) void distill_short_kernel(DistillParams p, int
         }
     }
     m = wave_max_all_f32(m);
-    const float sub = huge_ref(m) ? finite_ref(m) : 0.0f, ref = whole_ref(m, p.scale2);
+    const float sub = sub_ref(m, p.scale2), ref = whole_ref(m, p.scale2);
     float s = 0.0f;
 #pragma unroll
     for (int q = 0; q < NV * W; ++q) {

@@ -627,3 +627,87 @@ def test_refusals_of_the_binding():
                 lambda: pkg.sdtw_position_bias_backward(torch.zeros((1, 2, 4, 4), device="cuda"), 300)):
         with pytest.raises(pkg.SdtwError):
             bad()
+
+
+# ---------------------------------------------------------------- masks of every size
+
+def definition(z, t, ids, tau, lse, g):
+    """As `reference`, for rows whose masked columns hold any finite number: a share of the tokens outside the kept ones is
+    taken among those tokens, not as the quotient of two probabilities that are both 0."""
+    T, V = z.shape
+    loss, grad, scale = np.zeros(T), np.zeros((T, V)), np.zeros((T, V))
+    for i in range(T):
+        own, b = z[i] / tau, t[i] / tau
+        a = own - own.max()
+        log_sum = np.log(np.exp(a).sum())
+        p = np.exp(a - log_sum)
+        log_q = b - (b.max() + np.log(np.exp(b - b.max()).sum()) if lse is None else lse[i])
+        q = np.exp(log_q)
+        loss[i] = (q * (log_q - a[ids[i]] + log_sum)).sum()
+        kept = np.zeros(V, bool)
+        kept[ids[i]] = True
+        Q, share = 1.0, np.zeros(V)
+        if lse is not None:
+            rest = max(0.0, 1.0 - q.sum())
+            Q = q.sum() + rest
+            out = own[~kept]
+            w = np.exp(out - out.max())  # (each maximum is taken off by itself: beside 1e20 the rest would vanish even in 64 bits)
+            loss[i] += rest * (math.log(rest) - (out.max() - own.max()) - math.log(w.sum()) + log_sum)
+            share[~kept] = rest * w / w.sum()
+        d, size = Q * p - share, Q * p + share
+        d[ids[i]] -= q
+        size[ids[i]] += q
+        grad[i], scale[i] = g[i] / tau * d, g[i] / tau * size
+    with np.errstate(over="ignore"):
+        loss = np.where(np.isinf(loss.astype(np.float32)), np.inf * np.sign(loss), loss)  # (beyond float32)
+    return loss, grad, scale
+
+
+MASKS = [-1e4, -1e9, -1e10, -1e20, -1e30, -2e30, LOW, 1e10, 1e30]
+
+
+@pytest.mark.parametrize("tau", [1e-6, 0.1, 0.7, 1.0, 2.0, 1e4])
+@pytest.mark.parametrize("V,copies,kind", [(700, 1, "f32"), (700, 20, "bf16"), (5000, 20, "f32"), (9001, 1, "bf16"), (9001, 20, "bf16"), (33001, 1, "f32"),
+                                           (33001, 20, "f32"), (70001, 1, "f32"), (70001, 12, "bf16")])
+def test_masks_of_every_size(V, copies, kind, tau):
+    """Rows in which a thread, a wavefront, a slice, the kept tokens, those outside them or all tokens hold one finite mask."""
+    gen = np.random.default_rng(V)
+    K, rows, spread = 5, [], min(1.0, tau)
+    for mask in [max(m, torch.finfo(TYPES[kind]).min) for m in MASKS]:
+        for form in range(6):
+            z = spread * gen.standard_normal(V)
+            ids = V - 1 - gen.permutation(V // 20)[:K]
+            if form == 0:    # most of the row, from the front
+                z[:V - V // 20] = mask
+            elif form == 1:  # most of the row, anywhere
+                hide = gen.random(V) < 0.95
+                hide[ids] = False
+                z[hide] = mask
+            elif form == 2:  # the kept tokens
+                z[ids] = mask
+            elif form == 3:  # everything
+                z[:] = mask
+            elif form == 4:  # everything outside the kept tokens
+                z[:] = mask
+                z[ids] = spread * gen.standard_normal(K)
+            else:            # everything but one token that is not kept
+                z[:] = mask
+                z[V // 2] = 0.5 * spread
+            rows.append((z, ids, spread * gen.standard_normal(K)))
+    n = len(rows)
+    z = torch.from_numpy(np.stack([r[0] for r in rows])).to(TYPES[kind]).cuda()
+    ids, t = (torch.from_numpy(np.stack([r[k] for r in rows])).cuda() for k in (1, 2))
+    t = t.float()
+    g = torch.from_numpy(gen.uniform(0.5, 2.0, n).astype(np.float32)).cuda()
+    for tail in (False, True):
+        lse = (torch.logsumexp(t.double() / float(np.float32(tau)), 1) + 0.3).float() if tail else None
+        want = definition(f64(z), f64(t), ids.cpu().numpy(), float(np.float32(tau)), None if lse is None else f64(lse), f64(g))
+        many = [None if x is None else x.repeat(copies, *[1] * (x.dim() - 1)) for x in (z, t, ids, lse, g)]
+        more = {"temperature": tau, "teacher_lse": many[3]}
+        loss, stats = pkg.sdtw_distill_forward(*many[:3], **more)
+        dz = pkg.sdtw_distill_backward(*many[:3], stats, grad_loss=many[4], **more)
+        for lo, d in ((loss, dz), pkg.sdtw_distill_step(*many[:3], grad_loss=many[4], **more)):
+            assert not torch.isnan(lo).any() and not torch.isnan(d).any()
+            for c in {0, copies // 2, copies - 1}:
+                check_loss(lo[n * c:n * c + n], want[0])
+                check_grad(d[n * c:n * c + n], want[1], want[2], kind)
