@@ -341,8 +341,8 @@ __device__ __forceinline__ RowStats finish_row(const DistillParams &p, const Kep
     st.off = tail ? sum.m : all.m;
     st.out = st.top;
     if (tail) {
-        // with no mass outside the gradient there is 0
-        st.out = sum.s == 0.0f ? 0.0f : st.top * move_ref(sum.m, all.m, p.scale2) - kept.tail * __builtin_amdgcn_rcpf(sum.s);
+        // with no mass outside the gradient there is 0 (NaN in a row that holds one)
+        st.out = sum.s == 0.0f ? 0.0f * st.top : st.top * move_ref(sum.m, all.m, p.scale2) - kept.tail * __builtin_amdgcn_rcpf(sum.s);
     }
     st.lq_hi = kept.lq_hi;
     st.lq_lo = kept.lq_lo;

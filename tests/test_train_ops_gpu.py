@@ -711,3 +711,19 @@ def test_masks_of_every_size(V, copies, kind, tau):
             for c in {0, copies // 2, copies - 1}:
                 check_loss(lo[n * c:n * c + n], want[0])
                 check_grad(d[n * c:n * c + n], want[1], want[2], kind)
+
+
+@pytest.mark.parametrize("V", [6, 3001, 9001, 70001])
+@pytest.mark.parametrize("copies", [1, 1500])
+def test_a_nan_among_the_kept_tokens_with_no_mass_outside(V, copies):
+    """The whole gradient of such a row is NaN, that of the tokens outside too, although they have no mass."""
+    z = torch.full((2, V), -INF, device="cuda")
+    z[:, [1, V - 1]] = torch.tensor([[NAN, 1.0], [0.5, 1.0]], device="cuda")
+    more = {"teacher_lse": torch.full((2 * copies,), 2.0, device="cuda")}
+    z, t = z.repeat(copies, 1), torch.tensor([[1.0, 0.0]], device="cuda").repeat(2 * copies, 1)
+    ids = torch.tensor([[1, V - 1]], device="cuda").repeat(2 * copies, 1)
+    loss, stats = pkg.sdtw_distill_forward(z, t, ids, **more)
+    dz = pkg.sdtw_distill_backward(z, t, ids, stats, **more)
+    for lo, d in ((loss, dz), pkg.sdtw_distill_step(z, t, ids, **more)):
+        assert torch.isnan(lo[::2]).all() and torch.isnan(d[::2]).all()
+        assert (lo[1::2] == INF).all() and torch.isfinite(d[1::2]).all()
