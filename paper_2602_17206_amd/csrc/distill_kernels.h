@@ -20,9 +20,9 @@ struct RowStats {
     float top;      // Q / the sum of the exponentials relative to m: a kept token's gradient is top * exp_at(z, m) - q
     float off;      // the others' is out * exp_at(z, off)
     float out;
-    float lq_hi;    // logarithm of the teacher's normaliser, in two parts
+    float t_ref;    // a kept teacher logit t has the probability exp((t - t_ref) / temperature - lq)
+    float lq_hi;    // lq in two parts
     float lq_lo;
-    float spare;
     uint32_t flags;
 };
 static_assert(sizeof(RowStats) == SDTW_DISTILL_STATS * sizeof(float), "stats layout");
@@ -247,7 +247,7 @@ struct Kept {
     double rest;    // what the tail holds of the teacher's mass; 0 if there is no tail
     double inner;   // sum of q_k (log q_k - (z_k - m) / temperature)
     float m, s;     // maximum of the student's kept logits and sum of their exponentials, each token once
-    float lq_hi, lq_lo;  // logarithm of the teacher's normaliser, in two parts
+    float t_ref, lq_hi, lq_lo;  // as in RowStats
     float Q, tail;  // mass + rest, and rest, in float32
     float q_scale;  // reduce_slots leaves q_k / q_scale where the slots' teacher logits were
     int tokens;     // how many different ones
@@ -278,16 +278,18 @@ __device__ __forceinline__ Kept reduce_slots(const DistillParams &p, int r, cons
         o.flags = __any(invalid) ? kRowInvalid : kRowNoTarget;
         return o;
     }
-    const double ref = p.tail ? (double)p.teacher_lse[r] : (double)finite_ref(wave_max_all_f32(mt)) * it;
+    // (renormalised: the logarithm of the sum stays apart from the largest logit, beside which it could vanish)
+    o.t_ref = p.tail ? 0.0f : finite_ref(wave_max_all_f32(mt));
+    const double lse = p.tail ? (double)p.teacher_lse[r] : 0.0;
     mk = wave_max_all_f32(mk);
     const float z_ref = finite_ref(mk);
-    double sum = 0.0, inner = 0.0, lq = ref;
+    double sum = 0.0, inner = 0.0, lq = lse;
     float sk = 0.0f;
     int tokens = 0;
     for (int k = lane; k < p.top; k += 64) {
         const int id = sl.id[k];
         if (id < 0) continue;
-        const double lk = (double)sl.t[k] * it - ref, w = exp(lk);
+        const double lk = ((double)sl.t[k] - (double)o.t_ref) * it - lse, w = exp(lk);
         sum += w;
         sl.t[k] = (float)w;
         if (w != 0.0) inner += w * (lk - ((double)sl.z[k] - (double)z_ref) * p.student_inv_temperature);
@@ -306,7 +308,7 @@ __device__ __forceinline__ Kept reduce_slots(const DistillParams &p, int r, cons
         o.inner = inner;
     } else {
         const double log_sum = log_of((float)sum);
-        lq = ref + log_sum;
+        lq = log_sum;
         o.q_scale = (float)(1.0 / sum);
         o.mass = sum == sum ? 1.0 : sum;  // (a NaN among the teacher's logits stays one)
         o.inner = inner / sum - log_sum;
@@ -344,6 +346,7 @@ __device__ __forceinline__ RowStats finish_row(const DistillParams &p, const Kep
         // with no mass outside the gradient there is 0 (NaN in a row that holds one)
         st.out = sum.s == 0.0f ? 0.0f * st.top : st.top * move_ref(sum.m, all.m, p.scale2) - kept.tail * __builtin_amdgcn_rcpf(sum.s);
     }
+    st.t_ref = kept.t_ref;
     st.lq_hi = kept.lq_hi;
     st.lq_lo = kept.lq_lo;
     return st;
@@ -566,7 +569,7 @@ __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
         if (k >= p.top) continue;
         const RawSlot raw = fetch_slot(p, r, k);
         id[i] = slot_id(p, raw);
-        val[i] = (float)exp((double)slot_logit(p, raw) * p.inv_temperature_d - lq);
+        val[i] = (float)exp(((double)slot_logit(p, raw) - (double)st.t_ref) * p.inv_temperature_d - lq);
         ids[k] = id[i];
         qs[k] = val[i];
     }

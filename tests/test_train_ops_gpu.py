@@ -727,3 +727,21 @@ def test_a_nan_among_the_kept_tokens_with_no_mass_outside(V, copies):
     for lo, d in ((loss, dz), pkg.sdtw_distill_step(z, t, ids, **more)):
         assert torch.isnan(lo[::2]).all() and torch.isnan(d[::2]).all()
         assert (lo[1::2] == INF).all() and torch.isfinite(d[1::2]).all()
+
+
+@pytest.mark.parametrize("tau", [0.5, 1.0, 2.0])
+@pytest.mark.parametrize("V", [50, 9001, 70001])
+def test_teacher_rows_at_the_ends_of_the_type(V, tau):
+    """The logarithm of such a row's normaliser is nothing beside its largest logit, and over a temperature below 1 that is beyond
+    float32; the shares of the kept tokens are those of the differences all the same."""
+    gen = np.random.default_rng(4)
+    z = torch.from_numpy(gen.standard_normal((5, V)).astype(np.float32)).cuda()
+    t = [[LOW, LOW, LOW], [LOW, LOW, 0.0], [3e38, 3e38, LOW], [-1e38, -1e38, -1e38], [1e12, 1e12, -1e12]]
+    same = [[0.0, 0.0, 0.0], [-INF, -INF, 0.0], [0.0, 0.0, -INF], [0.0, 0.0, 0.0], [0.0, 0.0, -INF]]
+    t, ids = torch.tensor(t, device="cuda"), torch.tensor([[3, 40, 7]] * 5, device="cuda")
+    loss, stats = pkg.sdtw_distill_forward(z, t, ids, temperature=tau)
+    dz = pkg.sdtw_distill_backward(z, t, ids, stats, temperature=tau)
+    want = reference(f64(z), np.array(same), ids.cpu().numpy(), tau)
+    for lo, d in ((loss, dz), pkg.sdtw_distill_step(z, t, ids, temperature=tau)):
+        check_loss(lo, want[0])
+        check_grad(d, want[1], want[2], "f32")
