@@ -353,7 +353,8 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
  *   forward   out[b,h,i,j] = in[b,h,i,j] + table[h, bucket(r)]
  *   backward  dtable[h,u] = sum over b, i, j with bucket(r) = u of scale[b] * grad[b,h,i,j]
  * With length vectors only the cells i < row_len[b], j < col_len[b] take part: the others are copied from `in`
- * (0 without one) by the forward call and not looked at by the backward call.
+ * (0 without one) by the forward call and not looked at by the backward call.  Nor is scale[b] where sequence b has no cell
+ * of a bucket: it may be 1 / 0 for an empty sequence.
  * Any B, H, N, M >= 0.  A scalar or per-sequence offset serves rows that continue a cached sequence (N = 1: one new token).
  */
 typedef struct sdtw_bias_desc {

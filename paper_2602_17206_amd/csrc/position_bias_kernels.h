@@ -311,10 +311,13 @@ __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams 
 #pragma unroll
             for (int k = 0; k < R; ++k) f[k] = 0.0f;
         }
-        for (int q = lane; q < Q; q += 64) {
-            diag[wave][q] += scale * (double)pass_sum[wave][q];
-            pass_sum[wave][q] = 0.0f;
-        }
+        // The diagonals that have a cell; the others hold zeros still, and no weight is looked at for them (1 / 0 where a sequence is empty).
+        const int nr = min(rlen - i0, p.wave_rows), nc = min(clen - j0, 64 * W);
+        if (nr > 0 && nc > 0)
+            for (int q = Z - nr + 1 + lane; q < Z + nc; q += 64) {
+                diag[wave][q] += scale * (double)pass_sum[wave][q];
+                pass_sum[wave][q] = 0.0f;
+            }
         wavefront_order();
         if (p.offsets) {  // (every sequence has its own diagonals' buckets)
             to_buckets((int64_t)p.offsets[b]);

@@ -745,3 +745,28 @@ def test_teacher_rows_at_the_ends_of_the_type(V, tau):
     for lo, d in ((loss, dz), pkg.sdtw_distill_step(z, t, ids, temperature=tau)):
         check_loss(lo, want[0])
         check_grad(d, want[1], want[2], "f32")
+
+
+@pytest.mark.parametrize("offset", [0, "own"])
+@pytest.mark.parametrize("kind", sorted(TYPES))
+def test_what_has_no_cell_takes_no_part_whatever_its_weight(kind, offset):
+    """A mean over a sequence's cells has the weight 1 / 0 where there are none; and a weight is not looked at in buckets of which the
+    sequence has no cell."""
+    B, H, N, M, buckets = 6, 2, 150, 1100, 32
+    g = whole_numbers((B, H, N, M), kind, 11)
+    g[4] = 1.0
+    rlen = torch.tensor([N, 0, 7, N, 2, 0], dtype=torch.int32, device="cuda")
+    clen = torch.tensor([M, M, 0, 600, 1, 0], dtype=torch.int32, device="cuda")
+    scale = torch.tensor([1.0, INF, NAN, 0.5, INF, -INF], device="cuda")
+    at_d = 0 if offset == 0 else torch.tensor([0, 3, 5, -40, 0, 9], dtype=torch.int32, device="cuda")
+    want = np.zeros((H, buckets))
+    for b in (0, 3, 4):
+        r, c = int(rlen[b]), int(clen[b])
+        at = bucket_matrix(N, M, buckets, 128, True, 0 if offset == 0 else int(at_d[b]))[:r, :c].ravel()
+        for h in range(H):
+            np.add.at(want[h], at, float(scale[b]) * f64(g[b, h, :r, :c]).ravel())
+    assert np.isinf(want[:, :2]).all() and np.isfinite(want[:, 2:]).all()  # (rows 0 and 1 of a column: distances 0 and 1)
+    got = pkg.sdtw_position_bias_backward(g, buckets, offset=at_d, row_len=rlen, col_len=clen, scale=scale)
+    np.testing.assert_array_equal(f64(got), want)
+    got = pkg.sdtw_position_bias_backward(g[1:3], buckets, row_len=rlen[1:3].contiguous(), col_len=clen[1:3].contiguous(), scale=scale[1:3].contiguous())
+    np.testing.assert_array_equal(f64(got), 0.0)
