@@ -333,7 +333,8 @@ BiasParams bias_params(const sdtw_bias_desc *d, const void *in, const int32_t *o
     BiasParams p{};
     p.B = d->B; p.H = d->H; p.N = d->N; p.M = d->M;
     p.buckets = d->buckets; p.table_type = d->table_type;
-    p.offset = d->offset;
+    // (|j - i| is below 2^30 and max_distance at most 2^24: beyond 2^32 every distance is in a last bucket, whatever the offset)
+    p.offset = std::min(std::max(d->offset, -((int64_t)1 << 32)), (int64_t)1 << 32);
     for (int i = 0; i < 3; ++i) { p.in_stride[i] = d->in_stride[i]; p.out_stride[i] = d->out_stride[i]; }
     p.table_stride[0] = d->table_stride[0]; p.table_stride[1] = d->table_stride[1];
     p.in = in;

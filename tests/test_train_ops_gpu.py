@@ -770,3 +770,18 @@ def test_what_has_no_cell_takes_no_part_whatever_its_weight(kind, offset):
     np.testing.assert_array_equal(f64(got), want)
     got = pkg.sdtw_position_bias_backward(g[1:3], buckets, row_len=rlen[1:3].contiguous(), col_len=clen[1:3].contiguous(), scale=scale[1:3].contiguous())
     np.testing.assert_array_equal(f64(got), 0.0)
+
+
+@pytest.mark.parametrize("two_sided", [True, False])
+@pytest.mark.parametrize("offset", [(1 << 62) - 1, 1 - (1 << 62), (1 << 62) - 700, 700 - (1 << 62), 1 << 40, -(1 << 31), 1 << 31, 1 << 30])
+def test_bias_at_offsets_up_to_the_limit(offset, two_sided):
+    """Every distance is in one last bucket: forward and gradient agree on which."""
+    N, M, buckets = 300, 1300, 32
+    plane = torch.zeros((2, 1, N, M), device="cuda")
+    table = torch.arange(float(buckets), device="cuda")[None]
+    last = {(True, True): 15, (True, False): 31, (False, True): 31, (False, False): 0}[two_sided, offset > 0]
+    out = pkg.sdtw_position_bias_forward(table, plane, two_sided=two_sided, offset=offset)
+    assert (out == last).all()
+    want = torch.zeros((1, buckets), device="cuda")
+    want[0, last] = 2 * N * M
+    assert torch.equal(pkg.sdtw_position_bias_backward(plane + 1, buckets, two_sided=two_sided, offset=offset), want)
