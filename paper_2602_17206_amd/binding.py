@@ -5,6 +5,7 @@ pointers through, and raises :class:`SdtwError` on a non-zero status.  PyTorch s
 device memory and the current stream; nothing is computed in Python and there is no
 fallback: if the library has not been built, the first call raises.
 """
+import contextlib
 import ctypes
 import functools
 import os
@@ -631,9 +632,19 @@ def _type_of(t, name):
     return kind
 
 
+def _given_stream(stream, device):
+    """With ``stream`` (a raw handle) the calls in this context run as on that stream: what they allocate belongs to it too, so
+    that no other stream is given the memory while the kernels are still at work, and no memory is taken that is in use elsewhere."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+
+    handle = int(stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device))
+
+
 def _on_given_stream(call):
-    """With ``stream`` (a raw handle) the call runs as on that stream: what it allocates belongs to it too, so that no other
-    stream is given the memory while the kernels are still at work."""
+    """The call with ``stream=``: see :func:`_given_stream`."""
     @functools.wraps(call)
     def on_stream(*args, stream=None, **kw):
         if stream is None:
@@ -641,9 +652,7 @@ def _on_given_stream(call):
         import torch
 
         device = next((a.device for a in (*args, *kw.values()) if torch.is_tensor(a)), None)
-        handle = int(stream)
-        given = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
-        with torch.cuda.stream(given):
+        with _given_stream(stream, device):
             return call(*args, **kw)
     return on_stream
 
@@ -901,6 +910,8 @@ def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, of
     desc.bandwidth = int(bandwidth)
     desc.flags |= (FLAG_VALUE_ONLY if value_only else 0) | (FLAG_MIN_MEMORY if min_memory else 0)
     dev = x.device
+    if not x.is_cuda:
+        raise ValueError("x must be a contiguous device tensor")
     if table.dim() != 2 or table.device != dev or table.shape[0] < 1 or desc.B % table.shape[0]:
         raise ValueError("table must be [H, buckets] on the sequences' device, the number of pairs a multiple of H")
     H, buckets = table.shape
@@ -911,13 +922,16 @@ def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, of
         nbytes = sdtw_biased_workspace_bytes(desc, bias)
         if nbytes == 0:
             raise SdtwError(STATUS_INVALID_ARG, "sdtw_biased_workspace_bytes")
-        workspace = Workspace(nbytes, dev)
-    if value is None:
-        value = torch.empty(desc.B, dtype=torch.float32, device=dev)
-    rc = lib.sdtw_forward_biased(ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"),
-                                 _ptr(y, torch.float32, name="y"), table.data_ptr(), _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"),
-                                 _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"), _ptr(value, torch.float32, (desc.B,), "value"),
-                                 workspace.ptr, workspace.nbytes, _stream_ptr(stream))
+    with _given_stream(stream, dev):
+        handle = _stream_of(dev)
+        if workspace is None:
+            workspace = Workspace(nbytes, dev)
+        if value is None:
+            value = torch.empty(desc.B, dtype=torch.float32, device=dev)
+        rc = lib.sdtw_forward_biased(ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"),
+                                     _ptr(y, torch.float32, name="y"), table.data_ptr(),
+                                     _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"), _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"),
+                                     _ptr(value, torch.float32, (desc.B,), "value"), workspace.ptr, workspace.nbytes, handle)
     if rc != 0:
         raise SdtwError(rc, "sdtw_forward_biased")
     return value, (desc, bias), workspace
@@ -932,20 +946,24 @@ def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=N
     lib = load_library()
     desc, bias = state
     dev = x.device
-    if dx is None:
-        dx = torch.empty((desc.B, desc.N, desc.D), dtype=torch.float32, device=dev)
-    if dy is None:
-        dy = torch.empty((desc.B, desc.M, desc.D), dtype=torch.float32, device=dev)
-    if dtable is None:
-        dtable = torch.empty((bias.H, bias.buckets), dtype=torch.float32, device=dev)
-    if want_E and E is None:
-        E = torch.empty((desc.B, desc.N, desc.M), dtype=torch.float32, device=dev)
-    rc = lib.sdtw_backward_biased(
-        ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"), _ptr(y, torch.float32, name="y"), table.data_ptr(),
-        _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"), _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"),
-        _ptr(grad_value, torch.float32, (desc.B,), "grad_value"), _ptr(dx, torch.float32, (desc.B, desc.N, desc.D), "dx"),
-        _ptr(dy, torch.float32, (desc.B, desc.M, desc.D), "dy"), _ptr(dtable, torch.float32, (bias.H, bias.buckets), "dtable"),
-        _ptr(E, torch.float32, (desc.B, desc.N, desc.M), "E"), workspace.ptr, workspace.nbytes, _stream_ptr(stream))
+    if not x.is_cuda:
+        raise ValueError("x must be a contiguous device tensor")
+    with _given_stream(stream, dev):
+        handle = _stream_of(dev)
+        if dx is None:
+            dx = torch.empty((desc.B, desc.N, desc.D), dtype=torch.float32, device=dev)
+        if dy is None:
+            dy = torch.empty((desc.B, desc.M, desc.D), dtype=torch.float32, device=dev)
+        if dtable is None:
+            dtable = torch.empty((bias.H, bias.buckets), dtype=torch.float32, device=dev)
+        if want_E and E is None:
+            E = torch.empty((desc.B, desc.N, desc.M), dtype=torch.float32, device=dev)
+        rc = lib.sdtw_backward_biased(
+            ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"), _ptr(y, torch.float32, name="y"), table.data_ptr(),
+            _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"), _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"),
+            _ptr(grad_value, torch.float32, (desc.B,), "grad_value"), _ptr(dx, torch.float32, (desc.B, desc.N, desc.D), "dx"),
+            _ptr(dy, torch.float32, (desc.B, desc.M, desc.D), "dy"), _ptr(dtable, torch.float32, (bias.H, bias.buckets), "dtable"),
+            _ptr(E, torch.float32, (desc.B, desc.N, desc.M), "E"), workspace.ptr, workspace.nbytes, handle)
     if rc != 0:
         raise SdtwError(rc, "sdtw_backward_biased")
     return dx, dy, dtable, E

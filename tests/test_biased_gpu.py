@@ -116,3 +116,44 @@ def test_refusals():
     with pytest.raises(pkg.SdtwError) as e:
         pkg.sdtw_backward_biased(state, x, y, table, ws)
     assert e.value.status == binding.STATUS_STATE
+
+
+def biased_on(stream, x, y, table, **kw):
+    """(value, dx, dy, dtable, E) of both calls on a stream given by its handle, or the current one"""
+    value, state, ws = pkg.sdtw_forward_biased(x, y, table, 0.5, stream=stream, **kw)
+    return (value, *pkg.sdtw_backward_biased(state, x, y, table, ws, want_E=True, stream=stream))
+
+
+def test_memory_of_a_call_on_another_stream_belongs_to_it():
+    """What a call allocates is not the current stream's to give away, nor to take from what its pending kernels use."""
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(5, 8, 300, 290, 16))
+    table = torch.rand((2, 32), device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = biased_on(side.cuda_stream, x, y, table)
+    torch.cuda.synchronize()
+    sizes = [t.numel() for t in out]
+    places = {t.data_ptr() for t in out}
+    del out
+    taken = [torch.empty(n, device="cuda") for n in sizes for _ in range(8)]
+    assert not places & {t.data_ptr() for t in taken}
+
+
+def test_calls_on_a_busy_stream_keep_their_memory():
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(5, 8, 300, 290, 16))
+    table = torch.rand((2, 32), device="cuda")
+    want = biased_on(None, x, y, table)
+    busy = torch.randn((4096, 4096), device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(side):
+            for _ in range(4):
+                busy @ busy
+        got = biased_on(side.cuda_stream, x, y, table)
+        alone = pkg.sdtw_forward_biased(x, y, table, 0.5, value_only=True, stream=side.cuda_stream)[0]  # (its workspace is let go)
+        kept = [torch.full((t.numel(),), 7.0, device="cuda") for t in got for _ in range(4)] + [torch.full((1 << k,), 7.0, device="cuda") for k in (20, 22, 23)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(alone, want[0])
+        assert all((k == 7.0).all() for k in kept)
+    assert all(torch.equal(a, b) for a, b in zip(biased_on(0, x, y, table), want))  # the default stream by its handle
