@@ -939,7 +939,7 @@ def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, of
 
 def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=None, y_len=None, want_E=False, dx=None, dy=None,
                          dtable=None, E=None, stream=None):
-    """Gradients of the values :func:`sdtw_forward_biased` produced (same tensors).
+    """Gradients of the values :func:`sdtw_forward_biased` produced (same tensors; the table may have another type or layout by now).
     Returns (dx, dy, dtable [H, buckets] float32, E or None)."""
     import torch
 
@@ -948,6 +948,12 @@ def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=N
     dev = x.device
     if not x.is_cuda:
         raise ValueError("x must be a contiguous device tensor")
+    if table.shape != (bias.H, bias.buckets) or table.device != dev:
+        raise ValueError("table must be [%d, %d] on %s" % (bias.H, bias.buckets, dev))
+    bias = BiasDesc.from_buffer_copy(bias)
+    bias.table_type, bias.table_stride[:] = _type_of(table, "table"), table.stride()
+    x_shape = (desc.N, desc.D) if desc.x_batch_stride == 0 else (desc.B, desc.N, desc.D)
+    y_shape = (desc.M, desc.D) if desc.y_batch_stride == 0 else (desc.B, desc.M, desc.D)
     with _given_stream(stream, dev):
         handle = _stream_of(dev)
         if dx is None:
@@ -959,7 +965,7 @@ def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=N
         if want_E and E is None:
             E = torch.empty((desc.B, desc.N, desc.M), dtype=torch.float32, device=dev)
         rc = lib.sdtw_backward_biased(
-            ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, name="x"), _ptr(y, torch.float32, name="y"), table.data_ptr(),
+            ctypes.byref(desc), ctypes.byref(bias), _ptr(x, torch.float32, x_shape, "x"), _ptr(y, torch.float32, y_shape, "y"), table.data_ptr(),
             _vector_ptr(x_len, desc.B, dev, torch.int32, "x_len"), _vector_ptr(y_len, desc.B, dev, torch.int32, "y_len"),
             _ptr(grad_value, torch.float32, (desc.B,), "grad_value"), _ptr(dx, torch.float32, (desc.B, desc.N, desc.D), "dx"),
             _ptr(dy, torch.float32, (desc.B, desc.M, desc.D), "dy"), _ptr(dtable, torch.float32, (bias.H, bias.buckets), "dtable"),

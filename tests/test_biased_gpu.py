@@ -157,3 +157,28 @@ def test_calls_on_a_busy_stream_keep_their_memory():
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(alone, want[0])
         assert all((k == 7.0).all() for k in kept)
     assert all(torch.equal(a, b) for a, b in zip(biased_on(0, x, y, table), want))  # the default stream by its handle
+
+
+def test_the_gradient_call_looks_at_the_tensors_it_is_given():
+    """The table's place in memory is that of the tensor at hand, not of the one that the values were computed with."""
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(6, 4, 30, 40, 4))
+    table = (torch.randint(0, 8, (2, 32), device="cuda") - 2).float() / 4  # (whole quarters: the same in 16 bits)
+    value, state, ws = pkg.sdtw_forward_biased(x, y, table, 1.0)
+    want = pkg.sdtw_backward_biased(state, x, y, table, ws, want_E=True)
+    wide = torch.zeros((32, 5), device="cuda")
+    wide[:, 1:5:3] = table.t()
+    for same in (table.half(), table.bfloat16(), table.t().contiguous().t(), wide[:, 1:5:3].t()):
+        value, state, ws = pkg.sdtw_forward_biased(x, y, table, 1.0)
+        got = pkg.sdtw_backward_biased(state, x, y, same, ws, want_E=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for bad in (table.cpu(), table[:1], table[:, :31], table.t(), table.reshape(-1), table.int(), torch.zeros((1, 2, 32), device="cuda")):
+        with pytest.raises(ValueError):
+            pkg.sdtw_backward_biased(state, x, y, bad, ws)
+    for a, b in ((x[:, :29].contiguous(), y), (x, y[:3]), (x[0], y), (x, y[..., :3].contiguous()), (x.cpu(), y), (x, y.cpu()), (x.half(), y)):
+        with pytest.raises(ValueError):
+            pkg.sdtw_backward_biased(state, a, b, table, ws)
+    # a sequence that all pairs share
+    value, state, ws = pkg.sdtw_forward_biased(x[0], y, table, 1.0)
+    assert pkg.sdtw_backward_biased(state, x[0], y, table, ws)[0].shape == (4, 30, 4)
+    with pytest.raises(ValueError):
+        pkg.sdtw_backward_biased(state, x, y, table, ws)
