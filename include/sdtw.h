@@ -404,7 +404,8 @@ int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, co
  *         max_distance, two_sided, offset, table_type and table_stride as above; in_stride and out_stride are not used.
  *   x_len, y_len: as for sdtw_forward_ragged, or NULL.
  *   dtable [H, buckets]: device, float32, out: the sum over the pairs of grad_value times the bucket's cells of E; or NULL.
- * Everything else as sdtw_forward / sdtw_backward; the workspace also holds E for a call that is given no E_out.
+ * Everything else as sdtw_forward / sdtw_backward; the workspace also holds E for a call that is given no E_out, unless
+ * SDTW_FLAG_VALUE_ONLY says that no gradient follows.
  */
 size_t sdtw_biased_workspace_bytes(const sdtw_desc *desc, const sdtw_bias_desc *bias);
 int sdtw_forward_biased(const sdtw_desc *desc, const sdtw_bias_desc *bias, const float *x, const float *y, const void *table,

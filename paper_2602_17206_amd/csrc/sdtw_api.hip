@@ -686,8 +686,8 @@ int sdtw_backward_half(const sdtw_desc *desc, const float *grad_value, float *dx
                          nullptr, 1);
 }
 
-// Soft-DTW under a learned position penalty: the plain workspace first (its header carries the status word), then a
-// dense E for calls without E_out, then the partial sums of the table's gradient.
+// Soft-DTW under a learned position penalty: the plain workspace first (its header carries the status word), then, where a
+// gradient can follow, a dense E for calls without E_out and the partial sums of the table's gradient.
 struct BiasedLayout { size_t off_E, off_sums, total; sdtw_bias_desc planes; };
 
 static bool biased_layout(const sdtw_desc *d, const sdtw_bias_desc *bias, BiasedLayout *L)
@@ -702,7 +702,8 @@ static bool biased_layout(const sdtw_desc *d, const sdtw_bias_desc *bias, Biased
     L->planes.in_stride[2] = L->planes.out_stride[2] = d->M;
     const size_t sums = sdtw_position_bias_workspace_bytes(&L->planes);
     if (sums == 0) return false;
-    L->off_E = align_up(layout_of(d).total, 256);
+    L->off_E = L->off_sums = L->total = align_up(layout_of(d).total, 256);
+    if (d->flags & SDTW_FLAG_VALUE_ONLY) return true;
     L->off_sums = align_up(L->off_E + (size_t)d->B * cells * sizeof(float), 256);
     L->total = align_up(L->off_sums + sums, 256);
     return true;

@@ -199,3 +199,16 @@ def test_position_penalty_entry_points_refuse():
     assert both(d, b, table=None) == {binding.STATUS_INVALID_ARG}
     assert both(d, b, ws=None) == {binding.STATUS_WORKSPACE}
     assert both(d, b, nbytes=need - 1) == {binding.STATUS_WORKSPACE}
+
+
+@pytest.mark.parametrize("B,N,M,D", [(6, 8, 9, 4), (32, 1024, 1024, 128), (32, 8192, 8192, 128)])
+def test_values_alone_need_no_more_workspace_than_without_a_penalty(B, N, M, D):
+    lib = pkg.load_library()
+    b = bias_desc(B=B // 2, H=2, N=N, M=M)
+    for flags in (binding.FLAG_VALUE_ONLY, binding.FLAG_VALUE_ONLY | binding.FLAG_MIN_MEMORY):
+        d = binding.make_desc(B, N, M, D, 1.0, pkg.UNFUSED, flags=flags)
+        need = lib.sdtw_biased_workspace_bytes(ctypes.byref(d), ctypes.byref(b))
+        assert pkg.sdtw_workspace_bytes(d) <= need < pkg.sdtw_workspace_bytes(d) + 256
+        args = [FAKE, FAKE, FAKE, None, None, FAKE, FAKE]
+        assert lib.sdtw_forward_biased(ctypes.byref(d), ctypes.byref(b), *args, need - 256, None) == binding.STATUS_WORKSPACE
+        assert lib.sdtw_biased_workspace_bytes(ctypes.byref(d), ctypes.byref(bias_desc(B=B // 2, H=2, N=N, M=M, buckets=31))) == 0
