@@ -265,6 +265,7 @@ int sdtw_normalized_backward(const sdtw_desc *desc, const float *x, const float 
  * Element types of their tensors (SDTW_INPUT_F16 and SDTW_INPUT_BF16 name the same types above).  All
  * sums, maxima and exponentials are carried in 32 bits or more; results are rounded once, on store.
  * Pointers need the alignment of one element only; rows may start anywhere.
+ * A call one of whose kernels would take 2^32 threads or more (some 2^24 rows or planes) is refused: SDTW_ERR_INVALID_ARG.
  */
 enum { SDTW_TYPE_F32 = 0, SDTW_TYPE_F16 = 1, SDTW_TYPE_BF16 = 2 };
 enum { SDTW_ID_I32 = 0, SDTW_ID_I64 = 1 };
@@ -383,7 +384,7 @@ int sdtw_position_bias_starts(const sdtw_bias_desc *desc, int32_t *starts);
 int sdtw_position_bias_forward(const sdtw_bias_desc *desc, const void *table, const void *in, const int32_t *offsets,
                                const int32_t *row_len, const int32_t *col_len, void *out, void *stream);
 
-/* Bytes of workspace of sdtw_position_bias_backward; 0 if the descriptor is invalid or takes more than 2^31 workgroups.  Host only. */
+/* Bytes of workspace of sdtw_position_bias_backward; 0 if the descriptor is invalid or takes 2^24 workgroups or more.  Host only. */
 size_t sdtw_position_bias_workspace_bytes(const sdtw_bias_desc *desc);
 
 /*

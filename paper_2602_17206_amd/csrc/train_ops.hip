@@ -31,6 +31,9 @@ template <typename F> void with_type(int type, F f)
 
 int width_of(int type) { return type == SDTW_TYPE_F32 ? 4 : 8; }
 
+// A grid has fewer than 2^32 threads.
+bool grid_ok(int64_t workgroups, int threads) { return workgroups <= 0xffffffffll / threads; }
+
 // ---------------------------------------------------------------- distillation
 
 struct DistillPlan {
@@ -151,19 +154,28 @@ void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, boo
     }
 }
 
+// The gradient alone of rows of at most 512 vectors is a wavefront's each: 33 against 51 us at 16384 x 1000 float32, 22 against 42 in
+// bfloat16, and 56 against 58 at 16384 x 2000 float32; with twice as many vectors 60 against 52 at 8192 x 4000.
+bool wavefront_slices(const DistillPlan &P, int top) { return P.back_slices == 1 && P.back_vecs <= 512 && top <= kRowsTop; }
+
+// (256 threads each)
+int64_t distill_backward_workgroups(const DistillPlan &P, int32_t rows, int top)
+{
+    const int64_t slices = rows * (int64_t)P.back_slices;
+    return wavefront_slices(P, top) ? (slices + 3) / 4 : slices;
+}
+
 void launch_distill_backward(const DistillPlan &P, DistillParams p, int type, hipStream_t st)
 {
     p.slices = P.back_slices;
     p.slice_vecs = P.back_vecs;
     ProfScope ps("distill_backward", st);
-    const int64_t slices = p.rows * (int64_t)P.back_slices;
+    const unsigned grid = (unsigned)distill_backward_workgroups(P, p.rows, p.top);
     with_type(type, [&](auto t) {
-        // Rows of at most 512 vectors: a wavefront each, 33 against 51 us at 16384 x 1000 float32, 22 against 42 in bfloat16, and 56
-        // against 58 at 16384 x 2000 float32; with twice as many vectors 60 against 52 at 8192 x 4000.
-        if (P.back_slices == 1 && P.back_vecs <= 512 && p.top <= kRowsTop)
-            distill_backward_kernel<decltype(t), 64, kRowsTop><<<(unsigned)((slices + 3) / 4), 256, 0, st>>>(p);
+        if (wavefront_slices(P, p.top))
+            distill_backward_kernel<decltype(t), 64, kRowsTop><<<grid, 256, 0, st>>>(p);
         else
-            distill_backward_kernel<decltype(t), 256, kMaxTop><<<(unsigned)slices, 256, 0, st>>>(p);
+            distill_backward_kernel<decltype(t), 256, kMaxTop><<<grid, 256, 0, st>>>(p);
     });
 }
 
@@ -198,10 +210,13 @@ RowsShape rows_shape(const sdtw_distill_desc *d, const void *logits)
     return {0, 0, 0};
 }
 
+// (256 threads each)
+int64_t short_workgroups(const sdtw_distill_desc *d) { return ((int64_t)d->rows + 3) / 4; }
+
 template <bool GRAD> void launch_distill_short(const sdtw_distill_desc *d, int vectors, const DistillParams &p, hipStream_t st)
 {
     const int team = (d->top * 12 + vectors * 8 * width_of(d->logit_type) + 15) / 16 * 16;
-    const unsigned grid = (unsigned)(((int64_t)d->rows + 3) / 4);
+    const unsigned grid = (unsigned)short_workgroups(d);
     ProfScope ps(GRAD ? "distill_step" : "distill_forward", st);
     with_type(d->logit_type, [&](auto t) {
         using T = decltype(t);
@@ -234,10 +249,8 @@ void launch_distill_rows(const sdtw_distill_desc *d, RowsShape s, const DistillP
     });
 }
 
-bool distill_grid_ok(const sdtw_distill_desc *d, const DistillPlan &P)
-{
-    return (int64_t)d->rows * std::max(P.slices, P.back_slices) <= 0x7fffffff;
-}
+bool forward_grid_ok(const sdtw_distill_desc *d, const DistillPlan &P) { return grid_ok(d->rows * (int64_t)P.slices, P.threads); }
+bool backward_grid_ok(const sdtw_distill_desc *d, const DistillPlan &P) { return grid_ok(distill_backward_workgroups(P, d->rows, d->top), 256); }
 
 // ---------------------------------------------------------------- position bias
 
@@ -347,7 +360,7 @@ bool begins_on_vectors(const void *plane, const int64_t (&stride)[3], int W)
     return reinterpret_cast<uintptr_t>(plane) % 16 == 0 && stride[0] % W == 0 && stride[1] % W == 0 && stride[2] % W == 0;
 }
 
-// How the backward pass is split (`fits`: into workgroups that can be counted): tiles of the plane, then the batch, into 2048
+// How the backward pass is split (`fits`: into a grid that can be launched): tiles of the plane, then the batch, into 2048
 // workgroups where it has them.  Measured with 1024, 2048, 8192: 32 x 1 x 8192 x 8192 float32 1330, 1315, 1324 us,
 // 4 x 16 x 2048 x 2048 bfloat16 101, 99, 98 us; smaller planes are equal within 1 us.
 struct BiasPlan { bool fits; int64_t wave_rows, across, col_tiles, tiles, batch_per_part, batch_parts, parts; };
@@ -355,8 +368,8 @@ struct BiasPlan { bool fits; int64_t wave_rows, across, col_tiles, tiles, batch_
 BiasPlan bias_plan(const sdtw_bias_desc *d)
 {
     BiasPlan P{};
-    P.fits = true;
-    if (d->B == 0 || d->H == 0 || d->N == 0 || d->M == 0) return P;
+    P.fits = grid_ok(d->H * (int64_t)d->buckets, 256);  // (the second kernel)
+    if (!P.fits || d->B == 0 || d->H == 0 || d->N == 0 || d->M == 0) return P;
     const int64_t width = 64 * width_of(d->plane_type), want = 2048;
     P.across = d->M > 2 * width ? 4 : d->M > width ? 2 : 1;
     P.col_tiles = (d->M + P.across * width - 1) / (P.across * width);
@@ -369,7 +382,7 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
     // counts: 17.1 against 21.2 us at 4 x 1 x 64 x 64 float32, 22.5 and 26.4 at 16 x 8 x 300 x 300 bfloat16; but 38.3 against 34.5 at
     // 32 x 1 x 1024 x 1024 float32.
     tile(64);
-    P.fits = P.tiles <= 0x7fffffff / d->H;
+    P.fits = P.tiles <= 0x7fffffff / d->H;  // (what follows stays within 64 bits)
     if (!P.fits) return P;
     if (P.tiles * d->H * d->B <= 256) tile(16);
     const int64_t units = P.tiles * d->H;
@@ -377,7 +390,7 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
     P.batch_per_part = (d->B + P.batch_parts - 1) / P.batch_parts;
     P.batch_parts = (d->B + P.batch_per_part - 1) / P.batch_per_part;
     P.parts = P.tiles * P.batch_parts;
-    P.fits = P.parts <= 0x7fffffff / d->H;
+    P.fits = grid_ok(P.parts * d->H, 256);
     return P;
 }
 
@@ -405,7 +418,7 @@ int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalt
     p.col_tiles = (desc->M + cols - 1) / cols;
     p.row_tiles = (desc->N + rows - 1) / rows;
     const int64_t tiles = (int64_t)p.col_tiles * p.row_tiles, planes = (int64_t)desc->B * desc->H;
-    if (tiles > 0x7fffffff / planes) return SDTW_ERR_INVALID_ARG;
+    if (!grid_ok(planes, 256) || !grid_ok(tiles, 256) || !grid_ok(tiles * planes, 256)) return SDTW_ERR_INVALID_ARG;
     (void)hipGetLastError();
     const BucketRule rule = bucket_rule(desc);
     {
@@ -436,7 +449,7 @@ int position_bias_table_grad(const sdtw_bias_desc *desc, const void *penalty_tab
     if (desc->H == 0) return SDTW_OK;
     const BiasPlan P = bias_plan(desc);
     if (!dtable || (!grad && P.parts > 0)) return SDTW_ERR_INVALID_ARG;
-    if (!P.fits || (int64_t)desc->H * desc->buckets > 0x7fffffff) return SDTW_ERR_INVALID_ARG;
+    if (!P.fits) return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, sdtw_position_bias_workspace_bytes(desc))) return rc;
     (void)hipGetLastError();
     BiasParams p = bias_params(desc, grad, offsets, row_len, col_len);
@@ -484,7 +497,8 @@ int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, cons
     if (desc->rows == 0) return SDTW_OK;
     if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !loss || !stats) return SDTW_ERR_INVALID_ARG;
     const DistillPlan P = distill_plan(desc);
-    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    const int vectors = short_vectors(desc, logits, false);
+    if (!(vectors ? grid_ok(short_workgroups(desc), 256) : forward_grid_ok(desc, P))) return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
     (void)hipGetLastError();  // what an earlier, unrelated call left behind is not this call's error
     DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
@@ -492,7 +506,7 @@ int sdtw_distill_forward(const sdtw_distill_desc *desc, const void *logits, cons
     p.stats = reinterpret_cast<RowStats *>(stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (const int vectors = short_vectors(desc, logits, false))
+    if (vectors)
         launch_distill_short<false>(desc, vectors, p, st);
     else
         launch_distill_forward(P, p, desc->logit_type, true, st);
@@ -508,7 +522,7 @@ int sdtw_distill_backward(const sdtw_distill_desc *desc, const void *logits, con
     if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !stats || !dlogits) return SDTW_ERR_INVALID_ARG;
     if (dlogits == logits && desc->grad_stride != desc->logit_stride) return SDTW_ERR_INVALID_ARG;
     const DistillPlan P = distill_plan(desc);
-    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    if (!backward_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
     (void)hipGetLastError();
     DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
     p.grad_loss = grad_loss;
@@ -527,7 +541,11 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
     if (!distill_args_ok(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row) || !loss || !dlogits) return SDTW_ERR_INVALID_ARG;
     if (dlogits == logits && desc->grad_stride != desc->logit_stride) return SDTW_ERR_INVALID_ARG;
     const DistillPlan P = distill_plan(desc);
-    if (!distill_grid_ok(desc, P)) return SDTW_ERR_INVALID_ARG;
+    const int vectors = short_vectors(desc, logits, true);
+    const RowsShape shape = rows_shape(desc, logits);
+    const bool one_read = shape.vectors > 0 && desc->top <= kRowsTop;  // (a grid of what is resident)
+    if (!(vectors ? grid_ok(short_workgroups(desc), 256) : one_read || (forward_grid_ok(desc, P) && backward_grid_ok(desc, P))))
+        return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
     (void)hipGetLastError();
     DistillParams p = distill_params(desc, logits, teacher_logits, teacher_ids, teacher_lse, teacher_row);
@@ -537,12 +555,11 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
     p.stats = reinterpret_cast<RowStats *>(static_cast<char *>(workspace) + P.off_stats);
     p.partial = reinterpret_cast<float4 *>(static_cast<char *>(workspace) + P.off_partial);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (const int vectors = short_vectors(desc, logits, true)) {
+    if (vectors) {
         launch_distill_short<true>(desc, vectors, p, st);
         return hip_ok();
     }
-    const RowsShape shape = rows_shape(desc, logits);
-    if (shape.vectors > 0 && desc->top <= kRowsTop) {
+    if (one_read) {
         launch_distill_rows(desc, shape, p, st);
         return hip_ok();
     }

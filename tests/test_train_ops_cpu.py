@@ -212,3 +212,26 @@ def test_values_alone_need_no_more_workspace_than_without_a_penalty(B, N, M, D):
         args = [FAKE, FAKE, FAKE, None, None, FAKE, FAKE]
         assert lib.sdtw_forward_biased(ctypes.byref(d), ctypes.byref(b), *args, need - 256, None) == binding.STATUS_WORKSPACE
         assert lib.sdtw_biased_workspace_bytes(ctypes.byref(d), ctypes.byref(bias_desc(B=B // 2, H=2, N=N, M=M, buckets=31))) == 0
+
+
+def test_grids_of_2_to_the_32_threads_are_refused():
+    """Short rows take a quarter of a workgroup of 256 threads each, rows with many slots a workgroup, planes one at least."""
+    lib = pkg.load_library()
+    other = ctypes.c_void_p(0x20000)
+    for kw in (dict(rows=1 << 26, teacher_rows=1 << 26), dict(rows=1 << 25, teacher_rows=1 << 25, top=200, teacher_stride=200, id_stride=200),
+               dict(rows=(1 << 31) - 1, teacher_rows=(1 << 31) - 1), dict(rows=1 << 25, teacher_rows=1 << 25, vocab=1 << 20, logit_stride=1 << 20, grad_stride=1 << 20)):
+        d = distill_desc(**kw)
+        ref = ctypes.byref(d)
+        assert lib.sdtw_distill_forward(ref, FAKE, FAKE, FAKE, None, None, FAKE, FAKE, FAKE, 1 << 50, None) == binding.STATUS_INVALID_ARG, kw
+        assert lib.sdtw_distill_backward(ref, FAKE, FAKE, FAKE, None, None, None, FAKE, other, None) == binding.STATUS_INVALID_ARG, kw
+        assert lib.sdtw_distill_step(ref, FAKE, FAKE, FAKE, None, None, None, FAKE, other, FAKE, 1 << 50, None) == binding.STATUS_INVALID_ARG, kw
+    for kw in (dict(B=1, H=1 << 19, N=1, M=1), dict(B=1, H=1, N=1 << 29, M=1 << 29), dict(B=(1 << 31) - 1, H=(1 << 31) - 1, N=1, M=1)):
+        d = bias_desc(in_stride=(0, 0, 0), **kw)
+        assert lib.sdtw_position_bias_workspace_bytes(ctypes.byref(d)) == 0, kw
+        assert lib.sdtw_position_bias_backward(ctypes.byref(d), FAKE, None, None, None, None, other, FAKE, 1 << 50, None) == binding.STATUS_INVALID_ARG, kw
+    for kw in (dict(B=1 << 22, H=4, N=1, M=1, out_stride=(4, 1, 1)), dict(B=1, H=1, N=1 << 29, M=1 << 29, out_stride=(1, 1, 1 << 29))):
+        d = bias_desc(in_stride=(0, 0, 0), **kw)
+        assert lib.sdtw_position_bias_forward(ctypes.byref(d), FAKE, FAKE, None, None, None, other, None) == binding.STATUS_INVALID_ARG, kw
+    # what just fits is still planned for
+    d = bias_desc(B=1, H=(1 << 19) - 1, N=1, M=1)
+    assert lib.sdtw_position_bias_workspace_bytes(ctypes.byref(d)) >= 8 * 32 * ((1 << 19) - 1)
