@@ -42,11 +42,14 @@ struct DistillPlan {
     size_t off_stats, off_partial, total;
 };
 
+// log2(e) / temperature in float32, what the kernels scale a logit by
+float octaves_of(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
+
 bool distill_ok(const sdtw_distill_desc *d)
 {
     if (!d) return false;
     if (d->rows < 0 || d->vocab < 1 || d->vocab >= 1 << 30 || d->top < 1 || d->top > kMaxTop || d->teacher_rows < 1) return false;
-    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(1.0f / d->temperature)) return false;
+    if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(octaves_of(d->temperature))) return false;
     if (d->target != SDTW_DISTILL_RENORMALIZED && d->target != SDTW_DISTILL_TAIL) return false;
     if (!type_ok(d->logit_type) || !type_ok(d->teacher_type)) return false;
     if (d->id_type != SDTW_ID_I32 && d->id_type != SDTW_ID_I64) return false;
@@ -119,7 +122,7 @@ DistillParams distill_params(const sdtw_distill_desc *d, const void *logits, con
     p.teacher_type = d->teacher_type; p.id64 = d->id_type == SDTW_ID_I64; p.tail = d->target == SDTW_DISTILL_TAIL;
     p.inv_temperature_d = 1.0 / (double)d->temperature;
     p.inv_temperature = (float)p.inv_temperature_d;
-    p.scale2 = (float)(1.4426950408889634 * p.inv_temperature_d);
+    p.scale2 = octaves_of(d->temperature);
     p.student_inv_temperature = (double)p.scale2 * kLn2;
     p.logit_stride = d->logit_stride; p.grad_stride = d->grad_stride;
     p.teacher_stride = d->teacher_stride; p.id_stride = d->id_stride;

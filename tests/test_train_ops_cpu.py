@@ -235,3 +235,12 @@ def test_grids_of_2_to_the_32_threads_are_refused():
     # what just fits is still planned for
     d = bias_desc(B=1, H=(1 << 19) - 1, N=1, M=1)
     assert lib.sdtw_position_bias_workspace_bytes(ctypes.byref(d)) >= 8 * 32 * ((1 << 19) - 1)
+
+
+def test_temperatures_whose_scale_is_beyond_float32_are_refused():
+    lib = pkg.load_library()
+    for temperature, fine in ((3e-39, False), (4.2e-39, False), (4.3e-39, True), (1e-30, True), (3e38, True)):
+        d = distill_desc(temperature=temperature)
+        assert (lib.sdtw_distill_workspace_bytes(ctypes.byref(d)) > 0) == fine, temperature
+        if not fine:
+            assert lib.sdtw_distill_step(ctypes.byref(d), FAKE, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, 1 << 30, None) == binding.STATUS_INVALID_ARG
