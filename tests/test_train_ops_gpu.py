@@ -785,3 +785,72 @@ def test_bias_at_offsets_up_to_the_limit(offset, two_sided):
     want = torch.zeros((1, buckets), device="cuda")
     want[0, last] = 2 * N * M
     assert torch.equal(pkg.sdtw_position_bias_backward(plane + 1, buckets, two_sided=two_sided, offset=offset), want)
+
+
+# ---------------------------------------------------------------- several rows of a workgroup, sums beyond float32
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("T,V,kind,pad", [(2300, 5003, "bf16", 0), (2300, 5003, "f16", 2), (1300, 9001, "f32", 0), (800, 33001, "f32", 0), (800, 33001, "f32", 3),
+                                          (700, 50021, "bf16", 0)])
+def test_rows_that_a_workgroup_takes_one_after_the_other(T, V, kind, pad, tail):
+    """Rows that begin anywhere in a vector, more of them than workgroups: vectors shared by two rows, which other workgroups may hold, and
+    the ring of slots.  In place as well: a row's gradient is written while the next rows are read."""
+    s = problem(T, V, 30, kind, tail, 1.0, V, mapped=True, pad=pad)
+    more = {"teacher_lse": s["lse"], "teacher_row": s["at"], "grad_loss": s["g"]}
+    loss, dz = pkg.sdtw_distill_step(s["z"], s["t"], s["ids"], **more)
+    rows = torch.unique(torch.cat([torch.arange(0, T, 97), torch.arange(T - 5, T)])).cuda()
+    pick = lambda x: None if x is None else f64(x[rows])  # noqa: E731
+    want = reference(pick(s["z"]), f64(s["t"]), s["ids"].cpu().numpy(), 1.0, None if s["lse"] is None else f64(s["lse"]),
+                     s["at"][rows].cpu().numpy(), pick(s["g"]))
+    check_loss(loss[rows], want[0])
+    check_grad(dz[rows], want[1], want[2], kind)
+    # Every row's gradient sums to 0: to a rounding of its type for each element, and 4e-6 of Q p, of q and of the tail's share, 1 each in sum.
+    free = (s["at"] < 0)
+    assert (loss[free] == 0).all() and (dz[free] == 0).all()
+    size = dz.double().abs().sum(1)
+    assert (dz.double().sum(1).abs() <= HALF_ULP[kind] * size + 12e-6 * s["g"].double() + V * LEAST[kind]).all()
+    room = torch.empty((T, V + pad), dtype=TYPES[kind], device="cuda").fill_(7.0)
+    room[:, :V] = s["z"]
+    loss_in, _ = pkg.sdtw_distill_step(room[:, :V], s["t"], s["ids"], dlogits=room[:, :V], **more)
+    assert torch.equal(room[:, :V], dz) and torch.equal(loss_in, loss) and (room[:, V:] == 7.0).all()
+
+
+@pytest.mark.parametrize("scaled", [False, True])
+@pytest.mark.parametrize("kind,most", [("f32", 1 << 16), ("f16", 1 << 11), ("bf16", 1 << 8)])
+@pytest.mark.parametrize("B,H,N,M", [(3, 2, 2048, 2050), (40, 1, 600, 700), (2, 3, 65, 9000)])
+def test_bias_gradient_of_sums_beyond_float32(B, H, N, M, kind, most, scaled):
+    """Whole numbers whose sums over 64 rows of a diagonal are below 2^24, and over a bucket far above: carried in 64 bits they are exact, and
+    the table's entry is the sum rounded once.  (Weights of a few bits leave them exact.)"""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    g = torch.randint(most // 2, most + 1, (B, H, N, M), generator=gen, device="cuda")
+    g = (g * 2 - 1 if kind == "f32" else g).to(TYPES[kind])
+    scale = (torch.randint(32, 64, (B,), generator=gen, device="cuda") * 2 + 1).float() / 128 if scaled else None
+    dt = pkg.sdtw_position_bias_backward(g, 32, scale=scale)
+    at = torch.from_numpy(bucket_matrix(N, M, 32, 128, True, 0)).cuda()
+    total = (g.double() * (1.0 if scale is None else scale.double()[:, None, None, None])).sum(0)
+    want = torch.stack([torch.stack([(total[h] * (at == u)).sum() for u in range(32)]) for h in range(H)])
+    assert float(want.abs().max()) > 2 ** 25
+    assert torch.equal(dt, want.float())
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("B,H,N,M,lengths", [(4, 2, 900, 1100, True), (2, 1, 3000, 500, False), (1, 4, 130, 4100, True)])
+def test_bias_gradient_of_real_numbers(B, H, N, M, lengths, kind):
+    """Up to 64 terms of a diagonal are added in float32, the rest in 64 bits: an entry is off by (1 + 2^-24)^63 - 1 < 64 * 2^-24 of the sum of what
+    it adds up in magnitude at most, and by one rounding."""
+    gen = torch.Generator(device="cuda").manual_seed(N)
+    g = torch.randn((B, H, N, M), generator=gen, device="cuda").to(TYPES[kind])
+    scale = torch.rand(B, generator=gen, device="cuda") + 0.1
+    rlen = torch.randint(N // 2, N + 1, (B,), generator=gen, device="cuda", dtype=torch.int32) if lengths else None
+    clen = torch.randint(M // 2, M + 1, (B,), generator=gen, device="cuda", dtype=torch.int32) if lengths else None
+    dt = pkg.sdtw_position_bias_backward(g, 64, max_distance=700, two_sided=False, row_len=rlen, col_len=clen, scale=scale).double()
+    w = g.double() * scale.double()[:, None, None, None]
+    if lengths:
+        inside = (torch.arange(N, device="cuda")[:, None] < rlen[:, None, None]) & (torch.arange(M, device="cuda") < clen[:, None, None])
+        w = w * inside[:, None]
+    at = torch.from_numpy(bucket_matrix(N, M, 64, 700, False, 0)).cuda()
+    for h in range(H):
+        for u in range(64):
+            part = w[:, h][:, at == u]
+            want, size = float(part.sum()), float(part.abs().sum())
+            assert abs(float(dt[h, u]) - want) <= 64 * 2.0 ** -24 * size + 2.0 ** -24 * abs(want) + 1e-12 * size, (h, u)
