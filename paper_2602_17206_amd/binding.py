@@ -684,6 +684,19 @@ def _vector_ptr(t, n, device, dtype, name):
     return t.data_ptr()
 
 
+_I32, _I64 = 1 << 31, 1 << 63
+
+
+def _whole(v, limit, name):
+    """v as a whole number of [-limit, limit): a descriptor's field would drop what it does not hold."""
+    if type(v) is int and -limit <= v < limit:
+        return v
+    n = int(v)
+    if n != v or not -limit <= n < limit:
+        raise ValueError("%s must be a whole number below 2^%d" % (name, limit.bit_length() - 1))
+    return n
+
+
 def _distill_args(logits, teacher_logits, teacher_ids, temperature, teacher_lse, teacher_row):
     """(descriptor, the pointers every distillation call begins with)"""
     import torch
@@ -811,7 +824,7 @@ def _bias_args(plane, shape, dtype, device, buckets, max_distance, two_sided, of
     import torch
 
     B, H, N, M = shape
-    desc = BiasDesc(B, H, N, M, int(buckets), int(max_distance), 1 if two_sided else 0, 0, 0, 0)
+    desc = BiasDesc(B, H, N, M, _whole(buckets, _I32, "buckets"), _whole(max_distance, _I32, "max_distance"), 1 if two_sided else 0, 0, 0, 0)
     if plane is not None:
         if plane.dim() != 4 or not plane.is_cuda:
             raise ValueError("%s must be a device tensor [B, H, N, M]" % name)
@@ -822,15 +835,16 @@ def _bias_args(plane, shape, dtype, device, buckets, max_distance, two_sided, of
     if torch.is_tensor(offset):
         offsets = _vector_ptr(offset, B, device, torch.int32, "offset")
     else:
-        desc.offset = int(offset)
+        desc.offset = _whole(offset, _I64, "offset")
     return desc, (offsets, _vector_ptr(row_len, B, device, torch.int32, "row_len"),
                   _vector_ptr(col_len, B, device, torch.int32, "col_len"))
 
 
 def sdtw_position_bias_starts(buckets, max_distance=128, two_sided=True):
     """First distance of each bucket of a side (host)."""
-    desc = BiasDesc(1, 1, 1, 1, int(buckets), int(max_distance), 1 if two_sided else 0, 0, 0, 0)
-    starts = (ctypes.c_int32 * max(1, int(buckets)))()
+    buckets = _whole(buckets, _I32, "buckets")
+    desc = BiasDesc(1, 1, 1, 1, buckets, _whole(max_distance, _I32, "max_distance"), 1 if two_sided else 0, 0, 0, 0)
+    starts = (ctypes.c_int32 * 256)()  # (more buckets are refused)
     rc = load_library().sdtw_position_bias_starts(ctypes.byref(desc), starts)
     if rc != 0:
         raise SdtwError(rc, "sdtw_position_bias_starts")
@@ -915,8 +929,8 @@ def sdtw_forward_biased(x, y, table, gamma, max_distance=128, two_sided=True, of
     if table.dim() != 2 or table.device != dev or table.shape[0] < 1 or desc.B % table.shape[0]:
         raise ValueError("table must be [H, buckets] on the sequences' device, the number of pairs a multiple of H")
     H, buckets = table.shape
-    bias = BiasDesc(desc.B // H, H, desc.N, desc.M, buckets, int(max_distance), 1 if two_sided else 0, TYPE_F32,
-                    _type_of(table, "table"), 0, int(offset))
+    bias = BiasDesc(desc.B // H, H, desc.N, desc.M, buckets, _whole(max_distance, _I32, "max_distance"), 1 if two_sided else 0, TYPE_F32,
+                    _type_of(table, "table"), 0, _whole(offset, _I64, "offset"))
     bias.table_stride[:] = [table.stride(0), table.stride(1)]
     if workspace is None:
         nbytes = sdtw_biased_workspace_bytes(desc, bias)

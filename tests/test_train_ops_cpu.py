@@ -244,3 +244,10 @@ def test_temperatures_whose_scale_is_beyond_float32_are_refused():
         assert (lib.sdtw_distill_workspace_bytes(ctypes.byref(d)) > 0) == fine, temperature
         if not fine:
             assert lib.sdtw_distill_step(ctypes.byref(d), FAKE, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, 1 << 30, None) == binding.STATUS_INVALID_ARG
+
+
+def test_numbers_that_a_descriptor_does_not_hold_are_refused():
+    for buckets, far in ((32, (1 << 32) + 128), (32, 128.5), ((1 << 32) + 32, 128), (32.5, 128), (32, float("nan")), (32, float("inf"))):
+        with pytest.raises((ValueError, OverflowError)):
+            pkg.sdtw_position_bias_starts(buckets, far)
+    assert pkg.sdtw_position_bias_starts(32.0, 128.0) == pkg.sdtw_position_bias_starts(32, 128)

@@ -854,3 +854,16 @@ def test_bias_gradient_of_real_numbers(B, H, N, M, lengths, kind):
             part = w[:, h][:, at == u]
             want, size = float(part.sum()), float(part.abs().sum())
             assert abs(float(dt[h, u]) - want) <= 64 * 2.0 ** -24 * size + 2.0 ** -24 * abs(want) + 1e-12 * size, (h, u)
+
+
+def test_bias_refuses_numbers_that_a_descriptor_does_not_hold():
+    plane, table = torch.zeros((1, 1, 4, 4), device="cuda"), torch.zeros((1, 32), device="cuda")
+    for bad in (dict(offset=1 << 64), dict(offset=0.5), dict(offset=(1 << 63) + 7), dict(max_distance=(1 << 32) + 128), dict(max_distance=64.5)):
+        with pytest.raises(ValueError):
+            pkg.sdtw_position_bias_forward(table, plane, **bad)
+        with pytest.raises(ValueError):
+            pkg.sdtw_position_bias_backward(plane, 32, **bad)
+        with pytest.raises(ValueError):
+            pkg.sdtw_forward_biased(plane[0], plane[0], table, 1.0, **bad)
+    with pytest.raises(ValueError):
+        pkg.sdtw_position_bias_backward(plane, (1 << 32) + 32)
