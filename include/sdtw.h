@@ -399,7 +399,8 @@ int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, co
  * Soft-DTW under a learned position penalty: the cost of cell (i, j) of pair b is
  *   ||x_i - y_j||^2 + max(0, table[b mod H, bucket(j - i - offset)])
  * - the soft, learned counterpart of the band constraint.  Entries of the table are penalties: the sweeps skip what
- * non-negative costs prove to be empty, so a negative entry counts as 0 and has gradient 0.
+ * non-negative costs prove to be empty, so a negative entry counts as 0 and has gradient 0.  An entry of +inf (any beyond
+ * 3e38) forbids its cells: their E is 0, and so is the entry's gradient as long as there is a path around them.
  *   desc: as for sdtw_forward, SDTW_UNFUSED only (SDTW_ERR_UNSUPPORTED otherwise).
  *   bias: B * H == desc->B (pair b is sequence b / H, head b mod H), the same N and M, plane_type SDTW_TYPE_F32; buckets,
  *         max_distance, two_sided, offset, table_type and table_stride as above; in_stride and out_stride are not used.

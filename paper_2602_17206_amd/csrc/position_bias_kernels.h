@@ -38,7 +38,7 @@ struct BucketRule {
 
 struct BiasParams {
     int32_t B, H, N, M, buckets, table_type;
-    int32_t penalty;  // negative table entries count as 0
+    int32_t penalty;  // negative table entries count as 0, infinite ones as kForbidden
     int64_t offset;
     int64_t in_stride[3], out_stride[3], table_stride[2];
     const void *table, *in;
@@ -73,10 +73,13 @@ __device__ __forceinline__ int neighbours_together()
 // a position difference as 32 bits: beyond 2^30 every distance is in the last bucket
 __device__ __forceinline__ int clamp_rel(int64_t r) { return (int)min(max(r, (int64_t) - (1 << 30)), (int64_t)1 << 30); }
 
+// A penalty's entry of +inf forbids its cells: the sweeps take that as a cost of 3e38, as outside a band, and subtract costs.
+constexpr float kForbidden = 3.0e38f;
 __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
 {
     const float v = load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type);
-    return p.penalty && v < 0.0f ? 0.0f : v;
+    if (!p.penalty) return v;
+    return v < 0.0f ? 0.0f : v > kForbidden ? kForbidden : v;
 }
 
 // Bound by reading and writing the plane: 8 x 16 x 2048 x 2048 bfloat16 takes 357 us (6.0 TB/s both ways together), 8 x 16 x 1100 x

@@ -182,3 +182,25 @@ def test_the_gradient_call_looks_at_the_tensors_it_is_given():
     assert pkg.sdtw_backward_biased(state, x[0], y, table, ws)[0].shape == (4, 30, 4)
     with pytest.raises(ValueError):
         pkg.sdtw_backward_biased(state, x, y, table, ws)
+
+
+@pytest.mark.parametrize("B,N,M,D,gamma,min_memory", [(4, 40, 45, 8, 0.5, False), (3, 300, 290, 16, 0.1, False), (4, 260, 270, 8, 0.5, True), (70, 800, 790, 4, 0.5, False)])
+@pytest.mark.parametrize("kind", [torch.float32, torch.float16, torch.bfloat16])
+def test_an_infinite_penalty_forbids_its_cells(B, N, M, D, gamma, min_memory, kind):
+    """Nothing on distances up to 15 and +inf beyond is the band |i - j| <= 15."""
+    x, y = (torch.from_numpy(a).cuda() for a in normal_pairs(9, B, N, M, D))
+    w, last = 15, [16, 33]
+    assert pkg.sdtw_position_bias_starts(34, 17)[16] == w + 1
+    table = torch.zeros((1, 34), device="cuda", dtype=kind)
+    table[0, last] = float("inf")
+    value, desc, ws = pkg.sdtw_forward(x, y, gamma, pkg.UNFUSED, bandwidth=w, min_memory=min_memory)
+    dx, dy, E = pkg.sdtw_backward(desc, x, y, ws, want_E=True)
+    v, state, ws = pkg.sdtw_forward_biased(x, y, table, gamma, max_distance=17, min_memory=min_memory)
+    bx, by, bt, bE = pkg.sdtw_backward_biased(state, x, y, table, ws, want_E=True)
+    assert binding.workspace_status(ws) == 0
+    assert ((v - value).abs() <= 1e-4 * value.abs().clamp(min=1.0)).all()
+    outside = (torch.arange(N, device="cuda")[:, None] - torch.arange(M, device="cuda")).abs() > w
+    assert (bE[:, outside] == 0).all() and float((bE - E).abs().max()) <= 1e-3
+    for got, want in ((bx, dx), (by, dy)):
+        assert float((got - want).abs().max()) <= 1e-3 * float(want.abs().max())
+    assert torch.isfinite(bt).all() and (bt[0, last] == 0).all()
