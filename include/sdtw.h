@@ -295,7 +295,7 @@ typedef struct sdtw_distill_desc {
     int32_t rows;            /* rows of the student, >= 0 */
     int32_t vocab;           /* >= 1, < 2^30 */
     int32_t top;             /* slots per row of the teacher, 1..1024 */
-    int32_t teacher_rows;    /* rows of the teacher's arrays, >= 1 (>= rows without teacher_row) */
+    int32_t teacher_rows;    /* rows of the teacher's arrays, >= 1 (>= rows without teacher_row); 0 only with no rows */
     float temperature;       /* > 0, finite, and log2(e) / temperature finite in float32 (4.3e-39 is) */
     int32_t target;          /* SDTW_DISTILL_RENORMALIZED or SDTW_DISTILL_TAIL */
     int32_t logit_type;      /* SDTW_TYPE_*: logits and dlogits */

@@ -48,7 +48,8 @@ float octaves_of(float temperature) { return (float)(1.4426950408889634 / (doubl
 bool distill_ok(const sdtw_distill_desc *d)
 {
     if (!d) return false;
-    if (d->rows < 0 || d->vocab < 1 || d->vocab >= 1 << 30 || d->top < 1 || d->top > kMaxTop || d->teacher_rows < 1) return false;
+    if (d->rows < 0 || d->vocab < 1 || d->vocab >= 1 << 30 || d->top < 1 || d->top > kMaxTop) return false;
+    if (d->teacher_rows < (d->rows > 0 ? 1 : 0)) return false;
     if (!(d->temperature > 0.0f) || !std::isfinite(d->temperature) || !std::isfinite(octaves_of(d->temperature))) return false;
     if (d->target != SDTW_DISTILL_RENORMALIZED && d->target != SDTW_DISTILL_TAIL) return false;
     if (!type_ok(d->logit_type) || !type_ok(d->teacher_type)) return false;

@@ -251,3 +251,14 @@ def test_numbers_that_a_descriptor_does_not_hold_are_refused():
         with pytest.raises((ValueError, OverflowError)):
             pkg.sdtw_position_bias_starts(buckets, far)
     assert pkg.sdtw_position_bias_starts(32.0, 128.0) == pkg.sdtw_position_bias_starts(32, 128)
+
+
+def test_no_rows_of_the_teacher_either():
+    lib = pkg.load_library()
+    d = distill_desc(rows=0, teacher_rows=0)
+    assert lib.sdtw_distill_workspace_bytes(ctypes.byref(d)) > 0
+    assert lib.sdtw_distill_forward(ctypes.byref(d), *[None] * 8, 0, None) == binding.STATUS_OK
+    assert lib.sdtw_distill_backward(ctypes.byref(d), *[None] * 9) == binding.STATUS_OK
+    assert lib.sdtw_distill_step(ctypes.byref(d), *[None] * 9, 0, None) == binding.STATUS_OK
+    for bad in (dict(rows=0, teacher_rows=-1), dict(rows=1, teacher_rows=0)):
+        assert lib.sdtw_distill_workspace_bytes(ctypes.byref(distill_desc(**bad))) == 0

@@ -867,3 +867,13 @@ def test_bias_refuses_numbers_that_a_descriptor_does_not_hold():
             pkg.sdtw_forward_biased(plane[0], plane[0], table, 1.0, **bad)
     with pytest.raises(ValueError):
         pkg.sdtw_position_bias_backward(plane, (1 << 32) + 32)
+
+
+def test_distillation_of_an_empty_batch():
+    z, t = torch.zeros((0, 10), device="cuda", dtype=torch.bfloat16), torch.zeros((0, 3), device="cuda")
+    ids = torch.zeros((0, 3), dtype=torch.int32, device="cuda")
+    for more in ({}, {"teacher_lse": torch.zeros(0, device="cuda")}, {"teacher_row": torch.zeros(0, dtype=torch.int32, device="cuda")}):
+        loss, stats = pkg.sdtw_distill_forward(z, t, ids, **more)
+        assert loss.shape == (0,) and pkg.sdtw_distill_backward(z, t, ids, stats, **more).shape == (0, 10)
+        loss, dz = pkg.sdtw_distill_step(z, t, ids, **more)
+        assert loss.shape == (0,) and dz.shape == (0, 10)
