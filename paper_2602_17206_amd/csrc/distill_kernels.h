@@ -434,7 +434,7 @@ template <typename T, int U, bool STREAM> struct RowStream {
 };
 
 // One workgroup per row, or per slice of a row.  The first wavefront works on the slots while the others stream the columns.
-// Bound by reading the logits once: 8192 x 131072 bfloat16 takes 326 us (6.6 TB/s), 4096 x 32768 51 us.  A single row of 32768 takes
+// Bound by reading the logits once: 8192 x 131072 bfloat16 takes 314 us (6.8 TB/s), 4096 x 32768 47 us.  A single row of 32768 takes
 // 5 us, the way from its slots' addresses over their logits and exponentials to the loss.
 template <typename T, bool STREAM, int THREADS>
 __global__ __launch_bounds__(THREADS, THREADS == 320 ? 8 : 4) void distill_forward_kernel(DistillParams p)
@@ -524,7 +524,7 @@ __global__ __launch_bounds__(64) void distill_join_kernel(DistillParams p)
 
 // dlogits over a slice of a row: every element as one outside the kept ones, then the kept ones over it.  A workgroup a slice,
 // or a wavefront (TEAM 64, with at most TOP slots), where rows are short.  Bound by reading and writing: 1024 x 100003 float32 takes
-// 140 us (5.9 TB/s both ways together).
+// 137 us (6.0 TB/s both ways together).
 template <typename T, int TEAM, int TOP>
 __global__ __launch_bounds__(256) void distill_backward_kernel(DistillParams p)
 {
@@ -635,7 +635,8 @@ __device__ __forceinline__ int lane_again()
 // exponentials are kept as float32.  A workgroup takes row after row, `gridDim.x` apart.  The streaming wavefronts have a row's
 // vectors on their way while they finish the one before it; the slots' wavefront runs two rows ahead, and stores a row's
 // kept tokens when the others are known to have stored their vectors.  One barrier a row.  At most kRowsTop slots.
-// Bound by reading and writing: 4096 x 32768 bfloat16 takes 112 us (4.8 TB/s both ways together), two passes 148.
+// Bound by reading and writing: 4096 x 32768 bfloat16 takes 113 us (4.8 TB/s both ways together), two passes 142; 2048 x 12000 float32 42 and 53,
+// and 2048 x 40000, twelve vectors a thread, 127 (5.2 TB/s) and 155.
 constexpr int kRowsTop = 128;
 template <typename T, int NV, int WAVES_PER_SIMD>
 __global__ __launch_bounds__(1024, WAVES_PER_SIMD) void distill_rows_kernel(DistillParams p, int ring_bytes)
@@ -815,7 +816,8 @@ __global__ __launch_bounds__(1024, WAVES_PER_SIMD) void distill_rows_kernel(Dist
 
 // Short rows: a wavefront each, four of them a workgroup that know nothing of each other.  The row stays in registers, NV vectors a
 // lane, from its one read on; with GRAD its gradient is written, else its stats.  All loads of the row are on their way before
-// the slots' chain of dependent ones begins - which is what bounds it: 35 us at 16384 x 1000 float32 (3.8 TB/s), 59 at 2000 (4.5).
+// the slots' chain of dependent ones begins - which is what bounds it: with ten slots 32 us at 16384 x 1000 float32 (4.1 TB/s) and 55 at
+// 2000 (4.8), with 64 of them 46 and 87.
 template <typename T, int NV, bool GRAD>
 __global__ __launch_bounds__(256) void distill_short_kernel(DistillParams p, int team_bytes)
 {

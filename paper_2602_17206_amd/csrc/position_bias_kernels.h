@@ -83,7 +83,7 @@ __device__ __forceinline__ float load_bias(const BiasParams &p, int h, int u)
 }
 
 // Bound by reading and writing the plane: 8 x 16 x 2048 x 2048 bfloat16 takes 357 us (6.0 TB/s both ways together), 8 x 16 x 1100 x
-// 936 float16 96, with 937 columns, whose rows begin and end inside vectors, 108; a single row, 32 x 16 x 1 x 4097 bfloat16,
+// 936 float16 82, with 937 columns, whose rows begin and end inside vectors, 103; a single row, 32 x 16 x 1 x 4097 bfloat16,
 // 10 us, bound by the way from table to LDS to row.  STREAM_IN, STREAM_OUT: past the caches.
 template <typename T, bool STREAM_IN, bool STREAM_OUT>
 __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p, BucketRule rule)
@@ -173,8 +173,9 @@ __global__ __launch_bounds__(256) void position_bias_forward_kernel(BiasParams p
 // in LDS (different places in all lanes, W of them at a time), and the others stay.  Float32 up to there: at most 64 terms; what
 // a pass leaves there is added up in float64, scaled, and the buckets - neighbouring diagonals - are summed at the end.
 // Bound by reading the plane: 32 x 1 x 8192 x 8192 float32 takes 1.28 ms (6.7 TB/s), 4 x 16 x 2048 x 2048 bfloat16 85 us
-// (6.3 TB/s).  4 x 1 x 64 x 64 float32 takes 9 us: a wavefront's steps, then its buckets.  A walk along the diagonals, whose sums stay in registers the whole way, took 1.46 ms and 127 us: its rows'
-// loads begin one place further on from row to row, so hardly any of them is whole cache lines.
+// (6.3 TB/s).  4 x 1 x 64 x 64 float32 takes 9 us: a wavefront's steps, then its buckets.  A walk along the diagonals, whose sums stay in
+// registers the whole way, took 1.46 ms and 127 us: its rows' loads begin one place further on from row to row, so hardly any of
+// them is whole cache lines.
 template <typename T>
 __global__ __launch_bounds__(256) void position_bias_backward_kernel(BiasParams p, BucketRule rule)
 {

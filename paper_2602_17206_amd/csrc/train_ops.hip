@@ -75,12 +75,12 @@ DistillPlan distill_plan(const sdtw_distill_desc *d)
     const int W = width_of(d->logit_type);
     const int64_t rows = std::max(d->rows, 1), vecs = (d->vocab + W - 1) / W + 1;  // (a row may begin inside a vector)
     // Many rows: a workgroup each, of one streaming wavefront up to 2048 vectors, three up to 16384, then four, next to the
-    // one for the slots.  (One / three / four of them: 35 / 38 / 45 us at 8192 x 8000 bfloat16, 51 / 52 / 52 at 4096 x 32768,
-    // 452 / 350 / 338 at 8192 x 131072; 44 / 26 / 26 at 1024 x 32000 float32.)
-    // Fewer than 512: up to fifteen, so that a row is on its way at once: 8.8 us at 1 x 32768 bfloat16, 15.3 at 400 x 32768,
-    // 19.7 at 200 x 100000 float32; slices of a row and a second kernel that joins them took 13.7, 20.0 and 29.5.
-    // Slices are for the few long rows (1 x 131072 bfloat16 13.8 us against 15.6), and for those whose marks - one bit an
-    // element in LDS - would take more than 32 KB.
+    // one for the slots.  (One / three / four of them: 33 / 34 / 42 us at 8192 x 8000 bfloat16, 47 each at 4096 x 32768,
+    // 384 / 324 / 313 at 8192 x 131072; 40 / 23 / 23 at 1024 x 32000 float32.)
+    // Fewer than 512: up to fifteen, so that a row is on its way at once: 12.3 us at 1 x 32768 and at 400 x 32768 bfloat16,
+    // 15.3 at 200 x 100000 float32; slices of a row and a second kernel that joins them take 15.1, 17.7 and 43.5.
+    // Slices are for the few long rows (16 x 200000 bfloat16 15.1 us against 16.7; for one of 131072, 15.1 against 12.3, the second
+    // launch costs more than they give), and for those whose marks - one bit an element in LDS - would take more than 32 KB.
     const int64_t most = (1 << 18) / W;
     if (rows >= 512) {
         P.slice_vecs = slice_vectors(1, vecs, 1, 1, most);
@@ -94,8 +94,8 @@ DistillPlan distill_plan(const sdtw_distill_desc *d)
     }
     P.slices = (int32_t)((vecs + P.slice_vecs - 1) / P.slice_vecs);
     // The gradient alone: workgroups whose whole slice is on its way at once, four vectors a thread, where that makes 1024 of them
-    // or more: 143 us at 1024 x 100003 float32 (5.7 TB/s), 95 at 4096 x 32768 and 368 at 8192 x 65536 bfloat16; slices of 2048
-    // take 157, 96 and 376, whole rows 188, 103 and 415.  Fewer rows: two vectors a thread at least.
+    // or more: 137 us at 1024 x 100003 float32 (6.0 TB/s), 90 at 4096 x 32768 and 346 at 8192 x 65536 bfloat16; slices of 2048
+    // take 154, 92 and 367, whole rows 185, 101 and 418.  Fewer rows: two vectors a thread at least.
     P.back_vecs = slice_vectors(rows, vecs, 1024, 512, 1024);
     P.back_slices = (int32_t)((vecs + P.back_vecs - 1) / P.back_vecs);
     size_t o = 0;
@@ -158,8 +158,8 @@ void launch_distill_forward(const DistillPlan &P, DistillParams p, int type, boo
     }
 }
 
-// The gradient alone of rows of at most 512 vectors is a wavefront's each: 33 against 51 us at 16384 x 1000 float32, 22 against 42 in
-// bfloat16, and 56 against 58 at 16384 x 2000 float32; with twice as many vectors 60 against 52 at 8192 x 4000.
+// The gradient alone of rows of at most 512 vectors is a wavefront's each: with ten slots 29 against 43 us at 16384 x 1000 float32, 20 against
+// 37 in bfloat16, and 53 against 50 at 16384 x 2000 float32 (64 slots at 1000: 46 and 51); with twice as many vectors 54 against 46 at 8192 x 4000.
 bool wavefront_slices(const DistillPlan &P, int top) { return P.back_slices == 1 && P.back_vecs <= 512 && top <= kRowsTop; }
 
 // (256 threads each)
@@ -191,9 +191,10 @@ int64_t row_vectors(const sdtw_distill_desc *d, const void *logits)
     return ((int64_t)d->vocab + (aligned ? W - 1 : 2 * W - 2)) / W;
 }
 
-// Rows of up to 512 vectors are a wavefront's: its vectors a lane, 0 for longer rows.  Loss and gradient of 16384 x 1000 float32 take 35 us,
-// with a workgroup to a row (distill_rows_kernel) 44, of 16384 x 2000 59 and 64, of 256 x 1000 9 and 10; with more vectors a lane there are too few
-// wavefronts.  The loss alone only with many rows: 24 against 30 us at 16384 x 1000, 8.5 and 9.3 at 1024; 9.4 against 8.0 at 256 x 4000 bfloat16.
+// Rows of up to 512 vectors are a wavefront's: its vectors a lane, 0 for longer rows.  Loss and gradient of 16384 x 1000 float32 take 32 us
+// with ten slots and 46 with 64, with a workgroup to a row (distill_rows_kernel) 45 and 52, of 16384 x 2000 55 and 87 against 60 and 79; with more
+// vectors a lane there are too few wavefronts.  The loss alone only with many rows: 20 against 27 us at 16384 x 1000; 256 x 4000 bfloat16 waits for the
+// host, 12.5 us either way.
 int short_vectors(const sdtw_distill_desc *d, const void *logits, bool gradient)
 {
     const int64_t vecs = row_vectors(d, logits);
@@ -202,7 +203,8 @@ int short_vectors(const sdtw_distill_desc *d, const void *logits, bool gradient)
 }
 
 // The shape of the one-read kernel for longer rows: vectors a thread and wavefronts, or 0 for rows that are too long.  Eight vectors a
-// thread (4 / 8: 77 / 63 us at 8192 x 8000 bfloat16, 92 / 87 at 4096 x 24000), and twelve where only they hold a row of float32.
+// thread, and twelve where only they hold a row of float32.  (Four take 62 us at 8192 x 8000 bfloat16 and 73 at 4096 x 24000, eight 66 and 83:
+// they were slower, 77 and 92, in an earlier form of the kernel, and hold rows of half the length.)
 struct RowsShape { int vectors, waves, per_simd; };
 RowsShape rows_shape(const sdtw_distill_desc *d, const void *logits)
 {
@@ -365,8 +367,8 @@ bool begins_on_vectors(const void *plane, const int64_t (&stride)[3], int W)
 }
 
 // How the backward pass is split (`fits`: into a grid that can be launched): tiles of the plane, then the batch, into 2048
-// workgroups where it has them.  Measured with 1024, 2048, 8192: 32 x 1 x 8192 x 8192 float32 1330, 1315, 1324 us,
-// 4 x 16 x 2048 x 2048 bfloat16 101, 99, 98 us; smaller planes are equal within 1 us.
+// workgroups where it has them.  Measured with 1024, 2048, 8192: 32 x 1 x 8192 x 8192 float32 1294, 1286, 1294 us,
+// 4 x 16 x 2048 x 2048 bfloat16 89, 88, 88 us.
 struct BiasPlan { bool fits; int64_t wave_rows, across, col_tiles, tiles, batch_per_part, batch_parts, parts; };
 
 BiasPlan bias_plan(const sdtw_bias_desc *d)
@@ -383,7 +385,7 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
         P.tiles = P.col_tiles * ((d->N + rows - 1) / rows);
     };
     // A wavefront goes down 64 rows, 8 a step - or 16, where that makes no more than a workgroup for each compute unit, and the steps' latency
-    // counts: 17.1 against 21.2 us at 4 x 1 x 64 x 64 float32, 22.5 and 26.4 at 16 x 8 x 300 x 300 bfloat16; but 38.3 against 34.5 at
+    // counts: 13.9 against 14.5 us at 4 x 1 x 64 x 64 float32, 15.5 and 19.9 at 16 x 8 x 300 x 300 bfloat16; but 33.7 against 28.7 at
     // 32 x 1 x 1024 x 1024 float32.
     tile(64);
     P.fits = P.tiles <= 0x7fffffff / d->H;  // (what follows stays within 64 bits)
@@ -427,11 +429,13 @@ int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalt
     const BucketRule rule = bucket_rule(desc);
     {
         ProfScope ps("position_bias_forward", st);
-        // Planes that the memory-side cache of 256 MB cannot hold are written past it: 357 against 386 us at 8 x 16 x 2048 x 2048
-        // bfloat16, 93 against 100 at 8 x 16 x 1100 x 960 float16.  Others stay there for the next kernel: 73 against 88 us with a
-        // softmax behind it at 8 x 4 x 1024 x 1024 bfloat16; alone 44 against 48 at 32 x 1 x 1024 x 1024 float32.
+        // Planes that the memory-side cache of 256 MB cannot hold are written past it: 357 against 387 us at 8 x 16 x 2048 x 2048
+        // bfloat16.  (Just beyond its size that depends on what the cache held: 92 against 84 at 8 x 16 x 1100 x 960 float16 where the
+        // output's memory is that of the call before.)  Others stay there for the next kernel: 67 against 83 us with a softmax
+        // behind it at 8 x 4 x 1024 x 1024 bfloat16; alone 46 against 50 at 32 x 1 x 1024 x 1024 float32.
         // Rows that begin inside vectors share lines with their neighbours and go through the caches both ways: 382 against 391 us
-        // (read past them) and 407 (both) at 8 x 16 x 2001 x 2003 bfloat16, 175, 186 and 172 at 4 x 16 x 1001 x 1501 float32.
+        // (read past them) and 406 (both) at 8 x 16 x 2001 x 2003 bfloat16, 175, 175 and 170 at 4 x 16 x 1001 x 1501 float32; at 8 x 16 x
+        // 1100 x 937 float16, which just fits the cache, 103, 89 and 108.
         const bool vectors = begins_on_vectors(in, desc->in_stride, W) && begins_on_vectors(out, desc->out_stride, W);
         const bool stream = vectors && planes * desc->N * desc->M * (16 / W) >= (int64_t)256 << 20;
         with_type(desc->plane_type, [&](auto t) {
@@ -568,7 +572,7 @@ int sdtw_distill_step(const sdtw_distill_desc *desc, const void *logits, const v
         return hip_ok();
     }
     // Two passes.  Up to twice the memory-side cache of 256 MB the first one reads without the streaming hint, and the second
-    // finds part of it there: 140 against 151 us at 1024 x 131072 bfloat16; at 8192 x 65536 (1 GB) 609 against 576.
+    // finds part of it there - 136 us at 1024 x 131072 bfloat16, with the hint 135 to 151 -; at 8192 x 65536 (1 GB) 545 against 513.
     const int64_t bytes = (int64_t)desc->rows * desc->vocab * (16 / width_of(desc->logit_type));
     launch_distill_forward(P, p, desc->logit_type, bytes > (int64_t)512 << 20, st);
     launch_distill_backward(P, p, desc->logit_type, st);

@@ -1,5 +1,6 @@
 // Rows of float32, float16 or bfloat16 elements as 16-byte vectors, from any element-aligned address: gfx950 loads and
-// stores 16 bytes at any alignment in one instruction, so rows of odd strides need no path of their own.
+// stores 16 bytes at any alignment in one instruction, so rows of odd strides need no loads of their own - only other cache hints,
+// where two rows share a line.
 #pragma once
 #include <hip/hip_runtime.h>
 
