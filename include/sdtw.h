@@ -396,6 +396,99 @@ int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, co
                                 size_t workspace_bytes, void *stream);
 
 /*
+ * Softmax attention under the position bias, without the planes of scores in memory.
+ * Queries q [B,H,N,D], keys and values k, v [B,Hk,M,D]: head h of the queries goes with head h / (H / Hk) of the keys.
+ *   x = scale <q_i, k_j>;  cap > 0: x = cap tanh(x / cap);  s[i,j] = x + table[h, bucket(j - i - offset_b)]
+ *   forward   out[i] = sum_j exp(s[i,j] - lse[i]) v_j,  lse[i] = log sum_j exp(s[i,j])
+ *   backward  the gradients of q, k, v and the table for the gradient dout of out
+ * over the keys j that row i of sequence b sees, which are those with all of
+ *   j < col_len[b], where there are lengths;
+ *   causal: j <= i + offset_b, or j < prefix_b;
+ *   row_document[b,i] == col_document[b,j] >= 0, where there are documents (any order; negative: in none).
+ * A row that sees no key, that is not below row_len[b], or all of whose scores are -inf: out 0, lse -inf, gradients 0.
+ *   - The bucket of a distance is that of sdtw_bias_desc.  A table entry below -1e30 forbids its cells as -inf does.
+ *   - Keys and rows behind their length and in no document, and keys behind all that a causal row of the sequence sees, may hold
+ *     anything, NaN too.  Of other keys and rows, infinities and NaN may reach every row or key of their sequence.
+ *   - Scores, softmax and sums are carried in 32 bits.  For 16-bit types the softmax's numerators and the scores' gradients are rounded
+ *     to the type for the matrix cores, in float16 under a scale that keeps small ones.
+ *   - The same inputs give the same bits, forward and backward.
+ */
+typedef struct sdtw_attention_desc {
+    int32_t B, H, Hk, N, M, D;   /* B, H, N, M >= 0; N, M <= 2^28; Hk >= 1 divides H; 1 <= D <= 128 (more: SDTW_ERR_UNSUPPORTED) */
+    int32_t type;                /* SDTW_TYPE_*: q, k, v, out, dout, dq, dk, dv */
+    int32_t table_type;          /* SDTW_TYPE_*: table */
+    int32_t buckets;             /* 0: no bias; else as in sdtw_bias_desc, and so the next two */
+    int32_t max_distance;
+    int32_t two_sided;
+    int32_t causal;              /* 0 or 1 */
+    float scale;                 /* > 0, finite */
+    float cap;                   /* 0: none; else > 0, finite, and scale / cap finite */
+    uint32_t flags;              /* 0 */
+    int64_t offset;              /* offset_b of every sequence, |offset| < 2^62; not used with `offsets` */
+    int64_t prefix;              /* prefix_b of every sequence; 0 unless causal; not used with `prefixes` */
+    int64_t q_stride[4], k_stride[4], v_stride[4];  /* elements between sequences, heads, rows, features; >= 0 */
+    int64_t out_stride[4];       /* the same; features of out and of the gradients dq, dk, dv are contiguous (1), and different */
+    int64_t dout_stride[4];      /*   elements of what a call writes have different places */
+    int64_t dq_stride[4], dk_stride[4], dv_stride[4];
+    int64_t table_stride[2];     /* elements between heads and between buckets of the table */
+} sdtw_attention_desc;
+
+/* What differs by sequence or position: device, int32, read only, contiguous; each may be NULL. */
+typedef struct sdtw_attention_lists {
+    const int32_t *offsets;      /* [B] */
+    const int32_t *prefixes;     /* [B]; causal only */
+    const int32_t *row_len;      /* [B], clamped to [0, N] */
+    const int32_t *col_len;      /* [B], clamped to [0, M] */
+    const int32_t *row_document; /* [B, N]; both documents or none */
+    const int32_t *col_document; /* [B, M] */
+} sdtw_attention_lists;
+
+/* Bytes of workspace of the two calls; 0 if the descriptor is invalid or takes 2^32 threads or more.  Host only. */
+size_t sdtw_attention_forward_workspace_bytes(const sdtw_attention_desc *desc);
+size_t sdtw_attention_backward_workspace_bytes(const sdtw_attention_desc *desc);
+
+/*
+ *   table [H, buckets]: device, read only; NULL exactly without buckets.  lists: host, or NULL.
+ *   out [B,H,N,D], lse [B,H,N] (float32, contiguous): device, out.  They overlap no input.
+ */
+int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
+                           const sdtw_attention_lists *lists, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                           void *stream);
+
+/*
+ * out, lse: as the forward call with the same inputs left them.
+ *   dq [B,H,N,D], dk, dv [B,Hk,M,D]: device, out.  dtable [H, buckets]: device, float32, contiguous, out; NULL if it is not wanted
+ *   (the walk over the keys that serves it is then left out) and without buckets.
+ */
+int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
+                            const sdtw_attention_lists *lists, const void *out, const float *lse, const void *dout, void *dq,
+                            void *dk, void *dv, float *dtable, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The global norm of many gradients, and clipping: norm = the root of the sum of the squares of all elements of all tensors;
+ * out = gradient * min(1, max_norm / norm), rounded once.  Squares are summed in 64 bits: no gradient is too large or too small.
+ * If the norm is not finite (an element is NaN or infinite) the gradients go to `out` as they are, for the caller to see by `norm`.
+ * Elements are taken in the order of memory: a tensor and its `out` lie there alike, without gaps.
+ */
+typedef struct sdtw_gradient {
+    const void *data;            /* device; may be NULL with count 0 */
+    void *out;                   /* device: `data` itself (with the same type), or memory that overlaps no tensor's data */
+    int64_t count;               /* 0 <= count < 2^48 */
+    int32_t type, out_type;      /* SDTW_TYPE_* */
+} sdtw_gradient;
+
+/* Bytes of workspace of sdtw_gradient_clip; 0 if `count` is negative or above 2^20, or an entry is invalid.  Host only. */
+size_t sdtw_gradient_clip_workspace_bytes(const sdtw_gradient *gradients, int32_t count);
+
+/*
+ *   gradients [count]: HOST, read before the call returns.  Outputs may not overlap each other: a tensor stands in the list once.
+ *   max_norm: >= 0; +inf: nothing is scaled (and nothing written where `out` is `data`).
+ *   norm [1]: device, float32, out.
+ */
+int sdtw_gradient_clip(const sdtw_gradient *gradients, int32_t count, float max_norm, float *norm, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
  * Soft-DTW under a learned position penalty: the cost of cell (i, j) of pair b is
  *   ||x_i - y_j||^2 + max(0, table[b mod H, bucket(j - i - offset)])
  * - the soft, learned counterpart of the band constraint.  Entries of the table are penalties: the sweeps skip what

@@ -17,6 +17,8 @@ from .binding import (  # noqa: F401
     Workspace,
     library_path,
     load_library,
+    sdtw_attention_backward,
+    sdtw_attention_forward,
     sdtw_backward,
     sdtw_backward_biased,
     sdtw_backward_half,
@@ -32,6 +34,8 @@ from .binding import (  # noqa: F401
     sdtw_forward_biased,
     sdtw_forward_half,
     sdtw_forward_ragged,
+    sdtw_gradient_clip,
+    sdtw_gradient_norm,
     sdtw_normalized_backward,
     sdtw_normalized_forward,
     sdtw_normalized_workspace_bytes,

@@ -5,6 +5,7 @@ pointers through, and raises :class:`SdtwError` on a non-zero status.  PyTorch s
 device memory and the current stream; nothing is computed in Python and there is no
 fallback: if the library has not been built, the first call raises.
 """
+import array
 import contextlib
 import ctypes
 import functools
@@ -75,6 +76,23 @@ class BiasDesc(ctypes.Structure):
     ]
 
 
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hk", ctypes.c_int32), ("N", ctypes.c_int32), ("M", ctypes.c_int32),
+        ("D", ctypes.c_int32), ("type", ctypes.c_int32), ("table_type", ctypes.c_int32), ("buckets", ctypes.c_int32),
+        ("max_distance", ctypes.c_int32), ("two_sided", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("cap", ctypes.c_float), ("flags", ctypes.c_uint32),
+        ("offset", ctypes.c_int64), ("prefix", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64 * 4), ("k_stride", ctypes.c_int64 * 4), ("v_stride", ctypes.c_int64 * 4),
+        ("out_stride", ctypes.c_int64 * 4), ("dout_stride", ctypes.c_int64 * 4), ("dq_stride", ctypes.c_int64 * 4),
+        ("dk_stride", ctypes.c_int64 * 4), ("dv_stride", ctypes.c_int64 * 4), ("table_stride", ctypes.c_int64 * 2),
+    ]
+
+
+class AttentionLists(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("offsets", "prefixes", "row_len", "col_len", "row_document", "col_document")]
+
+
 EXPORTED_SYMBOLS = (
     "sdtw_version", "sdtw_status_string", "sdtw_workspace_bytes", "sdtw_forward", "sdtw_backward",
     "sdtw_barycenter_workspace_bytes", "sdtw_barycenter_step", "sdtw_workspace_status",
@@ -87,6 +105,8 @@ EXPORTED_SYMBOLS = (
     "sdtw_distill_workspace_bytes", "sdtw_distill_forward", "sdtw_distill_backward", "sdtw_distill_step",
     "sdtw_position_bias_starts", "sdtw_position_bias_forward", "sdtw_position_bias_workspace_bytes",
     "sdtw_position_bias_backward", "sdtw_biased_workspace_bytes", "sdtw_forward_biased", "sdtw_backward_biased",
+    "sdtw_attention_forward_workspace_bytes", "sdtw_attention_backward_workspace_bytes", "sdtw_attention_forward",
+    "sdtw_attention_backward", "sdtw_gradient_clip_workspace_bytes", "sdtw_gradient_clip",
 )
 
 
@@ -184,6 +204,17 @@ def load_library():
     lib.sdtw_forward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sdtw_backward_biased.restype = i32
     lib.sdtw_backward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    pa, pl = ctypes.POINTER(AttentionDesc), ctypes.POINTER(AttentionLists)
+    for name in ("sdtw_attention_forward_workspace_bytes", "sdtw_attention_backward_workspace_bytes"):
+        getattr(lib, name).restype, getattr(lib, name).argtypes = sz, [pa]
+    lib.sdtw_attention_forward.restype = i32
+    lib.sdtw_attention_forward.argtypes = [pa, vp, vp, vp, vp, pl, vp, vp, vp, sz, vp]
+    lib.sdtw_attention_backward.restype = i32
+    lib.sdtw_attention_backward.argtypes = [pa, vp, vp, vp, vp, pl, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sdtw_gradient_clip_workspace_bytes.restype = sz
+    lib.sdtw_gradient_clip_workspace_bytes.argtypes = [vp, i32]
+    lib.sdtw_gradient_clip.restype = i32
+    lib.sdtw_gradient_clip.argtypes = [vp, i32, ctypes.c_float, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -987,3 +1018,207 @@ def sdtw_backward_biased(state, x, y, table, workspace, grad_value=None, x_len=N
     if rc != 0:
         raise SdtwError(rc, "sdtw_backward_biased")
     return dx, dy, dtable, E
+
+
+def _positions_ptr(t, B, n, device, name):
+    if t is None:
+        return None
+    import torch
+
+    if t.device != device or t.dtype != torch.int32 or t.shape != (B, n) or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous int32 [%d, %d] on %s" % (name, B, n, device))
+    return t.data_ptr()
+
+
+def _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len, row_document,
+                    col_document):
+    """(descriptor without outputs, lists, pointers of q, k, v, table)"""
+    import torch
+
+    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda:
+        raise ValueError("q [B, H, N, D] and k, v [B, Hk, M, D] must be device tensors")
+    dev, dtype, (B, H, N, D), (_, Hk, M, _) = q.device, q.dtype, q.shape, k.shape
+    if k.shape != (B, Hk, M, D) or v.shape != k.shape or k.device != dev or v.device != dev or k.dtype != dtype or v.dtype != dtype:
+        raise ValueError("k and v must be [B, Hk, M, D] with q's B and D, on its device and of its type")
+    if Hk < 1 or H % Hk:
+        raise ValueError("the number of q's heads must be a multiple of that of k's")
+    desc = AttentionDesc(B, H, Hk, N, M, D, _type_of(q, "q"), 0, 0, 0, 0, 1 if causal else 0, D ** -0.5 if scale is None else scale, cap)
+    desc.q_stride[:], desc.k_stride[:], desc.v_stride[:] = q.stride(), k.stride(), v.stride()
+    tp = None
+    if table is not None:
+        if table.dim() != 2 or table.shape[0] != H or table.device != dev:
+            raise ValueError("table must be [%d, buckets] on %s" % (H, dev))
+        if table.shape[1] < 1:
+            raise ValueError("table must have buckets")
+        desc.table_type, desc.buckets = _type_of(table, "table"), table.shape[1]
+        desc.max_distance, desc.two_sided = _whole(max_distance, _I32, "max_distance"), 1 if two_sided else 0
+        desc.table_stride[:] = table.stride()
+        tp = table.data_ptr()
+    lists = AttentionLists()
+    if torch.is_tensor(offset):
+        lists.offsets = _vector_ptr(offset, B, dev, torch.int32, "offset")
+    else:
+        desc.offset = _whole(offset, _I64, "offset")
+    if prefix is not None:
+        if not causal:
+            raise ValueError("a prefix belongs to a causal mask")
+        if torch.is_tensor(prefix):
+            lists.prefixes = _vector_ptr(prefix, B, dev, torch.int32, "prefix")
+        else:
+            desc.prefix = _whole(prefix, _I64, "prefix")
+    lists.row_len = _vector_ptr(row_len, B, dev, torch.int32, "row_len")
+    lists.col_len = _vector_ptr(col_len, B, dev, torch.int32, "col_len")
+    if (row_document is None) != (col_document is None):
+        raise ValueError("row_document and col_document go together")
+    lists.row_document = _positions_ptr(row_document, B, N, dev, "row_document")
+    lists.col_document = _positions_ptr(col_document, B, M, dev, "col_document")
+    return desc, lists, (q.data_ptr(), k.data_ptr(), v.data_ptr(), tp)
+
+
+def _like(given, like, name):
+    """(a tensor as ``like``, with contiguous features)"""
+    import torch
+
+    if given is None:
+        given = torch.empty_like(like)  # (the same order of dimensions in memory)
+        return given if given.shape[3] <= 1 or given.stride(3) == 1 else torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    if given.shape != like.shape or given.dtype != like.dtype or given.device != like.device:
+        raise ValueError("%s must be %s of %s on %s" % (name, tuple(like.shape), like.dtype, like.device))
+    return given
+
+
+@_on_given_stream
+def sdtw_attention_forward(q, k, v, table=None, scale=None, cap=0.0, causal=False, max_distance=128, two_sided=True, offset=0, prefix=None,
+                           row_len=None, col_len=None, row_document=None, col_document=None, out=None, lse=None, workspace=None):
+    """Softmax attention of ``q`` [B, H, N, D] over ``k``, ``v`` [B, Hk, M, D] (any strides; H a multiple of Hk: heads share keys
+    in groups; D <= 128).  Scores are ``scale`` (None: 1 / sqrt(D)) times the products, ``cap`` > 0: cap * tanh(score / cap), plus
+    ``table`` [H, buckets] by the distance j - i - offset as in :func:`sdtw_position_bias_forward`.
+    Row i sees the keys j < col_len[b]; ``causal``: of these, j <= i + offset or j < ``prefix``; with documents (int32
+    [B, N] and [B, M], negative: none) those of its own.  ``offset`` and ``prefix``: numbers, or int32 [B].
+    One new token per sequence against a cache: N = 1, ``offset`` = its position, ``causal``.
+    Returns (out [B, H, N, D], lse [B, H, N] float32): 0 and -inf for a row that sees nothing or lies behind ``row_len``."""
+    import torch
+
+    lib = load_library()
+    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
+                                        row_document, col_document)
+    dev = q.device
+    out = _like(out, q, "out")
+    desc.out_stride[:] = out.stride()
+    ref = ctypes.byref(desc)
+    keep, wp, wn = _operator_workspace(lib.sdtw_attention_forward_workspace_bytes(ref), workspace, dev, "sdtw_attention_forward")
+    if lse is None:
+        lse = torch.empty((desc.B, desc.H, desc.N), dtype=torch.float32, device=dev)
+        lp = lse.data_ptr()
+    else:
+        lp = _ptr(lse, torch.float32, (desc.B, desc.H, desc.N), "lse")
+    rc = lib.sdtw_attention_forward(ref, *args, ctypes.byref(lists), out.data_ptr(), lp, wp, wn, _stream_of(dev))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_attention_forward")
+    return out, lse
+
+
+@_on_given_stream
+def sdtw_attention_backward(q, k, v, out, lse, dout, table=None, scale=None, cap=0.0, causal=False, max_distance=128, two_sided=True,
+                            offset=0, prefix=None, row_len=None, col_len=None, row_document=None, col_document=None, want_dtable=True,
+                            dq=None, dk=None, dv=None, dtable=None, workspace=None):
+    """Gradients of what :func:`sdtw_attention_forward` returned as ``out`` and ``lse`` (the same tensors and options), from ``dout``
+    [B, H, N, D] of any strides, broadcast ones too.  Returns (dq, dk, dv, dtable [H, buckets] float32, or None without a
+    table or with ``want_dtable=False``)."""
+    import torch
+
+    lib = load_library()
+    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
+                                        row_document, col_document)
+    dev = q.device
+    for t, name in ((out, "out"), (dout, "dout")):
+        if t.shape != q.shape or t.dtype != q.dtype or t.device != dev:
+            raise ValueError("%s must be %s of %s on %s" % (name, tuple(q.shape), q.dtype, dev))
+    dq, dk, dv = _like(dq, q, "dq"), _like(dk, k, "dk"), _like(dv, v, "dv")
+    desc.out_stride[:], desc.dout_stride[:] = out.stride(), dout.stride()
+    desc.dq_stride[:], desc.dk_stride[:], desc.dv_stride[:] = dq.stride(), dk.stride(), dv.stride()
+    dp = None
+    if table is None or not want_dtable:
+        dtable = None
+    elif dtable is None:
+        dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
+        dp = dtable.data_ptr()
+    else:
+        dp = _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable")
+    ref = ctypes.byref(desc)
+    keep, wp, wn = _operator_workspace(lib.sdtw_attention_backward_workspace_bytes(ref), workspace, dev, "sdtw_attention_backward")
+    rc = lib.sdtw_attention_backward(ref, *args, ctypes.byref(lists), out.data_ptr(), _ptr(lse, torch.float32, (desc.B, desc.H, desc.N), "lse"),
+                                     dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dp, wp, wn, _stream_of(dev))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_attention_backward")
+    return dq, dk, dv, dtable
+
+
+def _tensor_types(tensors, name):
+    kinds = {t.dtype for t in tensors}
+    if len(kinds) == 1:
+        return [_type_of(tensors[0], name)] * len(tensors)
+    return [_type_of(t, name) for t in tensors]
+
+
+def _without_gaps(t):
+    """Whether the elements fill their memory, in whatever order of the dimensions."""
+    span = 1
+    for size, stride in sorted(((n, s) for n, s in zip(t.shape, t.stride()) if n != 1), key=lambda x: x[1]):
+        if stride != span:
+            return t.numel() == 0
+        span *= size
+    return True
+
+
+@_on_given_stream
+def sdtw_gradient_clip(grads, max_norm, out=None, norm=None, workspace=None):
+    """Scales the tensors ``grads`` (a sequence; float32, float16 and bfloat16 mixed, any of them empty) down so that all of their elements
+    together have a 2-norm of at most ``max_norm``, in place or into the tensors ``out``: as many elements each, of any of the types.
+    If the norm is not finite they stay as they are.  A tensor's elements fill its memory; one that does so in another order
+    than its shape's goes with an ``out`` of its strides.  No tensor may stand in the list twice.
+    Returns the norm before, a float32 scalar on the device: nothing waits for it."""
+    import torch
+
+    lib = load_library()
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    n = len(grads)
+    if len(outs) != n:
+        raise ValueError("out must have a tensor for each of grads")
+    if n == 0 and norm is None:
+        raise ValueError("without gradients norm has to be given: its device is not known otherwise")
+    dev = (grads[0] if n else norm).device
+    if dev.type != "cuda" or any(set(map(torch.Tensor.get_device, x)) - {dev.index} for x in (grads, outs)):
+        raise ValueError("the gradients must be on one device")
+    counts = list(map(torch.Tensor.numel, grads))
+    if outs is not grads and counts != list(map(torch.Tensor.numel, outs)):
+        raise ValueError("out must have as many elements as the gradients")
+    for k in range(n) if not all(map(torch.Tensor.is_contiguous, grads)) or not all(map(torch.Tensor.is_contiguous, outs)) else ():
+        g, o = grads[k], outs[k]
+        if g.is_contiguous() and o.is_contiguous():
+            continue
+        if g.shape != o.shape or not _without_gaps(g) or any(a != b for a, b, m in zip(g.stride(), o.stride(), g.shape) if m != 1):
+            raise ValueError("a gradient's elements must fill its memory, and its out must have the same strides")
+    # struct sdtw_gradient as four 64-bit words
+    words = array.array("q", bytes(32 * n))
+    words[0::4] = array.array("q", map(torch.Tensor.data_ptr, grads))
+    words[1::4] = words[0::4] if outs is grads else array.array("q", map(torch.Tensor.data_ptr, outs))
+    words[2::4] = array.array("q", counts)
+    kinds = _tensor_types(grads, "grads") if n else []
+    out_kinds = kinds if outs is grads else _tensor_types(outs, "out") if n else []
+    words[3::4] = array.array("q", [a | b << 32 for a, b in zip(kinds, out_kinds)])
+    ptr = words.buffer_info()[0] if n else None
+    keep, wp, wn = _operator_workspace(lib.sdtw_gradient_clip_workspace_bytes(ptr, n), workspace, dev, "sdtw_gradient_clip")
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=dev)
+    np = _ptr(norm, torch.float32, (), "norm")
+    rc = lib.sdtw_gradient_clip(ptr, n, max_norm, np, wp, wn, _stream_of(dev))
+    if rc != 0:
+        raise SdtwError(rc, "sdtw_gradient_clip")
+    return norm
+
+
+def sdtw_gradient_norm(grads, norm=None, workspace=None, stream=None):
+    """The 2-norm of all elements of the tensors ``grads`` together, a float32 scalar on the device.  They are only read."""
+    return sdtw_gradient_clip(grads, float("inf"), norm=norm, workspace=workspace, stream=stream)

@@ -1,0 +1,105 @@
+// C entry points of attention's backward pass (declared in include/sdtw.h): checks, the split of the work, launches.
+#include "attention_backward_kernels.h"
+#include "attention_host.h"
+
+namespace {
+
+using namespace sdtw;
+
+struct BackwardPlan {
+    bool fits;
+    int64_t row_tiles, key_tiles;
+    size_t off_table, total;
+};
+
+BackwardPlan backward_plan(const sdtw_attention_desc *d)
+{
+    BackwardPlan P{};
+    P.row_tiles = ((int64_t)d->N + 127) / 128;
+    P.key_tiles = ((int64_t)d->M + 127) / 128;
+    P.fits = (int64_t)d->B * d->H <= 0x7fffffff && attention_grid_ok((int64_t)d->B * d->H * std::max<int64_t>(1, P.row_tiles)) &&
+             attention_grid_ok((int64_t)d->B * d->Hk * std::max<int64_t>(1, P.key_tiles)) && attention_grid_ok((int64_t)d->H * d->buckets);
+    if (!P.fits) return P;
+    P.off_table = align_up((size_t)d->B * d->H * d->N * sizeof(float), 256);
+    P.total = std::max<size_t>(256, P.off_table + align_up((size_t)d->H * d->buckets * d->B * P.row_tiles * sizeof(float), 256));
+    return P;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdtw_attention_backward_workspace_bytes(const sdtw_attention_desc *desc)
+{
+    BucketRule rule{};
+    if (attention_check(desc, &rule) != SDTW_OK) return 0;
+    const BackwardPlan P = backward_plan(desc);
+    return P.fits ? P.total : 0;
+}
+
+int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
+                            const sdtw_attention_lists *lists, const void *out, const float *lse, const void *dout, void *dq,
+                            void *dk, void *dv, float *dtable, void *workspace, size_t workspace_bytes, void *stream)
+{
+    BucketRule rule{};
+    if (int rc = attention_check(desc, &rule)) return rc;
+    if (!lists_ok(desc, lists)) return SDTW_ERR_INVALID_ARG;
+    const bool rows = desc->B > 0 && desc->H > 0 && desc->N > 0, keys = desc->B > 0 && desc->M > 0;
+    if (dtable && desc->buckets == 0) return SDTW_ERR_INVALID_ARG;
+    if (!rows && !keys && (!dtable || desc->H == 0)) return SDTW_OK;
+    if ((rows && (!q || !out || !lse || !dout || !dq)) || (keys && (!k || !v || !dk || !dv)) || !table == (desc->buckets != 0 && desc->H > 0))
+        return SDTW_ERR_INVALID_ARG;
+    if (!strides_ok(desc->out_stride, desc->B, desc->H, desc->N, desc->D) || !strides_ok(desc->dout_stride, desc->B, desc->H, desc->N, desc->D) ||
+        !strides_ok(desc->dq_stride, desc->B, desc->H, desc->N, desc->D) || !strides_ok(desc->dk_stride, desc->B, desc->Hk, desc->M, desc->D) ||
+        !strides_ok(desc->dv_stride, desc->B, desc->Hk, desc->M, desc->D))
+        return SDTW_ERR_INVALID_ARG;
+    if ((rows && !places_differ(desc->dq_stride, desc->B, desc->H, desc->N, desc->D)) ||
+        (keys && (!places_differ(desc->dk_stride, desc->B, desc->Hk, desc->M, desc->D) ||
+                  !places_differ(desc->dv_stride, desc->B, desc->Hk, desc->M, desc->D))))
+        return SDTW_ERR_INVALID_ARG;
+    const BackwardPlan P = backward_plan(desc);
+    if (!P.fits) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    (void)hipGetLastError();
+    AttentionParams p = attention_params(desc, lists);
+    p.q = q; p.k = k; p.v = v; p.table = table;
+    p.out = const_cast<void *>(out);
+    p.lse = const_cast<float *>(lse);
+    p.dout = dout;
+    p.dq = dq; p.dk = dk; p.dv = dv;
+    p.dtable = dtable;
+    p.row_tiles = (int32_t)P.row_tiles;
+    p.key_tiles = (int32_t)P.key_tiles;
+    p.delta = static_cast<float *>(workspace);
+    p.table_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.off_table);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    with_shape(desc->type, desc->D, [&](auto t, auto features) {
+        using T = decltype(t);
+        constexpr int DP = decltype(features)::value;
+        const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+        if (rows) {
+            ProfScope ps("attention_rows_gradient", st);
+            const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
+            if (dtable) {
+                p.table_columns = 32;
+                auto need = [&] { return bytes + (size_t)4 * p.buckets * p.table_columns * sizeof(float); };
+                while (need() + 1024 > kLdsBytes) p.table_columns /= 2;
+                attention_rows_gradient_kernel<T, DP, true><<<grid, 256, need(), st>>>(p, rule);
+            } else {
+                attention_rows_gradient_kernel<T, DP, false><<<grid, 256, bytes, st>>>(p, rule);
+            }
+        }
+        if (keys) {
+            ProfScope ps("attention_keys_gradient", st);
+            attention_keys_gradient_kernel<T, DP><<<(unsigned)((int64_t)p.B * p.Hk * p.key_tiles), 256, bytes, st>>>(p, rule);
+        }
+    });
+    if (dtable) {
+        ProfScope ps("attention_table", st);
+        if (!rows) p.row_tiles = 0;
+        attention_table_kernel<<<(unsigned)(p.H * p.buckets), 64, 0, st>>>(p);
+    }
+    return hip_ok();
+}
+
+}  // extern "C"

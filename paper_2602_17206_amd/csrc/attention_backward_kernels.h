@@ -1,0 +1,403 @@
+// Softmax attention under a learned position bias, backward.
+//
+// With p[i,j] = exp(s[i,j] - lse[i]), made again from the products, and dp[i,j] = <dout_i, v_j>:
+//   delta[i] = sum_j p dp,   ds = p (dp - delta),   dtable[h,u] = sum of ds where bucket(j - i - offset) = u
+//   dx = ds (1 - tanh^2) where scores are capped, else ds
+//   dv_j = sum_i p dout_i,   dq_i = scale sum_j dx k_j,   dk_j = scale sum_i dx q_i   (the last two over a group's heads too)
+// Two kernels, each the sole writer of what it sums: no atomics on memory, the same bits from the same inputs.
+//   rows   wavefronts own queries and walk over the keys: delta, dq, dtable
+//   keys   wavefronts own keys and walk over the queries of all heads of the group: dk, dv
+#pragma once
+#include "attention_tiles.h"
+
+namespace sdtw {
+
+// 2^(score - lse) with lse in octaves, and 1 - tanh^2 where there is a cap
+__device__ __forceinline__ void scale_scores_keep(Acc &s, Acc &slope, const AttentionParams &p)
+{
+    if (p.cap_out != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float t = tanh_fast(s[r] * p.cap_in);
+            s[r] = p.cap_out * t;
+            slope[r] = fmaf(-t, t, 1.0f);
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= p.scale2;
+    }
+}
+
+// float16 has 30 octaves for numbers that may be of any size (gradients of a mean are small): a column's numbers go into the
+// matrix cores times a power of two of the column's own, chosen from the first of them and made smaller whenever one would not fit.
+template <typename T, int DP> struct ColumnScale {
+    __device__ __forceinline__ void fit(Acc &, Acc (&)[DP / 32]) {}
+    __device__ __forceinline__ float undo() const { return 1.0f; }
+};
+template <int DP> struct ColumnScale<_Float16, DP> {
+    float by = 0.0f;  // 0: nothing but zeros so far
+    __device__ __forceinline__ void fit(Acc &x, Acc (&sums)[DP / 32])
+    {
+        float top = fabsf(x[0]);
+#pragma unroll
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(x[r]));
+        top = both_max(top);
+        const bool change = by == 0.0f ? top > 0.0f : top * by > 16384.0f;
+        if (__any(change)) {
+            if (change) {  // the largest to 8 .. 16: 10 octaves of room above, 17 below
+                const int e = __builtin_amdgcn_frexp_expf(fminf(top, 1e38f));
+                const float next = __builtin_amdgcn_ldexpf(1.0f, min(max(4 - e, -126), 126));
+                const float factor = by == 0.0f ? 0.0f : next / by;
+                by = next;
+#pragma unroll
+                for (int ft = 0; ft < DP / 32; ++ft) sums[ft] *= factor;
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] *= by;
+    }
+    __device__ __forceinline__ float undo() const { return by == 0.0f ? 0.0f : 1.0f / by; }
+};
+
+// The table's gradient of a wavefront's 32 rows, in LDS: [buckets][columns], the lanes c with the same c % columns share a place and take
+// turns (an addition in LDS is one instruction, and a wavefront's are carried out in the order of their issue).  Where all cells of a tile are in one bucket its sum stays in a register until the bucket changes.
+struct TableSum {
+    float *sum;
+    int columns, bucket;  // bucket: of `running`
+    float running;
+    __device__ __forceinline__ void turn(int lane, int u, float v)
+    {
+        for (int first = 0; first < 64; first += columns) {
+            wavefront_order();
+            if (lane / columns * columns == first)
+                __hip_atomic_fetch_add(sum + u * columns + lane % columns, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        }
+        wavefront_order();
+    }
+    __device__ __forceinline__ void flush(int lane)
+    {
+        if (bucket >= 0) turn(lane, bucket, running);
+        bucket = -1;
+        running = 0.0f;
+    }
+};
+
+// 4 wavefronts of 32 rows each, one head of one sequence.  TABLE: the table's gradient is wanted.  delta comes from the rows' outputs -
+// sum_j p dp = <dout, out> - unless the table's gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals
+// would show the rounding of a 16-bit `out`; so the keys are walked over once more, for delta alone.
+template <typename T, int DP, bool TABLE>
+__global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
+{
+    using Shape = TileShape<T, DP>;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ uint64_t live[4];
+    __shared__ int shared[4][4];
+    char *ktile = lds, *vtile = lds + Shape::bytes(kKeys);
+    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
+    int64_t id = neighbours_together();
+    const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);
+    id /= p.row_tiles;
+    const int h = (int)(id % p.H), b = (int)(id / p.H), hk = h / (p.H / p.Hk);
+    const Sight sight(p, b);
+    const int32_t *col_document = p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
+    WaveBias bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+    const int table_columns = TABLE ? p.table_columns : 0;
+    float *const table_sums = reinterpret_cast<float *>(lds + 2 * Shape::bytes(kKeys) + bias_bytes(4));
+    TableSum table{table_sums + wave * p.buckets * table_columns, table_columns, -1, 0.0f};
+    if (TABLE)
+        for (int x = thread; x < 4 * p.buckets * table_columns; x += 256) table_sums[x] = 0.0f;
+
+    const int first_row = rt * 128 + wave * 32, i = first_row + c;
+    const int64_t place = ((int64_t)b * p.H + h) * p.N + i;
+    bool valid = i < sight.rows;
+    int doc = 0;
+    if (p.row_document && valid) {
+        doc = p.row_document[(int64_t)b * p.N + i];
+        valid = doc >= 0;
+    }
+    int lim = valid ? sight.limit(i) : 0;
+    const int to = wave_max_i32(lim);
+    if (!valid) lim = 0x7fffffff;
+    const int from = wave_min_i32(lim);
+    const int low = wave_min_i32(valid ? doc : 0x7fffffff), high = wave_max_i32(valid ? doc : -1);
+    // (a row that sees nothing has no p: 2^(score - inf))
+    float lse = valid ? p.lse[place] : -INFINITY;
+    lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    Column<T, DP> q, dout;
+    {
+        const Rows<T> x = rows_of<T>(p.q, p.q_stride, b, h), y = rows_of<T>(p.dout, p.dout_stride, b, h);
+        q.load(x.base + i * x.row, x.feature, p.D, valid, half);
+        dout.load(y.base + i * y.row, y.feature, p.D, valid, half);
+    }
+    float delta = 0.0f;
+    if (!TABLE) {
+        const Rows<T> x = rows_of<T>(p.out, p.out_stride, b, h);
+        Column<T, DP> out;
+        out.load(x.base + i * x.row, x.feature, p.D, valid, half);
+#pragma unroll
+        for (int s = 0; s < Column<T, DP>::kSteps; ++s)
+#pragma unroll
+            for (int e = 0; e < Elem<T>::kWidth; ++e) delta = fmaf(Elem<T>::at(dout.v[s], e), Elem<T>::at(out.v[s], e), delta);
+        delta = both_sum(delta);
+        if (half == 0 && i < p.N) p.delta[place] = delta;
+    }
+    if (lane == 0) shared[wave][0] = to, shared[wave][1] = low, shared[wave][2] = high;
+    __syncthreads();
+    int end = 0, lowest = 0x7fffffff, highest = -1;
+    for (int w = 0; w < 4; ++w) end = max(end, shared[w][0]), lowest = min(lowest, shared[w][1]), highest = max(highest, shared[w][2]);
+
+    Acc dq[DP / 32];
+#pragma unroll
+    for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
+    ColumnScale<T, DP> fit;
+    const Rows<T> k = rows_of<T>(p.k, p.k_stride, b, hk), v = rows_of<T>(p.v, p.v_stride, b, hk);
+    TileWalk walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
+    Stage<T, DP, kKeys, 256> ks, vs;
+#pragma unroll 1
+    for (int pass = TABLE ? 0 : 1; pass < 2; ++pass) {
+        int t = walk.next(0);
+        if (t < walk.tiles) {
+            ks.load(k, p.D, t * kKeys, end, col_document, thread);
+            vs.load(v, p.D, t * kKeys, end, col_document, thread);
+        }
+        while (t < walk.tiles) {
+            __syncthreads();
+            ks.store(ktile, thread);
+            vs.store(vtile, thread);
+            __syncthreads();
+            const int now = t;
+            t = walk.next(t + 1);
+            if (t < walk.tiles) {
+                ks.load(k, p.D, t * kKeys, end, col_document, thread);
+                vs.load(v, p.D, t * kKeys, end, col_document, thread);
+            }
+#pragma unroll
+            for (int sub = 0; sub < kKeys / 32; ++sub) {
+                const int j0 = now * kKeys + sub * 32;
+                if (j0 >= to) break;
+                bool open = j0 + 32 <= from;
+                int key_doc = -1;
+                if (col_document) {
+                    key_doc = j0 + c < end ? col_document[j0 + c] : -1;
+                    open = open && low == high && __all(key_doc == low);
+                }
+                Acc s = along_features<T, DP>(ktile + Shape::bytes(sub * 32), q, lane), slope;
+                scale_scores_keep(s, slope, p);
+                if (p.buckets) {
+                    bias.look(rule, j0 - (first_row + 31) - sight.offset, lane);
+                    if (bias.same) {
+                        s += bias.one;
+                    } else {
+                        const float *at = bias.diagonal + 31 - c + 4 * half;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] += at[tile_row(r, 0)];
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - lse);
+                if (!open) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (j0 + tile_row(r, half) >= lim) s[r] = 0.0f;
+                    if (col_document) {
+#pragma unroll
+                        for (int r = 0; r < 16; ++r)
+                            if (__shfl(key_doc, tile_row(r, half)) != doc) s[r] = 0.0f;
+                    }
+                }
+                const Acc dp = along_features<T, DP>(vtile + Shape::bytes(sub * 32), dout, lane);
+                if (TABLE && pass == 0) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
+                    continue;
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+                if (TABLE) {
+                    if (bias.same) {
+                        if (bias.one_bucket != table.bucket) {
+                            table.flush(lane);
+                            table.bucket = bias.one_bucket;
+                        }
+                        float sum = s[0];
+#pragma unroll
+                        for (int r = 1; r < 16; ++r) sum += s[r];
+                        table.running += valid ? sum : 0.0f;
+                    } else {
+                        const uint8_t *at = bias.bucket + 31 - c + 4 * half;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) table.turn(lane, at[tile_row(r, 0)], valid ? s[r] : 0.0f);
+                    }
+                }
+                if (p.cap_out != 0.0f) s *= slope;
+                fit.fit(s, dq);
+                along_rows<T, DP>(dq, ktile + Shape::bytes(sub * 32), Weights<T>(s), lane);
+            }
+        }
+        if (TABLE && pass == 0) {
+            delta = both_sum(delta);
+            if (half == 0 && i < p.N) p.delta[place] = delta;
+        }
+    }
+    if (i < p.N) {
+        if (!valid) {
+#pragma unroll
+            for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
+        }
+        store_column<T, DP>(row_of<T>(p.dq, p.dq_stride, b, h, i), p.D, dq, p.scale * fit.undo(), half);
+    }
+    if (TABLE) {
+        table.flush(lane);
+        __syncthreads();
+        for (int u = thread; u < p.buckets; u += 256) {
+            float sum = 0.0f;
+            for (int w = 0; w < 4; ++w)
+                for (int x = 0; x < table_columns; ++x) sum += table_sums[(w * p.buckets + u) * table_columns + (x + u) % table_columns];
+            p.table_part[((int64_t)h * p.buckets + u) * ((int64_t)p.B * p.row_tiles) + (int64_t)b * p.row_tiles + rt] = sum;
+        }
+    }
+}
+
+// dtable [h][u] from its parts, in 64 bits and in a fixed order: a wavefront for each entry.
+__global__ __launch_bounds__(64) void attention_table_kernel(AttentionParams p)
+{
+    const int64_t parts = (int64_t)p.B * p.row_tiles;
+    const float *x = p.table_part + blockIdx.x * parts;
+    double sum = 0.0;
+    for (int64_t k = threadIdx.x; k < parts; k += 64) sum += x[k];
+    sum = wave_sum_f64(sum);
+    if (threadIdx.x == 0) p.dtable[blockIdx.x] = (float)sum;
+}
+
+// 4 wavefronts of 32 keys each, of one head of keys of one sequence; the queries of the group's heads go by in tiles of 64.
+template <typename T, int DP>
+__global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
+{
+    using Shape = TileShape<T, DP>;
+    extern __shared__ __align__(16) char lds[];
+    __shared__ uint64_t live[4];
+    __shared__ int shared[4][4];
+    __shared__ __align__(16) float row_lse[kKeys], row_delta[kKeys];
+    __shared__ __align__(16) int32_t row_doc[kKeys];
+    char *qtile = lds, *dtile = lds + Shape::bytes(kKeys);
+    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
+    int64_t id = neighbours_together();
+    const int kt = (int)(id % p.key_tiles);  // (the first keys are seen by the most rows of a causal sequence: they go first)
+    id /= p.key_tiles;
+    const int hk = (int)(id % p.Hk), b = (int)(id / p.Hk), G = p.H / p.Hk;
+    const Sight sight(p, b);
+    const int32_t *row_document = p.row_document ? p.row_document + (int64_t)b * p.N : nullptr;
+    const int first_key = kt * 128 + wave * 32, j = first_key + c;
+    bool valid = sight.rows > 0 && j < sight.limit(sight.rows - 1);  // (the last row sees the most; other keys may hold NaN)
+    int doc = 0;
+    if (p.col_document && valid) {
+        doc = p.col_document[(int64_t)b * p.M + j];
+        valid = doc >= 0;
+    }
+    const int low = wave_min_i32(valid ? doc : 0x7fffffff), high = wave_max_i32(valid ? doc : -1);
+    const bool any = __any(valid);
+    Column<T, DP> k, v;
+    {
+        const Rows<T> x = rows_of<T>(p.k, p.k_stride, b, hk), y = rows_of<T>(p.v, p.v_stride, b, hk);
+        k.load(x.base + j * x.row, x.feature, p.D, valid, half);
+        v.load(y.base + j * y.row, y.feature, p.D, valid, half);
+    }
+    if (lane == 0) shared[wave][1] = low, shared[wave][2] = high, shared[wave][3] = any;
+    __syncthreads();
+    int lowest = 0x7fffffff, highest = -1, some = 0;
+    for (int w = 0; w < 4; ++w) lowest = min(lowest, shared[w][1]), highest = max(highest, shared[w][2]), some |= shared[w][3];
+    // rows that see one of the keys: from first_row(the first key) on, as limits rise with the rows
+    const int begin = sight.first_row(kt * 128), mine = sight.first_row(first_key);
+    const int end = some ? sight.rows : 0;
+    Acc dk[DP / 32], dv[DP / 32];
+#pragma unroll
+    for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
+    ColumnScale<T, DP> fit;
+    constexpr float kWeight = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;  // p <= 1 (to rounding) into float16's upper octaves
+    TileWalk walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
+    Stage<T, DP, kKeys, 256> qs, ds;
+#pragma unroll 1
+    for (int g = 0; g < G; ++g) {
+        const int h = hk * G + g;
+        __syncthreads();
+        WaveBias bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+        const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, h), dout = rows_of<T>(p.dout, p.dout_stride, b, h);
+        const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
+        float next_lse = 0.0f, next_delta = 0.0f;
+        int next_doc = -1;
+        auto load = [&](int t) {
+            qs.load(q, p.D, t * kKeys, end, row_document, thread);
+            ds.load(dout, p.D, t * kKeys, end, row_document, thread);
+            if (thread < kKeys) {
+                const int i = t * kKeys + thread;
+                const bool in = i < end;
+                next_doc = in && row_document ? row_document[i] : in ? 0 : -1;
+                const float x = next_doc >= 0 ? lse[i] : -INFINITY;
+                next_lse = x == -INFINITY ? INFINITY : x * kLog2e;
+                next_delta = next_doc >= 0 ? delta[i] : 0.0f;
+            }
+        };
+        int t = walk.next(begin / kKeys);
+        if (t < walk.tiles) load(t);
+        while (t < walk.tiles) {
+            __syncthreads();
+            qs.store(qtile, thread);
+            ds.store(dtile, thread);
+            if (thread < kKeys) row_lse[thread] = next_lse, row_delta[thread] = next_delta, row_doc[thread] = next_doc;
+            __syncthreads();
+            const int now = t;
+            t = walk.next(t + 1);
+            if (t < walk.tiles) load(t);
+#pragma unroll
+            for (int sub = 0; sub < kKeys / 32; ++sub) {
+                const int i0 = now * kKeys + sub * 32;
+                if (i0 + 32 <= mine || i0 >= end || !any) continue;
+                bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
+                if (row_document) open = open && low == high && __all(row_doc[sub * 32 + c] == low);
+                Acc s = along_features<T, DP>(qtile + Shape::bytes(sub * 32), k, lane), slope;
+                scale_scores_keep(s, slope, p);
+                if (p.buckets) {
+                    bias.look(rule, first_key - (i0 + 31) - sight.offset, lane);
+                    if (bias.same) {
+                        s += bias.one;
+                    } else {
+                        const float *at = bias.diagonal + 31 + c - 4 * half;
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[r] += at[-tile_row(r, 0)];
+                    }
+                }
+                const float *at_lse = row_lse + sub * 32 + 4 * half, *at_delta = row_delta + sub * 32 + 4 * half;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - at_lse[tile_row(r, 0)]);
+                Acc dp = along_features<T, DP>(dtile + Shape::bytes(sub * 32), v, lane);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - at_delta[tile_row(r, 0)]);
+                if (!open) {  // (a key that only rows in no document would see may hold NaN: both are chosen, not multiplied away)
+                    const bool always = j < sight.prefix || !sight.causal;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        bool seen = always || j <= i0 + tile_row(r, half) + sight.offset;
+                        if (row_document) seen = seen && row_doc[sub * 32 + tile_row(r, half)] == doc;
+                        s[r] = seen ? s[r] : 0.0f;
+                        dp[r] = seen ? dp[r] : 0.0f;
+                    }
+                }
+                if (p.cap_out != 0.0f) dp *= slope;
+                if (kWeight != 1.0f) s *= kWeight;
+                along_rows<T, DP>(dv, dtile + Shape::bytes(sub * 32), Weights<T>(s), lane);
+                fit.fit(dp, dk);
+                along_rows<T, DP>(dk, qtile + Shape::bytes(sub * 32), Weights<T>(dp), lane);
+            }
+        }
+    }
+    if (j < p.M) {
+        if (!valid) {
+#pragma unroll
+            for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
+        }
+        store_column<T, DP>(row_of<T>(p.dk, p.dk_stride, b, hk, j), p.D, dk, p.scale * fit.undo(), half);
+        store_column<T, DP>(row_of<T>(p.dv, p.dv_stride, b, hk, j), p.D, dv, 1.0f / kWeight, half);
+    }
+}
+
+}  // namespace sdtw

@@ -1,0 +1,104 @@
+// C entry points of attention's forward pass (declared in include/sdtw.h): checks, the split of the work, launches.
+#include "attention_forward_kernels.h"
+#include "attention_host.h"
+
+namespace {
+
+using namespace sdtw;
+
+struct ForwardPlan {
+    bool fits, few;
+    int64_t row_tiles, splits, workgroups;
+    size_t total;
+};
+
+size_t few_rows_lds(const sdtw_attention_desc *d)
+{
+    const int width = d->type == SDTW_TYPE_F32 ? 4 : 2, features = (d->D + 31) / 32 * 32;
+    return (size_t)8 * 32 * (features * width + 16) +
+           (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 : 0);
+}
+
+ForwardPlan forward_plan(const sdtw_attention_desc *d)
+{
+    ForwardPlan P{};
+    P.fits = true;
+    P.splits = 1;
+    P.total = 256;
+    if (d->B == 0 || d->H == 0 || d->N == 0) return P;
+    const int64_t tiles = (d->N + 127) / 128, G = d->H / d->Hk;
+    P.few = (int64_t)d->B * d->H * tiles < 256 && few_rows_lds(d) + 2048 <= kLdsBytes;
+    if (!P.few) {
+        P.row_tiles = tiles;
+        P.workgroups = (int64_t)d->B * d->H * tiles;
+        P.fits = (int64_t)d->B * d->H <= 0x7fffffff && attention_grid_ok(P.workgroups);
+        return P;
+    }
+    P.row_tiles = ((int64_t)d->N * G + 31) / 32;
+    const int64_t units = (int64_t)d->B * d->Hk * P.row_tiles;
+    P.splits = std::min<int64_t>(std::min<int64_t>((512 + units - 1) / units, (d->M + 127) / 128), 1024);
+    P.splits = std::max<int64_t>(P.splits, 1);
+    P.workgroups = units * P.splits;
+    P.fits = attention_grid_ok(P.workgroups) && attention_grid_ok((int64_t)d->B * d->H * d->N);
+    if (P.splits > 1) P.total = align_up((size_t)d->B * d->H * d->N * P.splits * (d->D + 2) * sizeof(float), 256);
+    return P;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdtw_attention_forward_workspace_bytes(const sdtw_attention_desc *desc)
+{
+    BucketRule rule{};
+    if (attention_check(desc, &rule) != SDTW_OK) return 0;
+    const ForwardPlan P = forward_plan(desc);
+    return P.fits ? P.total : 0;
+}
+
+int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
+                           const sdtw_attention_lists *lists, void *out, float *lse, void *workspace, size_t workspace_bytes,
+                           void *stream)
+{
+    BucketRule rule{};
+    if (int rc = attention_check(desc, &rule)) return rc;
+    if (!lists_ok(desc, lists)) return SDTW_ERR_INVALID_ARG;
+    if (desc->B == 0 || desc->H == 0 || desc->N == 0) return SDTW_OK;
+    if (!q || !out || !lse || (desc->M > 0 && (!k || !v)) || !table == (desc->buckets != 0)) return SDTW_ERR_INVALID_ARG;
+    if (!strides_ok(desc->out_stride, desc->B, desc->H, desc->N, desc->D) ||
+        !places_differ(desc->out_stride, desc->B, desc->H, desc->N, desc->D))
+        return SDTW_ERR_INVALID_ARG;
+    const ForwardPlan P = forward_plan(desc);
+    if (!P.fits) return SDTW_ERR_INVALID_ARG;
+    if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    (void)hipGetLastError();
+    AttentionParams p = attention_params(desc, lists);
+    p.q = q; p.k = k; p.v = v; p.table = table;
+    p.out = out;
+    p.lse = lse;
+    p.row_tiles = (int32_t)P.row_tiles;
+    p.splits = (int32_t)P.splits;
+    p.part = static_cast<float *>(workspace);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    with_shape(desc->type, desc->D, [&](auto t, auto features) {
+        using T = decltype(t);
+        constexpr int DP = decltype(features)::value;
+        if (!P.few) {
+            ProfScope ps("attention_forward", st);
+            const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+            attention_forward_kernel<T, DP, 1><<<(unsigned)P.workgroups, 256, bytes, st>>>(p, rule);
+            return;
+        }
+        {
+            ProfScope ps("attention_few_rows", st);
+            attention_few_rows_kernel<T, DP><<<(unsigned)P.workgroups, 256, few_rows_lds(desc), st>>>(p, rule);
+        }
+        if (P.splits > 1) {
+            ProfScope ps("attention_join", st);
+            attention_join_kernel<T><<<(unsigned)((int64_t)p.B * p.H * p.N), 128, 0, st>>>(p);
+        }
+    });
+    return hip_ok();
+}
+
+}  // extern "C"

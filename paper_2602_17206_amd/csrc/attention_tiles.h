@@ -1,0 +1,397 @@
+// What the attention kernels are made of: tiles of rows in LDS, and products of such a tile with vectors that lanes hold.
+//
+// A wavefront works on 32 "columns" (queries, or keys in the kernel for the keys' gradients), column lane % 32 in the two lanes
+// c and c + 32, and on tiles of 32 rows X [32][D] of what passes by.  With v_mfma_f32_32x32x* there are two products:
+//   along_features   S [row][column] = sum_f X[row][f] R[column][f], R in registers
+//   along_rows       O [f][column] += sum_row X[row][f] P[row][column], P in registers as S came out
+// S leaves lane (c, half) with rows 8 (r / 4) + 4 half + r % 4 of its column in register r.  The order of a product's inner index
+// is free as long as both operands have the same: along_rows takes the rows in that very order, so that P goes back into the
+// matrix cores as it is, without a way through LDS, and statistics of a column stay in its two lanes.
+#pragma once
+#include <type_traits>
+
+#include "bucket_rule.h"
+#include "vector_io.h"
+
+namespace sdtw {
+
+typedef float Acc __attribute__((ext_vector_type(16)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// the row of register r within its tile
+__device__ __forceinline__ constexpr int tile_row(int r, int half) { return 8 * (r >> 2) + 4 * half + (r & 3); }
+
+// The other half's value: of the two lanes of a column, each gets both.
+struct Halves { float lower, upper; };
+__device__ __forceinline__ Halves halves(float v)
+{
+    const uint32_t x = __float_as_uint(v);
+    const auto w = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return {__uint_as_float(w[0]), __uint_as_float(w[1])};
+}
+__device__ __forceinline__ float both_sum(float v) { const Halves h = halves(v); return h.lower + h.upper; }
+__device__ __forceinline__ float both_max(float v) { const Halves h = halves(v); return fmaxf(h.lower, h.upper); }
+
+__device__ __forceinline__ int wave_min_i32(int v)
+{
+    for (int d = 1; d < 64; d *= 2) v = min(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max_i32(int v)
+{
+    for (int d = 1; d < 64; d *= 2) v = max(v, __shfl_xor(v, d));
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+// ------------------------------------------------------------------ tiles in LDS
+
+// Rows of DP features (D and zeros behind it) with 16 bytes between them: the same chunk of neighbouring rows falls into different
+// banks.
+template <typename T, int DP> struct TileShape {
+    static constexpr int W = Elem<T>::kWidth;
+    static constexpr int kChunks = DP / W;  // 16-byte chunks of a row
+    static constexpr int kStride = DP * (int)sizeof(T) + 16;
+    static constexpr int bytes(int rows) { return rows * kStride; }
+};
+
+// A matrix [rows][D] in memory, of any strides.
+template <typename T> struct Rows {
+    const T *base;
+    int64_t row, feature;  // strides
+};
+
+// Chunk ch of a row: D features and zeros behind them.  A chunk that hangs over the end is read further in and shifted.
+template <typename T> __device__ __forceinline__ Bits4 load_chunk(const T *row, int64_t feature, int D, int ch)
+{
+    constexpr int W = Elem<T>::kWidth;
+    const int f = ch * W;
+    if (feature == 1) {
+        if (f + W <= D) return load_vec<false>(row + f);
+        if (f >= D) return Bits4{};
+        if (D >= W) return shift_vec(load_vec<false>(row + D - W), (f + W - D) * 8 * (int)sizeof(T));
+    }
+    Bits4 v{};
+#pragma unroll
+    for (int e = 0; e < W; ++e)
+        if (f + e < D) {
+            const T x = row[(f + e) * feature];
+            uint32_t bits;
+            if constexpr (sizeof(T) == 4) {
+                v[e] = __builtin_bit_cast(uint32_t, x);
+            } else {
+                bits = (uint32_t)__builtin_bit_cast(uint16_t, x) << (e & 1 ? 16 : 0);
+                v[e >> 1] |= bits;
+            }
+        }
+    return v;
+}
+
+// A tile on its way from memory to LDS: loaded to registers, later stored.  `who` of THREADS threads; ROWS rows.
+template <typename T, int DP, int ROWS, int THREADS> struct Stage {
+    using Shape = TileShape<T, DP>;
+    static constexpr int kEach = ROWS * Shape::kChunks / THREADS;
+    static_assert(kEach * THREADS == ROWS * Shape::kChunks, "a tile is dealt out evenly");
+    Bits4 v[kEach];
+    // rows first .. first + ROWS; zeros from `limit` on and for rows whose document is negative
+    __device__ __forceinline__ void load(const Rows<T> &x, int D, int first, int limit, const int32_t *document, int who)
+    {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int id = who + k * THREADS, row = id / Shape::kChunks, ch = id % Shape::kChunks;
+            const int j = first + row;
+            v[k] = Bits4{};
+            if (j < limit && (!document || document[j] >= 0)) v[k] = load_chunk(x.base + j * x.row, x.feature, D, ch);
+        }
+    }
+    __device__ __forceinline__ void store(char *tile, int who) const
+    {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int id = who + k * THREADS, row = id / Shape::kChunks, ch = id % Shape::kChunks;
+            *reinterpret_cast<Bits4 *>(tile + row * Shape::kStride + ch * 16) = v[k];
+        }
+    }
+};
+
+// ------------------------------------------------------------------ products
+
+// A column's features, as along_features takes them: chunks half, half + 2, ...
+template <typename T, int DP> struct Column {
+    static constexpr int kSteps = TileShape<T, DP>::kChunks / 2;
+    Bits4 v[kSteps];
+    __device__ __forceinline__ void load(const T *row, int64_t feature, int D, bool valid, int half)
+    {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            v[s] = Bits4{};
+            if (valid) v[s] = load_chunk(row, feature, D, 2 * s + half);
+        }
+    }
+};
+
+template <typename T> __device__ __forceinline__ void mma(Acc &acc, const Bits4 &a, const Bits4 &b)
+{
+    if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = a[e], y = b[e];
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x), __uint_as_float(y), acc, 0, 0, 0);
+        }
+    } else if constexpr (std::is_same<T, Bf16>::value) {
+        typedef __bf16 V __attribute__((ext_vector_type(8)));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
+    } else {
+        typedef _Float16 V __attribute__((ext_vector_type(8)));
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), acc, 0, 0, 0);
+    }
+}
+
+// S = X R for the 32 rows of `tile`
+template <typename T, int DP> __device__ __forceinline__ Acc along_features(const char *tile, const Column<T, DP> &col, int lane)
+{
+    const char *at = tile + (lane & 31) * TileShape<T, DP>::kStride + (lane >> 5) * 16;
+    Acc acc = {};
+#pragma unroll
+    for (int s = 0; s < Column<T, DP>::kSteps; ++s) mma<T>(acc, *reinterpret_cast<const Bits4 *>(at + s * 32), col.v[s]);
+    return acc;
+}
+
+// P [32 rows][column] as the matrix cores take it: rounded to T, except for float32
+template <typename T> struct Weights {
+    Bits4 v[2];
+    __device__ __forceinline__ explicit Weights(const Acc &p)
+    {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const float x[8] = {p[8 * s], p[8 * s + 1], p[8 * s + 2], p[8 * s + 3], p[8 * s + 4], p[8 * s + 5], p[8 * s + 6], p[8 * s + 7]};
+            v[s] = Elem<T>::pack(x);
+        }
+    }
+};
+template <> struct Weights<float> {
+    Acc v;
+    __device__ __forceinline__ explicit Weights(const Acc &p) : v(p) {}
+};
+
+typedef short Short4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) Short4 LdsShort4;
+
+// O += X^T P: feature 32 ft + tile_row(r, half) of the column in register r of acc[ft]
+template <typename T, int DP> __device__ __forceinline__ void along_rows(Acc (&acc)[DP / 32], const char *tile, const Weights<T> &w, int lane)
+{
+    constexpr int kStride = TileShape<T, DP>::kStride;
+    if constexpr (std::is_same<T, float>::value) {
+        const char *at = tile + 4 * (lane >> 5) * kStride + (lane & 31) * 4;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+#pragma unroll
+            for (int ft = 0; ft < DP / 32; ++ft) {
+                const float x = *reinterpret_cast<const float *>(at + tile_row(r, 0) * kStride + ft * 128);
+                acc[ft] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w.v[r], acc[ft], 0, 0, 0);
+            }
+    } else {
+        // ds_read_b64_tr_b16: sixteen lanes read 4 rows of 16 elements, four elements a lane, and each gets a column of them
+        const char *at = tile + (4 * (lane >> 5) + (lane >> 2 & 3)) * kStride + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int ft = 0; ft < DP / 32; ++ft) {
+                Bits4 a;
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const Short4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (LdsShort4 *)(at + (16 * s + 8 * q) * kStride + ft * 64));
+                    const uint64_t bits = __builtin_bit_cast(uint64_t, x);
+                    a[2 * q] = (uint32_t)bits;
+                    a[2 * q + 1] = (uint32_t)(bits >> 32);
+                }
+                mma<T>(acc[ft], a, w.v[s]);
+            }
+    }
+}
+
+// A column's result, `factor` times acc, as row `out` of D features in memory.
+template <typename T, int DP> __device__ __forceinline__ void store_column(T *out, int D, const Acc (&acc)[DP / 32], float factor, int half)
+{
+    typedef uint32_t Two __attribute__((ext_vector_type(2)));
+    typedef Two TwoAny __attribute__((aligned(2)));
+#pragma unroll
+    for (int ft = 0; ft < DP / 32; ++ft)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int f = 32 * ft + 8 * g + 4 * half;
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = acc[ft][4 * g + e] * factor;
+            if (f + 4 <= D) {
+                if constexpr (sizeof(T) == 4)
+                    store_vec<false>(out + f, Elem<T>::pack(x));
+                else
+                    *reinterpret_cast<TwoAny *>(out + f) = Two{Elem<T>::pack2(x[0], x[1]), Elem<T>::pack2(x[2], x[3])};
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (f + e < D) out[f + e] = Elem<T>::down(x[e]);
+            }
+        }
+}
+
+// ------------------------------------------------------------------ scores
+
+struct AttentionParams {
+    int32_t B, H, Hk, N, M, D;
+    int32_t buckets, table_type, causal;
+    int32_t offset, prefix;
+    float scale, scale2;        // of the products; times log2(e)
+    float cap_in, cap_out;      // scale / cap and cap log2(e); cap_out 0: no cap
+    const void *q, *k, *v, *table, *dout;
+    void *out, *dq, *dk, *dv;
+    float *lse;                 // [B, H, N]
+    const int32_t *offsets, *prefixes, *row_len, *col_len, *row_document, *col_document;
+    int64_t q_stride[4], k_stride[4], v_stride[4], out_stride[4], dout_stride[4], dq_stride[4], dk_stride[4], dv_stride[4];
+    int64_t table_stride[2];
+    // how the work is split
+    int32_t row_tiles, key_tiles, splits, table_columns;
+    float *part;                // [B, H, N, splits][D + 2]: unfinished sums, their reference and total
+    float *delta;               // [B, H, N]
+    float *table_part;          // [H, buckets][B * row_tiles]
+    float *dtable;              // [H, buckets]
+};
+
+template <typename T> __device__ __forceinline__ Rows<T> rows_of(const void *base, const int64_t (&stride)[4], int b, int h)
+{
+    return {static_cast<const T *>(base) + b * stride[0] + h * stride[1], stride[2], stride[3]};
+}
+template <typename T> __device__ __forceinline__ T *row_of(void *base, const int64_t (&stride)[4], int b, int h, int64_t i)
+{
+    return static_cast<T *>(base) + b * stride[0] + h * stride[1] + i * stride[2];
+}
+
+// What a sequence's rows see: row i the keys below limit(i) (of its document).
+struct Sight {
+    int rows, keys, offset, prefix, causal;
+    __device__ __forceinline__ Sight(const AttentionParams &p, int b)
+    {
+        rows = clamp_len(p.row_len, b, p.N);
+        keys = clamp_len(p.col_len, b, p.M);
+        // (|j - i| is below 2^28 and max_distance at most 2^24: beyond 2^29 nothing changes)
+        offset = p.offsets ? min(max(p.offsets[b], -(1 << 29)), 1 << 29) : p.offset;
+        prefix = p.prefixes ? p.prefixes[b] : p.prefix;
+        causal = p.causal;
+    }
+    __device__ __forceinline__ int limit(int i) const { return causal ? min(keys, max(i + offset + 1, prefix)) : keys; }
+    // the first row that sees key j, if any does
+    __device__ __forceinline__ int first_row(int j) const { return causal && j >= prefix ? max(0, j - offset) : 0; }
+};
+
+// tanh from an exponential; for small arguments, where that cancels, Lambert's continued fraction to its fifth denominator (off by
+// 3e-11 of the value at 0.5).  One division serves both.
+__device__ __forceinline__ float tanh_fast(float x)
+{
+    const float y = fminf(fmaxf(x, -20.0f), 20.0f), z = y * y;  // (1 to the last bit from there on)
+    const float e = exp2_fast(2.0f * kLog2e * y);
+    const bool small = fabsf(y) < 0.5f;
+    const float above = small ? y * fmaf(z + 105.0f, z, 945.0f) : e - 1.0f;
+    const float below = small ? fmaf(fmaf(15.0f, z, 420.0f), z, 945.0f) : e + 1.0f;
+    return x != x ? x : above * __builtin_amdgcn_rcpf(below);
+}
+
+// An entry below -1e30 forbids its cells, as -inf does.
+__device__ __forceinline__ float octaves_of_entry(float v) { return v < -1e30f ? -INFINITY : v * kLog2e; }
+
+// The bias of 32 x 32 cells (or of the cells of one key and one row): what a wavefront knows of the 63 diagonals of its tile.
+struct WaveBias {
+    const float *values;     // LDS: the head's entries, in octaves
+    const int32_t *starts;   // LDS
+    float *diagonal;         // LDS, 64 of the wavefront's own
+    uint8_t *bucket;         // LDS, 64 of the wavefront's own
+    float one;               // the bias of all cells, where it is the same
+    int one_bucket;
+    bool same;
+    // `lowest`: j - i - offset on the lowest of the diagonals
+    __device__ __forceinline__ void look(const BucketRule &rule, int lowest, int lane)
+    {
+        const int u = rule.bucket(lowest + min(lane, 62), starts);
+        one_bucket = __builtin_amdgcn_readfirstlane(u);
+        same = __all(u == one_bucket);
+        if (same) {
+            one = values[one_bucket];
+        } else {
+            wavefront_order();
+            diagonal[lane] = values[u];
+            bucket[lane] = (uint8_t)u;
+            wavefront_order();
+        }
+    }
+};
+
+// LDS that the bias takes: 256 entries, the rule's starts, and 64 diagonals (4 + 1 bytes) for each wavefront.
+constexpr int kBiasStarts = (kMaxBuckets / 2 + 1 + 3) / 4 * 4;
+constexpr int bias_bytes(int waves) { return kMaxBuckets * 4 + kBiasStarts * 4 + waves * 64 * 5; }
+
+// Lays the bias's part of LDS out and fills it; a barrier has to follow.
+__device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const BucketRule &rule, char *lds, int h, int wave, int waves, int thread,
+                                               int threads)
+{
+    float *values = reinterpret_cast<float *>(lds);
+    int32_t *starts = reinterpret_cast<int32_t *>(lds + kMaxBuckets * 4);
+    float *diagonal = reinterpret_cast<float *>(lds + kMaxBuckets * 4 + kBiasStarts * 4);
+    uint8_t *bucket = reinterpret_cast<uint8_t *>(diagonal + 64 * waves);
+    if (p.buckets) {
+        for (int u = thread; u < p.buckets; u += threads)
+            values[u] = octaves_of_entry(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
+        for (int k = thread; k <= rule.m; k += threads) starts[k] = rule.start[k];
+    }
+    return WaveBias{values, starts, diagonal + 64 * wave, bucket + 64 * wave, 0.0f, 0, true};
+}
+
+constexpr int kKeys = 64;  // keys of a tile in LDS
+
+// The tiles of 64 keys (or rows) that a workgroup of 4 wavefronts walks through.  Where the sequence is packed from documents, those
+// without one of the documents lowest .. highest are stepped over: found out for 256 tiles at a time.
+struct TileWalk {
+    const int32_t *document;
+    int keys, tiles, lowest, highest, batch;
+    uint64_t *live;  // LDS, 4
+    __device__ __forceinline__ int next(int t)  // the first tile from t on; `tiles` if there is none.  The same in all threads.
+    {
+        if (!document) return t;
+        while (t < tiles) {
+            if (t / 256 != batch) {
+                batch = t / 256;
+                const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, first = batch * 256 + wave * 64;
+                uint64_t mine = 0;
+#pragma unroll 8
+                for (int k = 0; k < 64; ++k) {
+                    const int j = (first + k) * 64 + lane;
+                    const int d = j < keys ? document[j] : -1;
+                    if (__any(d >= lowest && d <= highest)) mine |= (uint64_t)1 << k;
+                }
+                __syncthreads();
+                if (lane == 0) live[wave] = mine;
+                __syncthreads();
+            }
+            const uint64_t word = live[t % 256 / 64] >> (t % 64);
+            if (word) return min(tiles, t + (int)__builtin_ctzll(word));
+            t = (t / 64 + 1) * 64;
+        }
+        return tiles;
+    }
+};
+
+// Products into scores, in octaves.
+__device__ __forceinline__ void scale_scores(Acc &s, const AttentionParams &p)
+{
+    if (p.cap_out != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = p.cap_out * tanh_fast(s[r] * p.cap_in);
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] *= p.scale2;
+    }
+}
+
+}  // namespace sdtw

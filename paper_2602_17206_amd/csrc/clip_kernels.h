@@ -1,0 +1,184 @@
+// The norm of many tensors together, and the tensors scaled by what it asks for.
+//
+// Two launches (for up to 128 tensors, whose places come as kernel arguments: nothing is copied to the device): the squares, summed
+// up in 64 bits by workgroups; then every workgroup adds those sums up itself, in one order, and scales its share.
+// Both read all of the gradients.  The second walks from the end to the beginning: what was read last is still in
+// the memory-side cache.
+#pragma once
+#include "vector_io.h"
+
+namespace sdtw {
+
+constexpr int kClipTensors = 128;
+constexpr int kClipChunk = 8192;  // elements
+constexpr int kClipParts = 2048;
+
+struct ClipList {
+    const void *data[kClipTensors];
+    void *out[kClipTensors];
+    uint64_t count_types[kClipTensors];  // count, type << 56, out_type << 60
+    int32_t first[kClipTensors + 1];     // chunks before each tensor
+    int32_t tensors;
+};
+
+struct ClipParams {
+    double *parts;    // [all_parts]
+    int32_t part, all_parts;  // the first of this launch's
+    float max_norm;
+    float *norm;      // nullptr but for the launch that writes it
+};
+
+// The sum over the 256 threads of a workgroup, in every one of them.
+__device__ __forceinline__ double workgroup_sum_f64(double v, double *lds)
+{
+    v = wave_sum_f64(v);
+    __syncthreads();
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// Calls f(tensor, first element, elements) for the workgroup's chunks, the last ones first if BACKWARD.
+template <bool BACKWARD, typename F> __device__ __forceinline__ void clip_chunks(const ClipList &list, F f)
+{
+    const int64_t chunks = list.first[list.tensors];
+    const int begin = (int)(chunks * blockIdx.x / gridDim.x), end = (int)(chunks * (blockIdx.x + 1) / gridDim.x);
+    if (begin >= end) return;
+    const int start = BACKWARD ? end - 1 : begin;
+    int lo = 0, hi = list.tensors - 1;  // the tensor that holds chunk `start`
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (list.first[mid] <= start) lo = mid;
+        else hi = mid - 1;
+    }
+    int tensor = lo;
+    for (int n = 0; n < end - begin; ++n) {
+        const int chunk = BACKWARD ? start - n : start + n;
+        while (chunk < list.first[tensor]) --tensor;
+        while (chunk >= list.first[tensor + 1]) ++tensor;
+        const int64_t count = (int64_t)(list.count_types[tensor] & 0xffffffffffffull);
+        const int64_t at = (int64_t)(chunk - list.first[tensor]) * kClipChunk;
+        f(tensor, at, (int)min(count - at, (int64_t)kClipChunk));
+    }
+}
+
+template <typename T> __device__ __forceinline__ double clip_squares(const T *x, int n)
+{
+    constexpr int W = Elem<T>::kWidth, kSteps = kClipChunk / 256 / W;
+    double sum = 0.0, more = 0.0;
+    if (n == kClipChunk) {
+        Bits4 v[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) v[s] = load_vec<false>(x + (s * 256 + (int)threadIdx.x) * W);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+            for (int e = 0; e < W; e += 2) {
+                const double a = Elem<T>::at(v[s], e), b = Elem<T>::at(v[s], e + 1);
+                sum = fma(a, a, sum);
+                more = fma(b, b, more);
+            }
+        return sum + more;
+    }
+    int i = threadIdx.x * W;
+    for (; i + W <= n; i += 256 * W) {
+        const Bits4 v = load_vec<false>(x + i);
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const double a = Elem<T>::at(v, e);
+            sum = fma(a, a, sum);
+        }
+    }
+    for (; i < n; ++i) {  // (one thread's at most, fewer than a vector)
+        const double a = Elem<T>::up(x[i]);
+        sum = fma(a, a, sum);
+    }
+    return sum;
+}
+
+template <typename T, typename U> __device__ __forceinline__ void clip_store(U *out, const Bits4 &v, float factor)
+{
+    constexpr int W = Elem<T>::kWidth, V = Elem<U>::kWidth;
+    if constexpr (V >= W) {
+        // (four float32 to 16 bits: eight bytes)
+        float x[V] = {};
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[e] = Elem<T>::at(v, e) * factor;
+        const Bits4 y = Elem<U>::pack(x);
+        if constexpr (V == W) {
+            store_vec<true>(out, y);
+        } else {
+            typedef uint32_t Two __attribute__((ext_vector_type(2)));
+            typedef Two TwoAny __attribute__((aligned(2)));
+            *reinterpret_cast<TwoAny *>(out) = Two{y[0], y[1]};
+        }
+    } else {
+#pragma unroll
+        for (int p = 0; p < W / V; ++p) {
+            float x[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = Elem<T>::at(v, p * V + e) * factor;
+            store_vec<true>(out + p * V, Elem<U>::pack(x));
+        }
+    }
+}
+
+template <typename T, typename U> __device__ __forceinline__ void clip_scale(const T *in, U *out, int n, float factor)
+{
+    constexpr int W = Elem<T>::kWidth, kSteps = kClipChunk / 256 / W;
+    if (n == kClipChunk) {
+        Bits4 v[kSteps];
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) v[s] = load_vec<false>(in + (s * 256 + (int)threadIdx.x) * W);
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) clip_store<T, U>(out + (s * 256 + (int)threadIdx.x) * W, v[s], factor);
+        return;
+    }
+    int i = threadIdx.x * W;
+    for (; i + W <= n; i += 256 * W) clip_store<T, U>(out + i, load_vec<false>(in + i), factor);
+    for (; i < n; ++i) out[i] = Elem<U>::down(Elem<T>::up(in[i]) * factor);
+}
+
+// Calls f with the element that SDTW_TYPE_* `type` stands for.
+template <typename F> __device__ __forceinline__ void clip_typed(int type, F f)
+{
+    if (type == SDTW_TYPE_F32) f(float{});
+    else if (type == SDTW_TYPE_F16) f(_Float16{});
+    else f(Bf16{});
+}
+
+__global__ __launch_bounds__(256) void clip_squares_kernel(ClipList list, ClipParams p)
+{
+    __shared__ double lds[4];
+    double sum = 0.0;
+    clip_chunks<false>(list, [&](int tensor, int64_t at, int n) {
+        clip_typed((int)(list.count_types[tensor] >> 56 & 15), [&](auto t) {
+            sum += clip_squares(static_cast<const decltype(t) *>(list.data[tensor]) + at, n);
+        });
+    });
+    sum = workgroup_sum_f64(sum, lds);
+    if (threadIdx.x == 0) p.parts[p.part + blockIdx.x] = sum;
+}
+
+__global__ __launch_bounds__(256) void clip_scale_kernel(ClipList list, ClipParams p)
+{
+    __shared__ double lds[4];
+    double sum = 0.0;
+    for (int k = threadIdx.x; k < p.all_parts; k += 256) sum += p.parts[k];
+    const double norm = sqrt(workgroup_sum_f64(sum, lds));
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+    const bool scaled = norm > (double)p.max_norm && norm < INFINITY;  // (false for a NaN)
+    const float factor = scaled ? (float)((double)p.max_norm / norm) : 1.0f;
+    clip_chunks<true>(list, [&](int tensor, int64_t at, int n) {
+        if (!scaled && list.out[tensor] == list.data[tensor]) return;
+        const uint64_t types = list.count_types[tensor];
+        clip_typed((int)(types >> 56 & 15), [&](auto t) {
+            clip_typed((int)(types >> 60), [&](auto u) {
+                clip_scale(static_cast<const decltype(t) *>(list.data[tensor]) + at, static_cast<decltype(u) *>(list.out[tensor]) + at, n,
+                           factor);
+            });
+        });
+    });
+}
+
+}  // namespace sdtw

@@ -28,6 +28,10 @@ inline int check_ws(const void *ws, size_t bytes, size_t need)
 
 inline int hip_ok() { return hipGetLastError() == hipSuccess ? SDTW_OK : SDTW_ERR_HIP; }
 
+// The rule of a bias descriptor's buckets (train_ops.hip); false if the descriptor is invalid.
+struct BucketRule;
+bool position_bias_rule(const sdtw_bias_desc *d, BucketRule *rule);
+
 // The position bias (train_ops.hip) as the Soft-DTW calls use it: with `penalty` negative table entries count as 0.
 int position_bias_add(const sdtw_bias_desc *d, const void *table, bool penalty, const void *in, const int32_t *offsets,
                       const int32_t *row_len, const int32_t *col_len, void *out, hipStream_t st);

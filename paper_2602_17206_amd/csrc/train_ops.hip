@@ -404,6 +404,13 @@ BiasPlan bias_plan(const sdtw_bias_desc *d)
 
 namespace sdtw {
 
+bool position_bias_rule(const sdtw_bias_desc *d, BucketRule *rule)
+{
+    if (!bias_ok(d)) return false;
+    *rule = bucket_rule(d);
+    return true;
+}
+
 int position_bias_add(const sdtw_bias_desc *desc, const void *table, bool penalty, const void *in, const int32_t *offsets,
                       const int32_t *row_len, const int32_t *col_len, void *out, hipStream_t st)
 {

@@ -1,0 +1,597 @@
+"""Attention under the position bias, forward and backward, against plain implementations in 64 bits.
+
+Bars, from the arithmetic, with eps = 2^-24 (float32) and u half a step of the inputs' type, relative:
+  scores      products of 16-bit numbers are exact in float32, those of float32 round once; D additions, a scaling, the tanh and the bias
+              by a few ulps: a score is off by ds = (D + 4) eps scale sum |q k| + 16 eps (|x| + |bias|)
+  softmax     exp of a difference of scores over a sum of M of them: relative 2 max ds + (M + 40) eps; the numerators are rounded
+              to the type for the matrix cores (u; none in float32), in float16 with steps of 2^-24 beside a largest one of 1
+  out         that on each term of sum p |v|, M additions (eps each), and one rounding to the type
+  lse         max ds, and the sum's error as a logarithm's
+  backward    p once more from lse: relative 2 max ds + (M + 40) eps + 8 eps |lse|; dp off by (D + 2) eps sum |dout v|; delta by what its
+              terms are off, or by u of the terms of sum dout out where it comes from the rounded output; ds = p (dp - delta) by
+              these; rounded to the type for the products (float16: steps of 2^-28 of the column's largest), then sums of M or N terms
+  underflow   whatever is below 2^-126, the least normal number of float32 and bfloat16, may be taken as 0: a weight p, a ds, a product of one
+              of them and an element, a sum: LOW on each p and each ds, and (M or N) LOW on each result
+They are sums of worst cases: nothing in them is measured."""
+import math
+
+import pytest
+import torch
+
+import paper_2602_17206_amd as pkg
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+LEAST = {"f32": 2.0 ** -149, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}
+EPS = 2.0 ** -24
+LOW = 2.0 ** -126
+INF, NAN = float("inf"), float("nan")
+
+
+def bucket_matrix(N, M, buckets, max_distance, two_sided, offset):
+    starts = torch.tensor(pkg.sdtw_position_bias_starts(buckets, max_distance, two_sided), device="cuda")
+    r = torch.arange(M, device="cuda") - torch.arange(N, device="cuda")[:, None] - offset
+    d = r.abs() if two_sided else (-r).clamp(min=0)
+    return torch.searchsorted(starts, d, right=True) - 1 + (buckets // 2 * (r > 0) if two_sided else 0)
+
+
+def visible(N, M, b, causal=False, offset=0, prefix=None, row_len=None, col_len=None, row_document=None, col_document=None, **_):
+    i, j = torch.arange(N, device="cuda")[:, None], torch.arange(M, device="cuda")
+    own = lambda x: int(x[b]) if torch.is_tensor(x) else x  # noqa: E731
+    seen = torch.ones((N, M), dtype=torch.bool, device="cuda")
+    if causal:
+        seen &= (j <= i + own(offset)) | (j < (own(prefix) if prefix is not None else 0))
+    if row_len is not None:
+        seen &= i < own(row_len)
+    if col_len is not None:
+        seen &= j < own(col_len)
+    if row_document is not None:
+        seen &= (row_document[b][:, None] == col_document[b]) & (row_document[b][:, None] >= 0)
+    return seen
+
+
+def reference(q, k, v, dout=None, table=None, scale=None, cap=0.0, max_distance=128, two_sided=True, offset=0, want_dtable=True, **masks):
+    """What the calls return, in 64 bits, and the bars of each: {name: (value, bar)}"""
+    kind = {t: n for n, t in TYPES.items()}[q.dtype]
+    u = HALF_ULP[kind]
+    uw = 0.0 if kind == "f32" else u
+    (B, H, N, D), (_, Hk, M, _) = q.shape, k.shape
+    scale = D ** -0.5 if scale is None else scale
+    zeros = lambda *s: torch.zeros(s, dtype=torch.float64, device="cuda")  # noqa: E731
+    out, out_bar, lse, lse_bar = zeros(B, H, N, D), zeros(B, H, N, D), zeros(B, H, N) - INF, zeros(B, H, N)
+    dq, dq_bar = zeros(B, H, N, D), zeros(B, H, N, D)
+    dk, dk_bar, dv, dv_bar = (zeros(B, Hk, M, D) for _ in range(4))
+    buckets = 0 if table is None else table.shape[1]
+    dt, dt_bar = zeros(H, max(1, buckets)), zeros(H, max(1, buckets))
+    for b in range(B):
+        seen = visible(N, M, b, offset=offset, **masks)
+        rows, cols = seen.any(1), seen.any(0)
+        at = bucket_matrix(N, M, buckets, max_distance, two_sided, int(offset[b]) if torch.is_tensor(offset) else offset) if buckets else None
+        for h in range(H):
+            g = h // (H // Hk)
+            clean = lambda x, keep: torch.where(keep[:, None], x.double(), 0.0)  # noqa: E731
+            Q, K, V = clean(q[b, h], rows), clean(k[b, g], cols), clean(v[b, g], cols)
+            x = scale * Q @ K.t()
+            t = None
+            if cap:
+                t = torch.tanh(x / cap)
+                x = cap * t
+            ds = (D + 4) * EPS * scale * Q.abs() @ K.abs().t() + 16 * EPS * x.abs()
+            s = x
+            if buckets:
+                bias = table[h].double()[at]
+                s = torch.where(bias < -1e30, -INF, x + bias)
+                ds = ds + torch.where(bias < -1e30, 0.0, 16 * EPS * bias.abs())
+            s = torch.where(seen, s, -INF)
+            some = (s > -INF).any(1)
+            ds = torch.where(s > -INF, ds, 0.0).amax(1, keepdim=True) if M else zeros(N, 1)
+            lse_h = torch.where(some, torch.logsumexp(s, 1), -INF)
+            p = torch.where(some[:, None], torch.exp(s - torch.where(some, lse_h, 0.0)[:, None]), 0.0)
+            rel = 2 * ds + (M + 40) * EPS
+            o = p @ V
+            out[b, h], lse[b, h] = o, lse_h
+            tiny = 2.0 ** -25 * V.abs().sum(0) if kind == "f16" else 0.0
+            out_bar[b, h] = (rel + uw + M * EPS) * (p @ V.abs()) + 1.01 * u * o.abs() + LEAST[kind] + tiny * some[:, None] + LOW * (M + V.abs().sum(0))
+            lse_bar[b, h] = rel[:, 0] + 4 * EPS * lse_h.abs().nan_to_num(posinf=0.0)
+            if dout is None:
+                continue
+            G = clean(dout[b, h], some)
+            rel = rel + 8 * EPS * torch.where(some, lse_h, 0.0).abs()[:, None]
+            dp, dp_bar = G @ V.t(), (D + 2) * EPS * G.abs() @ V.abs().t()
+            delta = (p * dp).sum(1, keepdim=True)
+            if buckets and want_dtable:
+                delta_bar = ((rel + M * EPS) * p * dp.abs() + p * dp_bar).sum(1, keepdim=True)
+            else:
+                delta_bar = (G.abs() * (out_bar[b, h] + D * EPS * o.abs())).sum(1, keepdim=True)
+            dz = p * (dp - delta)
+            e = rel * p * (dp.abs() + delta.abs()) + p * (dp_bar + delta_bar + 2 * EPS * (dp.abs() + delta.abs())) + LOW * (1.0 + dp.abs() + delta.abs())
+            if buckets:
+                for c in range(buckets):
+                    here = at == c
+                    dt[h, c] += dz[here].sum()
+                    dt_bar[h, c] += e[here].sum() + (N + M + 100) * EPS * dz[here].abs().sum()
+            if cap:
+                dz, e = dz * (1 - t * t), (e + 16 * EPS * dz.abs())
+            dx_bar_rows = e + (uw + M * EPS) * dz.abs()
+            dx_bar_cols = e + (uw + H // Hk * N * EPS) * dz.abs()
+            if kind == "f16":
+                dx_bar_rows = dx_bar_rows + 2.0 ** -28 * dz.abs().amax(1, keepdim=True) if M else dx_bar_rows
+                dx_bar_cols = dx_bar_cols + 2.0 ** -28 * dz.abs().amax(0, keepdim=True)
+            dq[b, h] = scale * dz @ K
+            dq_bar[b, h] = scale * dx_bar_rows @ K.abs()
+            dk[b, g] += scale * dz.t() @ Q
+            dk_bar[b, g] += scale * dx_bar_cols.t() @ Q.abs()
+            dv[b, g] += p.t() @ G
+            dv_bar[b, g] += ((rel + uw + H // Hk * N * EPS) * p + (2.0 ** -38 if kind == "f16" else LOW) * some[:, None]).t() @ G.abs()
+    found = {"out": (out, out_bar), "lse": (lse, lse_bar)}
+    if dout is not None:
+        for name, x, bar in (("dq", dq, dq_bar), ("dk", dk, dk_bar), ("dv", dv, dv_bar)):
+            found[name] = (x, bar + 1.01 * u * x.abs() + LEAST[kind] + (M + H * N) * LOW)
+        if buckets and want_dtable:
+            found["dtable"] = (dt, dt_bar + 2 * EPS * dt.abs() + N * M * LOW)
+    return found
+
+
+def compare(got, want):
+    for name, (x, bar) in want.items():
+        y = got[name].double()
+        assert y.shape == x.shape, name
+        fine = torch.isfinite(x)
+        assert torch.equal(y[~fine], x[~fine]), name
+        off = (y - x).abs()[fine]
+        assert (off <= bar[fine]).all(), (name, float((off - bar[fine]).max()), float(off.max()), torch.isnan(off).any().item())
+
+
+def values(shape, kind, gen, size=1.0):
+    return (size * torch.randn(shape, generator=gen, device="cuda")).to(TYPES[kind])
+
+
+def problem(B, H, Hk, N, M, D, kind, seed=0, size=1.5):
+    """q, k, v, dout, laid out position by position with the heads side by side"""
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    made = [values((B, n, h, D), kind, gen, s).transpose(1, 2) for n, h, s in ((N, H, size), (M, Hk, size), (M, Hk, 1.0), (N, H, 1.0))]
+    return made, gen
+
+
+def hide(x, seen_dim):
+    """NaN wherever nothing may look: rows (or keys) [B, n] that are marked"""
+    return x.masked_fill(seen_dim[:, None, :, None], NAN)
+
+
+def spoil(q, k, v, dout, masks):
+    """The tensors with NaN behind the lengths, outside all documents, and behind the last key that a causal row may see."""
+    (B, H, N, D), (_, Hk, M, _) = q.shape, k.shape
+    i, j = torch.arange(N, device="cuda"), torch.arange(M, device="cuda")
+    row, col = torch.zeros((B, N), dtype=torch.bool, device="cuda"), torch.zeros((B, M), dtype=torch.bool, device="cuda")
+    if masks.get("row_len") is not None:
+        row |= i >= masks["row_len"][:, None]
+    if masks.get("col_len") is not None:
+        col |= j >= masks["col_len"][:, None]
+    if masks.get("row_document") is not None:
+        row, col = row | (masks["row_document"] < 0), col | (masks["col_document"] < 0)
+    if masks.get("causal"):
+        own = lambda x: torch.as_tensor(0 if x is None else x, device="cuda").long().expand(B)[:, None]  # noqa: E731
+        last = torch.where(~row, i, -(1 << 40)).amax(1, keepdim=True) if N else torch.full((B, 1), -(1 << 40), device="cuda")
+        col |= (j > last + own(masks.get("offset", 0))) & (j >= own(masks.get("prefix")))
+    return hide(q, row), hide(k, col), hide(v, col), hide(dout, row)
+
+
+def check(B, H, Hk, N, M, D, kind, seed=0, table=None, size=1.5, **more):
+    (q, k, v, dout), _ = problem(B, H, Hk, N, M, D, kind, seed, size)
+    q, k, v, dout = spoil(q, k, v, dout, more)
+    return check_these(q, k, v, dout, table=table, **more)
+
+
+def check_these(q, k, v, dout, table=None, **more):
+    want = reference(q, k, v, dout, table, **more)
+    options = {x: y for x, y in more.items() if x != "want_dtable"}
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table, **options)
+    compare({"out": out, "lse": lse}, {x: want[x] for x in ("out", "lse")})
+    dq, dk, dv, dt = pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, **more)
+    assert (dt is None) == ("dtable" not in want)
+    compare({"dq": dq, "dk": dk, "dv": dv, "dtable": dt}, {x: y for x, y in want.items() if x not in ("out", "lse")})
+    return out, lse, dq, dk, dv, dt
+
+
+def some_table(H, buckets, seed=0, kind="f32"):
+    gen = torch.Generator(device="cuda").manual_seed(100 + seed)
+    return torch.randn((buckets, H), generator=gen, device="cuda").to(TYPES[kind]).t()
+
+
+# ---------------------------------------------------------------- sizes, types, heads
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("N,M,D", [(1, 1, 1), (1, 2, 3), (2, 1, 7), (3, 31, 8), (31, 32, 9), (32, 33, 16), (33, 64, 31), (64, 65, 32), (65, 127, 33),
+                                   (127, 128, 40), (128, 129, 63), (129, 200, 64), (200, 100, 65), (97, 300, 80), (300, 97, 95), (70, 130, 96),
+                                   (140, 70, 97), (100, 90, 127), (260, 150, 128)])
+def test_every_size(N, M, D, kind):
+    check(2, 2, 2, N, M, D, kind, seed=N + M + D)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("D", [20, 64, 128])
+@pytest.mark.parametrize("B,H,Hk,N,M", [(24, 12, 12, 130, 70), (3, 128, 32, 40, 100), (2, 160, 160, 33, 64)])
+def test_many_heads(B, H, Hk, N, M, D, kind):
+    check(B, H, Hk, N, M, D, kind, seed=D, table=some_table(H, 16), two_sided=True, max_distance=40)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("H,Hk,N,M,D", [(8, 8, 1, 257, 64), (16, 4, 1, 1000, 128), (16, 2, 4, 3001, 128), (40, 1, 1, 700, 96), (35, 1, 3, 129, 24), (6, 3, 5, 4097, 32),
+                                        (1, 1, 1, 20000, 80), (64, 1, 2, 300, 128), (4, 4, 70, 5000, 48)])
+def test_few_rows_against_many_keys(H, Hk, N, M, D, kind):
+    gen = torch.Generator().manual_seed(M)
+    lens = torch.randint(N, M + 1, (3,), generator=gen, dtype=torch.int32).cuda()
+    lens[0] = M
+    check(3, H, Hk, N, M, D, kind, seed=N, table=some_table(H, 32), two_sided=False, causal=True, offset=lens - N, col_len=lens)
+    check(3, H, Hk, N, M, D, kind, seed=N, cap=5.0)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("size", [0.01, 6.0, 40.0])
+def test_flat_and_decided_rows(kind, size):
+    check(2, 3, 1, 150, 333, 64, kind, size=size)
+    check(2, 3, 1, 150, 333, 64, kind, size=size, cap=20.0)
+
+
+# ---------------------------------------------------------------- bias
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("buckets,max_distance,two_sided", [(32, 128, True), (32, 128, False), (2, 2, False), (4, 2, True), (3, 100, False), (128, 4096, False),
+                                                            (256, 300, True), (256, 1 << 24, False), (16, 50, True)])
+def test_bias_rules(buckets, max_distance, two_sided, kind):
+    rule = dict(max_distance=max_distance, two_sided=two_sided)
+    check(2, 2, 1, 300, 270, 40, kind, table=some_table(2, buckets), **rule)
+    check(1, 2, 2, 140, 520, 128, kind, table=some_table(2, buckets, kind=kind), offset=37, causal=True, **rule)
+    check(2, 4, 2, 2, 900, 33, kind, table=some_table(4, buckets), offset=torch.tensor([-400, 1000], dtype=torch.int32, device="cuda"), **rule)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("offset", [(1 << 62) - 1, 1 - (1 << 62), 1 << 31, -(1 << 31), 5000, -5000])
+def test_bias_at_far_offsets(offset, kind):
+    check(1, 2, 1, 70, 100, 16, kind, table=some_table(2, 32), offset=offset)
+    check(1, 2, 1, 70, 100, 16, kind, table=some_table(2, 32), offset=offset, causal=True)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("low", [-INF, -1.1e30, torch.finfo(torch.float32).min])
+@pytest.mark.parametrize("N,M", [(200, 170), (2, 300)])
+def test_forbidden_distances(N, M, low, kind):
+    """Entries that forbid their cells: a few of them, those of a band, all of them."""
+    for forbidden in ([3], list(range(8)), list(range(8, 32)), list(range(32))):
+        table = some_table(2, 32).clone()
+        table[0, forbidden] = low
+        check(1, 2, 1, N, M, 32, kind, table=table)
+
+
+def test_bias_without_its_gradient():
+    check(2, 2, 1, 200, 300, 64, "bf16", table=some_table(2, 32), want_dtable=False)
+
+
+# ---------------------------------------------------------------- masks
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("N,M", [(150, 150), (200, 300), (300, 200), (3, 400), (129, 1)])
+def test_causal_masks(N, M, kind):
+    own = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    check(1, 2, 1, N, M, 32, kind, causal=True)
+    check(1, 2, 1, N, M, 32, kind, causal=True, offset=M - N, table=some_table(2, 16), max_distance=30, two_sided=False)
+    check(4, 1, 1, N, M, 32, kind, causal=True, offset=own(-N, 0, M, -7))
+    check(1, 2, 2, N, M, 32, kind, causal=True, prefix=M // 3, table=some_table(2, 16), max_distance=30)
+    check(4, 1, 1, N, M, 32, kind, causal=True, prefix=own(0, M // 2, 10 * M, -5), offset=own(-20, 3, -N, 5))
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("N,M", [(150, 130), (300, 200), (3, 400)])
+def test_lengths(N, M, kind):
+    own = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    rows, cols = own(N, 0, 1, N - 1, 2 * N, -3), own(M - 1, M, 0, 1, 32, 64)
+    check(6, 2, 1, N, M, 40, kind, row_len=rows, col_len=cols, table=some_table(2, 32))
+    check(6, 2, 1, N, M, 40, kind, row_len=rows, col_len=cols, causal=True, offset=3)
+    check(6, 2, 2, N, M, 40, kind, col_len=cols, cap=4.0)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("N,D", [(200, 32), (1500, 64), (40, 128)])
+def test_documents(N, D, causal, kind):
+    gen = torch.Generator().manual_seed(N)
+    packed = torch.sort(torch.randint(0, 5, (2, N), generator=gen, dtype=torch.int32), 1)[0]
+    packed[:, N - 13:] = -1
+    packed[1, :N // 2] = 77
+    for document in (packed.cuda(), torch.randint(-1, 4, (2, N), generator=gen, dtype=torch.int32).cuda()):  # (packed, and strewn about)
+        check(2, 2, 1, N, N, D, kind, causal=causal, row_document=document, col_document=document, table=some_table(2, 32))
+    other = torch.randint(2, 7, (2, N + 30), generator=gen, dtype=torch.int32).cuda()  # (rows of documents without keys, keys without rows)
+    check(2, 2, 2, N, N + 30, D, kind, causal=causal, row_document=document, col_document=other, want_dtable=False)
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_documents_of_a_long_sequence(causal):
+    """More tiles than are looked through at once, whole stretches of them without a key that counts."""
+    N, M = 260, 256 * 64 * 2 + 100
+    rows = torch.full((1, N), 5, dtype=torch.int32, device="cuda")
+    rows[:, 130:] = 9
+    cols = torch.full((1, M), 3, dtype=torch.int32, device="cuda")
+    cols[:, 100:120], cols[:, 256 * 64 - 5:256 * 64 + 3], cols[:, -40:] = 5, 9, 9
+    for H in (1, 128):
+        check(1, H, 1, N, M, 16, "bf16", causal=causal, offset=M, row_document=rows, col_document=cols)
+        check(1, H, 1, M, N, 16, "bf16", causal=causal, offset=M, row_document=cols, col_document=rows)
+
+
+def test_a_document_mask_with_lengths_prefix_and_offsets():
+    gen = torch.Generator().manual_seed(3)
+    own = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    document = torch.randint(-1, 3, (3, 210), generator=gen, dtype=torch.int32).cuda()
+    for kind in sorted(TYPES):
+        check(3, 4, 2, 210, 210, 72, kind, causal=True, prefix=own(40, 0, 210), offset=own(0, -3, 9), row_len=own(210, 100, 0), col_len=own(190, 210, 50),
+              row_document=document, col_document=document, table=some_table(4, 32), cap=6.0)
+
+
+# ---------------------------------------------------------------- strides, empties, far offsets in memory
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("D", [5, 40, 128])
+def test_strides(D, kind):
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    B, H, N, M = 2, 4, 75, 90
+    # rows that begin at odd elements, the heads outside
+    odd = lambda h, n: values((B, h, n, D + 3), kind, gen)[..., 1:D + 1]  # noqa: E731
+    check_these(odd(H, N), odd(2, M), odd(2, M), odd(H, N), table=some_table(H, 16))
+    # features apart, positions next to each other
+    turned = lambda h, n: values((B, h, D, n), kind, gen).transpose(2, 3)  # noqa: E731
+    check_these(turned(H, N), turned(2, M), turned(2, M), turned(H, N))
+    # one set of keys for all sequences and heads, one query for all rows, a gradient that is the same everywhere
+    one = values((1, 1, M, D), kind, gen).expand(B, H, M, D)
+    check_these(values((B, 1, 1, D), kind, gen).expand(B, H, N, D), one, one, values((1, 1, 1, 1), kind, gen).expand(B, H, N, D))
+    # q, k, v as one projection leaves them
+    qkv = values((B, N, 3, H, D), kind, gen)
+    check_these(*[qkv[:, :, x].transpose(1, 2) for x in range(3)], values((B, N, H, D), kind, gen).transpose(1, 2), causal=True)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("N", [3, 300])
+def test_outputs_in_the_memory_that_is_given(N, kind):
+    (q, k, v, dout), gen = problem(2, 4, 2, N, 100, 20, kind)
+    table = some_table(4, 16)
+    room = lambda like: torch.full((*like.shape[:2], like.shape[2] + 1, like.shape[3] + 5), 7.0, dtype=like.dtype, device="cuda")  # noqa: E731
+    rooms = [room(x) for x in (q, q, k, v)]
+    out, dq, dk, dv = (r[:, :, :-1, 3:-2] for r in rooms)
+    lse, dt = torch.empty((2, 4, N), device="cuda"), torch.empty((4, 16), device="cuda")
+    got = pkg.sdtw_attention_forward(q, k, v, table, out=out, lse=lse)
+    assert got[0] is out and got[1] is lse
+    back = pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, dq=dq, dk=dk, dv=dv, dtable=dt)
+    assert back[0] is dq and back[1] is dk and back[2] is dv and back[3] is dt
+    want = reference(q, k, v, dout, table)
+    compare({"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv, "dtable": dt}, want)
+    for r in rooms:
+        r[:, :, :-1, 3:-2] = 7.0
+        assert (r == 7.0).all()
+
+
+def test_empty_problems():
+    q = torch.ones((2, 4, 3, 8), device="cuda")
+    none = torch.ones((2, 2, 0, 8), device="cuda")
+    table = some_table(4, 16)
+    out, lse = pkg.sdtw_attention_forward(q, none, none, table)
+    assert (out == 0).all() and (lse == -INF).all()
+    dq, dk, dv, dt = pkg.sdtw_attention_backward(q, none, none, out, lse, q, table)
+    assert (dq == 0).all() and dk.shape == none.shape and dv.shape == none.shape and (dt == 0).all()
+    k = torch.ones((2, 2, 5, 8), device="cuda")
+    out, lse = pkg.sdtw_attention_forward(q[:, :, :0], k, k, table)
+    assert out.shape == (2, 4, 0, 8) and lse.shape == (2, 4, 0)
+    dq, dk, dv, dt = pkg.sdtw_attention_backward(q[:, :, :0], k, k, out, lse, out, table)
+    assert dq.shape == (2, 4, 0, 8) and (dk == 0).all() and (dv == 0).all() and (dt == 0).all()
+    out, lse = pkg.sdtw_attention_forward(q[:0], k[:0], k[:0], table)
+    dq, dk, dv, dt = pkg.sdtw_attention_backward(q[:0], k[:0], k[:0], out, lse, out, table)
+    assert dq.shape == (0, 4, 3, 8) and (dt == 0).all()
+    out, lse = pkg.sdtw_attention_forward(q[:, :0], k, k)
+    dq, dk, dv, dt = pkg.sdtw_attention_backward(q[:, :0], k, k, out, lse, out)
+    assert dq.shape == (2, 0, 3, 8) and (dk == 0).all() and (dv == 0).all() and dt is None
+
+
+@pytest.mark.parametrize("N", [2, 300])
+def test_caches_beyond_32_bit_offsets(N):
+    """Rows of a cache 2^20 elements apart: the last ones lie more than 2^31 elements in."""
+    M, D, B = 1100, 32, 2
+    room = torch.zeros((B * M + 1) << 20, dtype=torch.bfloat16, device="cuda")
+    cache = torch.as_strided(room, (B, 1, M, D), (M << 20, 0, 1 << 20, 1))
+    (q, k, v, dout), _ = problem(B, 2, 1, N, M, D, "bf16")
+    cache.copy_(k)
+    check_these(q, cache, v, dout, causal=True, offset=M - N, table=some_table(2, 32))
+    out, lse = pkg.sdtw_attention_forward(q, k, v)
+    big = torch.as_strided(room, (B, 1, M, D), (M << 20, 0, 1 << 20, 1))
+    dq, dk, dv, _ = pkg.sdtw_attention_backward(q, k, v, out, lse, dout, dk=big)
+    want = reference(q, k, v, dout)
+    compare({"dk": big}, {"dk": want["dk"]})
+
+
+# ---------------------------------------------------------------- what is not a number
+
+@pytest.mark.parametrize("N", [2, 130])
+def test_nan_and_infinity_reach_their_rows(N):
+    (q, k, v, dout), _ = problem(1, 2, 2, N, 200, 16, "f32")
+    q = q.clone()
+    q[0, 0, 1, 3] = NAN
+    out, lse = pkg.sdtw_attention_forward(q, k, v)
+    assert torch.isnan(out[0, 0, 1]).all() and torch.isnan(lse[0, 0, 1])
+    keep = torch.ones((2, N), dtype=torch.bool, device="cuda")
+    keep[0, 1] = False
+    assert torch.isfinite(out[0][keep]).all()
+    v = v.clone()
+    v[0, 1, 7, 2] = INF
+    out, _ = pkg.sdtw_attention_forward(q, k, v)
+    assert not torch.isfinite(out[0, 1, :, 2]).any() and torch.isfinite(out[0, 1, :, 3]).all()
+
+
+# ---------------------------------------------------------------- gradients against differences
+
+@pytest.mark.parametrize("more", [dict(), dict(cap=3.0), dict(causal=True, prefix=5)])
+def test_gradients_against_differences(more):
+    """Of sum(out * dout), by central differences of the plain forward pass in 64 bits: with steps of 1e-5 they are good to about 1e-9."""
+    B, H, Hk, N, M, D = 1, 2, 1, 9, 11, 6
+    (q, k, v, dout), gen = problem(B, H, Hk, N, M, D, "f32")
+    table = some_table(H, 8)
+    rule = dict(max_distance=6, two_sided=True)
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table, **rule, **more)
+    got = dict(zip(("q", "k", "v", "table"), pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, **rule, **more)))
+    bars = reference(q, k, v, dout, table, **rule, **more)
+
+    def loss(x):
+        z = x["q"] @ x["k"].repeat_interleave(H // Hk, 1).transpose(2, 3) * D ** -0.5
+        if more.get("cap"):
+            z = more["cap"] * torch.tanh(z / more["cap"])
+        z = z + x["table"][:, bucket_matrix(N, M, 8, 6, True, 0)]
+        z = z.masked_fill(~visible(N, M, 0, **more), -INF)
+        return float((torch.softmax(z, 3) @ x["v"].repeat_interleave(H // Hk, 1) * dout.double()).sum())
+    at = {"q": q.double(), "k": k.double(), "v": v.double(), "table": table.double()}
+    for name, g in got.items():
+        bar = bars["d" + name][1].reshape(-1)
+        for e in range(0, g.numel(), 3):
+            ends = []
+            for step in (1e-5, -1e-5):
+                moved = at[name].clone().contiguous()
+                moved.view(-1)[e] += step
+                ends.append(loss({**at, name: moved}))
+            assert abs(float(g.reshape(-1)[e]) - (ends[0] - ends[1]) / 2e-5) <= float(bar[e]) + 1e-8, (name, e)
+
+
+# ---------------------------------------------------------------- streams, graphs, bits
+
+def pair(q, k, v, dout, table, **more):
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table, **more)
+    return (out, lse, *pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, **more))
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("N,M", [(400, 500), (3, 3000)])
+def test_the_same_inputs_give_the_same_bits(N, M, kind):
+    (q, k, v, dout), _ = problem(2, 4, 2, N, M, 64, kind)
+    table = some_table(4, 32)
+    first = pair(q, k, v, dout, table, two_sided=False)
+    for _ in range(3):
+        for a, b in zip(first, pair(q, k, v, dout, table, two_sided=False)):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,M", [(200, 300), (2, 2000)])
+def test_attention_in_a_graph(N, M):
+    """Captured once, replayed on other inputs, with eager calls of the same tensors and others between the replays."""
+    (q, k, v, dout), gen = problem(2, 4, 2, N, M, 32, "bf16")
+    table = some_table(4, 32).clone()
+    lens = torch.tensor([M, M // 2], dtype=torch.int32, device="cuda")
+    document = torch.zeros((2, N), dtype=torch.int32, device="cuda"), torch.zeros((2, M), dtype=torch.int32, device="cuda")
+    more = dict(causal=True, offset=lens - N, col_len=lens, row_document=document[0], col_document=document[1])
+    pair(q, k, v, dout, table, **more)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = pair(q, k, v, dout, table, **more)
+    for step in range(4):
+        for x in (q, k, v, dout, table):
+            x.copy_(torch.randn(x.shape, generator=gen, device="cuda"))
+        lens[1] = M // 2 + 17 * step
+        more["offset"].copy_(lens - N)
+        document[1][:, : 5 * step] = -1
+        graph.replay()
+        for a, b in zip(got, pair(q, k, v, dout, table, **more)):
+            assert torch.equal(a, b), step
+        torch.cuda.synchronize()
+
+
+def test_attention_on_the_stream_it_is_given():
+    (q, k, v, dout), _ = problem(2, 4, 2, 3, 5000, 64, "bf16")
+    table = some_table(4, 32)
+    want = pair(q, k, v, dout, table)
+    torch.cuda.synchronize()
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    busy = torch.randn((4096, 4096), device="cuda")
+    late = torch.zeros_like(q)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            busy = busy @ busy * 1e-3
+        late.copy_(q)  # the call has to come behind this
+    with torch.cuda.stream(other):  # the current stream is another one
+        out, lse = pkg.sdtw_attention_forward(late, k, v, table, stream=side.cuda_stream)
+        got = pkg.sdtw_attention_backward(late, k, v, out, lse, dout, table, stream=side.cuda_stream)
+    side.synchronize()
+    for a, b in zip(want, (out, lse, *got)):
+        assert torch.equal(a, b)
+
+
+def test_calls_side_by_side():
+    """Two calls on two streams, each with memory of its own, many times over."""
+    one, _ = problem(2, 4, 2, 2, 4000, 64, "f16")
+    two, _ = problem(2, 4, 2, 300, 200, 64, "f16", seed=1)
+    table = some_table(4, 32)
+    want = [pair(*x, table) for x in (one, two)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for n, x in enumerate((one, two)):
+            with torch.cuda.stream(streams[n]):
+                got[n].append(pair(*x, table))
+    torch.cuda.synchronize()
+    for n in range(2):
+        for each in got[n]:
+            for a, b in zip(each, want[n]):
+                assert torch.equal(a, b)
+
+
+# ---------------------------------------------------------------- refusals
+
+def test_refusals_of_the_binding():
+    (q, k, v, dout), _ = problem(2, 4, 2, 6, 7, 8, "bf16")
+    table = some_table(4, 16)
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table)
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")  # noqa: E731
+    bad = [
+        dict(q=q[0]), dict(q=q.cpu()), dict(q=q.float()), dict(k=k[:, :, :, :4]), dict(k=k[:1]), dict(v=v[:, :, :5]), dict(v=v.half()), dict(k=k.cpu()),
+        dict(q=q[:, :3]), dict(table=table[:3]), dict(table=table[0]), dict(table=table.cpu()), dict(table=table.double()), dict(table=table[:, :0]),
+        dict(offset=0.5), dict(offset=1 << 64), dict(offset=i32(3)), dict(offset=i32(2).long()), dict(prefix=3), dict(prefix=i32(2)),
+        dict(row_len=i32(3)), dict(col_len=i32(2).float()), dict(row_document=i32(2, 6)), dict(col_document=i32(2, 7)),
+        dict(row_document=i32(2, 7), col_document=i32(2, 7)), dict(row_document=i32(2, 12)[:, ::2], col_document=i32(2, 7)),
+        dict(out=torch.empty_like(out)[:, :, :5]), dict(out=torch.empty_like(out).float()), dict(lse=lse[:1]), dict(lse=lse.double()),
+        dict(max_distance=1 << 40), dict(max_distance=2.5),
+    ]
+    for kw in bad:
+        a = {"q": q, "k": k, "v": v, "table": table, **kw}
+        with pytest.raises(ValueError):
+            pkg.sdtw_attention_forward(a.pop("q"), a.pop("k"), a.pop("v"), a.pop("table"), **a)
+    overlapping = torch.empty(1, dtype=q.dtype, device="cuda").expand(q.shape)
+    apart = torch.empty((2, 4, 8, 6), dtype=q.dtype, device="cuda").transpose(2, 3)
+    wrong = [dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(cap=-1.0), dict(cap=NAN), dict(cap=INF), dict(cap=1e-44),
+             dict(max_distance=4), dict(offset=1 << 62), dict(prefix=-1, causal=True), dict(out=overlapping), dict(out=apart)]
+    for kw in wrong:
+        with pytest.raises(pkg.SdtwError):
+            pkg.sdtw_attention_forward(q, k, v, table, **kw)
+    wide = torch.zeros((1, 1, 4, 129), device="cuda")
+    with pytest.raises(pkg.SdtwError):
+        pkg.sdtw_attention_forward(wide, wide, wide)
+    for kw in (dict(dout=dout[:, :, :5]), dict(dout=dout.float()), dict(out=out[:1]), dict(lse=lse[:, :3]), dict(lse=lse.half()), dict(dq=k),
+               dict(dk=torch.empty_like(k).float()), dict(dtable=table[:, :3])):
+        a = {"out": out, "lse": lse, "dout": dout, **kw}
+        with pytest.raises(ValueError):
+            pkg.sdtw_attention_backward(q, k, v, a.pop("out"), a.pop("lse"), a.pop("dout"), table, **a)
+    for kw in (dict(dq=overlapping), dict(dk=torch.empty(1, dtype=q.dtype, device="cuda").expand(k.shape))):
+        with pytest.raises(pkg.SdtwError):
+            pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, **kw)
+    small = pkg.Workspace(256)
+    small.nbytes = 100
+    with pytest.raises(pkg.SdtwError):
+        pkg.sdtw_attention_backward(q, k, v, out, lse, dout, table, workspace=small)
+
+
+def test_attention_is_the_chain_of_the_operators_that_were_there():
+    """Products, the bias on planes, a softmax and a product, as a model without this call strings them together."""
+    (q, k, v, _), _ = problem(2, 3, 3, 130, 170, 32, "f32")
+    table = some_table(3, 32)
+    lens = torch.tensor([170, 60], dtype=torch.int32, device="cuda")
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table, col_len=lens)
+    scores = pkg.sdtw_position_bias_forward(table, (q @ k.transpose(2, 3).contiguous()) / math.sqrt(32))
+    scores = scores.masked_fill((torch.arange(170, device="cuda") >= lens[:, None])[:, None, None], -INF)
+    # two float32 chains: each within the bars of the module's head, here about 1e-5
+    assert (out - scores.softmax(3) @ v).abs().max() < 2e-5
+    assert (lse - scores.logsumexp(3)).abs().max() < 2e-5
