@@ -9,7 +9,7 @@ using namespace sdtw;
 struct BackwardPlan {
     bool fits;
     int64_t row_tiles, key_tiles;
-    size_t off_table, total;
+    size_t off_table, off_packed, total;
 };
 
 BackwardPlan backward_plan(const sdtw_attention_desc *d)
@@ -21,7 +21,11 @@ BackwardPlan backward_plan(const sdtw_attention_desc *d)
              attention_grid_ok((int64_t)d->B * d->Hk * std::max<int64_t>(1, P.key_tiles)) && attention_grid_ok((int64_t)d->H * d->buckets);
     if (!P.fits) return P;
     P.off_table = align_up((size_t)d->B * d->H * d->N * sizeof(float), 256);
-    P.total = std::max<size_t>(256, P.off_table + align_up((size_t)d->H * d->buckets * d->B * P.row_tiles * sizeof(float), 256));
+    P.off_packed = P.off_table + align_up((size_t)d->H * d->buckets * d->B * P.row_tiles * sizeof(float), 256);
+    P.total = P.off_packed;
+    for (const auto *stride : {&d->q_stride, &d->out_stride, &d->dout_stride}) P.total += packed_bytes(d, *stride, d->H, d->N);
+    for (const auto *stride : {&d->k_stride, &d->v_stride}) P.total += packed_bytes(d, *stride, d->Hk, d->M);
+    P.total = std::max<size_t>(256, P.total);
     return P;
 }
 
@@ -73,26 +77,42 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
     p.delta = static_cast<float *>(workspace);
     p.table_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.off_table);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    char *room = static_cast<char *>(workspace) + P.off_packed;
+    const void *packed_out = p.out;
+    if (rows) {
+        pack(desc, p.q, p.q_stride, desc->H, desc->N, room, st);
+        pack(desc, p.dout, p.dout_stride, desc->H, desc->N, room, st);
+        if (!dtable) pack(desc, packed_out, p.out_stride, desc->H, desc->N, room, st);
+    }
+    p.out = const_cast<void *>(packed_out);
+    if (keys) {
+        pack(desc, p.k, p.k_stride, desc->Hk, desc->M, room, st);
+        pack(desc, p.v, p.v_stride, desc->Hk, desc->M, room, st);
+    }
     with_shape(desc->type, desc->D, [&](auto t, auto features) {
         using T = decltype(t);
         constexpr int DP = decltype(features)::value;
-        const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
-        if (rows) {
-            ProfScope ps("attention_rows_gradient", st);
-            const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
-            if (dtable) {
-                p.table_columns = 32;
-                auto need = [&] { return bytes + (size_t)4 * p.buckets * p.table_columns * sizeof(float); };
-                while (need() + 1024 > kLdsBytes) p.table_columns /= 2;
-                attention_rows_gradient_kernel<T, DP, true><<<grid, 256, need(), st>>>(p, rule);
-            } else {
-                attention_rows_gradient_kernel<T, DP, false><<<grid, 256, bytes, st>>>(p, rule);
+        with_variant(desc, lists, [&](auto variant) {
+            constexpr int F = decltype(variant)::value;
+            const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+            if (rows) {
+                ProfScope ps("attention_rows_gradient", st);
+                const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
+                if constexpr ((F & kBias) != 0) {
+                    if (dtable) {
+                        p.table_columns = 32;
+                        auto need = [&] { return bytes + (size_t)4 * p.buckets * p.table_columns * sizeof(float); };
+                        while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
+                        attention_rows_gradient_kernel<T, DP, F, true><<<grid, 256, need(), st>>>(p, rule);
+                    }
+                }
+                if (!dtable) attention_rows_gradient_kernel<T, DP, F, false><<<grid, 256, bytes, st>>>(p, rule);
             }
-        }
-        if (keys) {
-            ProfScope ps("attention_keys_gradient", st);
-            attention_keys_gradient_kernel<T, DP><<<(unsigned)((int64_t)p.B * p.Hk * p.key_tiles), 256, bytes, st>>>(p, rule);
-        }
+            if (keys) {
+                ProfScope ps("attention_keys_gradient", st);
+                attention_keys_gradient_kernel<T, DP, F><<<(unsigned)((int64_t)p.B * p.Hk * p.key_tiles), 256, bytes, st>>>(p, rule);
+            }
+        });
     });
     if (dtable) {
         ProfScope ps("attention_table", st);

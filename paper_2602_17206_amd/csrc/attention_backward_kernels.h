@@ -12,21 +12,29 @@
 
 namespace sdtw {
 
-// 2^(score - lse) with lse in octaves, and 1 - tanh^2 where there is a cap
-__device__ __forceinline__ void scale_scores_keep(Acc &s, Acc &slope, const AttentionParams &p)
-{
-    if (p.cap_out != 0.0f) {
+// Products into scores, in octaves, and 1 - tanh^2 where there may be a cap.
+template <bool CAP> struct CappedScores {
+    Acc slope;
+    __device__ __forceinline__ explicit CappedScores(Acc &s, const AttentionParams &p)
+    {
+        if (p.cap_out != 0.0f) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float t = tanh_fast(s[r] * p.cap_in);
-            s[r] = p.cap_out * t;
-            slope[r] = fmaf(-t, t, 1.0f);
+            for (int r = 0; r < 16; ++r) {
+                const float t = tanh_fast(s[r] * p.cap_in);
+                s[r] = p.cap_out * t;
+                slope[r] = fmaf(-t, t, 1.0f);
+            }
+        } else {
+            s *= p.scale2;
+            slope = Acc{} + 1.0f;
         }
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= p.scale2;
     }
-}
+    __device__ __forceinline__ void apply(Acc &x) const { x *= slope; }
+};
+template <> struct CappedScores<false> {
+    __device__ __forceinline__ explicit CappedScores(Acc &s, const AttentionParams &p) { s *= p.scale2; }
+    __device__ __forceinline__ void apply(Acc &) const {}
+};
 
 // float16 has 30 octaves for numbers that may be of any size (gradients of a mean are small): a column's numbers go into the
 // matrix cores times a power of two of the column's own, chosen from the first of them and made smaller whenever one would not fit.
@@ -82,16 +90,21 @@ struct TableSum {
     }
 };
 
+// Wavefronts on a SIMD that registers are kept for.
+template <typename T, int DP> constexpr int kRowsWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : 2;
+
 // 4 wavefronts of 32 rows each, one head of one sequence.  TABLE: the table's gradient is wanted.  delta comes from the rows' outputs -
 // sum_j p dp = <dout, out> - unless the table's gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals
 // would show the rounding of a 16-bit `out`; so the keys are walked over once more, for delta alone.
-template <typename T, int DP, bool TABLE>
-__global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
+template <typename T, int DP, int F, bool TABLE>
+__global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
+    __shared__ __align__(16) int32_t documents[kKeys];
     char *ktile = lds, *vtile = lds + Shape::bytes(kKeys);
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     int64_t id = neighbours_together();
@@ -99,8 +112,9 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
     id /= p.row_tiles;
     const int h = (int)(id % p.H), b = (int)(id / p.H), hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
-    const int32_t *col_document = p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+    const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
+    WaveBias bias{};
+    if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
     const int table_columns = TABLE ? p.table_columns : 0;
     float *const table_sums = reinterpret_cast<float *>(lds + 2 * Shape::bytes(kKeys) + bias_bytes(4));
     TableSum table{table_sums + wave * p.buckets * table_columns, table_columns, -1, 0.0f};
@@ -111,7 +125,7 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
     const int64_t place = ((int64_t)b * p.H + h) * p.N + i;
     bool valid = i < sight.rows;
     int doc = 0;
-    if (p.row_document && valid) {
+    if (DOCUMENTS && p.row_document && valid) {
         doc = p.row_document[(int64_t)b * p.N + i];
         valid = doc >= 0;
     }
@@ -126,14 +140,14 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
     Column<T, DP> q, dout;
     {
         const Rows<T> x = rows_of<T>(p.q, p.q_stride, b, h), y = rows_of<T>(p.dout, p.dout_stride, b, h);
-        q.load(x.base + i * x.row, x.feature, p.D, valid, half);
-        dout.load(y.base + i * y.row, y.feature, p.D, valid, half);
+        q.load(x.base + i * x.row, p.loaded, valid, half);
+        dout.load(y.base + i * y.row, p.loaded, valid, half);
     }
     float delta = 0.0f;
     if (!TABLE) {
         const Rows<T> x = rows_of<T>(p.out, p.out_stride, b, h);
         Column<T, DP> out;
-        out.load(x.base + i * x.row, x.feature, p.D, valid, half);
+        out.load(x.base + i * x.row, p.loaded, valid, half);
 #pragma unroll
         for (int s = 0; s < Column<T, DP>::kSteps; ++s)
 #pragma unroll
@@ -150,41 +164,31 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
     ColumnScale<T, DP> fit;
-    const Rows<T> k = rows_of<T>(p.k, p.k_stride, b, hk), v = rows_of<T>(p.v, p.v_stride, b, hk);
-    TileWalk walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
+    TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
+    const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
+    ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, thread);
+    vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
 #pragma unroll 1
     for (int pass = TABLE ? 0 : 1; pass < 2; ++pass) {
-        int t = walk.next(0);
-        if (t < walk.tiles) {
-            ks.load(k, p.D, t * kKeys, end, col_document, thread);
-            vs.load(v, p.D, t * kKeys, end, col_document, thread);
-        }
-        while (t < walk.tiles) {
-            __syncthreads();
-            ks.store(ktile, thread);
-            vs.store(vtile, thread);
-            __syncthreads();
-            const int now = t;
-            t = walk.next(t + 1);
+        int now = -1, t = walk.next(0), next_doc = -1;
+        for (;;) {
             if (t < walk.tiles) {
-                ks.load(k, p.D, t * kKeys, end, col_document, thread);
-                vs.load(v, p.D, t * kKeys, end, col_document, thread);
+                ks.load(t * kKeys, end);
+                vs.load(t * kKeys, end);
+                if (DOCUMENTS && thread < kKeys) next_doc = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
             }
-#pragma unroll
-            for (int sub = 0; sub < kKeys / 32; ++sub) {
+#pragma unroll 1
+            for (int sub = 0; now >= 0 && sub < kKeys / 32; ++sub) {
                 const int j0 = now * kKeys + sub * 32;
+                const char *const kt = ktile + Shape::bytes(sub * 32), *const vt = vtile + Shape::bytes(sub * 32);
                 if (j0 >= to) break;
                 bool open = j0 + 32 <= from;
-                int key_doc = -1;
-                if (col_document) {
-                    key_doc = j0 + c < end ? col_document[j0 + c] : -1;
-                    open = open && low == high && __all(key_doc == low);
-                }
-                Acc s = along_features<T, DP>(ktile + Shape::bytes(sub * 32), q, lane), slope;
-                scale_scores_keep(s, slope, p);
-                if (p.buckets) {
-                    bias.look(rule, j0 - (first_row + 31) - sight.offset, lane);
+                if (DOCUMENTS) open = open && low == high && __all(documents[sub * 32 + c] == low);
+                Acc s = along_features<T, DP>(kt, q, lane);
+                const CappedScores<CAP> capped(s, p);
+                if (BIAS) {
+                    bias.look(rule, j0 - base, lane);
                     if (bias.same) {
                         s += bias.one;
                     } else {
@@ -196,16 +200,11 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - lse);
                 if (!open) {
+                    const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents + sub * 32, doc, half);
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (j0 + tile_row(r, half) >= lim) s[r] = 0.0f;
-                    if (col_document) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (__shfl(key_doc, tile_row(r, half)) != doc) s[r] = 0.0f;
-                    }
+                    for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
                 }
-                const Acc dp = along_features<T, DP>(vtile + Shape::bytes(sub * 32), dout, lane);
+                const Acc dp = along_features<T, DP>(vt, dout, lane);
                 if (TABLE && pass == 0) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
@@ -229,10 +228,21 @@ __global__ __launch_bounds__(256, 1) void attention_rows_gradient_kernel(Attenti
                         for (int r = 0; r < 16; ++r) table.turn(lane, at[tile_row(r, 0)], valid ? s[r] : 0.0f);
                     }
                 }
-                if (p.cap_out != 0.0f) s *= slope;
+                capped.apply(s);
                 fit.fit(s, dq);
-                along_rows<T, DP>(dq, ktile + Shape::bytes(sub * 32), Weights<T>(s), lane);
+                along_rows<T, DP>(dq, kt, Weights<T>(s), lane);
             }
+            if (t >= walk.tiles) break;
+            __syncthreads();
+            if (DOCUMENTS) {
+                if (thread < kKeys) documents[thread] = next_doc;
+                __syncthreads();
+            }
+            ks.template store<DOCUMENTS>(ktile, documents, thread);
+            vs.template store<DOCUMENTS>(vtile, documents, thread);
+            __syncthreads();
+            now = t;
+            t = walk.next(t + 1);
         }
         if (TABLE && pass == 0) {
             delta = both_sum(delta);
@@ -270,10 +280,11 @@ __global__ __launch_bounds__(64) void attention_table_kernel(AttentionParams p)
 }
 
 // 4 wavefronts of 32 keys each, of one head of keys of one sequence; the queries of the group's heads go by in tiles of 64.
-template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
+template <typename T, int DP, int F>
+__global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
@@ -286,11 +297,11 @@ __global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(Attenti
     id /= p.key_tiles;
     const int hk = (int)(id % p.Hk), b = (int)(id / p.Hk), G = p.H / p.Hk;
     const Sight sight(p, b);
-    const int32_t *row_document = p.row_document ? p.row_document + (int64_t)b * p.N : nullptr;
+    const int32_t *row_document = DOCUMENTS && p.row_document ? p.row_document + (int64_t)b * p.N : nullptr;
     const int first_key = kt * 128 + wave * 32, j = first_key + c;
     bool valid = sight.rows > 0 && j < sight.limit(sight.rows - 1);  // (the last row sees the most; other keys may hold NaN)
     int doc = 0;
-    if (p.col_document && valid) {
+    if (DOCUMENTS && p.col_document && valid) {
         doc = p.col_document[(int64_t)b * p.M + j];
         valid = doc >= 0;
     }
@@ -299,8 +310,8 @@ __global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(Attenti
     Column<T, DP> k, v;
     {
         const Rows<T> x = rows_of<T>(p.k, p.k_stride, b, hk), y = rows_of<T>(p.v, p.v_stride, b, hk);
-        k.load(x.base + j * x.row, x.feature, p.D, valid, half);
-        v.load(y.base + j * y.row, y.feature, p.D, valid, half);
+        k.load(x.base + j * x.row, p.loaded, valid, half);
+        v.load(y.base + j * y.row, p.loaded, valid, half);
     }
     if (lane == 0) shared[wave][1] = low, shared[wave][2] = high, shared[wave][3] = any;
     __syncthreads();
@@ -314,49 +325,42 @@ __global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(Attenti
     for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
     ColumnScale<T, DP> fit;
     constexpr float kWeight = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;  // p <= 1 (to rounding) into float16's upper octaves
-    TileWalk walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
+    TileWalk<DOCUMENTS> walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> qs, ds;
 #pragma unroll 1
     for (int g = 0; g < G; ++g) {
         const int h = hk * G + g;
         __syncthreads();
-        WaveBias bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
-        const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, h), dout = rows_of<T>(p.dout, p.dout_stride, b, h);
+        WaveBias bias{};
+        if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
         const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
+        qs.begin(rows_of<T>(p.q, p.q_stride, b, h), p.loaded, thread);
+        ds.begin(rows_of<T>(p.dout, p.dout_stride, b, h), p.loaded, thread);
         float next_lse = 0.0f, next_delta = 0.0f;
         int next_doc = -1;
-        auto load = [&](int t) {
-            qs.load(q, p.D, t * kKeys, end, row_document, thread);
-            ds.load(dout, p.D, t * kKeys, end, row_document, thread);
-            if (thread < kKeys) {
-                const int i = t * kKeys + thread;
-                const bool in = i < end;
-                next_doc = in && row_document ? row_document[i] : in ? 0 : -1;
-                const float x = next_doc >= 0 ? lse[i] : -INFINITY;
-                next_lse = x == -INFINITY ? INFINITY : x * kLog2e;
-                next_delta = next_doc >= 0 ? delta[i] : 0.0f;
+        int now = -1, t = walk.next(begin / kKeys);
+        for (;;) {
+            if (t < walk.tiles) {
+                qs.load(t * kKeys, end);
+                ds.load(t * kKeys, end);
+                if (thread < kKeys) {
+                    const int i = t * kKeys + thread;
+                    next_doc = i >= end ? -1 : row_document ? row_document[i] : 0;
+                    const float x = next_doc >= 0 ? lse[i] : -INFINITY;
+                    next_lse = x == -INFINITY ? INFINITY : x * kLog2e;
+                    next_delta = next_doc >= 0 ? delta[i] : 0.0f;
+                }
             }
-        };
-        int t = walk.next(begin / kKeys);
-        if (t < walk.tiles) load(t);
-        while (t < walk.tiles) {
-            __syncthreads();
-            qs.store(qtile, thread);
-            ds.store(dtile, thread);
-            if (thread < kKeys) row_lse[thread] = next_lse, row_delta[thread] = next_delta, row_doc[thread] = next_doc;
-            __syncthreads();
-            const int now = t;
-            t = walk.next(t + 1);
-            if (t < walk.tiles) load(t);
-#pragma unroll
-            for (int sub = 0; sub < kKeys / 32; ++sub) {
+#pragma unroll 1
+            for (int sub = 0; now >= 0 && sub < kKeys / 32; ++sub) {
                 const int i0 = now * kKeys + sub * 32;
+                const char *const qt = qtile + Shape::bytes(sub * 32), *const dt = dtile + Shape::bytes(sub * 32);
                 if (i0 + 32 <= mine || i0 >= end || !any) continue;
                 bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
-                if (row_document) open = open && low == high && __all(row_doc[sub * 32 + c] == low);
-                Acc s = along_features<T, DP>(qtile + Shape::bytes(sub * 32), k, lane), slope;
-                scale_scores_keep(s, slope, p);
-                if (p.buckets) {
+                if (DOCUMENTS) open = open && low == high && __all(row_doc[sub * 32 + c] == low);
+                Acc s = along_features<T, DP>(qt, k, lane);
+                const CappedScores<CAP> capped(s, p);
+                if (BIAS) {
                     bias.look(rule, first_key - (i0 + 31) - sight.offset, lane);
                     if (bias.same) {
                         s += bias.one;
@@ -369,25 +373,35 @@ __global__ __launch_bounds__(256, 1) void attention_keys_gradient_kernel(Attenti
                 const float *at_lse = row_lse + sub * 32 + 4 * half, *at_delta = row_delta + sub * 32 + 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - at_lse[tile_row(r, 0)]);
-                Acc dp = along_features<T, DP>(dtile + Shape::bytes(sub * 32), v, lane);
+                Acc dp = along_features<T, DP>(dt, v, lane);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - at_delta[tile_row(r, 0)]);
                 if (!open) {  // (a key that only rows in no document would see may hold NaN: both are chosen, not multiplied away)
-                    const bool always = j < sight.prefix || !sight.causal;
+                    // rows from `before` on see the key; documents of rows behind the last are negative
+                    const int before = j < sight.prefix || !sight.causal ? -0x40000000 : j - sight.offset;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        bool seen = always || j <= i0 + tile_row(r, half) + sight.offset;
-                        if (row_document) seen = seen && row_doc[sub * 32 + tile_row(r, half)] == doc;
+                        bool seen = tile_row(r, 0) >= before - i0 - 4 * half;
+                        if (DOCUMENTS) seen = seen && row_doc[sub * 32 + 4 * half + tile_row(r, 0)] == doc;
                         s[r] = seen ? s[r] : 0.0f;
                         dp[r] = seen ? dp[r] : 0.0f;
                     }
                 }
-                if (p.cap_out != 0.0f) dp *= slope;
+                capped.apply(dp);
                 if (kWeight != 1.0f) s *= kWeight;
-                along_rows<T, DP>(dv, dtile + Shape::bytes(sub * 32), Weights<T>(s), lane);
+                along_rows<T, DP>(dv, dt, Weights<T>(s), lane);
                 fit.fit(dp, dk);
-                along_rows<T, DP>(dk, qtile + Shape::bytes(sub * 32), Weights<T>(dp), lane);
+                along_rows<T, DP>(dk, qt, Weights<T>(dp), lane);
             }
+            if (t >= walk.tiles) break;
+            __syncthreads();
+            if (thread < kKeys) row_lse[thread] = next_lse, row_delta[thread] = next_delta, row_doc[thread] = next_doc;
+            if (DOCUMENTS) __syncthreads();
+            qs.template store<DOCUMENTS>(qtile, row_doc, thread);
+            ds.template store<DOCUMENTS>(dtile, row_doc, thread);
+            __syncthreads();
+            now = t;
+            t = walk.next(t + 1);
         }
     }
     if (j < p.M) {

@@ -9,7 +9,7 @@ using namespace sdtw;
 struct ForwardPlan {
     bool fits, few;
     int64_t row_tiles, splits, workgroups;
-    size_t total;
+    size_t off_packed, total;
 };
 
 size_t few_rows_lds(const sdtw_attention_desc *d)
@@ -19,12 +19,11 @@ size_t few_rows_lds(const sdtw_attention_desc *d)
            (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 : 0);
 }
 
-ForwardPlan forward_plan(const sdtw_attention_desc *d)
+ForwardPlan split_forward(const sdtw_attention_desc *d)
 {
     ForwardPlan P{};
     P.fits = true;
     P.splits = 1;
-    P.total = 256;
     if (d->B == 0 || d->H == 0 || d->N == 0) return P;
     const int64_t tiles = (d->N + 127) / 128, G = d->H / d->Hk;
     P.few = (int64_t)d->B * d->H * tiles < 256 && few_rows_lds(d) + 2048 <= kLdsBytes;
@@ -40,7 +39,15 @@ ForwardPlan forward_plan(const sdtw_attention_desc *d)
     P.splits = std::max<int64_t>(P.splits, 1);
     P.workgroups = units * P.splits;
     P.fits = attention_grid_ok(P.workgroups) && attention_grid_ok((int64_t)d->B * d->H * d->N);
-    if (P.splits > 1) P.total = align_up((size_t)d->B * d->H * d->N * P.splits * (d->D + 2) * sizeof(float), 256);
+    if (P.splits > 1) P.off_packed = align_up((size_t)d->B * d->H * d->N * P.splits * (d->D + 2) * sizeof(float), 256);
+    return P;
+}
+
+ForwardPlan forward_plan(const sdtw_attention_desc *d)
+{
+    ForwardPlan P = split_forward(d);
+    P.total = std::max<size_t>(256, P.off_packed + packed_bytes(d, d->q_stride, d->H, d->N) + packed_bytes(d, d->k_stride, d->Hk, d->M) +
+                                        packed_bytes(d, d->v_stride, d->Hk, d->M));
     return P;
 }
 
@@ -80,19 +87,24 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
     p.splits = (int32_t)P.splits;
     p.part = static_cast<float *>(workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    char *room = static_cast<char *>(workspace) + P.off_packed;
+    pack(desc, p.q, p.q_stride, desc->H, desc->N, room, st);
+    pack(desc, p.k, p.k_stride, desc->Hk, desc->M, room, st);
+    pack(desc, p.v, p.v_stride, desc->Hk, desc->M, room, st);
     with_shape(desc->type, desc->D, [&](auto t, auto features) {
         using T = decltype(t);
         constexpr int DP = decltype(features)::value;
-        if (!P.few) {
-            ProfScope ps("attention_forward", st);
-            const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
-            attention_forward_kernel<T, DP, 1><<<(unsigned)P.workgroups, 256, bytes, st>>>(p, rule);
-            return;
-        }
-        {
-            ProfScope ps("attention_few_rows", st);
-            attention_few_rows_kernel<T, DP><<<(unsigned)P.workgroups, 256, few_rows_lds(desc), st>>>(p, rule);
-        }
+        with_variant(desc, lists, [&](auto variant) {
+            constexpr int F = decltype(variant)::value;
+            if (P.few) {
+                ProfScope ps("attention_few_rows", st);
+                attention_few_rows_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, few_rows_lds(desc), st>>>(p, rule);
+            } else {
+                ProfScope ps("attention_forward", st);
+                const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+                attention_forward_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, bytes, st>>>(p, rule);
+            }
+        });
         if (P.splits > 1) {
             ProfScope ps("attention_join", st);
             attention_join_kernel<T><<<(unsigned)((int64_t)p.B * p.H * p.N), 128, 0, st>>>(p);

@@ -9,8 +9,11 @@
 
 namespace sdtw {
 
-// A row's running softmax; its two lanes hold the same m and half of l each.
+// A row's running softmax; its two lanes hold the same m and half of l each.  m follows the largest score only where that is ahead by
+// more than 8 octaves: the sums' scale does not matter within float32's range, and rescaling them for every new maximum
+// would cost as much as a tenth of the work.
 template <int DP> struct Running {
+    static constexpr float kAhead = 8.0f;
     float m, l;
     Acc o[DP / 32];
     __device__ __forceinline__ void clear()
@@ -20,14 +23,10 @@ template <int DP> struct Running {
 #pragma unroll
         for (int ft = 0; ft < DP / 32; ++ft) o[ft] = Acc{};
     }
-    // takes scores in, and leaves 2^(s - m) in their place
-    __device__ __forceinline__ void take(Acc &s)
+    // a new largest score
+    __device__ __forceinline__ void raise(float top)
     {
-        float top = s[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
-        top = both_max(top);
-        if (__any(top > m)) {
+        if (__any(top > m + kAhead)) {
             const float to = fmaxf(m, top);
             const float factor = m == to ? 1.0f : exp2_fast(m - to);
             m = to;
@@ -35,25 +34,45 @@ template <int DP> struct Running {
 #pragma unroll
             for (int ft = 0; ft < DP / 32; ++ft) o[ft] *= factor;
         }
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float sum = 0.0f;
+    }
+    // Takes in scores of SUBS * 32 keys and leaves 2^(score - m) in their place.  The scores are s * factor + add.
+    template <int SUBS> __device__ __forceinline__ void take(Acc (&s)[SUBS], float factor, float add)
+    {
+        float top[SUBS];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = exp2_fast(s[r] - ref);
-            sum += s[r];
+        for (int x = 0; x < SUBS; ++x) {
+            top[x] = fmaxf(s[x][0], s[x][1]);
+#pragma unroll
+            for (int r = 2; r < 16; r += 2) top[x] = fmaxf(fmaxf(s[x][r], s[x][r + 1]), top[x]);
         }
-        l += sum;
+        raise(fmaf(both_max(SUBS == 2 ? fmaxf(top[0], top[SUBS - 1]) : top[0]), factor, add));
+        const float from = add - (m == -INFINITY ? 0.0f : m);
+        float sum[2] = {};
+#pragma unroll
+        for (int x = 0; x < SUBS; ++x)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[x][r] = exp2_fast(fmaf(s[x][r], factor, from));
+                sum[r & 1] += s[x][r];
+            }
+        l += sum[0] + sum[1];
     }
 };
 
-// 4 wavefronts of 32 * NT rows each, one head of one sequence.
-template <typename T, int DP, int NT>
-__global__ __launch_bounds__(256, 1) void attention_forward_kernel(AttentionParams p, BucketRule rule)
+// Wavefronts on a SIMD that registers are kept for.
+template <typename T, int DP> constexpr int kForwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 3 : DP <= 64 ? 2 : 1) : DP <= 32 ? 4 : DP <= 64 ? 3 : 2;
+
+// 4 wavefronts of 32 rows each, one head of one sequence.
+template <typename T, int DP, int F>
+__global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr int SUBS = kKeys / 32;
+    constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
+    __shared__ __align__(16) int32_t documents[kKeys];
     char *ktile = lds, *vtile = lds + Shape::bytes(kKeys);
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     int64_t id = neighbours_together();
@@ -61,122 +80,117 @@ __global__ __launch_bounds__(256, 1) void attention_forward_kernel(AttentionPara
     id /= p.row_tiles;
     const int h = (int)(id % p.H), b = (int)(id / p.H), hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
-    const int32_t *col_document = p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+    const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
+    WaveBias bias{};
+    if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
 
-    const int first_row = rt * 128 * NT + wave * 32 * NT;
-    const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, h);
-    Column<T, DP> col[NT];
-    int lim[NT], doc[NT];
-    bool valid[NT];
-    int from = 0x7fffffff, to = 0, low = 0x7fffffff, high = -1;  // limits and documents of the wavefront's rows
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int i = first_row + 32 * n + c;
-        valid[n] = i < sight.rows;
-        doc[n] = 0;
-        if (p.row_document && valid[n]) {
-            doc[n] = p.row_document[(int64_t)b * p.N + i];
-            valid[n] = doc[n] >= 0;
-        }
-        lim[n] = valid[n] ? sight.limit(i) : 0;
-        if (valid[n]) from = min(from, lim[n]), to = max(to, lim[n]), low = min(low, doc[n]), high = max(high, doc[n]);
-        else lim[n] = 0x7fffffff;  // (what such a row computes is not looked at)
-        col[n].load(q.base + i * q.row, q.feature, p.D, valid[n], half);
+    const int first_row = rt * 128 + wave * 32, i = first_row + c;
+    bool valid = i < sight.rows;
+    int doc = 0;
+    if (DOCUMENTS && p.row_document && valid) {
+        doc = p.row_document[(int64_t)b * p.N + i];
+        valid = doc >= 0;
     }
-    from = wave_min_i32(from), to = wave_max_i32(to), low = wave_min_i32(low), high = wave_max_i32(high);
+    int lim = valid ? sight.limit(i) : 0;
+    const int to = wave_max_i32(lim);
+    if (!valid) lim = 0x7fffffff;  // (what such a row computes is not looked at)
+    const int from = wave_min_i32(lim);  // every row sees the keys below it
+    const int low = wave_min_i32(valid ? doc : 0x7fffffff), high = wave_max_i32(valid ? doc : -1);
+    Column<T, DP> col;
+    {
+        const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, h);
+        col.load(q.base + i * q.row, p.loaded, valid, half);
+    }
     if (lane == 0) shared[wave][0] = to, shared[wave][1] = low, shared[wave][2] = high;
     __syncthreads();
     int end = 0, lowest = 0x7fffffff, highest = -1;
     for (int w = 0; w < 4; ++w) end = max(end, shared[w][0]), lowest = min(lowest, shared[w][1]), highest = max(highest, shared[w][2]);
+    end = __builtin_amdgcn_readfirstlane(end);
 
-    Running<DP> run[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) run[n].clear();
-    const Rows<T> k = rows_of<T>(p.k, p.k_stride, b, hk), v = rows_of<T>(p.v, p.v_stride, b, hk);
-    TileWalk walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
+    Running<DP> run;
+    run.clear();
+    TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
-    int t = walk.next(0);
-    if (t < walk.tiles) {
-        ks.load(k, p.D, t * kKeys, end, col_document, thread);
-        vs.load(v, p.D, t * kKeys, end, col_document, thread);
-    }
-    while (t < walk.tiles) {
-        __syncthreads();
-        ks.store(ktile, thread);
-        vs.store(vtile, thread);
-        __syncthreads();
-        const int now = t;
-        t = walk.next(t + 1);
+    ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, thread);
+    vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
+    const float scale2 = p.scale2, cap_out = p.cap_out;
+    const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
+    int now = -1, t = walk.next(0), next_doc = -1;
+    for (;;) {
         if (t < walk.tiles) {
-            ks.load(k, p.D, t * kKeys, end, col_document, thread);
-            vs.load(v, p.D, t * kKeys, end, col_document, thread);
+            ks.load(t * kKeys, end);
+            vs.load(t * kKeys, end);
+            if (DOCUMENTS && thread < kKeys) next_doc = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
         }
+        const int j0 = now * kKeys;
+        if (now >= 0 && j0 < to) {
+            Acc s[SUBS];
 #pragma unroll
-        for (int sub = 0; sub < kKeys / 32; ++sub) {
-            const int j0 = now * kKeys + sub * 32;
-            if (j0 >= to) break;
-            bool open = j0 + 32 <= from;  // every row sees all of these keys
-            int key_doc = -1;
-            if (col_document) {
-                key_doc = j0 + c < end ? col_document[j0 + c] : -1;
-                open = open && low == high && __all(key_doc == low);
-            }
+            for (int x = 0; x < SUBS; ++x) s[x] = along_features<T, DP>(ktile + Shape::bytes(x * 32), col, lane);
+            bool open = j0 + kKeys <= from;
+            if (DOCUMENTS) open = open && low == high && __all(documents[lane] == low);
+            // scores that are products times a number, plus a number?
+            if (open && (!CAP || cap_out == 0.0f) && (!BIAS || bias.far(rule, j0 - base, j0 - base + 94))) {
+                run.take(s, scale2, BIAS ? bias.one : 0.0f);
+            } else {
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                Acc s = along_features<T, DP>(ktile + Shape::bytes(sub * 32), col[n], lane);
-                scale_scores(s, p);
-                if (p.buckets) {
-                    const int i0 = first_row + 32 * n;
-                    bias.look(rule, j0 - (i0 + 31) - sight.offset, lane);
-                    if (bias.same) {
-                        s += bias.one;
-                    } else {
-                        const float *at = bias.diagonal + 31 - c + 4 * half;
+                for (int x = 0; x < SUBS; ++x) {
+                    scale_scores<CAP>(s[x], p);
+                    if (BIAS) {
+                        bias.look(rule, j0 + 32 * x - base, lane);
+                        if (bias.same) {
+                            s[x] += bias.one;
+                        } else {
+                            const float *at = bias.diagonal + 31 - c + 4 * half;
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] += at[tile_row(r, 0)];
+                            for (int r = 0; r < 16; ++r) s[x][r] += at[tile_row(r, 0)];
+                        }
+                    }
+                    if (!open) {
+                        const Seen<DOCUMENTS> seen(lim - j0 - 32 * x - 4 * half, documents + 32 * x, doc, half);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[x][r] = seen.at[r] ? s[x][r] : -INFINITY;
                     }
                 }
-                if (!open) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (j0 + tile_row(r, half) >= lim[n]) s[r] = -INFINITY;
-                    if (col_document) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (__shfl(key_doc, tile_row(r, half)) != doc[n]) s[r] = -INFINITY;
-                    }
-                }
-                run[n].take(s);
-                along_rows<T, DP>(run[n].o, vtile + Shape::bytes(sub * 32), Weights<T>(s), lane);
+                run.take(s, 1.0f, 0.0f);
             }
-        }
-    }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int i = first_row + 32 * n + c;
-        const float total = both_sum(run[n].l);
-        const bool some = valid[n] && total != 0.0f;  // (a NaN is something)
-        if (i >= p.N) continue;
-        const float factor = some ? 1.0f / total : 0.0f;
-        if (!some) {
-#pragma unroll
-            for (int ft = 0; ft < DP / 32; ++ft) run[n].o[ft] = Acc{};
+            for (int x = 0; x < SUBS; ++x) along_rows<T, DP>(run.o, vtile + Shape::bytes(x * 32), Weights<T>(s[x]), lane);
         }
-        store_column<T, DP>(row_of<T>(p.out, p.out_stride, b, h, i), p.D, run[n].o, factor, half);
-        if (half == 0) p.lse[((int64_t)b * p.H + h) * p.N + i] = some ? (run[n].m + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
+        if (t >= walk.tiles) break;
+        __syncthreads();
+        if (DOCUMENTS) {
+            if (thread < kKeys) documents[thread] = next_doc;
+            __syncthreads();
+        }
+        ks.template store<DOCUMENTS>(ktile, documents, thread);
+        vs.template store<DOCUMENTS>(vtile, documents, thread);
+        __syncthreads();
+        now = t;
+        t = walk.next(t + 1);
     }
+    const float total = both_sum(run.l);
+    const bool some = valid && total != 0.0f;  // (a NaN is something)
+    if (i >= p.N) return;
+    if (!some) {
+#pragma unroll
+        for (int ft = 0; ft < DP / 32; ++ft) run.o[ft] = Acc{};
+    }
+    store_column<T, DP>(row_of<T>(p.out, p.out_stride, b, h, i), p.D, run.o, some ? 1.0f / total : 0.0f, half);
+    if (half == 0) p.lse[((int64_t)b * p.H + h) * p.N + i] = some ? (run.m + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
 }
 
 // A few rows against many keys.  The rows of a group of heads that share their keys stand in one wavefront's columns together: row t is
 // query t / G of head t % G of the group.  Each of 4 wavefronts takes every fourth 32 keys of the workgroup's share, on its own; then
 // they are joined in LDS, and the workgroups of a row by attention_join_kernel.
-template <typename T, int DP>
-__global__ __launch_bounds__(256, 1) void attention_few_rows_kernel(AttentionParams p, BucketRule rule)
+template <typename T, int DP, int F>
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_rows_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(16) char lds[];
     __shared__ float ref[4][32], tot[4][32];
+    __shared__ __align__(16) int32_t documents[4][32];
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     char *ktile = lds + wave * 2 * Shape::bytes(32), *vtile = ktile + Shape::bytes(32);
     int64_t id = neighbours_together();
@@ -186,11 +200,11 @@ __global__ __launch_bounds__(256, 1) void attention_few_rows_kernel(AttentionPar
     id /= p.row_tiles;
     const int hk = (int)(id % p.Hk), b = (int)(id / p.Hk), G = p.H / p.Hk;
     const Sight sight(p, b);
-    const int32_t *col_document = p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
+    const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     const int row = rt * 32 + c, i = row / G, h = hk * G + row % G;
     bool valid = i < sight.rows;
     int doc = 0;
-    if (p.row_document && valid) {
+    if (DOCUMENTS && p.row_document && valid) {
         doc = p.row_document[(int64_t)b * p.N + i];
         valid = doc >= 0;
     }
@@ -201,13 +215,13 @@ __global__ __launch_bounds__(256, 1) void attention_few_rows_kernel(AttentionPar
     Column<T, DP> col;
     {
         const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, valid ? h : 0);
-        col.load(q.base + (valid ? i : 0) * q.row, q.feature, p.D, valid, half);
+        col.load(q.base + (valid ? i : 0) * q.row, p.loaded, valid, half);
     }
     // the entries of every head that is here, and the rule's starts
     float *values = reinterpret_cast<float *>(lds + 8 * Shape::bytes(32));
     int32_t *starts = reinterpret_cast<int32_t *>(values + min(G, 32) * p.buckets);
     const int first_head = G <= 32 ? 0 : rt * 32 % G;  // (the heads of 32 rows of a larger group follow each other, round its end)
-    if (p.buckets) {
+    if (BIAS) {
         for (int u = thread; u < min(G, 32) * p.buckets; u += 256) {
             const int head = hk * G + (first_head + u / p.buckets) % G;
             values[u] = octaves_of_entry(load_typed(p.table, head * p.table_stride[0] + u % p.buckets * p.table_stride[1], p.table_type));
@@ -220,28 +234,32 @@ __global__ __launch_bounds__(256, 1) void attention_few_rows_kernel(AttentionPar
     // the workgroup's tiles of 128 keys
     const int tiles = (to + 127) / 128, each = (tiles + p.splits - 1) / p.splits;
     const int begin = min(tiles, split * each), end = min(tiles, begin + each);
-    const Rows<T> k = rows_of<T>(p.k, p.k_stride, b, hk), v = rows_of<T>(p.v, p.v_stride, b, hk);
     Running<DP> run;
     run.clear();
     Stage<T, DP, 32, 64> ks, vs;
-    if (begin < end) {
-        ks.load(k, p.D, begin * 128 + wave * 32, to, col_document, lane);
-        vs.load(v, p.D, begin * 128 + wave * 32, to, col_document, lane);
-    }
-    for (int t = begin; t < end; ++t) {
+    ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, lane);
+    vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, lane);
+    int next_doc = -1;
+    for (int t = begin - 1; t < end; ++t) {
         const int j0 = t * 128 + wave * 32;
-        wavefront_order();
-        ks.store(ktile, lane);
-        vs.store(vtile, lane);
-        wavefront_order();
-        if (t + 1 < end) {
-            ks.load(k, p.D, j0 + 128, to, col_document, lane);
-            vs.load(v, p.D, j0 + 128, to, col_document, lane);
+        if (t >= begin) {
+            wavefront_order();
+            if (DOCUMENTS && half == 0) documents[wave][c] = next_doc;
+            wavefront_order();
+            ks.template store<DOCUMENTS>(ktile, documents[wave], lane);
+            vs.template store<DOCUMENTS>(vtile, documents[wave], lane);
+            wavefront_order();
         }
-        if (j0 >= to) continue;
-        Acc s = along_features<T, DP>(ktile, col, lane);
-        scale_scores(s, p);
-        if (p.buckets) {
+        if (t + 1 < end && j0 + 128 < to) {
+            ks.load(j0 + 128, to);
+            vs.load(j0 + 128, to);
+            if (DOCUMENTS) next_doc = j0 + 128 + c >= to ? -1 : col_document ? col_document[j0 + 128 + c] : 0;
+        }
+        if (t < begin || j0 >= to) continue;
+        Acc scores[1] = {along_features<T, DP>(ktile, col, lane)};
+        Acc &s = scores[0];
+        scale_scores<CAP>(s, p);
+        if (BIAS) {
             const int near = j0 - i - sight.offset;
             const int u0 = rule.bucket(near, starts), u1 = rule.bucket(near + 31, starts);
             if (__all(u0 == u1 && (near > 0 || near + 31 <= 0))) {
@@ -251,18 +269,12 @@ __global__ __launch_bounds__(256, 1) void attention_few_rows_kernel(AttentionPar
                 for (int r = 0; r < 16; ++r) s[r] += mine[rule.bucket(near + tile_row(r, half), starts)];
             }
         }
-        if (j0 + 32 > from) {
+        if (DOCUMENTS || j0 + 32 > from) {
+            const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents[wave], doc, half);
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (j0 + tile_row(r, half) >= lim) s[r] = -INFINITY;
+            for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : -INFINITY;
         }
-        if (col_document) {
-            const int key_doc = j0 + c < to ? col_document[j0 + c] : -1;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (__shfl(key_doc, tile_row(r, half)) != doc) s[r] = -INFINITY;
-        }
-        run.take(s);
+        run.take(scores, 1.0f, 0.0f);
         along_rows<T, DP>(run.o, vtile, Weights<T>(s), lane);
     }
     const float total = both_sum(run.l);

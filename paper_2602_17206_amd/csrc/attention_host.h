@@ -20,6 +20,13 @@ inline bool attention_grid_ok(int64_t workgroups) { return workgroups <= 0xfffff
 constexpr int kMaxFeatures = 128;
 constexpr size_t kLdsBytes = 160 << 10;
 
+// D rounded up to whole 16-byte chunks
+inline int loaded_features(const sdtw_attention_desc *d)
+{
+    const int W = d->type == SDTW_TYPE_F32 ? 4 : 8;
+    return (d->D + W - 1) / W * W;
+}
+
 inline sdtw_bias_desc bias_of(const sdtw_attention_desc *d)
 {
     sdtw_bias_desc b{};
@@ -86,6 +93,7 @@ inline AttentionParams attention_params(const sdtw_attention_desc *d, const sdtw
 {
     AttentionParams p{};
     p.B = d->B; p.H = d->H; p.Hk = d->Hk; p.N = d->N; p.M = d->M; p.D = d->D;
+    p.loaded = loaded_features(d);
     p.buckets = d->buckets; p.table_type = d->table_type; p.causal = d->causal;
     p.offset = (int32_t)std::min<int64_t>(std::max<int64_t>(d->offset, -(1 << 29)), 1 << 29);
     p.prefix = (int32_t)std::min<int64_t>(d->prefix, 1 << 29);
@@ -106,8 +114,52 @@ inline AttentionParams attention_params(const sdtw_attention_desc *d, const sdtw
     return p;
 }
 
+// Inputs whose features are apart or do not fill 16-byte chunks, or whose rows are 2^22 elements and more apart (64 of them are a tile, whose
+// bytes are counted in 31 bits): the kernels read a packed copy of them, [B, heads, rows, loaded].
+inline bool packed(const sdtw_attention_desc *d, const int64_t (&stride)[4])
+{
+    return d->D != loaded_features(d) || (stride[3] != 1 && d->D > 1) || stride[2] >= (int64_t)1 << 22;
+}
+inline size_t packed_bytes(const sdtw_attention_desc *d, const int64_t (&stride)[4], int64_t heads, int64_t rows)
+{
+    return packed(d, stride) ? align_up((size_t)d->B * heads * rows * loaded_features(d) * (d->type == SDTW_TYPE_F32 ? 4 : 2), 256) : 0;
+}
+
+// Launches the copy where one is needed; `x` and its strides become those of the copy, `room` moves on behind it.
+inline void pack(const sdtw_attention_desc *d, const void *&x, int64_t (&stride)[4], int64_t heads, int64_t rows, char *&room, hipStream_t st)
+{
+    const size_t bytes = packed_bytes(d, stride, heads, rows);
+    if (bytes == 0) return;
+    const int64_t loaded = loaded_features(d), vectors = (int64_t)d->B * heads * rows * loaded / (d->type == SDTW_TYPE_F32 ? 4 : 8);
+    ProfScope ps("attention_pack", st);
+    PackParams p{};
+    p.in = x;
+    p.out = room;
+    for (int i = 0; i < 4; ++i) p.stride[i] = stride[i];
+    p.heads = heads; p.rows = rows; p.D = d->D; p.loaded = (int32_t)loaded; p.vectors = vectors;
+    const unsigned grid = (unsigned)std::min<int64_t>((vectors + 255) / 256, 8192);
+    if (d->type == SDTW_TYPE_F32) attention_pack_kernel<uint32_t><<<grid, 256, 0, st>>>(p);
+    else attention_pack_kernel<uint16_t><<<grid, 256, 0, st>>>(p);
+    x = room;
+    room += bytes;
+    stride[3] = 1; stride[2] = loaded; stride[1] = loaded * rows; stride[0] = loaded * rows * heads;
+}
+
 // Calls f with a value of the element type and, as a type, the features rounded up to 32, 64, 96 or 128.
 template <int DP> struct Features { static constexpr int value = DP; };
+template <int F> struct Variant { static constexpr int value = F; };
+// ... and what the kernel has to be compiled for.
+template <typename F> void with_variant(const sdtw_attention_desc *d, const sdtw_attention_lists *lists, F f)
+{
+    const bool more = d->cap > 0.0f || (lists && lists->row_document);
+    if (d->buckets) {
+        if (more) f(Variant<kBias | kCap | kDocuments>{});
+        else f(Variant<kBias>{});
+    } else {
+        if (more) f(Variant<kCap | kDocuments>{});
+        else f(Variant<0>{});
+    }
+}
 template <typename F> void with_shape(int type, int D, F f)
 {
     auto sized = [&](auto t) {

@@ -57,61 +57,58 @@ template <typename T, int DP> struct TileShape {
     static constexpr int bytes(int rows) { return rows * kStride; }
 };
 
-// A matrix [rows][D] in memory, of any strides.
+// A matrix [rows][D] in memory whose features are contiguous and fill whole 16-byte chunks (others are packed beforehand).
 template <typename T> struct Rows {
     const T *base;
-    int64_t row, feature;  // strides
+    int64_t row;  // stride
 };
 
-// Chunk ch of a row: D features and zeros behind them.  A chunk that hangs over the end is read further in and shifted.
-template <typename T> __device__ __forceinline__ Bits4 load_chunk(const T *row, int64_t feature, int D, int ch)
+// The memory from `base` on, `bytes` of it: what is read beyond them is 0.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *base, uint32_t bytes)
 {
-    constexpr int W = Elem<T>::kWidth;
-    const int f = ch * W;
-    if (feature == 1) {
-        if (f + W <= D) return load_vec<false>(row + f);
-        if (f >= D) return Bits4{};
-        if (D >= W) return shift_vec(load_vec<false>(row + D - W), (f + W - D) * 8 * (int)sizeof(T));
-    }
-    Bits4 v{};
-#pragma unroll
-    for (int e = 0; e < W; ++e)
-        if (f + e < D) {
-            const T x = row[(f + e) * feature];
-            uint32_t bits;
-            if constexpr (sizeof(T) == 4) {
-                v[e] = __builtin_bit_cast(uint32_t, x);
-            } else {
-                bits = (uint32_t)__builtin_bit_cast(uint16_t, x) << (e & 1 ? 16 : 0);
-                v[e >> 1] |= bits;
-            }
-        }
-    return v;
+    const uint64_t a = reinterpret_cast<uint64_t>(base);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a), hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 
-// A tile on its way from memory to LDS: loaded to registers, later stored.  `who` of THREADS threads; ROWS rows.
+// A tile on its way from memory to LDS: loaded to registers, later stored.  `who` of THREADS threads; ROWS rows.  A tile's address is a scalar,
+// each thread's places within it do not change, and rows and features behind the end come as zeros without a branch.
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     using Shape = TileShape<T, DP>;
     static constexpr int kEach = ROWS * Shape::kChunks / THREADS;
     static_assert(kEach * THREADS == ROWS * Shape::kChunks, "a tile is dealt out evenly");
     Bits4 v[kEach];
-    // rows first .. first + ROWS; zeros from `limit` on and for rows whose document is negative
-    __device__ __forceinline__ void load(const Rows<T> &x, int D, int first, int limit, const int32_t *document, int who)
+    uint32_t at[kEach];
+    Rows<T> x;
+    uint32_t row_bytes, last_bytes;
+    static __device__ __forceinline__ int row(int who, int k) { return (who + k * THREADS) / Shape::kChunks; }
+    static __device__ __forceinline__ int chunk(int who, int k) { return (who + k * THREADS) % Shape::kChunks; }
+    __device__ __forceinline__ void begin(const Rows<T> &rows, int D, int who)
     {
+        x = rows;
+        row_bytes = (uint32_t)x.row * (uint32_t)sizeof(T);
+        last_bytes = (uint32_t)D * (uint32_t)sizeof(T);
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int id = who + k * THREADS, row = id / Shape::kChunks, ch = id % Shape::kChunks;
-            const int j = first + row;
-            v[k] = Bits4{};
-            if (j < limit && (!document || document[j] >= 0)) v[k] = load_chunk(x.base + j * x.row, x.feature, D, ch);
+            const uint32_t f = (uint32_t)chunk(who, k) * 16;
+            at[k] = f < last_bytes ? (uint32_t)row(who, k) * row_bytes + f : 0x7fffffffu;
         }
     }
-    __device__ __forceinline__ void store(char *tile, int who) const
+    // rows first .. first + ROWS; zeros from `limit` on (first < limit)
+    __device__ __forceinline__ void load(int first, int limit)
+    {
+        const auto tile = window(x.base + first * x.row, (uint32_t)min(limit - first, ROWS) * row_bytes - row_bytes + last_bytes);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) v[k] = __builtin_bit_cast(Bits4, __builtin_amdgcn_raw_buffer_load_b128(tile, at[k], 0, 0));
+    }
+    // DOCUMENTS: zeros for rows whose document is negative
+    template <bool DOCUMENTS> __device__ __forceinline__ void store(char *tile, const int32_t *documents, int who) const
     {
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const int id = who + k * THREADS, row = id / Shape::kChunks, ch = id % Shape::kChunks;
-            *reinterpret_cast<Bits4 *>(tile + row * Shape::kStride + ch * 16) = v[k];
+            Bits4 x = v[k];
+            if (DOCUMENTS) x = documents[row(who, k)] < 0 ? Bits4{} : x;
+            *reinterpret_cast<Bits4 *>(tile + row(who, k) * Shape::kStride + chunk(who, k) * 16) = x;
         }
     }
 };
@@ -122,13 +119,14 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
 template <typename T, int DP> struct Column {
     static constexpr int kSteps = TileShape<T, DP>::kChunks / 2;
     Bits4 v[kSteps];
-    __device__ __forceinline__ void load(const T *row, int64_t feature, int D, bool valid, int half)
+    __device__ __forceinline__ void load(const T *row, int D, bool valid, int half)
     {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            v[s] = Bits4{};
-            if (valid) v[s] = load_chunk(row, feature, D, 2 * s + half);
-        }
+        for (int s = 0; s < kSteps; ++s) v[s] = Bits4{};
+        if (!valid) return;
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s)
+            if ((2 * s + half) * Elem<T>::kWidth < D) v[s] = load_vec<false>(row + (2 * s + half) * Elem<T>::kWidth);
     }
 };
 
@@ -241,8 +239,12 @@ template <typename T, int DP> __device__ __forceinline__ void store_column(T *ou
 
 // ------------------------------------------------------------------ scores
 
+// What a kernel is compiled for; calls without any of it take one that has none of it, which has registers to spare.
+enum { kBias = 1, kCap = 2, kDocuments = 4 };
+
 struct AttentionParams {
     int32_t B, H, Hk, N, M, D;
+    int32_t loaded;             // D rounded up to whole chunks, where D does not fill them
     int32_t buckets, table_type, causal;
     int32_t offset, prefix;
     float scale, scale2;        // of the products; times log2(e)
@@ -263,7 +265,7 @@ struct AttentionParams {
 
 template <typename T> __device__ __forceinline__ Rows<T> rows_of(const void *base, const int64_t (&stride)[4], int b, int h)
 {
-    return {static_cast<const T *>(base) + b * stride[0] + h * stride[1], stride[2], stride[3]};
+    return {static_cast<const T *>(base) + b * stride[0] + h * stride[1], stride[2]};
 }
 template <typename T> __device__ __forceinline__ T *row_of(void *base, const int64_t (&stride)[4], int b, int h, int64_t i)
 {
@@ -308,12 +310,23 @@ struct WaveBias {
     const int32_t *starts;   // LDS
     float *diagonal;         // LDS, 64 of the wavefront's own
     uint8_t *bucket;         // LDS, 64 of the wavefront's own
+    int last;                // first distance of a side's last bucket
     float one;               // the bias of all cells, where it is the same
     int one_bucket;
     bool same;
+    // whether all cells with lowest <= j - i - offset <= highest are in the last bucket of their side (or in the one of all later keys)
+    __device__ __forceinline__ bool far(const BucketRule &rule, int lowest, int highest)
+    {
+        const int before = highest <= -last ? rule.n - 1 : -1, behind = rule.two_sided ? (lowest >= last ? 2 * rule.n - 1 : -1) : lowest >= 0 ? 0 : -1;
+        one_bucket = max(before, behind);
+        same = one_bucket >= 0;
+        if (same) one = values[one_bucket];
+        return same;
+    }
     // `lowest`: j - i - offset on the lowest of the diagonals
     __device__ __forceinline__ void look(const BucketRule &rule, int lowest, int lane)
     {
+        if (far(rule, lowest, lowest + 62)) return;
         const int u = rule.bucket(lowest + min(lane, 62), starts);
         one_bucket = __builtin_amdgcn_readfirstlane(u);
         same = __all(u == one_bucket);
@@ -345,20 +358,40 @@ __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const B
             values[u] = octaves_of_entry(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
         for (int k = thread; k <= rule.m; k += threads) starts[k] = rule.start[k];
     }
-    return WaveBias{values, starts, diagonal + 64 * wave, bucket + 64 * wave, 0.0f, 0, true};
+    return WaveBias{values, starts, diagonal + 64 * wave, bucket + 64 * wave, rule.first(rule.n - 1), 0.0f, 0, true};
 }
 
 constexpr int kKeys = 64;  // keys of a tile in LDS
 
+// A column's view of 32 positions that pass by: for the position of register r, whether it is below the column's limit and of its document.
+// `documents`: those of the 32 positions, in LDS; `rest`: the column's limit less the first position less 4 half.
+template <bool DOCUMENTS> struct Seen {
+    bool at[16];
+    __device__ __forceinline__ Seen(int rest, const int32_t *documents, int doc, int half)
+    {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) at[r] = tile_row(r, 0) < rest;
+        if (DOCUMENTS) {
+            typedef int32_t Four __attribute__((ext_vector_type(4)));
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const Four d = *reinterpret_cast<const Four *>(documents + 8 * g + 4 * half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at[4 * g + e] = at[4 * g + e] && d[e] == doc;
+            }
+        }
+    }
+};
+
 // The tiles of 64 keys (or rows) that a workgroup of 4 wavefronts walks through.  Where the sequence is packed from documents, those
 // without one of the documents lowest .. highest are stepped over: found out for 256 tiles at a time.
-struct TileWalk {
+template <bool DOCUMENTS> struct TileWalk {
     const int32_t *document;
     int keys, tiles, lowest, highest, batch;
     uint64_t *live;  // LDS, 4
     __device__ __forceinline__ int next(int t)  // the first tile from t on; `tiles` if there is none.  The same in all threads.
     {
-        if (!document) return t;
+        if (!DOCUMENTS || !document) return t;
         while (t < tiles) {
             if (t / 256 != batch) {
                 batch = t / 256;
@@ -383,14 +416,40 @@ struct TileWalk {
 };
 
 // Products into scores, in octaves.
-__device__ __forceinline__ void scale_scores(Acc &s, const AttentionParams &p)
+template <bool CAP> __device__ __forceinline__ void scale_scores(Acc &s, const AttentionParams &p)
 {
-    if (p.cap_out != 0.0f) {
+    if (CAP && p.cap_out != 0.0f) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = p.cap_out * tanh_fast(s[r] * p.cap_in);
     } else {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] *= p.scale2;
+    }
+}
+
+struct PackParams {
+    const void *in;
+    void *out;
+    int64_t stride[4], heads, rows, vectors;
+    int32_t D, loaded;
+};
+// Rows of any strides into contiguous ones of whole chunks, zeros behind their D features.
+template <typename U> __global__ __launch_bounds__(256) void attention_pack_kernel(PackParams p)
+{
+    constexpr int W = 16 / (int)sizeof(U);
+    const int chunks = p.loaded / W;
+    for (int64_t x = blockIdx.x * (int64_t)256 + threadIdx.x; x < p.vectors; x += gridDim.x * (int64_t)256) {
+        int64_t row = x / chunks;
+        const int f = (int)(x - row * chunks) * W;
+        const int64_t i = row % p.rows;
+        row /= p.rows;
+        const U *in = static_cast<const U *>(p.in) + row / p.heads * p.stride[0] + row % p.heads * p.stride[1] + i * p.stride[2];
+        U v[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[e] = f + e < p.D ? in[(f + e) * p.stride[3]] : (U)0;
+        Bits4 b;
+        __builtin_memcpy(&b, v, 16);
+        static_cast<Bits4 *>(p.out)[x] = b;
     }
 }
 
