@@ -94,7 +94,7 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
         constexpr int DP = decltype(features)::value;
         with_variant(desc, lists, [&](auto variant) {
             constexpr int F = decltype(variant)::value;
-            const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+            const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
             if (rows) {
                 ProfScope ps("attention_rows_gradient", st);
                 const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);

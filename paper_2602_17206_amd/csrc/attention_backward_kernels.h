@@ -104,8 +104,8 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
-    __shared__ __align__(16) int32_t documents[kKeys];
-    char *ktile = lds, *vtile = lds + Shape::bytes(kKeys);
+    __shared__ __align__(16) int32_t documents[2][kKeys];
+    constexpr int kTile = Shape::bytes(kKeys);
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     int64_t id = neighbours_together();
     const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);
@@ -114,9 +114,9 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
-    if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+    if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
     const int table_columns = TABLE ? p.table_columns : 0;
-    float *const table_sums = reinterpret_cast<float *>(lds + 2 * Shape::bytes(kKeys) + bias_bytes(4));
+    float *const table_sums = reinterpret_cast<float *>(lds + 4 * kTile + bias_bytes(4));
     TableSum table{table_sums + wave * p.buckets * table_columns, table_columns, -1, 0.0f};
     if (TABLE)
         for (int x = thread; x < 4 * p.buckets * table_columns; x += 256) table_sums[x] = 0.0f;
@@ -169,22 +169,38 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
     ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, thread);
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
+    auto fetch = [&](int t, int buffer) {
+        ks.copy(lds + buffer * kTile, t * kKeys, end, thread);
+        vs.copy(lds + (2 + buffer) * kTile, t * kKeys, end, thread);
+        if (DOCUMENTS && thread < kKeys)
+            documents[buffer][thread] = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
+    };
 #pragma unroll 1
     for (int pass = TABLE ? 0 : 1; pass < 2; ++pass) {
-        int now = -1, t = walk.next(0), next_doc = -1;
-        for (;;) {
-            if (t < walk.tiles) {
-                ks.load(t * kKeys, end);
-                vs.load(t * kKeys, end);
-                if (DOCUMENTS && thread < kKeys) next_doc = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
+        int t = walk.next(0), buffer = 0;
+        __syncthreads();  // (the tiles of the pass before are not read any more)
+        if (t < walk.tiles) fetch(t, 0);
+        while (t < walk.tiles) {
+            const int first = t * kKeys;
+            char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
+            const int32_t *const document = documents[buffer];
+            copies_done();
+            __syncthreads();
+            if (DOCUMENTS && __any(document[lane] < 0)) {
+                clear_rows<T, DP, kKeys, 256>(ktile, document, thread);
+                clear_rows<T, DP, kKeys, 256>(vtile, document, thread);
+                __syncthreads();
             }
+            t = walk.next(t + 1);
+            buffer ^= 1;
+            if (t < walk.tiles) fetch(t, buffer);
 #pragma unroll 1
-            for (int sub = 0; now >= 0 && sub < kKeys / 32; ++sub) {
-                const int j0 = now * kKeys + sub * 32;
+            for (int sub = 0; sub < kKeys / 32; ++sub) {
+                const int j0 = first + sub * 32;
                 const char *const kt = ktile + Shape::bytes(sub * 32), *const vt = vtile + Shape::bytes(sub * 32);
                 if (j0 >= to) break;
                 bool open = j0 + 32 <= from;
-                if (DOCUMENTS) open = open && low == high && __all(documents[sub * 32 + c] == low);
+                if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(kt, q, lane);
                 const CappedScores<CAP> capped(s, p);
                 if (BIAS) {
@@ -200,7 +216,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - lse);
                 if (!open) {
-                    const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents + sub * 32, doc, half);
+                    const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
                 }
@@ -232,17 +248,6 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
                 fit.fit(s, dq);
                 along_rows<T, DP>(dq, kt, Weights<T>(s), lane);
             }
-            if (t >= walk.tiles) break;
-            __syncthreads();
-            if (DOCUMENTS) {
-                if (thread < kKeys) documents[thread] = next_doc;
-                __syncthreads();
-            }
-            ks.template store<DOCUMENTS>(ktile, documents, thread);
-            vs.template store<DOCUMENTS>(vtile, documents, thread);
-            __syncthreads();
-            now = t;
-            t = walk.next(t + 1);
         }
         if (TABLE && pass == 0) {
             delta = both_sum(delta);
@@ -288,9 +293,9 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
-    __shared__ __align__(16) float row_lse[kKeys], row_delta[kKeys];
-    __shared__ __align__(16) int32_t row_doc[kKeys];
-    char *qtile = lds, *dtile = lds + Shape::bytes(kKeys);
+    __shared__ __align__(16) float row_lse[2][kKeys], row_delta[2][kKeys];
+    __shared__ __align__(16) int32_t row_doc[2][kKeys];
+    constexpr int kTile = Shape::bytes(kKeys);
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     int64_t id = neighbours_together();
     const int kt = (int)(id % p.key_tiles);  // (the first keys are seen by the most rows of a causal sequence: they go first)
@@ -332,32 +337,43 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
         const int h = hk * G + g;
         __syncthreads();
         WaveBias bias{};
-        if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+        if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
         const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
         qs.begin(rows_of<T>(p.q, p.q_stride, b, h), p.loaded, thread);
         ds.begin(rows_of<T>(p.dout, p.dout_stride, b, h), p.loaded, thread);
-        float next_lse = 0.0f, next_delta = 0.0f;
-        int next_doc = -1;
-        int now = -1, t = walk.next(begin / kKeys);
-        for (;;) {
-            if (t < walk.tiles) {
-                qs.load(t * kKeys, end);
-                ds.load(t * kKeys, end);
-                if (thread < kKeys) {
-                    const int i = t * kKeys + thread;
-                    next_doc = i >= end ? -1 : row_document ? row_document[i] : 0;
-                    const float x = next_doc >= 0 ? lse[i] : -INFINITY;
-                    next_lse = x == -INFINITY ? INFINITY : x * kLog2e;
-                    next_delta = next_doc >= 0 ? delta[i] : 0.0f;
-                }
+        auto fetch = [&](int t, int buffer) {
+            qs.copy(lds + buffer * kTile, t * kKeys, end, thread);
+            ds.copy(lds + (2 + buffer) * kTile, t * kKeys, end, thread);
+            if (thread < kKeys) {
+                const int i = t * kKeys + thread, d = i >= end ? -1 : row_document ? row_document[i] : 0;
+                const float x = d >= 0 ? lse[i] : -INFINITY;
+                row_doc[buffer][thread] = d;
+                row_lse[buffer][thread] = x == -INFINITY ? INFINITY : x * kLog2e;
+                row_delta[buffer][thread] = d >= 0 ? delta[i] : 0.0f;
             }
+        };
+        int t = walk.next(begin / kKeys), buffer = 0;
+        if (t < walk.tiles) fetch(t, 0);
+        while (t < walk.tiles) {
+            const int first = t * kKeys, now = buffer;
+            char *const qtile = lds + buffer * kTile, *const dtile = lds + (2 + buffer) * kTile;
+            copies_done();
+            __syncthreads();
+            if (DOCUMENTS && row_document && __any(row_doc[now][lane] < 0)) {
+                clear_rows<T, DP, kKeys, 256>(qtile, row_doc[now], thread);
+                clear_rows<T, DP, kKeys, 256>(dtile, row_doc[now], thread);
+                __syncthreads();
+            }
+            t = walk.next(t + 1);
+            buffer ^= 1;
+            if (t < walk.tiles) fetch(t, buffer);
 #pragma unroll 1
-            for (int sub = 0; now >= 0 && sub < kKeys / 32; ++sub) {
-                const int i0 = now * kKeys + sub * 32;
+            for (int sub = 0; sub < kKeys / 32; ++sub) {
+                const int i0 = first + sub * 32;
                 const char *const qt = qtile + Shape::bytes(sub * 32), *const dt = dtile + Shape::bytes(sub * 32);
                 if (i0 + 32 <= mine || i0 >= end || !any) continue;
                 bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
-                if (DOCUMENTS) open = open && low == high && __all(row_doc[sub * 32 + c] == low);
+                if (DOCUMENTS) open = open && low == high && __all(row_doc[now][sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(qt, k, lane);
                 const CappedScores<CAP> capped(s, p);
                 if (BIAS) {
@@ -370,7 +386,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                         for (int r = 0; r < 16; ++r) s[r] += at[-tile_row(r, 0)];
                     }
                 }
-                const float *at_lse = row_lse + sub * 32 + 4 * half, *at_delta = row_delta + sub * 32 + 4 * half;
+                const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - at_lse[tile_row(r, 0)]);
                 Acc dp = along_features<T, DP>(dt, v, lane);
@@ -382,7 +398,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         bool seen = tile_row(r, 0) >= before - i0 - 4 * half;
-                        if (DOCUMENTS) seen = seen && row_doc[sub * 32 + 4 * half + tile_row(r, 0)] == doc;
+                        if (DOCUMENTS) seen = seen && row_doc[now][sub * 32 + 4 * half + tile_row(r, 0)] == doc;
                         s[r] = seen ? s[r] : 0.0f;
                         dp[r] = seen ? dp[r] : 0.0f;
                     }
@@ -393,15 +409,6 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                 fit.fit(dp, dk);
                 along_rows<T, DP>(dk, qt, Weights<T>(dp), lane);
             }
-            if (t >= walk.tiles) break;
-            __syncthreads();
-            if (thread < kKeys) row_lse[thread] = next_lse, row_delta[thread] = next_delta, row_doc[thread] = next_doc;
-            if (DOCUMENTS) __syncthreads();
-            qs.template store<DOCUMENTS>(qtile, row_doc, thread);
-            ds.template store<DOCUMENTS>(dtile, row_doc, thread);
-            __syncthreads();
-            now = t;
-            t = walk.next(t + 1);
         }
     }
     if (j < p.M) {

@@ -14,9 +14,9 @@ struct ForwardPlan {
 
 size_t few_rows_lds(const sdtw_attention_desc *d)
 {
-    const int width = d->type == SDTW_TYPE_F32 ? 4 : 2, features = (d->D + 31) / 32 * 32;
-    return (size_t)8 * 32 * (features * width + 16) +
-           (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 : 0);
+    size_t bytes = 0;
+    with_shape(d->type, d->D, [&](auto t, auto features) { bytes = (size_t)few_rows_bytes<decltype(t), decltype(features)::value>(); });
+    return bytes + (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 : 0);
 }
 
 ForwardPlan split_forward(const sdtw_attention_desc *d)
@@ -26,7 +26,7 @@ ForwardPlan split_forward(const sdtw_attention_desc *d)
     P.splits = 1;
     if (d->B == 0 || d->H == 0 || d->N == 0) return P;
     const int64_t tiles = (d->N + 127) / 128, G = d->H / d->Hk;
-    P.few = (int64_t)d->B * d->H * tiles < 256 && few_rows_lds(d) + 2048 <= kLdsBytes;
+    P.few = (d->N * G <= 64 || (int64_t)d->B * d->H * tiles < 256) && few_rows_lds(d) + 4096 <= kLdsBytes;
     if (!P.few) {
         P.row_tiles = tiles;
         P.workgroups = (int64_t)d->B * d->H * tiles;
@@ -101,13 +101,13 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
                 attention_few_rows_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, few_rows_lds(desc), st>>>(p, rule);
             } else {
                 ProfScope ps("attention_forward", st);
-                const size_t bytes = 2 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+                const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
                 attention_forward_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, bytes, st>>>(p, rule);
             }
         });
         if (P.splits > 1) {
             ProfScope ps("attention_join", st);
-            attention_join_kernel<T><<<(unsigned)((int64_t)p.B * p.H * p.N), 128, 0, st>>>(p);
+            attention_join_kernel<T><<<(unsigned)((int64_t)p.B * p.H * p.N), 256, 0, st>>>(p);
         }
     });
     return hip_ok();

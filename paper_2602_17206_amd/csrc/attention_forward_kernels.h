@@ -72,8 +72,8 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
     extern __shared__ __align__(16) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
-    __shared__ __align__(16) int32_t documents[kKeys];
-    char *ktile = lds, *vtile = lds + Shape::bytes(kKeys);
+    __shared__ __align__(16) int32_t documents[2][kKeys];
+    constexpr int kTile = Shape::bytes(kKeys);  // (two tiles of keys, then two of values: one is read while the other is filled)
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
     int64_t id = neighbours_together();
     const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);  // (the last rows see the most keys of a causal sequence: they go first)
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
-    if (BIAS) bias = begin_bias(p, rule, lds + 2 * Shape::bytes(kKeys), h, wave, 4, thread, 256);
+    if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
     bool valid = i < sight.rows;
@@ -115,20 +115,34 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
     const float scale2 = p.scale2, cap_out = p.cap_out;
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
-    int now = -1, t = walk.next(0), next_doc = -1;
-    for (;;) {
-        if (t < walk.tiles) {
-            ks.load(t * kKeys, end);
-            vs.load(t * kKeys, end);
-            if (DOCUMENTS && thread < kKeys) next_doc = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
+    auto fetch = [&](int t, int buffer) {
+        ks.copy(lds + buffer * kTile, t * kKeys, end, thread);
+        vs.copy(lds + (2 + buffer) * kTile, t * kKeys, end, thread);
+        if (DOCUMENTS && thread < kKeys)
+            documents[buffer][thread] = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
+    };
+    int t = walk.next(0), buffer = 0;
+    if (t < walk.tiles) fetch(t, 0);
+    while (t < walk.tiles) {
+        const int j0 = t * kKeys;
+        char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
+        const int32_t *const document = documents[buffer];
+        copies_done();
+        __syncthreads();
+        if (DOCUMENTS && __any(document[lane] < 0)) {  // (the same in all wavefronts)
+            clear_rows<T, DP, kKeys, 256>(ktile, document, thread);
+            clear_rows<T, DP, kKeys, 256>(vtile, document, thread);
+            __syncthreads();
         }
-        const int j0 = now * kKeys;
-        if (now >= 0 && j0 < to) {
+        t = walk.next(t + 1);
+        buffer ^= 1;
+        if (t < walk.tiles) fetch(t, buffer);
+        if (j0 < to) {
             Acc s[SUBS];
 #pragma unroll
             for (int x = 0; x < SUBS; ++x) s[x] = along_features<T, DP>(ktile + Shape::bytes(x * 32), col, lane);
             bool open = j0 + kKeys <= from;
-            if (DOCUMENTS) open = open && low == high && __all(documents[lane] == low);
+            if (DOCUMENTS) open = open && low == high && __all(document[lane] == low);
             // scores that are products times a number, plus a number?
             if (open && (!CAP || cap_out == 0.0f) && (!BIAS || bias.far(rule, j0 - base, j0 - base + 94))) {
                 run.take(s, scale2, BIAS ? bias.one : 0.0f);
@@ -147,7 +161,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
                         }
                     }
                     if (!open) {
-                        const Seen<DOCUMENTS> seen(lim - j0 - 32 * x - 4 * half, documents + 32 * x, doc, half);
+                        const Seen<DOCUMENTS> seen(lim - j0 - 32 * x - 4 * half, document + 32 * x, doc, half);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) s[x][r] = seen.at[r] ? s[x][r] : -INFINITY;
                     }
@@ -157,17 +171,6 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
 #pragma unroll
             for (int x = 0; x < SUBS; ++x) along_rows<T, DP>(run.o, vtile + Shape::bytes(x * 32), Weights<T>(s[x]), lane);
         }
-        if (t >= walk.tiles) break;
-        __syncthreads();
-        if (DOCUMENTS) {
-            if (thread < kKeys) documents[thread] = next_doc;
-            __syncthreads();
-        }
-        ks.template store<DOCUMENTS>(ktile, documents, thread);
-        vs.template store<DOCUMENTS>(vtile, documents, thread);
-        __syncthreads();
-        now = t;
-        t = walk.next(t + 1);
     }
     const float total = both_sum(run.l);
     const bool some = valid && total != 0.0f;  // (a NaN is something)
@@ -180,6 +183,14 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
     if (half == 0) p.lse[((int64_t)b * p.H + h) * p.N + i] = some ? (run.m + __builtin_amdgcn_logf(total)) * kLn2 : -INFINITY;
 }
 
+// LDS of the kernel below: its wavefronts' tiles, or their sums, [4][32][DP + 4].
+template <typename T, int DP> constexpr int kFewBuffers = TileShape<T, DP>::bytes(32) <= 8192 ? 2 : 1;
+template <typename T, int DP> constexpr int few_rows_bytes()
+{
+    const int tiles = 4 * 2 * kFewBuffers<T, DP> * TileShape<T, DP>::bytes(32), sums = 4 * 32 * (DP + 4) * 4;
+    return tiles > sums ? tiles : sums;
+}
+
 // A few rows against many keys.  The rows of a group of heads that share their keys stand in one wavefront's columns together: row t is
 // query t / G of head t % G of the group.  Each of 4 wavefronts takes every fourth 32 keys of the workgroup's share, on its own; then
 // they are joined in LDS, and the workgroups of a row by attention_join_kernel.
@@ -190,9 +201,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(16) char lds[];
     __shared__ float ref[4][32], tot[4][32];
-    __shared__ __align__(16) int32_t documents[4][32];
+    __shared__ __align__(16) int32_t documents[4][2][32];
     const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
-    char *ktile = lds + wave * 2 * Shape::bytes(32), *vtile = ktile + Shape::bytes(32);
+    // two tiles of keys and two of values for each wavefront, where there is room
+    constexpr int kTile = Shape::bytes(32), kBuffers = kFewBuffers<T, DP>;
+    char *const tiles_of = lds + wave * 2 * kBuffers * kTile;
     int64_t id = neighbours_together();
     const int split = (int)(id % p.splits);
     id /= p.splits;
@@ -218,7 +231,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
         col.load(q.base + (valid ? i : 0) * q.row, p.loaded, valid, half);
     }
     // the entries of every head that is here, and the rule's starts
-    float *values = reinterpret_cast<float *>(lds + 8 * Shape::bytes(32));
+    float *values = reinterpret_cast<float *>(lds + few_rows_bytes<T, DP>());
     int32_t *starts = reinterpret_cast<int32_t *>(values + min(G, 32) * p.buckets);
     const int first_head = G <= 32 ? 0 : rt * 32 % G;  // (the heads of 32 rows of a larger group follow each other, round its end)
     if (BIAS) {
@@ -239,23 +252,31 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     Stage<T, DP, 32, 64> ks, vs;
     ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, lane);
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, lane);
-    int next_doc = -1;
-    for (int t = begin - 1; t < end; ++t) {
-        const int j0 = t * 128 + wave * 32;
-        if (t >= begin) {
-            wavefront_order();
-            if (DOCUMENTS && half == 0) documents[wave][c] = next_doc;
-            wavefront_order();
-            ks.template store<DOCUMENTS>(ktile, documents[wave], lane);
-            vs.template store<DOCUMENTS>(vtile, documents[wave], lane);
+    auto fetch = [&](int t, int buffer) {
+        const int j = t * 128 + wave * 32;
+        if (j >= to) return;
+        ks.copy(tiles_of + buffer * 2 * kTile, j, to, lane);
+        vs.copy(tiles_of + (buffer * 2 + 1) * kTile, j, to, lane);
+        if (DOCUMENTS && half == 0) documents[wave][buffer][c] = j + c >= to ? -1 : col_document ? col_document[j + c] : 0;
+    };
+    if (kBuffers == 2 && begin < end) fetch(begin, 0);
+    for (int t = begin; t < end; ++t) {
+        const int j0 = t * 128 + wave * 32, buffer = kBuffers == 2 ? (t - begin) & 1 : 0;
+        char *const ktile = tiles_of + buffer * 2 * kTile, *const vtile = ktile + kTile;
+        wavefront_order();
+        if (kBuffers == 1) {
+            copies_done();
+            fetch(t, 0);
+        }
+        copies_done();
+        wavefront_order();
+        if (kBuffers == 2 && t + 1 < end) fetch(t + 1, buffer ^ 1);
+        if (j0 >= to) continue;
+        if (DOCUMENTS && __any(documents[wave][buffer][c] < 0)) {
+            clear_rows<T, DP, 32, 64>(ktile, documents[wave][buffer], lane);
+            clear_rows<T, DP, 32, 64>(vtile, documents[wave][buffer], lane);
             wavefront_order();
         }
-        if (t + 1 < end && j0 + 128 < to) {
-            ks.load(j0 + 128, to);
-            vs.load(j0 + 128, to);
-            if (DOCUMENTS) next_doc = j0 + 128 + c >= to ? -1 : col_document ? col_document[j0 + 128 + c] : 0;
-        }
-        if (t < begin || j0 >= to) continue;
         Acc scores[1] = {along_features<T, DP>(ktile, col, lane)};
         Acc &s = scores[0];
         scale_scores<CAP>(s, p);
@@ -270,7 +291,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
             }
         }
         if (DOCUMENTS || j0 + 32 > from) {
-            const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents[wave], doc, half);
+            const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents[wave][buffer], doc, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : -INFINITY;
         }
@@ -319,30 +340,53 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     }
 }
 
-// A row's parts joined, in their order: a workgroup of 128 threads for each row.
-template <typename T> __global__ __launch_bounds__(128) void attention_join_kernel(AttentionParams p)
+// A row's parts joined, in one order: a workgroup of 256 threads for each row.
+template <typename T> __global__ __launch_bounds__(256) void attention_join_kernel(AttentionParams p)
 {
-    __shared__ float factor[1024];
+    __shared__ float factor[1024], sums[256];
+    __shared__ float best[4];
     const int64_t place = blockIdx.x;
-    const int i = (int)(place % p.N), h = (int)(place / p.N % p.H), b = (int)(place / p.N / p.H);
-    const float *part = p.part + place * p.splits * (p.D + 2);
+    const int thread = threadIdx.x, i = (int)(place % p.N), h = (int)(place / p.N % p.H), b = (int)(place / p.N / p.H);
+    const int pitch = p.D + 2;
+    const float *part = p.part + place * p.splits * pitch;
     const Sight sight(p, b);
     const bool valid = i < sight.rows && !(p.row_document && p.row_document[(int64_t)b * p.N + i] < 0);
-    float top = -INFINITY, all = 0.0f;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, part[s * (p.D + 2) + p.D]);
-    for (int s = threadIdx.x; s < p.splits; s += 128) {
-        const float m = part[s * (p.D + 2) + p.D];
-        factor[s] = m == top ? 1.0f : exp2_fast(m - top);
+    float top = -INFINITY;
+    for (int s = thread; s < p.splits; s += 256) {
+        factor[s] = part[s * pitch + p.D];
+        top = fmaxf(top, factor[s]);
     }
+    top = wave_max_all_f32(top);
+    if (thread % 64 == 0) best[thread / 64] = top;
     __syncthreads();
-    for (int s = 0; s < p.splits; ++s) all += part[s * (p.D + 2) + p.D + 1] * factor[s];
-    const bool seen = valid && all != 0.0f;
-    for (int f = threadIdx.x; f < p.D; f += 128) {
-        float sum = 0.0f;
-        for (int s = 0; s < p.splits; ++s) sum += part[s * (p.D + 2) + f] * factor[s];
-        row_of<T>(p.out, p.out_stride, b, h, i)[f] = Elem<T>::down(seen ? sum / all : 0.0f);
+    top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+    float all = 0.0f;
+    for (int s = thread; s < p.splits; s += 256) {
+        const float m = factor[s];
+        factor[s] = m == top ? 1.0f : exp2_fast(m - top);
+        all = fmaf(part[s * pitch + p.D + 1], factor[s], all);
     }
-    if (threadIdx.x == 0) p.lse[place] = seen ? (top + __builtin_amdgcn_logf(all)) * kLn2 : -INFINITY;
+    all = wave_sum_all_f32(all);
+    __syncthreads();
+    if (thread % 64 == 0) best[thread / 64] = all;
+    __syncthreads();
+    all = (best[0] + best[1]) + (best[2] + best[3]);
+    const bool seen = valid && all != 0.0f;
+    // `groups` threads for each feature
+    const int wide = p.D <= 32 ? 32 : p.D <= 64 ? 64 : 128, groups = 256 / wide, f = thread % wide;
+    float sum = 0.0f;
+    if (f < p.D) {
+#pragma unroll 8
+        for (int s = thread / wide; s < p.splits; s += groups) sum = fmaf(part[s * pitch + f], factor[s], sum);
+    }
+    sums[thread] = sum;
+    __syncthreads();
+    if (thread < p.D) {
+        sum = sums[thread];
+        for (int g = 1; g < groups; ++g) sum += sums[thread + g * wide];
+        row_of<T>(p.out, p.out_stride, b, h, i)[thread] = Elem<T>::down(seen ? sum / all : 0.0f);
+    }
+    if (thread == 0) p.lse[place] = seen ? (top + __builtin_amdgcn_logf(all)) * kLn2 : -INFINITY;
 }
 
 }  // namespace sdtw

@@ -48,13 +48,19 @@ __device__ __forceinline__ int wave_max_i32(int v)
 
 // ------------------------------------------------------------------ tiles in LDS
 
-// Rows of DP features (D and zeros behind it) with 16 bytes between them: the same chunk of neighbouring rows falls into different
-// banks.
+// Rows of DP features (D and zeros behind it) without gaps, as memory is copied into LDS 64 chunks of 16 bytes at a time.  Within a row
+// the chunks change places, chunk ch to ch ^ turn(row): so that neighbouring rows' chunks of one number fall into different banks,
+// and so do two neighbouring chunks of four rows, for the two kinds of reads.
 template <typename T, int DP> struct TileShape {
     static constexpr int W = Elem<T>::kWidth;
     static constexpr int kChunks = DP / W;  // 16-byte chunks of a row
-    static constexpr int kStride = DP * (int)sizeof(T) + 16;
+    static constexpr int kStride = DP * (int)sizeof(T);
+    static constexpr bool kEight = kChunks % 8 == 0;  // places change among eight chunks, else among four
     static constexpr int bytes(int rows) { return rows * kStride; }
+    static __device__ __forceinline__ constexpr int turn(int row)
+    {
+        return kEight ? (row & 3) << 1 | (row >> 2 & 1) : (row & 2) | (row >> 2 & 1);
+    }
 };
 
 // A matrix [rows][D] in memory whose features are contiguous and fill whole 16-byte chunks (others are packed beforehand).
@@ -71,18 +77,28 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *base, uint3
     return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 
-// A tile on its way from memory to LDS: loaded to registers, later stored.  `who` of THREADS threads; ROWS rows.  A tile's address is a scalar,
-// each thread's places within it do not change, and rows and features behind the end come as zeros without a branch.
+typedef __attribute__((address_space(3))) char LdsByte;
+__device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)reinterpret_cast<uintptr_t>((LdsByte *)p); }
+
+// 16 bytes a lane from the window straight into LDS, lane after lane from `lds` on.  Written out because the compiler, which cannot tell the
+// tile that is being filled from the one that is being read, would wait for it before every read.
+__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t at, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from), "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory");
+}
+// All that the wavefront asked for is there, and what it read from LDS has left it.
+__device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
+
+// A tile of ROWS rows, copied by THREADS threads (`who`).  A tile's address is a scalar, each thread's places within it do not change,
+// and rows and features behind the end come as zeros without a branch.
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     using Shape = TileShape<T, DP>;
     static constexpr int kEach = ROWS * Shape::kChunks / THREADS;
     static_assert(kEach * THREADS == ROWS * Shape::kChunks, "a tile is dealt out evenly");
-    Bits4 v[kEach];
     uint32_t at[kEach];
     Rows<T> x;
     uint32_t row_bytes, last_bytes;
-    static __device__ __forceinline__ int row(int who, int k) { return (who + k * THREADS) / Shape::kChunks; }
-    static __device__ __forceinline__ int chunk(int who, int k) { return (who + k * THREADS) % Shape::kChunks; }
     __device__ __forceinline__ void begin(const Rows<T> &rows, int D, int who)
     {
         x = rows;
@@ -90,28 +106,28 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
         last_bytes = (uint32_t)D * (uint32_t)sizeof(T);
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            const uint32_t f = (uint32_t)chunk(who, k) * 16;
-            at[k] = f < last_bytes ? (uint32_t)row(who, k) * row_bytes + f : 0x7fffffffu;
+            const int id = who + k * THREADS, row = id / Shape::kChunks;
+            const uint32_t f = (uint32_t)((id % Shape::kChunks) ^ Shape::turn(row)) * 16;
+            at[k] = f < last_bytes ? (uint32_t)row * row_bytes + f : 0x7fffffffu;
         }
     }
     // rows first .. first + ROWS; zeros from `limit` on (first < limit)
-    __device__ __forceinline__ void load(int first, int limit)
+    __device__ __forceinline__ void copy(char *tile, int first, int limit, int who) const
     {
-        const auto tile = window(x.base + first * x.row, (uint32_t)min(limit - first, ROWS) * row_bytes - row_bytes + last_bytes);
+        const auto from = window(x.base + first * x.row, (uint32_t)min(limit - first, ROWS) * row_bytes - row_bytes + last_bytes);
+        const uint32_t to = lds_address(tile) + (uint32_t)(who / 64) * 1024u;
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) v[k] = __builtin_bit_cast(Bits4, __builtin_amdgcn_raw_buffer_load_b128(tile, at[k], 0, 0));
-    }
-    // DOCUMENTS: zeros for rows whose document is negative
-    template <bool DOCUMENTS> __device__ __forceinline__ void store(char *tile, const int32_t *documents, int who) const
-    {
-#pragma unroll
-        for (int k = 0; k < kEach; ++k) {
-            Bits4 x = v[k];
-            if (DOCUMENTS) x = documents[row(who, k)] < 0 ? Bits4{} : x;
-            *reinterpret_cast<Bits4 *>(tile + row(who, k) * Shape::kStride + chunk(who, k) * 16) = x;
-        }
+        for (int k = 0; k < kEach; ++k) copy_to_lds(from, at[k], to + (uint32_t)k * (THREADS * 16u));
     }
 };
+
+// Zeros for the rows of a tile whose document is negative: they may hold anything.  `documents`: of the ROWS rows, in LDS.
+template <typename T, int DP, int ROWS, int THREADS> __device__ __forceinline__ void clear_rows(char *tile, const int32_t *documents, int who)
+{
+    using Shape = TileShape<T, DP>;
+    for (int id = who; id < ROWS * Shape::kChunks; id += THREADS)
+        if (documents[id / Shape::kChunks] < 0) *reinterpret_cast<Bits4 *>(tile + id * 16) = Bits4{};
+}
 
 // ------------------------------------------------------------------ products
 
@@ -147,13 +163,18 @@ template <typename T> __device__ __forceinline__ void mma(Acc &acc, const Bits4 
     }
 }
 
-// S = X R for the 32 rows of `tile`
+// S = X R for the 32 rows of `tile` (which begins at a multiple of 8 rows)
 template <typename T, int DP> __device__ __forceinline__ Acc along_features(const char *tile, const Column<T, DP> &col, int lane)
 {
-    const char *at = tile + (lane & 31) * TileShape<T, DP>::kStride + (lane >> 5) * 16;
+    using Shape = TileShape<T, DP>;
+    constexpr int kTurns = Shape::kEight ? 7 : 3;
+    const int row = lane & 31, turn = (lane >> 5) ^ Shape::turn(row);  // (chunk 2 s + half; half is its lowest bit)
     Acc acc = {};
 #pragma unroll
-    for (int s = 0; s < Column<T, DP>::kSteps; ++s) mma<T>(acc, *reinterpret_cast<const Bits4 *>(at + s * 32), col.v[s]);
+    for (int s = 0; s < Column<T, DP>::kSteps; ++s) {
+        const char *at = tile + (row * Shape::kStride + (turn ^ (2 * s & kTurns)) * 16);
+        mma<T>(acc, *reinterpret_cast<const Bits4 *>(at + (2 * s & ~kTurns) * 16), col.v[s]);
+    }
     return acc;
 }
 
@@ -180,34 +201,39 @@ typedef __attribute__((address_space(3))) Short4 LdsShort4;
 // O += X^T P: feature 32 ft + tile_row(r, half) of the column in register r of acc[ft]
 template <typename T, int DP> __device__ __forceinline__ void along_rows(Acc (&acc)[DP / 32], const char *tile, const Weights<T> &w, int lane)
 {
-    constexpr int kStride = TileShape<T, DP>::kStride;
+    using Shape = TileShape<T, DP>;
+    constexpr int kStride = Shape::kStride;
+    const int half = lane >> 5;
     if constexpr (std::is_same<T, float>::value) {
-        const char *at = tile + 4 * (lane >> 5) * kStride + (lane & 31) * 4;
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
+        for (int r = 0; r < 16; ++r) {
+            const char *at = tile + ((4 * half + (r & 3)) * kStride + ((((lane & 31) >> 2) ^ half ^ (r & 3) << 1) * 16 + (lane & 3) * 4));
 #pragma unroll
             for (int ft = 0; ft < DP / 32; ++ft) {
-                const float x = *reinterpret_cast<const float *>(at + tile_row(r, 0) * kStride + ft * 128);
+                const float x = *reinterpret_cast<const float *>(at + 8 * (r >> 2) * kStride + ft * 128);
                 acc[ft] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w.v[r], acc[ft], 0, 0, 0);
             }
+        }
     } else {
         // ds_read_b64_tr_b16: sixteen lanes read 4 rows of 16 elements, four elements a lane, and each gets a column of them
-        const char *at = tile + (4 * (lane >> 5) + (lane >> 2 & 3)) * kStride + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        const int row = 4 * half + (lane >> 2 & 3), chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int ft = 0; ft < DP / 32; ++ft) {
+            const int place = (chunk ^ Shape::turn(row)) ^ (Shape::kEight ? ft * 4 & 7 : 0);
+            const char *at = tile + (row * kStride + place * 16 + (lane & 1) * 8) + (Shape::kEight ? ft * 4 & ~7 : ft * 4) * 16;
 #pragma unroll
-            for (int ft = 0; ft < DP / 32; ++ft) {
+            for (int s = 0; s < 2; ++s) {
                 Bits4 a;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const Short4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (LdsShort4 *)(at + (16 * s + 8 * q) * kStride + ft * 64));
+                    const Short4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(at + (16 * s + 8 * q) * kStride));
                     const uint64_t bits = __builtin_bit_cast(uint64_t, x);
                     a[2 * q] = (uint32_t)bits;
                     a[2 * q + 1] = (uint32_t)(bits >> 32);
                 }
                 mma<T>(acc[ft], a, w.v[s]);
             }
+        }
     }
 }
 
