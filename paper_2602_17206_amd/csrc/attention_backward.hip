@@ -8,8 +8,8 @@ using namespace sdtw;
 
 struct BackwardPlan {
     bool fits;
-    int64_t row_tiles, key_tiles;
-    size_t off_table, off_packed, total;
+    int64_t row_tiles, key_tiles, parts;
+    size_t off_table, off_keys, off_packed, total;
 };
 
 BackwardPlan backward_plan(const sdtw_attention_desc *d)
@@ -17,11 +17,17 @@ BackwardPlan backward_plan(const sdtw_attention_desc *d)
     BackwardPlan P{};
     P.row_tiles = ((int64_t)d->N + 127) / 128;
     P.key_tiles = ((int64_t)d->M + 127) / 128;
+    // The keys' kernel is split over the rows until there are about four workgroups for each compute unit, of four tiles of rows at least.
+    const int64_t units = (int64_t)d->B * d->Hk * P.key_tiles, steps = (int64_t)(d->H / d->Hk) * (((int64_t)d->N + 63) / 64);
+    P.parts = units > 0 && units < (1 << 20) ? std::max<int64_t>(1, std::min<int64_t>((1024 + units - 1) / units, steps / 4)) : 1;
     P.fits = (int64_t)d->B * d->H <= 0x7fffffff && attention_grid_ok((int64_t)d->B * d->H * std::max<int64_t>(1, P.row_tiles)) &&
-             attention_grid_ok((int64_t)d->B * d->Hk * std::max<int64_t>(1, P.key_tiles)) && attention_grid_ok((int64_t)d->H * d->buckets);
+             (int64_t)d->B * d->Hk <= 0x7fffffff &&
+             attention_grid_ok((int64_t)d->B * d->Hk * std::max<int64_t>(1, P.key_tiles) * P.parts) && attention_grid_ok((int64_t)d->H * d->buckets);
     if (!P.fits) return P;
     P.off_table = align_up((size_t)d->B * d->H * d->N * sizeof(float), 256);
-    P.off_packed = P.off_table + align_up((size_t)d->H * d->buckets * d->B * P.row_tiles * sizeof(float), 256);
+    P.off_keys = P.off_table + align_up((size_t)d->H * d->buckets * d->B * P.row_tiles * sizeof(float), 256);
+    P.off_packed = P.off_keys + (P.parts > 1 ? align_up((size_t)P.parts * 2 * d->B * d->Hk * d->M * d->D * sizeof(float), 256) : 0);
+    if (P.parts > 1) P.fits = attention_grid_ok(((int64_t)2 * d->B * d->Hk * d->M * d->D + 255) / 256);
     P.total = P.off_packed;
     for (const auto *stride : {&d->q_stride, &d->out_stride, &d->dout_stride}) P.total += packed_bytes(d, *stride, d->H, d->N);
     for (const auto *stride : {&d->k_stride, &d->v_stride}) P.total += packed_bytes(d, *stride, d->Hk, d->M);
@@ -75,6 +81,8 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
     p.row_tiles = (int32_t)P.row_tiles;
     p.key_tiles = (int32_t)P.key_tiles;
     p.delta = static_cast<float *>(workspace);
+    p.parts = (int32_t)P.parts;
+    p.key_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.off_keys);
     p.table_part = reinterpret_cast<float *>(static_cast<char *>(workspace) + P.off_table);
     hipStream_t st = static_cast<hipStream_t>(stream);
     char *room = static_cast<char *>(workspace) + P.off_packed;
@@ -110,9 +118,15 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
             }
             if (keys) {
                 ProfScope ps("attention_keys_gradient", st);
-                attention_keys_gradient_kernel<T, DP, F><<<(unsigned)((int64_t)p.B * p.Hk * p.key_tiles), 256, bytes, st>>>(p, rule);
+                attention_keys_gradient_kernel<T, DP, F><<<(unsigned)((int64_t)p.B * p.Hk * p.key_tiles * p.parts), 256, bytes, st>>>(p, rule);
             }
         });
+        if (keys && p.parts > 1) {
+            ProfScope ps("attention_keys_join", st);
+            const int64_t elements = (int64_t)2 * p.B * p.Hk * p.M * p.D;
+            if (p.D % 4 == 0) attention_keys_join_kernel<T, 4><<<(unsigned)((elements / 4 + 255) / 256), 256, 0, st>>>(p);
+            else attention_keys_join_kernel<T, 1><<<(unsigned)((elements + 255) / 256), 256, 0, st>>>(p);
+        }
     });
     if (dtable) {
         ProfScope ps("attention_table", st);

@@ -12,29 +12,12 @@
 
 namespace sdtw {
 
-// Products into scores, in octaves, and 1 - tanh^2 where there may be a cap.
-template <bool CAP> struct CappedScores {
-    Acc slope;
-    __device__ __forceinline__ explicit CappedScores(Acc &s, const AttentionParams &p)
-    {
-        if (p.cap_out != 0.0f) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float t = tanh_fast(s[r] * p.cap_in);
-                s[r] = p.cap_out * t;
-                slope[r] = fmaf(-t, t, 1.0f);
-            }
-        } else {
-            s *= p.scale2;
-            slope = Acc{} + 1.0f;
-        }
-    }
-    __device__ __forceinline__ void apply(Acc &x) const { x *= slope; }
-};
-template <> struct CappedScores<false> {
-    __device__ __forceinline__ explicit CappedScores(Acc &s, const AttentionParams &p) { s *= p.scale2; }
-    __device__ __forceinline__ void apply(Acc &) const {}
-};
+// Times 1 - tanh^2, where `capped` holds the capped scores and `inverse` 1 over the cap, both in octaves; 0 without a cap.
+__device__ __forceinline__ void through_cap(Acc &x, const Acc &capped, float inverse)
+{
+    const Acc t = capped * inverse;
+    x = x - x * t * t;
+}
 
 // float16 has 30 octaves for numbers that may be of any size (gradients of a mean are small): a column's numbers go into the
 // matrix cores times a power of two of the column's own, chosen from the first of them and made smaller whenever one would not fit.
@@ -91,13 +74,13 @@ struct TableSum {
 };
 
 // Wavefronts on a SIMD that registers are kept for.
-template <typename T, int DP> constexpr int kRowsWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : 2;
+template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : DP <= 96 || !MORE ? 2 : 1;
 
 // 4 wavefronts of 32 rows each, one head of one sequence.  TABLE: the table's gradient is wanted.  delta comes from the rows' outputs -
 // sum_j p dp = <dout, out> - unless the table's gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals
 // would show the rounding of a 16-bit `out`; so the keys are walked over once more, for delta alone.
 template <typename T, int DP, int F, bool TABLE>
-__global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
+__global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
@@ -106,11 +89,10 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
     __shared__ int shared[4][4];
     __shared__ __align__(16) int32_t documents[2][kKeys];
     constexpr int kTile = Shape::bytes(kKeys);
-    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
-    int64_t id = neighbours_together();
-    const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);
-    id /= p.row_tiles;
-    const int h = (int)(id % p.H), b = (int)(id / p.H), hk = h / (p.H / p.Hk);
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
+    const Place at_work(p.B * p.H);
+    const int rt = p.row_tiles - 1 - at_work.tile;  // (the last rows see the most keys of a causal sequence)
+    const int h = at_work.unit % p.H, b = at_work.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
@@ -164,6 +146,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
     ColumnScale<T, DP> fit;
+    const float inverse_cap = CAP && p.cap_out != 0.0f ? 1.0f / p.cap_out : 0.0f;
     TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
@@ -202,7 +185,8 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
                 bool open = j0 + 32 <= from;
                 if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(kt, q, lane);
-                const CappedScores<CAP> capped(s, p);
+                scale_scores<CAP>(s, p);
+                const Acc capped = s;
                 if (BIAS) {
                     bias.look(rule, j0 - base, lane);
                     if (bias.same) {
@@ -244,7 +228,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_rows_gradi
                         for (int r = 0; r < 16; ++r) table.turn(lane, at[tile_row(r, 0)], valid ? s[r] : 0.0f);
                     }
                 }
-                capped.apply(s);
+                if (CAP) through_cap(s, capped, inverse_cap);
                 fit.fit(s, dq);
                 along_rows<T, DP>(dq, kt, Weights<T>(s), lane);
             }
@@ -284,9 +268,10 @@ __global__ __launch_bounds__(64) void attention_table_kernel(AttentionParams p)
     if (threadIdx.x == 0) p.dtable[blockIdx.x] = (float)sum;
 }
 
-// 4 wavefronts of 32 keys each, of one head of keys of one sequence; the queries of the group's heads go by in tiles of 64.
+// 4 wavefronts of 32 keys each, of one head of keys of one sequence; the queries of the group's heads go by in tiles of 64, or one part
+// of them does: then attention_keys_join_kernel adds the parts up.
 template <typename T, int DP, int F>
-__global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
+__global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 : DP, F != 0>)) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
@@ -296,11 +281,10 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
     __shared__ __align__(16) float row_lse[2][kKeys], row_delta[2][kKeys];
     __shared__ __align__(16) int32_t row_doc[2][kKeys];
     constexpr int kTile = Shape::bytes(kKeys);
-    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
-    int64_t id = neighbours_together();
-    const int kt = (int)(id % p.key_tiles);  // (the first keys are seen by the most rows of a causal sequence: they go first)
-    id /= p.key_tiles;
-    const int hk = (int)(id % p.Hk), b = (int)(id / p.Hk), G = p.H / p.Hk;
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
+    const Place at_work(p.B * p.Hk);
+    const int kt = at_work.tile / p.parts, part = at_work.tile % p.parts;  // (the first keys are seen by the most rows of a causal sequence)
+    const int hk = at_work.unit % p.Hk, b = at_work.unit / p.Hk, G = p.H / p.Hk;
     const Sight sight(p, b);
     const int32_t *row_document = DOCUMENTS && p.row_document ? p.row_document + (int64_t)b * p.N : nullptr;
     const int first_key = kt * 128 + wave * 32, j = first_key + c;
@@ -329,12 +313,20 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
     ColumnScale<T, DP> fit;
+    const float inverse_cap = CAP && p.cap_out != 0.0f ? 1.0f / p.cap_out : 0.0f;
     constexpr float kWeight = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;  // p <= 1 (to rounding) into float16's upper octaves
     TileWalk<DOCUMENTS> walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> qs, ds;
+    // tiles from_tile .. walk.tiles of each head, all heads' one after the other: this part's share of them
+    const int from_tile = min(begin / kKeys, walk.tiles), each = walk.tiles - from_tile;
+    const int64_t all = (int64_t)G * each;
+    const int64_t share_begin = all * part / p.parts, share_end = all * (part + 1) / p.parts;
+    const int first_head = each ? (int)(share_begin / each) : 0, last_head = each ? (int)((share_end + each - 1) / each) : 0;
 #pragma unroll 1
-    for (int g = 0; g < G; ++g) {
+    for (int g = first_head; g < last_head; ++g) {
         const int h = hk * G + g;
+        const int first_tile = from_tile + (int)max(share_begin - (int64_t)g * each, (int64_t)0);
+        walk.tiles = from_tile + (int)min(share_end - (int64_t)g * each, (int64_t)each);
         __syncthreads();
         WaveBias bias{};
         if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
@@ -352,7 +344,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                 row_delta[buffer][thread] = d >= 0 ? delta[i] : 0.0f;
             }
         };
-        int t = walk.next(begin / kKeys), buffer = 0;
+        int t = walk.next(first_tile), buffer = 0;
         if (t < walk.tiles) fetch(t, 0);
         while (t < walk.tiles) {
             const int first = t * kKeys, now = buffer;
@@ -375,7 +367,8 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                 bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
                 if (DOCUMENTS) open = open && low == high && __all(row_doc[now][sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(qt, k, lane);
-                const CappedScores<CAP> capped(s, p);
+                scale_scores<CAP>(s, p);
+                const Acc capped = s;
                 if (BIAS) {
                     bias.look(rule, first_key - (i0 + 31) - sight.offset, lane);
                     if (bias.same) {
@@ -392,6 +385,7 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                 Acc dp = along_features<T, DP>(dt, v, lane);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - at_delta[tile_row(r, 0)]);
+                if (CAP) through_cap(dp, capped, inverse_cap);
                 if (!open) {  // (a key that only rows in no document would see may hold NaN: both are chosen, not multiplied away)
                     // rows from `before` on see the key; documents of rows behind the last are negative
                     const int before = j < sight.prefix || !sight.causal ? -0x40000000 : j - sight.offset;
@@ -403,7 +397,6 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
                         dp[r] = seen ? dp[r] : 0.0f;
                     }
                 }
-                capped.apply(dp);
                 if (kWeight != 1.0f) s *= kWeight;
                 along_rows<T, DP>(dv, dt, Weights<T>(s), lane);
                 fit.fit(dp, dk);
@@ -416,9 +409,34 @@ __global__ __launch_bounds__(256, (kRowsWaves<T, DP>)) void attention_keys_gradi
 #pragma unroll
             for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
         }
-        store_column<T, DP>(row_of<T>(p.dk, p.dk_stride, b, hk, j), p.D, dk, p.scale * fit.undo(), half);
-        store_column<T, DP>(row_of<T>(p.dv, p.dv_stride, b, hk, j), p.D, dv, 1.0f / kWeight, half);
+        if (p.parts == 1) {
+            store_column<T, DP>(row_of<T>(p.dk, p.dk_stride, b, hk, j), p.D, dk, p.scale * fit.undo(), half);
+            store_column<T, DP>(row_of<T>(p.dv, p.dv_stride, b, hk, j), p.D, dv, 1.0f / kWeight, half);
+        } else {
+            float *const out = p.key_part + ((int64_t)part * 2 * p.B * p.Hk + b * p.Hk + hk) * p.M * p.D + (int64_t)j * p.D;
+            store_column<float, DP>(out, p.D, dk, p.scale * fit.undo(), half);
+            store_column<float, DP>(out + (int64_t)p.B * p.Hk * p.M * p.D, p.D, dv, 1.0f / kWeight, half);
+        }
     }
+}
+
+// dk and dv from their parts, in their order.  key_part [parts][2][B, Hk, M, D]; four features a thread where four divide D.
+template <typename T, int W> __global__ __launch_bounds__(256) void attention_keys_join_kernel(AttentionParams p)
+{
+    const int64_t all = (int64_t)p.B * p.Hk * p.M * p.D;
+    const int64_t x = (blockIdx.x * (int64_t)256 + threadIdx.x) * W;
+    if (x >= 2 * all) return;
+    float sum[W] = {};
+    for (int part = 0; part < p.parts; ++part) {
+        const float *in = p.key_part + part * 2 * all + x;
+#pragma unroll
+        for (int e = 0; e < W; ++e) sum[e] += in[e];
+    }
+    const int64_t y = x < all ? x : x - all, row = y / p.D;
+    const int64_t j = row % p.M, hk = row / p.M % p.Hk, b = row / p.M / p.Hk;
+    T *out = x < all ? row_of<T>(p.dk, p.dk_stride, b, hk, j) : row_of<T>(p.dv, p.dv_stride, b, hk, j);
+#pragma unroll
+    for (int e = 0; e < W; ++e) out[y - row * p.D + e] = Elem<T>::down(sum[e]);
 }
 
 }  // namespace sdtw

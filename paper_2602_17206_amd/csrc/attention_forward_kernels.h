@@ -60,11 +60,12 @@ template <int DP> struct Running {
 };
 
 // Wavefronts on a SIMD that registers are kept for.
-template <typename T, int DP> constexpr int kForwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 3 : DP <= 64 ? 2 : 1) : DP <= 32 ? 4 : DP <= 64 ? 3 : 2;
+template <typename T, int DP, int F>
+constexpr int kForwardWaves = (sizeof(T) == 4 ? (DP <= 32 ? 4 : DP <= 64 ? 3 : 1) : DP <= 64 ? 4 : DP <= 96 ? 3 : 2) - (F & kCap && DP <= 96 ? 1 : 0);
 
 // 4 wavefronts of 32 rows each, one head of one sequence.
 template <typename T, int DP, int F>
-__global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward_kernel(AttentionParams p, BucketRule rule)
+__global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forward_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
     constexpr int SUBS = kKeys / 32;
@@ -74,11 +75,10 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
     __shared__ int shared[4][4];
     __shared__ __align__(16) int32_t documents[2][kKeys];
     constexpr int kTile = Shape::bytes(kKeys);  // (two tiles of keys, then two of values: one is read while the other is filled)
-    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
-    int64_t id = neighbours_together();
-    const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);  // (the last rows see the most keys of a causal sequence: they go first)
-    id /= p.row_tiles;
-    const int h = (int)(id % p.H), b = (int)(id / p.H), hk = h / (p.H / p.Hk);
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
+    const Place place(p.B * p.H);
+    const int rt = p.row_tiles - 1 - place.tile;  // (the last rows see the most keys of a causal sequence)
+    const int h = place.unit % p.H, b = place.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
@@ -143,10 +143,13 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
             for (int x = 0; x < SUBS; ++x) s[x] = along_features<T, DP>(ktile + Shape::bytes(x * 32), col, lane);
             bool open = j0 + kKeys <= from;
             if (DOCUMENTS) open = open && low == high && __all(document[lane] == low);
-            // scores that are products times a number, plus a number?
-            if (open && (!CAP || cap_out == 0.0f) && (!BIAS || bias.far(rule, j0 - base, j0 - base + 94))) {
-                run.take(s, scale2, BIAS ? bias.one : 0.0f);
+            // The scores are the products times a number, plus a number: or made so, by 1 and 0.
+            float factor = scale2, add = 0.0f;
+            const bool plain = open && (!CAP || cap_out == 0.0f) && (!BIAS || bias.far(rule, j0 - base, j0 - base + 94));
+            if (plain) {
+                if (BIAS) add = bias.one;
             } else {
+                factor = 1.0f;
 #pragma unroll
                 for (int x = 0; x < SUBS; ++x) {
                     scale_scores<CAP>(s[x], p);
@@ -166,8 +169,8 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP>)) void attention_forward
                         for (int r = 0; r < 16; ++r) s[x][r] = seen.at[r] ? s[x][r] : -INFINITY;
                     }
                 }
-                run.take(s, 1.0f, 0.0f);
             }
+            run.take(s, factor, add);
 #pragma unroll
             for (int x = 0; x < SUBS; ++x) along_rows<T, DP>(run.o, vtile + Shape::bytes(x * 32), Weights<T>(s[x]), lane);
         }
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     extern __shared__ __align__(16) char lds[];
     __shared__ float ref[4][32], tot[4][32];
     __shared__ __align__(16) int32_t documents[4][2][32];
-    const int thread = threadIdx.x, wave = thread / 64, lane = thread % 64, c = lane % 32, half = lane / 32;
+    const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
     // two tiles of keys and two of values for each wavefront, where there is room
     constexpr int kTile = Shape::bytes(32), kBuffers = kFewBuffers<T, DP>;
     char *const tiles_of = lds + wave * 2 * kBuffers * kTile;

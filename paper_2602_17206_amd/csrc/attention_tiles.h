@@ -96,7 +96,10 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     using Shape = TileShape<T, DP>;
     static constexpr int kEach = ROWS * Shape::kChunks / THREADS;
     static_assert(kEach * THREADS == ROWS * Shape::kChunks, "a tile is dealt out evenly");
-    uint32_t at[kEach];
+    // Where the threads take whole groups of eight rows a thread's places are one, kStep rows further on each time.
+    static constexpr int kStep = THREADS / Shape::kChunks;
+    static constexpr bool kOne = THREADS % Shape::kChunks == 0 && kStep % 8 == 0;
+    uint32_t at[kOne ? 1 : kEach];
     Rows<T> x;
     uint32_t row_bytes, last_bytes;
     __device__ __forceinline__ void begin(const Rows<T> &rows, int D, int who)
@@ -105,7 +108,7 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
         row_bytes = (uint32_t)x.row * (uint32_t)sizeof(T);
         last_bytes = (uint32_t)D * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) {
+        for (int k = 0; k < (kOne ? 1 : kEach); ++k) {
             const int id = who + k * THREADS, row = id / Shape::kChunks;
             const uint32_t f = (uint32_t)((id % Shape::kChunks) ^ Shape::turn(row)) * 16;
             at[k] = f < last_bytes ? (uint32_t)row * row_bytes + f : 0x7fffffffu;
@@ -114,10 +117,15 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     // rows first .. first + ROWS; zeros from `limit` on (first < limit)
     __device__ __forceinline__ void copy(char *tile, int first, int limit, int who) const
     {
-        const auto from = window(x.base + first * x.row, (uint32_t)min(limit - first, ROWS) * row_bytes - row_bytes + last_bytes);
         const uint32_t to = lds_address(tile) + (uint32_t)(who / 64) * 1024u;
+        const T *from = x.base + first * x.row;
+        const int rows = min(limit - first, ROWS);
 #pragma unroll
-        for (int k = 0; k < kEach; ++k) copy_to_lds(from, at[k], to + (uint32_t)k * (THREADS * 16u));
+        for (int k = 0; k < kEach; ++k) {
+            const int before = kOne ? k * kStep : 0;
+            const uint32_t bytes = rows > before ? (uint32_t)(rows - before) * row_bytes - row_bytes + last_bytes : 0;
+            copy_to_lds(window(from + before * x.row, bytes), at[kOne ? 0 : k], to + (uint32_t)k * (THREADS * 16u));
+        }
     }
 };
 
@@ -282,9 +290,10 @@ struct AttentionParams {
     int64_t q_stride[4], k_stride[4], v_stride[4], out_stride[4], dout_stride[4], dq_stride[4], dk_stride[4], dv_stride[4];
     int64_t table_stride[2];
     // how the work is split
-    int32_t row_tiles, key_tiles, splits, table_columns;
+    int32_t row_tiles, key_tiles, splits, parts, table_columns;
     float *part;                // [B, H, N, splits][D + 2]: unfinished sums, their reference and total
     float *delta;               // [B, H, N]
+    float *key_part;            // [parts][2][B, Hk, M, D]: parts of dk and dv
     float *table_part;          // [H, buckets][B * row_tiles]
     float *dtable;              // [H, buckets]
 };
@@ -297,6 +306,19 @@ template <typename T> __device__ __forceinline__ T *row_of(void *base, const int
 {
     return static_cast<T *>(base) + b * stride[0] + h * stride[1] + i * stride[2];
 }
+
+// The workgroup's tile and unit (head of a sequence): all units' first tiles come first, so that those with the most work begin early, and
+// where eight divides their number a unit's tiles are on one XCD (workgroups go round the eight of them), neighbouring units too.
+struct Place {
+    int tile, unit;
+    __device__ __forceinline__ explicit Place(int units)
+    {
+        const int x = blockIdx.x;
+        tile = x / units;
+        unit = x - tile * units;
+        if (units % 8 == 0) unit = unit % 8 * (units / 8) + unit / 8;
+    }
+};
 
 // What a sequence's rows see: row i the keys below limit(i) (of its document).
 struct Sight {
