@@ -109,7 +109,7 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
                 if constexpr ((F & kBias) != 0) {
                     if (dtable) {
                         p.table_columns = 32;
-                        auto need = [&] { return bytes + (size_t)4 * p.buckets * p.table_columns * sizeof(float); };
+                        auto need = [&] { return bytes + ((size_t)4 * p.buckets * p.table_columns + 512) * sizeof(float); };
                         while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
                         attention_rows_gradient_kernel<T, DP, F, true><<<grid, 256, need(), st>>>(p, rule);
                     }

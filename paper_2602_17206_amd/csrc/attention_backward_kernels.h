@@ -12,7 +12,18 @@
 
 namespace sdtw {
 
-// Times 1 - tanh^2, where `capped` holds the capped scores and `inverse` 1 over the cap, both in octaves; 0 without a cap.
+// Scores, capped, from products (or scaled, where this call has no cap).
+__device__ __forceinline__ void cap_scores(Acc &s, const AttentionParams &p, float scale)
+{
+    const float cap = p.cap;
+    if (cap != 0.0f) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = cap * tanh_fast(s[r] * p.cap_in);
+    } else {
+        s *= scale;
+    }
+}
+// Times 1 - tanh^2, where `capped` holds the capped scores and `inverse` is 1 over the cap; 0 without a cap.
 __device__ __forceinline__ void through_cap(Acc &x, const Acc &capped, float inverse)
 {
     const Acc t = capped * inverse;
@@ -50,26 +61,45 @@ template <int DP> struct ColumnScale<_Float16, DP> {
     __device__ __forceinline__ float undo() const { return by == 0.0f ? 0.0f : 1.0f / by; }
 };
 
-// The table's gradient of a wavefront's 32 rows, in LDS: [buckets][columns], the lanes c with the same c % columns share a place and take
-// turns (an addition in LDS is one instruction, and a wavefront's are carried out in the order of their issue).  Where all cells of a tile are in one bucket its sum stays in a register until the bucket changes.
+// The table's gradient of a wavefront's 32 rows, in LDS: [buckets][columns].  Where all cells of a tile are in one bucket its sum stays in a
+// register until the bucket changes.  Else the cells are added up by their diagonals first - the cells of a register lie on 32
+// different ones in each half, so that an addition in LDS has its place to itself - and then lane d adds diagonal d to its bucket, in a
+// column that it shares with the lanes d' = d (modulo columns), taking turns.  An addition in LDS is one instruction, and a
+// wavefront's are carried out in the order of their issue: the sums do not depend on chance.
 struct TableSum {
-    float *sum;
+    float *sum;       // [buckets][columns]
+    float *diagonal;  // [2][64], zeros between tiles
     int columns, bucket;  // bucket: of `running`
     float running;
-    __device__ __forceinline__ void turn(int lane, int u, float v)
+    static __device__ __forceinline__ void add(float *at, float v)
+    {
+        __hip_atomic_fetch_add(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    }
+    __device__ __forceinline__ void turns(int lane, int u, float v)
     {
         for (int first = 0; first < 64; first += columns) {
             wavefront_order();
-            if (lane / columns * columns == first)
-                __hip_atomic_fetch_add(sum + u * columns + lane % columns, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            if (lane >= first && lane < first + columns) add(sum + u * columns + lane - first, v);
         }
         wavefront_order();
     }
     __device__ __forceinline__ void flush(int lane)
     {
-        if (bucket >= 0) turn(lane, bucket, running);
+        if (bucket >= 0) turns(lane, bucket, running);
         bucket = -1;
         running = 0.0f;
+    }
+    // ds of 32 keys and 32 rows; `place`: the diagonal of register 0; `buckets`: of the 64 diagonals, in LDS
+    __device__ __forceinline__ void by_diagonals(const Acc &ds, int lane, int place, const uint8_t *buckets)
+    {
+        float *const at = diagonal + (lane >> 5) * 64 + place;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) add(at + tile_row(r, 0), ds[r]);
+        wavefront_order();
+        const float v = diagonal[lane] + diagonal[64 + lane];
+        diagonal[lane] = 0.0f;
+        diagonal[64 + lane] = 0.0f;
+        turns(lane, buckets[lane], v);
     }
 };
 
@@ -84,7 +114,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
 {
     using Shape = TileShape<T, DP>;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(256) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
     __shared__ __align__(16) int32_t documents[2][kKeys];
@@ -96,12 +126,12 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
-    if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
+    if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
     const int table_columns = TABLE ? p.table_columns : 0;
     float *const table_sums = reinterpret_cast<float *>(lds + 4 * kTile + bias_bytes(4));
-    TableSum table{table_sums + wave * p.buckets * table_columns, table_columns, -1, 0.0f};
+    TableSum table{table_sums + wave * p.buckets * table_columns, table_sums + 4 * p.buckets * table_columns + wave * 128, table_columns, -1, 0.0f};
     if (TABLE)
-        for (int x = thread; x < 4 * p.buckets * table_columns; x += 256) table_sums[x] = 0.0f;
+        for (int x = thread; x < 4 * p.buckets * table_columns + 512; x += 256) table_sums[x] = 0.0f;
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
     const int64_t place = ((int64_t)b * p.H + h) * p.N + i;
@@ -118,7 +148,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
     const int low = wave_min_i32(valid ? doc : 0x7fffffff), high = wave_max_i32(valid ? doc : -1);
     // (a row that sees nothing has no p: 2^(score - inf))
     float lse = valid ? p.lse[place] : -INFINITY;
-    lse = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (lse == -INFINITY) lse = INFINITY;
     Column<T, DP> q, dout;
     {
         const Rows<T> x = rows_of<T>(p.q, p.q_stride, b, h), y = rows_of<T>(p.dout, p.dout_stride, b, h);
@@ -146,7 +176,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
     ColumnScale<T, DP> fit;
-    const float inverse_cap = CAP && p.cap_out != 0.0f ? 1.0f / p.cap_out : 0.0f;
+    const float inverse_cap = CAP && p.cap != 0.0f ? 1.0f / p.cap : 0.0f, scale = p.scale;
     TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
@@ -185,8 +215,14 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
                 bool open = j0 + 32 <= from;
                 if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(kt, q, lane);
-                scale_scores<CAP>(s, p);
-                const Acc capped = s;
+                Acc capped;
+                if (CAP) {
+                    cap_scores(s, p, scale);
+                    capped = s;
+                }
+                // (the difference first: what is left to round is small)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - lse : fmaf(s[r], scale, -lse);
                 if (BIAS) {
                     bias.look(rule, j0 - base, lane);
                     if (bias.same) {
@@ -198,7 +234,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
                     }
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - lse);
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
                 if (!open) {
                     const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
 #pragma unroll
@@ -221,16 +257,14 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
                         float sum = s[0];
 #pragma unroll
                         for (int r = 1; r < 16; ++r) sum += s[r];
-                        table.running += valid ? sum : 0.0f;
+                        table.running += sum;
                     } else {
-                        const uint8_t *at = bias.bucket + 31 - c + 4 * half;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) table.turn(lane, at[tile_row(r, 0)], valid ? s[r] : 0.0f);
+                        table.by_diagonals(s, lane, 31 - c + 4 * half, bias.bucket);
                     }
                 }
                 if (CAP) through_cap(s, capped, inverse_cap);
                 fit.fit(s, dq);
-                along_rows<T, DP>(dq, kt, Weights<T>(s), lane);
+                along_rows_twice<T, DP>(dq, kt, s, lane);
             }
         }
         if (TABLE && pass == 0) {
@@ -275,7 +309,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
 {
     using Shape = TileShape<T, DP>;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(256) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
     __shared__ __align__(16) float row_lse[2][kKeys], row_delta[2][kKeys];
@@ -313,7 +347,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
     ColumnScale<T, DP> fit;
-    const float inverse_cap = CAP && p.cap_out != 0.0f ? 1.0f / p.cap_out : 0.0f;
+    const float inverse_cap = CAP && p.cap != 0.0f ? 1.0f / p.cap : 0.0f, scale = p.scale;
     constexpr float kWeight = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;  // p <= 1 (to rounding) into float16's upper octaves
     TileWalk<DOCUMENTS> walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> qs, ds;
@@ -329,7 +363,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
         walk.tiles = from_tile + (int)min(share_end - (int64_t)g * each, (int64_t)each);
         __syncthreads();
         WaveBias bias{};
-        if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
+        if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
         const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
         qs.begin(rows_of<T>(p.q, p.q_stride, b, h), p.loaded, thread);
         ds.begin(rows_of<T>(p.dout, p.dout_stride, b, h), p.loaded, thread);
@@ -340,7 +374,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                 const int i = t * kKeys + thread, d = i >= end ? -1 : row_document ? row_document[i] : 0;
                 const float x = d >= 0 ? lse[i] : -INFINITY;
                 row_doc[buffer][thread] = d;
-                row_lse[buffer][thread] = x == -INFINITY ? INFINITY : x * kLog2e;
+                row_lse[buffer][thread] = x == -INFINITY ? INFINITY : x;
                 row_delta[buffer][thread] = d >= 0 ? delta[i] : 0.0f;
             }
         };
@@ -367,8 +401,14 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                 bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
                 if (DOCUMENTS) open = open && low == high && __all(row_doc[now][sub * 32 + c] == low);
                 Acc s = along_features<T, DP>(qt, k, lane);
-                scale_scores<CAP>(s, p);
-                const Acc capped = s;
+                Acc capped;
+                if (CAP) {
+                    cap_scores(s, p, scale);
+                    capped = s;
+                }
+                const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - at_lse[tile_row(r, 0)] : fmaf(s[r], scale, -at_lse[tile_row(r, 0)]);
                 if (BIAS) {
                     bias.look(rule, first_key - (i0 + 31) - sight.offset, lane);
                     if (bias.same) {
@@ -379,9 +419,8 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                         for (int r = 0; r < 16; ++r) s[r] += at[-tile_row(r, 0)];
                     }
                 }
-                const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] - at_lse[tile_row(r, 0)]);
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
                 Acc dp = along_features<T, DP>(dt, v, lane);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - at_delta[tile_row(r, 0)]);

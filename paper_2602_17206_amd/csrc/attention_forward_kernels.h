@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     using Shape = TileShape<T, DP>;
     constexpr int SUBS = kKeys / 32;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(256) char lds[];
     __shared__ uint64_t live[4];
     __shared__ int shared[4][4];
     __shared__ __align__(16) int32_t documents[2][kKeys];
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
     WaveBias bias{};
-    if (BIAS) bias = begin_bias(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
+    if (BIAS) bias = begin_bias<true>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
     bool valid = i < sight.rows;
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
 {
     using Shape = TileShape<T, DP>;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
-    extern __shared__ __align__(16) char lds[];
+    extern __shared__ __align__(256) char lds[];
     __shared__ float ref[4][32], tot[4][32];
     __shared__ __align__(16) int32_t documents[4][2][32];
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     if (BIAS) {
         for (int u = thread; u < min(G, 32) * p.buckets; u += 256) {
             const int head = hk * G + (first_head + u / p.buckets) % G;
-            values[u] = octaves_of_entry(load_typed(p.table, head * p.table_stride[0] + u % p.buckets * p.table_stride[1], p.table_type));
+            values[u] = entry_of<true>(load_typed(p.table, head * p.table_stride[0] + u % p.buckets * p.table_stride[1], p.table_type));
         }
         for (int u = thread; u <= rule.m; u += 256) starts[u] = rule.start[u];
         __syncthreads();

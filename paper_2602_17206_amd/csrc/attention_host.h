@@ -99,6 +99,7 @@ inline AttentionParams attention_params(const sdtw_attention_desc *d, const sdtw
     p.prefix = (int32_t)std::min<int64_t>(d->prefix, 1 << 29);
     p.scale = d->scale;
     p.scale2 = d->scale * kLog2e;
+    p.cap = d->cap;
     if (d->cap > 0.0f) p.cap_in = d->scale / d->cap, p.cap_out = d->cap * kLog2e;
     if (lists) {
         p.offsets = lists->offsets; p.prefixes = lists->prefixes;

@@ -48,18 +48,20 @@ __device__ __forceinline__ int wave_max_i32(int v)
 
 // ------------------------------------------------------------------ tiles in LDS
 
-// Rows of DP features (D and zeros behind it) without gaps, as memory is copied into LDS 64 chunks of 16 bytes at a time.  Within a row
-// the chunks change places, chunk ch to ch ^ turn(row): so that neighbouring rows' chunks of one number fall into different banks,
-// and so do two neighbouring chunks of four rows, for the two kinds of reads.
+// Rows of DP features (D and zeros behind it) without gaps, as memory is copied into LDS 64 chunks of 16 bytes at a time; a tile begins at
+// a multiple of 256 bytes.  Within a row the chunks change places, chunk ch to ch ^ turn(row), so that what a read wants at once lies in
+// different ones of the 16 chunks that the 64 banks hold: of 16 bytes a lane, rows 0-3, 12-15, 20-23 and 24-27 (and so on), which
+// bits 2 and 3 of the row tell apart beside the lowest two; of the transposing read, four neighbouring chunks of four rows.
 template <typename T, int DP> struct TileShape {
     static constexpr int W = Elem<T>::kWidth;
     static constexpr int kChunks = DP / W;  // 16-byte chunks of a row
     static constexpr int kStride = DP * (int)sizeof(T);
-    static constexpr bool kEight = kChunks % 8 == 0;  // places change among eight chunks, else among four
+    static constexpr int kMask = kChunks % 16 == 0 ? 15 : kChunks % 8 == 0 ? 7 : 3;  // places change among so many chunks, plus one
     static constexpr int bytes(int rows) { return rows * kStride; }
     static __device__ __forceinline__ constexpr int turn(int row)
     {
-        return kEight ? (row & 3) << 1 | (row >> 2 & 1) : (row & 2) | (row >> 2 & 1);
+        const int low = (row >> 2 & 1) | (row >> 3 & 1) << 1;
+        return kMask == 15 ? (row & 3) << 2 | low : kMask == 7 ? (row >> 1 & 1) << 2 | low : low;
     }
 };
 
@@ -96,9 +98,9 @@ template <typename T, int DP, int ROWS, int THREADS> struct Stage {
     using Shape = TileShape<T, DP>;
     static constexpr int kEach = ROWS * Shape::kChunks / THREADS;
     static_assert(kEach * THREADS == ROWS * Shape::kChunks, "a tile is dealt out evenly");
-    // Where the threads take whole groups of eight rows a thread's places are one, kStep rows further on each time.
+    // Where the threads take whole groups of sixteen rows a thread's places are one, kStep rows further on each time.
     static constexpr int kStep = THREADS / Shape::kChunks;
-    static constexpr bool kOne = THREADS % Shape::kChunks == 0 && kStep % 8 == 0;
+    static constexpr bool kOne = THREADS % Shape::kChunks == 0 && kStep % 16 == 0;
     uint32_t at[kOne ? 1 : kEach];
     Rows<T> x;
     uint32_t row_bytes, last_bytes;
@@ -171,18 +173,23 @@ template <typename T> __device__ __forceinline__ void mma(Acc &acc, const Bits4 
     }
 }
 
-// S = X R for the 32 rows of `tile` (which begins at a multiple of 8 rows)
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t address, int offset)
+{
+    typedef __attribute__((address_space(3))) const char Byte;
+    typedef __attribute__((address_space(3))) const V Value;
+    return *(Value *)((Byte *)(uintptr_t)address + offset);
+}
+
+// S = X R for the 32 rows of `tile`
 template <typename T, int DP> __device__ __forceinline__ Acc along_features(const char *tile, const Column<T, DP> &col, int lane)
 {
     using Shape = TileShape<T, DP>;
-    constexpr int kTurns = Shape::kEight ? 7 : 3;
-    const int row = lane & 31, turn = (lane >> 5) ^ Shape::turn(row);  // (chunk 2 s + half; half is its lowest bit)
+    const int row = lane & 31;
+    const uint32_t at = lds_address(tile) + (uint32_t)(row * Shape::kStride + ((lane >> 5) ^ Shape::turn(row)) * 16);  // chunk 2 s + half
     Acc acc = {};
 #pragma unroll
-    for (int s = 0; s < Column<T, DP>::kSteps; ++s) {
-        const char *at = tile + (row * Shape::kStride + (turn ^ (2 * s & kTurns)) * 16);
-        mma<T>(acc, *reinterpret_cast<const Bits4 *>(at + (2 * s & ~kTurns) * 16), col.v[s]);
-    }
+    for (int s = 0; s < Column<T, DP>::kSteps; ++s)
+        mma<T>(acc, lds_read<Bits4>(at ^ (uint32_t)(2 * s & Shape::kMask) * 16, (2 * s & ~Shape::kMask) * 16), col.v[s]);
     return acc;
 }
 
@@ -207,41 +214,61 @@ typedef short Short4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) Short4 LdsShort4;
 
 // O += X^T P: feature 32 ft + tile_row(r, half) of the column in register r of acc[ft]
-template <typename T, int DP> __device__ __forceinline__ void along_rows(Acc (&acc)[DP / 32], const char *tile, const Weights<T> &w, int lane)
+// (`more`: other weights whose products are added as well)
+template <typename T, int DP>
+__device__ __forceinline__ void along_rows(Acc (&acc)[DP / 32], const char *tile, const Weights<T> &w, int lane, const Weights<T> *more = nullptr)
 {
     using Shape = TileShape<T, DP>;
-    constexpr int kStride = Shape::kStride;
+    constexpr int kStride = Shape::kStride, kMask = Shape::kMask;
     const int half = lane >> 5;
     if constexpr (std::is_same<T, float>::value) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            const char *at = tile + ((4 * half + (r & 3)) * kStride + ((((lane & 31) >> 2) ^ half ^ (r & 3) << 1) * 16 + (lane & 3) * 4));
+            const int row = 4 * half + (r & 3);  // (of the row, 8 (r / 4) is left out: it moves bit 1 of the place)
+            const uint32_t at = lds_address(tile) + (uint32_t)(row * kStride + (((lane & 31) >> 2) ^ Shape::turn(row)) * 16 + (lane & 3) * 4);
 #pragma unroll
             for (int ft = 0; ft < DP / 32; ++ft) {
-                const float x = *reinterpret_cast<const float *>(at + 8 * (r >> 2) * kStride + ft * 128);
+                const float x = lds_read<float>(at ^ (uint32_t)((ft * 8 & kMask) ^ (r >> 2 & 1) << 1) * 16, 8 * (r >> 2) * kStride + (ft * 8 & ~kMask) * 16);
                 acc[ft] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, w.v[r], acc[ft], 0, 0, 0);
             }
         }
     } else {
         // ds_read_b64_tr_b16: sixteen lanes read 4 rows of 16 elements, four elements a lane, and each gets a column of them
         const int row = 4 * half + (lane >> 2 & 3), chunk = (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+        const uint32_t at = lds_address(tile) + (uint32_t)(row * kStride + (chunk ^ Shape::turn(row)) * 16 + (lane & 1) * 8);
+        typedef __attribute__((address_space(3))) char Byte;
 #pragma unroll
-        for (int ft = 0; ft < DP / 32; ++ft) {
-            const int place = (chunk ^ Shape::turn(row)) ^ (Shape::kEight ? ft * 4 & 7 : 0);
-            const char *at = tile + (row * kStride + place * 16 + (lane & 1) * 8) + (Shape::kEight ? ft * 4 & ~7 : ft * 4) * 16;
+        for (int ft = 0; ft < DP / 32; ++ft)
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 Bits4 a;
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    const Short4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsShort4 *)(at + (16 * s + 8 * q) * kStride));
+                    const uint32_t place = at ^ (uint32_t)((ft * 4 & kMask) ^ q << 1) * 16;
+                    const Short4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (LdsShort4 *)((Byte *)(uintptr_t)place + (16 * s + 8 * q) * kStride + (ft * 4 & ~kMask) * 16));
                     const uint64_t bits = __builtin_bit_cast(uint64_t, x);
                     a[2 * q] = (uint32_t)bits;
                     a[2 * q + 1] = (uint32_t)(bits >> 32);
                 }
                 mma<T>(acc[ft], a, w.v[s]);
+                if (more) mma<T>(acc[ft], a, more->v[s]);
             }
-        }
+    }
+}
+
+// The same with P to twice the type's digits, as the sum of two numbers of the type: the tile's reads serve both.
+template <typename T, int DP> __device__ __forceinline__ void along_rows_twice(Acc (&acc)[DP / 32], const char *tile, const Acc &p, int lane)
+{
+    if constexpr (std::is_same<T, float>::value) {
+        along_rows<T, DP>(acc, tile, Weights<T>(p), lane);
+    } else {
+        const Weights<T> w(p);
+        Acc rest;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) rest[r] = p[r] - Elem<T>::at(w.v[r / 8], r % 8);
+        const Weights<T> v(rest);
+        along_rows<T, DP>(acc, tile, w, lane, &v);
     }
 }
 
@@ -282,7 +309,7 @@ struct AttentionParams {
     int32_t buckets, table_type, causal;
     int32_t offset, prefix;
     float scale, scale2;        // of the products; times log2(e)
-    float cap_in, cap_out;      // scale / cap and cap log2(e); cap_out 0: no cap
+    float cap, cap_in, cap_out; // 0: no cap; scale / cap; cap log2(e)
     const void *q, *k, *v, *table, *dout;
     void *out, *dq, *dk, *dv;
     float *lse;                 // [B, H, N]
@@ -350,11 +377,11 @@ __device__ __forceinline__ float tanh_fast(float x)
 }
 
 // An entry below -1e30 forbids its cells, as -inf does.
-__device__ __forceinline__ float octaves_of_entry(float v) { return v < -1e30f ? -INFINITY : v * kLog2e; }
+template <bool OCTAVES> __device__ __forceinline__ float entry_of(float v) { return v < -1e30f ? -INFINITY : OCTAVES ? v * kLog2e : v; }
 
 // The bias of 32 x 32 cells (or of the cells of one key and one row): what a wavefront knows of the 63 diagonals of its tile.
 struct WaveBias {
-    const float *values;     // LDS: the head's entries, in octaves
+    const float *values;     // LDS: the head's entries
     const int32_t *starts;   // LDS
     float *diagonal;         // LDS, 64 of the wavefront's own
     uint8_t *bucket;         // LDS, 64 of the wavefront's own
@@ -393,7 +420,8 @@ struct WaveBias {
 constexpr int kBiasStarts = (kMaxBuckets / 2 + 1 + 3) / 4 * 4;
 constexpr int bias_bytes(int waves) { return kMaxBuckets * 4 + kBiasStarts * 4 + waves * 64 * 5; }
 
-// Lays the bias's part of LDS out and fills it; a barrier has to follow.
+// Lays the bias's part of LDS out and fills it; a barrier has to follow.  OCTAVES: the entries times log2(e).
+template <bool OCTAVES>
 __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const BucketRule &rule, char *lds, int h, int wave, int waves, int thread,
                                                int threads)
 {
@@ -403,7 +431,7 @@ __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const B
     uint8_t *bucket = reinterpret_cast<uint8_t *>(diagonal + 64 * waves);
     if (p.buckets) {
         for (int u = thread; u < p.buckets; u += threads)
-            values[u] = octaves_of_entry(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
+            values[u] = entry_of<OCTAVES>(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
         for (int k = thread; k <= rule.m; k += threads) starts[k] = rule.start[k];
     }
     return WaveBias{values, starts, diagonal + 64 * wave, bucket + 64 * wave, rule.first(rule.n - 1), 0.0f, 0, true};
