@@ -79,6 +79,7 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
     p.dq = dq; p.dk = dk; p.dv = dv;
     p.dtable = dtable;
     p.row_tiles = (int32_t)P.row_tiles;
+    p.near = near_diagonals(desc, rule);
     p.key_tiles = (int32_t)P.key_tiles;
     p.delta = static_cast<float *>(workspace);
     p.parts = (int32_t)P.parts;
@@ -102,19 +103,23 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
         constexpr int DP = decltype(features)::value;
         with_variant(desc, lists, [&](auto variant) {
             constexpr int F = decltype(variant)::value;
-            const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
-            if (rows) {
-                ProfScope ps("attention_rows_gradient", st);
-                const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
+            const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4, p.near);
+            const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
+            if (rows && dtable) {
                 if constexpr ((F & kBias) != 0) {
-                    if (dtable) {
-                        p.table_columns = 32;
-                        auto need = [&] { return bytes + ((size_t)4 * p.buckets * p.table_columns + 512) * sizeof(float); };
-                        while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
-                        attention_rows_gradient_kernel<T, DP, F, true><<<grid, 256, need(), st>>>(p, rule);
+                    {
+                        ProfScope ps("attention_delta", st);
+                        attention_rows_gradient_kernel<T, DP, F, kRowsDelta><<<grid, 256, bytes, st>>>(p, rule);
                     }
+                    ProfScope ps("attention_rows_gradient", st);
+                    p.table_columns = 32;
+                    auto need = [&] { return bytes + ((size_t)4 * p.buckets * p.table_columns + 512) * sizeof(float); };
+                    while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
+                    attention_rows_gradient_kernel<T, DP, F, kRowsTable><<<grid, 256, need(), st>>>(p, rule);
                 }
-                if (!dtable) attention_rows_gradient_kernel<T, DP, F, false><<<grid, 256, bytes, st>>>(p, rule);
+            } else if (rows) {
+                ProfScope ps("attention_rows_gradient", st);
+                attention_rows_gradient_kernel<T, DP, F, kRowsPlain><<<grid, 256, bytes, st>>>(p, rule);
             }
             if (keys) {
                 ProfScope ps("attention_keys_gradient", st);

@@ -12,17 +12,6 @@
 
 namespace sdtw {
 
-// Scores, capped, from products (or scaled, where this call has no cap).
-__device__ __forceinline__ void cap_scores(Acc &s, const AttentionParams &p, float scale)
-{
-    const float cap = p.cap;
-    if (cap != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = cap * tanh_fast(s[r] * p.cap_in);
-    } else {
-        s *= scale;
-    }
-}
 // Times 1 - tanh^2, where `capped` holds the capped scores and `inverse` is 1 over the cap; 0 without a cap.
 __device__ __forceinline__ void through_cap(Acc &x, const Acc &capped, float inverse)
 {
@@ -104,15 +93,18 @@ struct TableSum {
 };
 
 // Wavefronts on a SIMD that registers are kept for.
+template <typename T, int DP> constexpr int kDeltaWaves = sizeof(T) == 4 ? (DP <= 32 ? 4 : DP <= 64 ? 2 : 1) : DP <= 64 ? 4 : 3;
 template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : DP <= 96 || !MORE ? 2 : 1;
 
-// 4 wavefronts of 32 rows each, one head of one sequence.  TABLE: the table's gradient is wanted.  delta comes from the rows' outputs -
-// sum_j p dp = <dout, out> - unless the table's gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals
-// would show the rounding of a 16-bit `out`; so the keys are walked over once more, for delta alone.
-template <typename T, int DP, int F, bool TABLE>
-__global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
+// 4 wavefronts of 32 rows each, one head of one sequence.  delta comes from the rows' outputs - sum_j p dp = <dout, out> - unless the table's
+// gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals would show the rounding of a 16-bit `out`; then
+// the keys are walked over once more beforehand, for delta alone.
+enum { kRowsPlain, kRowsDelta, kRowsTable };
+template <typename T, int DP, int F, int WORK>
+__global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBackwardWaves<T, DP, WORK == kRowsTable>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr bool TABLE = WORK == kRowsTable;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(256) char lds[];
     __shared__ uint64_t live[4];
@@ -125,10 +117,10 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
     const int h = at_work.unit % p.H, b = at_work.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias{};
+    WaveBias bias;
     if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
     const int table_columns = TABLE ? p.table_columns : 0;
-    float *const table_sums = reinterpret_cast<float *>(lds + 4 * kTile + bias_bytes(4));
+    float *const table_sums = reinterpret_cast<float *>(lds + 4 * kTile + bias_bytes(4, p.near));
     TableSum table{table_sums + wave * p.buckets * table_columns, table_sums + 4 * p.buckets * table_columns + wave * 128, table_columns, -1, 0.0f};
     if (TABLE)
         for (int x = thread; x < 4 * p.buckets * table_columns + 512; x += 256) table_sums[x] = 0.0f;
@@ -156,7 +148,8 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
         dout.load(y.base + i * y.row, p.loaded, valid, half);
     }
     float delta = 0.0f;
-    if (!TABLE) {
+    if (TABLE && valid) delta = p.delta[place];
+    if (WORK == kRowsPlain) {
         const Rows<T> x = rows_of<T>(p.out, p.out_stride, b, h);
         Column<T, DP> out;
         out.load(x.base + i * x.row, p.loaded, valid, half);
@@ -188,89 +181,87 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, TABLE>)) void attention
         if (DOCUMENTS && thread < kKeys)
             documents[buffer][thread] = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
     };
-#pragma unroll 1
-    for (int pass = TABLE ? 0 : 1; pass < 2; ++pass) {
-        int t = walk.next(0), buffer = 0;
-        __syncthreads();  // (the tiles of the pass before are not read any more)
-        if (t < walk.tiles) fetch(t, 0);
-        while (t < walk.tiles) {
-            const int first = t * kKeys;
-            char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
-            const int32_t *const document = documents[buffer];
-            copies_done();
+    int t = walk.next(0), buffer = 0;
+    if (t < walk.tiles) fetch(t, 0);
+    while (t < walk.tiles) {
+        const int first = t * kKeys;
+        char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
+        const int32_t *const document = documents[buffer];
+        copies_done();
+        __syncthreads();
+        if (DOCUMENTS && __any(document[lane] < 0)) {
+            clear_rows<T, DP, kKeys, 256>(ktile, document, thread);
+            clear_rows<T, DP, kKeys, 256>(vtile, document, thread);
             __syncthreads();
-            if (DOCUMENTS && __any(document[lane] < 0)) {
-                clear_rows<T, DP, kKeys, 256>(ktile, document, thread);
-                clear_rows<T, DP, kKeys, 256>(vtile, document, thread);
-                __syncthreads();
-            }
-            t = walk.next(t + 1);
-            buffer ^= 1;
-            if (t < walk.tiles) fetch(t, buffer);
+        }
+        t = walk.next(t + 1);
+        buffer ^= 1;
+        if (t < walk.tiles) fetch(t, buffer);
 #pragma unroll 1
-            for (int sub = 0; sub < kKeys / 32; ++sub) {
-                const int j0 = first + sub * 32;
-                const char *const kt = ktile + Shape::bytes(sub * 32), *const vt = vtile + Shape::bytes(sub * 32);
-                if (j0 >= to) break;
-                bool open = j0 + 32 <= from;
-                if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
-                Acc s = along_features<T, DP>(kt, q, lane);
-                Acc capped;
-                if (CAP) {
-                    cap_scores(s, p, scale);
-                    capped = s;
-                }
-                // (the difference first: what is left to round is small)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - lse : fmaf(s[r], scale, -lse);
-                if (BIAS) {
-                    bias.look(rule, j0 - base, lane);
-                    if (bias.same) {
-                        s += bias.one;
-                    } else {
-                        const float *at = bias.diagonal + 31 - c + 4 * half;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] += at[tile_row(r, 0)];
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
-                if (!open) {
-                    const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
-                }
-                const Acc dp = along_features<T, DP>(vt, dout, lane);
-                if (TABLE && pass == 0) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
-                    continue;
-                }
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
-                if (TABLE) {
-                    if (bias.same) {
-                        if (bias.one_bucket != table.bucket) {
-                            table.flush(lane);
-                            table.bucket = bias.one_bucket;
-                        }
-                        float sum = s[0];
-#pragma unroll
-                        for (int r = 1; r < 16; ++r) sum += s[r];
-                        table.running += sum;
-                    } else {
-                        table.by_diagonals(s, lane, 31 - c + 4 * half, bias.bucket);
-                    }
-                }
-                if (CAP) through_cap(s, capped, inverse_cap);
-                fit.fit(s, dq);
-                along_rows_twice<T, DP>(dq, kt, s, lane);
+        for (int sub = 0; sub < kKeys / 32; ++sub) {
+            const int j0 = first + sub * 32;
+            const char *const kt = ktile + Shape::bytes(sub * 32), *const vt = vtile + Shape::bytes(sub * 32);
+            if (j0 >= to) break;
+            bool open = j0 + 32 <= from;
+            if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
+            Acc s = along_features<T, DP>(kt, q, lane);
+            Acc capped;
+            if (CAP) {
+                if (p.cap != 0.0f) cap_scores(s, p.cap_in, p.cap);
+                else s *= scale;
+                capped = s;
             }
+            // (the difference first: what is left to round is small)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - lse : fmaf(s[r], scale, -lse);
+            if (BIAS) {
+                bias.look(rule, j0 - base, lane);
+                if (bias.same) {
+                    s += bias.one;
+                } else {
+                    const float *at = bias.at + 31 - c + 4 * half;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] += at[tile_row(r, 0)];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
+            if (!open) {
+                const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
+            }
+            const Acc dp = along_features<T, DP>(vt, dout, lane);
+            if (WORK == kRowsDelta) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
+                continue;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+            if (TABLE) {
+                if (bias.same) {
+                    if (bias.one_bucket != table.bucket) {
+                        table.flush(lane);
+                        table.bucket = bias.one_bucket;
+                    }
+                    float sum = s[0];
+#pragma unroll
+                    for (int r = 1; r < 16; ++r) sum += s[r];
+                    table.running += sum;
+                } else {
+                    table.by_diagonals(s, lane, 31 - c + 4 * half, bias.at_bucket);
+                }
+            }
+            if (CAP) through_cap(s, capped, inverse_cap);
+            fit.fit(s, dq);
+            along_rows_twice<T, DP>(dq, kt, s, lane);
         }
-        if (TABLE && pass == 0) {
-            delta = both_sum(delta);
-            if (half == 0 && i < p.N) p.delta[place] = delta;
-        }
+    }
+    if (WORK == kRowsDelta) {
+        delta = both_sum(delta);
+        if (half == 0 && i < p.N) p.delta[place] = delta;
+        return;
     }
     if (i < p.N) {
         if (!valid) {
@@ -362,7 +353,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
         const int first_tile = from_tile + (int)max(share_begin - (int64_t)g * each, (int64_t)0);
         walk.tiles = from_tile + (int)min(share_end - (int64_t)g * each, (int64_t)each);
         __syncthreads();
-        WaveBias bias{};
+        WaveBias bias;
         if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
         const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
         qs.begin(rows_of<T>(p.q, p.q_stride, b, h), p.loaded, thread);
@@ -403,7 +394,8 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                 Acc s = along_features<T, DP>(qt, k, lane);
                 Acc capped;
                 if (CAP) {
-                    cap_scores(s, p, scale);
+                    if (p.cap != 0.0f) cap_scores(s, p.cap_in, p.cap);
+                    else s *= scale;
                     capped = s;
                 }
                 const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
@@ -414,7 +406,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                     if (bias.same) {
                         s += bias.one;
                     } else {
-                        const float *at = bias.diagonal + 31 + c - 4 * half;
+                        const float *at = bias.at + 31 + c - 4 * half;
 #pragma unroll
                         for (int r = 0; r < 16; ++r) s[r] += at[-tile_row(r, 0)];
                     }

@@ -84,6 +84,7 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
     p.out = out;
     p.lse = lse;
     p.row_tiles = (int32_t)P.row_tiles;
+    p.near = near_diagonals(desc, rule);
     p.splits = (int32_t)P.splits;
     p.part = static_cast<float *>(workspace);
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -101,7 +102,7 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
                 attention_few_rows_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, few_rows_lds(desc), st>>>(p, rule);
             } else {
                 ProfScope ps("attention_forward", st);
-                const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4);
+                const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4, p.near);
                 attention_forward_kernel<T, DP, F><<<(unsigned)P.workgroups, 256, bytes, st>>>(p, rule);
             }
         });

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     const int h = place.unit % p.H, b = place.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias{};
+    WaveBias bias;
     if (BIAS) bias = begin_bias<true>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
                         if (bias.same) {
                             s[x] += bias.one;
                         } else {
-                            const float *at = bias.diagonal + 31 - c + 4 * half;
+                            const float *at = bias.at + 31 - c + 4 * half;
 #pragma unroll
                             for (int r = 0; r < 16; ++r) s[x][r] += at[tile_row(r, 0)];
                         }
@@ -187,10 +187,9 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
 }
 
 // LDS of the kernel below: its wavefronts' tiles, or their sums, [4][32][DP + 4].
-template <typename T, int DP> constexpr int kFewBuffers = TileShape<T, DP>::bytes(32) <= 8192 ? 2 : 1;
 template <typename T, int DP> constexpr int few_rows_bytes()
 {
-    const int tiles = 4 * 2 * kFewBuffers<T, DP> * TileShape<T, DP>::bytes(32), sums = 4 * 32 * (DP + 4) * 4;
+    const int tiles = 4 * 2 * TileShape<T, DP>::bytes(32), sums = 4 * 32 * (DP + 4) * 4;
     return tiles > sums ? tiles : sums;
 }
 
@@ -204,11 +203,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(256) char lds[];
     __shared__ float ref[4][32], tot[4][32];
-    __shared__ __align__(16) int32_t documents[4][2][32];
+    __shared__ __align__(16) int32_t documents[4][32];
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
-    // two tiles of keys and two of values for each wavefront, where there is room
-    constexpr int kTile = Shape::bytes(32), kBuffers = kFewBuffers<T, DP>;
-    char *const tiles_of = lds + wave * 2 * kBuffers * kTile;
+    constexpr int kTile = Shape::bytes(32);
+    char *const ktile = lds + wave * 2 * kTile, *const vtile = ktile + kTile;
     int64_t id = neighbours_together();
     const int split = (int)(id % p.splits);
     id /= p.splits;
@@ -255,33 +253,32 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     Stage<T, DP, 32, 64> ks, vs;
     ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, lane);
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, lane);
-    auto fetch = [&](int t, int buffer) {
-        const int j = t * 128 + wave * 32;
-        if (j >= to) return;
-        ks.copy(tiles_of + buffer * 2 * kTile, j, to, lane);
-        vs.copy(tiles_of + (buffer * 2 + 1) * kTile, j, to, lane);
-        if (DOCUMENTS && half == 0) documents[wave][buffer][c] = j + c >= to ? -1 : col_document ? col_document[j + c] : 0;
-    };
-    if (kBuffers == 2 && begin < end) fetch(begin, 0);
+    // The next keys are asked for as soon as the products with these are done, the next values likewise: half of a wavefront's share of LDS
+    // is always on its way.
+    auto fetch_keys = [&](int t) { if (t < end && t * 128 + wave * 32 < to) ks.copy(ktile, t * 128 + wave * 32, to, lane); };
+    auto fetch_values = [&](int t) { if (t < end && t * 128 + wave * 32 < to) vs.copy(vtile, t * 128 + wave * 32, to, lane); };
+    fetch_keys(begin);
+    fetch_values(begin);
     for (int t = begin; t < end; ++t) {
-        const int j0 = t * 128 + wave * 32, buffer = kBuffers == 2 ? (t - begin) & 1 : 0;
-        char *const ktile = tiles_of + buffer * 2 * kTile, *const vtile = ktile + kTile;
-        wavefront_order();
-        if (kBuffers == 1) {
+        const int j0 = t * 128 + wave * 32;
+        if (j0 >= to) break;
+        int doc_here = 0;
+        if (DOCUMENTS) {
+            doc_here = j0 + c >= to ? -1 : col_document ? col_document[j0 + c] : 0;
+            if (half == 0) documents[wave][c] = doc_here;
             copies_done();
-            fetch(t, 0);
-        }
-        copies_done();
-        wavefront_order();
-        if (kBuffers == 2 && t + 1 < end) fetch(t + 1, buffer ^ 1);
-        if (j0 >= to) continue;
-        if (DOCUMENTS && __any(documents[wave][buffer][c] < 0)) {
-            clear_rows<T, DP, 32, 64>(ktile, documents[wave][buffer], lane);
-            clear_rows<T, DP, 32, 64>(vtile, documents[wave][buffer], lane);
+            if (__any(doc_here < 0)) {
+                clear_rows<T, DP, 32, 64>(ktile, documents[wave], lane);
+                clear_rows<T, DP, 32, 64>(vtile, documents[wave], lane);
+            }
             wavefront_order();
+        } else {
+            copies_left<decltype(vs)::kEach>();  // (the values may still be on their way)
         }
         Acc scores[1] = {along_features<T, DP>(ktile, col, lane)};
         Acc &s = scores[0];
+        reads_done();
+        fetch_keys(t + 1);
         scale_scores<CAP>(s, p);
         if (BIAS) {
             const int near = j0 - i - sight.offset;
@@ -294,12 +291,16 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
             }
         }
         if (DOCUMENTS || j0 + 32 > from) {
-            const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents[wave][buffer], doc, half);
+            const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, documents[wave], doc, half);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : -INFINITY;
         }
         run.take(scores, 1.0f, 0.0f);
+        if (t + 1 < end && j0 + 128 < to) copies_left<decltype(ks)::kEach>();
+        else copies_left<0>();
         along_rows<T, DP>(run.o, vtile, Weights<T>(s), lane);
+        reads_done();
+        fetch_values(t + 1);
     }
     const float total = both_sum(run.l);
     if (half == 0) ref[wave][c] = run.m, tot[wave][c] = total;

@@ -146,6 +146,16 @@ inline void pack(const sdtw_attention_desc *d, const void *&x, int64_t (&stride)
     stride[3] = 1; stride[2] = loaded; stride[1] = loaded * rows; stride[0] = loaded * rows * heads;
 }
 
+// Diagonals from the last bucket's first distance on either side, and a margin; 0 beyond 2048 of them (10 KB of LDS), which take longer to lay
+// out than to look up tile by tile.
+inline int near_diagonals(const sdtw_attention_desc *d, const BucketRule &rule)
+{
+    if (!d->buckets) return 0;
+    const int64_t last = rule.n - 1 < rule.e ? rule.n - 1 : rule.start[rule.n - 1 - rule.e];
+    const int64_t all = last + kBiasMargin + 1 + (rule.two_sided ? last + kBiasMargin : kBiasMargin);
+    return all <= 2048 ? (int)all : 0;
+}
+
 // Calls f with a value of the element type and, as a type, the features rounded up to 32, 64, 96 or 128.
 template <int DP> struct Features { static constexpr int value = DP; };
 template <int F> struct Variant { static constexpr int value = F; };

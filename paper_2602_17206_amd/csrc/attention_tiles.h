@@ -92,6 +92,11 @@ __device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint32_
 // All that the wavefront asked for is there, and what it read from LDS has left it.
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
+// All but the last N copies that the wavefront asked for are there.
+template <int N> __device__ __forceinline__ void copies_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// What the wavefront read from LDS has left it.
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // A tile of ROWS rows, copied by THREADS threads (`who`).  A tile's address is a scalar, each thread's places within it do not change,
 // and rows and features behind the end come as zeros without a branch.
 template <typename T, int DP, int ROWS, int THREADS> struct Stage {
@@ -318,6 +323,7 @@ struct AttentionParams {
     int64_t table_stride[2];
     // how the work is split
     int32_t row_tiles, key_tiles, splits, parts, table_columns;
+    int32_t near;               // diagonals of the neighbourhood that is laid out; 0: it is too wide
     float *part;                // [B, H, N, splits][D + 2]: unfinished sums, their reference and total
     float *delta;               // [B, H, N]
     float *key_part;            // [parts][2][B, Hk, M, D]: parts of dk and dv
@@ -376,19 +382,50 @@ __device__ __forceinline__ float tanh_fast(float x)
     return x != x ? x : above * __builtin_amdgcn_rcpf(below);
 }
 
+// s = out tanh(in s).  Scores rarely come near their cap: where all of a wavefront's are below half of it, tanh(x) / x is a polynomial in x^2
+// (interpolated at the Chebyshev nodes of [0, 1/4]; off by 1.4e-8, in float32 by 6e-8), which takes a third of the time.
+__device__ __forceinline__ void cap_scores(Acc &s, float in, float out)
+{
+    float top = fabsf(s[0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, fabsf(s[r]));
+    if (__all(top * in < 0.5f)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float x = s[r] * in, z = x * x;
+            float y = fmaf(z, 0.017131344428621548f, -0.05298423882762508f);
+            y = fmaf(y, z, 0.13324750504782334f);
+            y = fmaf(y, z, -0.33333067944422656f);
+            y = fmaf(y, z, 0.9999999867573899f);
+            s[r] = out * x * y;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = out * tanh_fast(s[r] * in);
+    }
+}
+
 // An entry below -1e30 forbids its cells, as -inf does.
 template <bool OCTAVES> __device__ __forceinline__ float entry_of(float v) { return v < -1e30f ? -INFINITY : OCTAVES ? v * kLog2e : v; }
 
-// The bias of 32 x 32 cells (or of the cells of one key and one row): what a wavefront knows of the 63 diagonals of its tile.
+// Diagonals kept on each side of those that are not all in one bucket: a tile of 64 x 32 cells that touches these reaches over by 94.
+constexpr int kBiasMargin = 95;
+
+// The bias of tiles of 32 x 32 cells.  Far from the diagonal it is one number.  Near it, cells take it from `at`, by their diagonal: of the
+// whole neighbourhood, which is laid out once where that is small, else of the tile's 63 diagonals.
 struct WaveBias {
     const float *values;     // LDS: the head's entries
     const int32_t *starts;   // LDS
+    const float *near;       // LDS: the entry of j - i - offset = 0, and of its neighbours around it; nullptr where there are too many
+    const uint8_t *near_bucket;
     float *diagonal;         // LDS, 64 of the wavefront's own
     uint8_t *bucket;         // LDS, 64 of the wavefront's own
     int last;                // first distance of a side's last bucket
     float one;               // the bias of all cells, where it is the same
     int one_bucket;
     bool same;
+    const float *at;         // else: of the tile's lowest diagonal and those above it
+    const uint8_t *at_bucket;
     // whether all cells with lowest <= j - i - offset <= highest are in the last bucket of their side (or in the one of all later keys)
     __device__ __forceinline__ bool far(const BucketRule &rule, int lowest, int highest)
     {
@@ -402,23 +439,24 @@ struct WaveBias {
     __device__ __forceinline__ void look(const BucketRule &rule, int lowest, int lane)
     {
         if (far(rule, lowest, lowest + 62)) return;
-        const int u = rule.bucket(lowest + min(lane, 62), starts);
-        one_bucket = __builtin_amdgcn_readfirstlane(u);
-        same = __all(u == one_bucket);
-        if (same) {
-            one = values[one_bucket];
-        } else {
-            wavefront_order();
-            diagonal[lane] = values[u];
-            bucket[lane] = (uint8_t)u;
-            wavefront_order();
+        if (near) {
+            at = near + lowest;
+            at_bucket = near_bucket + lowest;
+            return;
         }
+        at = diagonal;
+        at_bucket = bucket;
+        const int u = rule.bucket(lowest + min(lane, 62), starts);
+        wavefront_order();
+        diagonal[lane] = values[u];
+        bucket[lane] = (uint8_t)u;
+        wavefront_order();
     }
 };
 
-// LDS that the bias takes: 256 entries, the rule's starts, and 64 diagonals (4 + 1 bytes) for each wavefront.
+// LDS that the bias takes: 256 entries, the rule's starts, 64 diagonals (4 + 1 bytes) for each wavefront, and the neighbourhood.
 constexpr int kBiasStarts = (kMaxBuckets / 2 + 1 + 3) / 4 * 4;
-constexpr int bias_bytes(int waves) { return kMaxBuckets * 4 + kBiasStarts * 4 + waves * 64 * 5; }
+constexpr int bias_bytes(int waves, int near) { return kMaxBuckets * 4 + kBiasStarts * 4 + waves * 64 * 5 + (near + 3) / 4 * 4 * 5; }
 
 // Lays the bias's part of LDS out and fills it; a barrier has to follow.  OCTAVES: the entries times log2(e).
 template <bool OCTAVES>
@@ -426,15 +464,34 @@ __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const B
                                                int threads)
 {
     float *values = reinterpret_cast<float *>(lds);
-    int32_t *starts = reinterpret_cast<int32_t *>(lds + kMaxBuckets * 4);
-    float *diagonal = reinterpret_cast<float *>(lds + kMaxBuckets * 4 + kBiasStarts * 4);
-    uint8_t *bucket = reinterpret_cast<uint8_t *>(diagonal + 64 * waves);
+    int32_t *starts = reinterpret_cast<int32_t *>(values + kMaxBuckets);
+    float *diagonal = reinterpret_cast<float *>(starts + kBiasStarts);
+    float *near = diagonal + 64 * waves;
+    uint8_t *near_bucket = reinterpret_cast<uint8_t *>(near + (p.near + 3) / 4 * 4);
+    uint8_t *bucket = near_bucket + (p.near + 3) / 4 * 4;
+    const int last = rule.first(rule.n - 1);
     if (p.buckets) {
         for (int u = thread; u < p.buckets; u += threads)
             values[u] = entry_of<OCTAVES>(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
         for (int k = thread; k <= rule.m; k += threads) starts[k] = rule.start[k];
+        if (p.near) {
+            __syncthreads();
+            for (int d = thread; d < p.near; d += threads) {
+                const int u = rule.bucket(d - last - kBiasMargin, starts);
+                near[d] = values[u];
+                near_bucket[d] = (uint8_t)u;
+            }
+        }
     }
-    return WaveBias{values, starts, diagonal + 64 * wave, bucket + 64 * wave, rule.first(rule.n - 1), 0.0f, 0, true};
+    WaveBias b{};
+    b.values = values;
+    b.starts = starts;
+    b.near = p.near ? near + last + kBiasMargin : nullptr;
+    b.near_bucket = near_bucket + last + kBiasMargin;
+    b.diagonal = diagonal + 64 * wave;
+    b.bucket = bucket + 64 * wave;
+    b.last = last;
+    return b;
 }
 
 constexpr int kKeys = 64;  // keys of a tile in LDS
@@ -494,13 +551,10 @@ template <bool DOCUMENTS> struct TileWalk {
 // Products into scores, in octaves.
 template <bool CAP> __device__ __forceinline__ void scale_scores(Acc &s, const AttentionParams &p)
 {
-    if (CAP && p.cap_out != 0.0f) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = p.cap_out * tanh_fast(s[r] * p.cap_in);
-    } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] *= p.scale2;
-    }
+    if (CAP && p.cap_out != 0.0f)
+        cap_scores(s, p.cap_in, p.cap_out);
+    else
+        s *= p.scale2;
 }
 
 struct PackParams {
