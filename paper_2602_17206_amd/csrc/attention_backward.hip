@@ -113,7 +113,8 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
                     }
                     ProfScope ps("attention_rows_gradient", st);
                     p.table_columns = 32;
-                    auto need = [&] { return bytes + ((size_t)4 * p.buckets * p.table_columns + 512) * sizeof(float); };
+                    const size_t tiles = TileShape<T, DP>::bytes(kKeys) >= 16384 ? 2 * TileShape<T, DP>::bytes(kKeys) : 0;  // (one buffer, see there)
+                    auto need = [&] { return bytes - tiles + ((size_t)4 * p.buckets * p.table_columns + 4 * TableSum::kTile) * sizeof(float); };
                     while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
                     attention_rows_gradient_kernel<T, DP, F, kRowsTable><<<grid, 256, need(), st>>>(p, rule);
                 }

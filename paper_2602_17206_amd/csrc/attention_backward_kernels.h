@@ -51,24 +51,21 @@ template <int DP> struct ColumnScale<_Float16, DP> {
 };
 
 // The table's gradient of a wavefront's 32 rows, in LDS: [buckets][columns].  Where all cells of a tile are in one bucket its sum stays in a
-// register until the bucket changes.  Else the cells are added up by their diagonals first - the cells of a register lie on 32
-// different ones in each half, so that an addition in LDS has its place to itself - and then lane d adds diagonal d to its bucket, in a
-// column that it shares with the lanes d' = d (modulo columns), taking turns.  An addition in LDS is one instruction, and a
-// wavefront's are carried out in the order of their issue: the sums do not depend on chance.
+// register until the bucket changes.  Else the cells are added up by their diagonals first and then lane d adds diagonal d to its bucket,
+// in a column that it shares with the lanes d' = d (modulo columns), taking turns: one order of additions, whatever happens.
+// (LDS's own atomic additions are one instruction, but take 3 cycles a lane: 224 us against 99 without the table's gradient at
+// 4 x 16 x 2048 x 2048 x 64 bfloat16 causal.)
 struct TableSum {
+    static constexpr int kPitch = 33, kTile = 32 * kPitch;
     float *sum;       // [buckets][columns]
-    float *diagonal;  // [2][64], zeros between tiles
+    float *tile;      // [32 rows][kPitch]
     int columns, bucket;  // bucket: of `running`
     float running;
-    static __device__ __forceinline__ void add(float *at, float v)
-    {
-        __hip_atomic_fetch_add(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-    }
     __device__ __forceinline__ void turns(int lane, int u, float v)
     {
         for (int first = 0; first < 64; first += columns) {
             wavefront_order();
-            if (lane >= first && lane < first + columns) add(sum + u * columns + lane - first, v);
+            if (lane >= first && lane < first + columns) sum[u * columns + lane - first] += v;
         }
         wavefront_order();
     }
@@ -78,19 +75,32 @@ struct TableSum {
         bucket = -1;
         running = 0.0f;
     }
-    // ds of 32 keys and 32 rows; `place`: the diagonal of register 0; `buckets`: of the 64 diagonals, in LDS
-    __device__ __forceinline__ void by_diagonals(const Acc &ds, int lane, int place, const uint8_t *buckets)
+    // ds of 32 keys and 32 rows; `buckets`: of the 63 diagonals key - row + 31, and one more, in LDS.  Lane l of a half walks over 16 keys t and
+    // the rows (t + 31 - l) mod 32: diagonal l as far as t <= l, and diagonal l + 32 from there on.
+    __device__ __forceinline__ void by_diagonals(const Acc &ds, int lane, uint32_t buckets)
     {
-        float *const at = diagonal + (lane >> 5) * 64 + place;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) add(at + tile_row(r, 0), ds[r]);
+        const int l = lane & 31, half = lane >> 5;
+        float *const to = tile + l * kPitch + 4 * half;
         wavefront_order();
-        const float v = diagonal[lane] + diagonal[64 + lane];
-        diagonal[lane] = 0.0f;
-        diagonal[64 + lane] = 0.0f;
-        turns(lane, buckets[lane], v);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) to[tile_row(r, 0)] = ds[r];
+        wavefront_order();
+        const float *const low = tile + (31 - l) * kPitch + half * 16 * (kPitch + 1), *const high = low - kTile;
+        const int turn = l - half * 16;  // the last key of diagonal l among this half's
+        float first = 0.0f, all = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const float v = (t <= turn ? low : high)[t * (kPitch + 1)];
+            all += v;
+            first = t <= turn ? all : first;
+        }
+        const float mine = both_sum(first), next = both_sum(all - first);
+        turns(lane, lds_read<uint8_t>(buckets + (uint32_t)lane, 0), half ? next : mine);
     }
 };
+
+// Both products of a tile before anything else, where there are registers for it: the matrix cores go on while the scores are worked on.
+template <int DP> constexpr bool kEarly = DP < 128;
 
 // Wavefronts on a SIMD that registers are kept for.
 template <typename T, int DP> constexpr int kDeltaWaves = sizeof(T) == 4 ? (DP <= 32 ? 4 : DP <= 64 ? 2 : 1) : DP <= 64 ? 4 : 3;
@@ -101,7 +111,7 @@ template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T
 // the keys are walked over once more beforehand, for delta alone.
 enum { kRowsPlain, kRowsDelta, kRowsTable };
 template <typename T, int DP, int F, int WORK>
-__global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBackwardWaves<T, DP, WORK == kRowsTable>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
+__global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBackwardWaves<T, DP, false>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
     constexpr bool TABLE = WORK == kRowsTable;
@@ -111,19 +121,20 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
     __shared__ int shared[4][4];
     __shared__ __align__(16) int32_t documents[2][kKeys];
     constexpr int kTile = Shape::bytes(kKeys);
+    constexpr int kBuffers = TABLE && kTile >= 16384 ? 1 : 2;  // (with one, two workgroups still fit into LDS beside the table's sums)
+    // (16-bit results take exponents in octaves as they are; 32-bit ones want them rounded as late as can be)
+    constexpr bool OCTAVES = sizeof(T) == 2 && WORK == kRowsPlain;
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
     const Place at_work(p.B * p.H);
     const int rt = p.row_tiles - 1 - at_work.tile;  // (the last rows see the most keys of a causal sequence)
     const int h = at_work.unit % p.H, b = at_work.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias;
-    if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
     const int table_columns = TABLE ? p.table_columns : 0;
-    float *const table_sums = reinterpret_cast<float *>(lds + 4 * kTile + bias_bytes(4, p.near));
-    TableSum table{table_sums + wave * p.buckets * table_columns, table_sums + 4 * p.buckets * table_columns + wave * 128, table_columns, -1, 0.0f};
+    float *const table_sums = reinterpret_cast<float *>(lds + 2 * kBuffers * kTile + bias_bytes(4, p.near));
+    TableSum table{table_sums + wave * p.buckets * table_columns, table_sums + 4 * p.buckets * table_columns + wave * TableSum::kTile, table_columns, -1, 0.0f};
     if (TABLE)
-        for (int x = thread; x < 4 * p.buckets * table_columns + 512; x += 256) table_sums[x] = 0.0f;
+        for (int x = thread; x < 4 * p.buckets * table_columns; x += 256) table_sums[x] = 0.0f;
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
     const int64_t place = ((int64_t)b * p.H + h) * p.N + i;
@@ -140,7 +151,7 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
     const int low = wave_min_i32(valid ? doc : 0x7fffffff), high = wave_max_i32(valid ? doc : -1);
     // (a row that sees nothing has no p: 2^(score - inf))
     float lse = valid ? p.lse[place] : -INFINITY;
-    if (lse == -INFINITY) lse = INFINITY;
+    lse = lse == -INFINITY ? INFINITY : OCTAVES ? lse * kLog2e : lse;
     Column<T, DP> q, dout;
     {
         const Rows<T> x = rows_of<T>(p.q, p.q_stride, b, h), y = rows_of<T>(p.dout, p.dout_stride, b, h);
@@ -169,7 +180,7 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dq[ft] = Acc{};
     ColumnScale<T, DP> fit;
-    const float inverse_cap = CAP && p.cap != 0.0f ? 1.0f / p.cap : 0.0f, scale = p.scale;
+    const float cap = OCTAVES ? p.cap_out : p.cap, inverse_cap = CAP && cap != 0.0f ? 1.0f / cap : 0.0f, scale = OCTAVES ? p.scale2 : p.scale;
     TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
@@ -177,16 +188,22 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
     auto fetch = [&](int t, int buffer) {
         ks.copy(lds + buffer * kTile, t * kKeys, end, thread);
-        vs.copy(lds + (2 + buffer) * kTile, t * kKeys, end, thread);
+        vs.copy(lds + (kBuffers + buffer) * kTile, t * kKeys, end, thread);
         if (DOCUMENTS && thread < kKeys)
             documents[buffer][thread] = t * kKeys + thread >= end ? -1 : col_document ? col_document[t * kKeys + thread] : 0;
     };
     int t = walk.next(0), buffer = 0;
-    if (t < walk.tiles) fetch(t, 0);
+    if (kBuffers == 2 && t < walk.tiles) fetch(t, 0);
+    WaveBias bias;
+    if (BIAS) bias = begin_bias(p, rule, OCTAVES ? kLog2e : 1.0f, lds + 2 * kBuffers * kTile, h, wave, 4, thread, 256);
     while (t < walk.tiles) {
         const int first = t * kKeys;
-        char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
+        char *const ktile = lds + buffer * kTile, *const vtile = lds + (kBuffers + buffer) * kTile;
         const int32_t *const document = documents[buffer];
+        if (kBuffers == 1) {
+            __syncthreads();
+            fetch(t, 0);
+        }
         copies_done();
         __syncthreads();
         if (DOCUMENTS && __any(document[lane] < 0)) {
@@ -195,8 +212,10 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
             __syncthreads();
         }
         t = walk.next(t + 1);
-        buffer ^= 1;
-        if (t < walk.tiles) fetch(t, buffer);
+        if (kBuffers == 2) {
+            buffer ^= 1;
+            if (t < walk.tiles) fetch(t, buffer);
+        }
 #pragma unroll 1
         for (int sub = 0; sub < kKeys / 32; ++sub) {
             const int j0 = first + sub * 32;
@@ -204,10 +223,10 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
             if (j0 >= to) break;
             bool open = j0 + 32 <= from;
             if (DOCUMENTS) open = open && low == high && __all(document[sub * 32 + c] == low);
-            Acc s = along_features<T, DP>(kt, q, lane);
-            Acc capped;
+            Acc s = along_features<T, DP>(kt, q, lane), dp, capped;
+            if (kEarly<DP>) dp = along_features<T, DP>(vt, dout, lane);
             if (CAP) {
-                if (p.cap != 0.0f) cap_scores(s, p.cap_in, p.cap);
+                if (cap != 0.0f) cap_scores(s, p.cap_in, cap);
                 else s *= scale;
                 capped = s;
             }
@@ -216,22 +235,16 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
             for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - lse : fmaf(s[r], scale, -lse);
             if (BIAS) {
                 bias.look(rule, j0 - base, lane);
-                if (bias.same) {
-                    s += bias.one;
-                } else {
-                    const float *at = bias.at + 31 - c + 4 * half;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] += at[tile_row(r, 0)];
-                }
+                bias.add_to_rows(s, lane);
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
+            for (int r = 0; r < 16; ++r) s[r] = exp2_fast(OCTAVES ? s[r] : s[r] * kLog2e);
             if (!open) {
                 const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
             }
-            const Acc dp = along_features<T, DP>(vt, dout, lane);
+            if (!kEarly<DP>) dp = along_features<T, DP>(vt, dout, lane);
             if (WORK == kRowsDelta) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
@@ -250,7 +263,7 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
                     for (int r = 1; r < 16; ++r) sum += s[r];
                     table.running += sum;
                 } else {
-                    table.by_diagonals(s, lane, 31 - c + 4 * half, bias.at_bucket);
+                    table.by_diagonals(s, lane, bias.at_bucket);
                 }
             }
             if (CAP) through_cap(s, capped, inverse_cap);
@@ -296,9 +309,10 @@ __global__ __launch_bounds__(64) void attention_table_kernel(AttentionParams p)
 // 4 wavefronts of 32 keys each, of one head of keys of one sequence; the queries of the group's heads go by in tiles of 64, or one part
 // of them does: then attention_keys_join_kernel adds the parts up.
 template <typename T, int DP, int F>
-__global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 : DP, F != 0>)) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
+__global__ __launch_bounds__(256, (kBackwardWaves<T, DP, (F & kCap) != 0>)) void attention_keys_gradient_kernel(AttentionParams p, BucketRule rule)
 {
     using Shape = TileShape<T, DP>;
+    constexpr bool OCTAVES = sizeof(T) == 2;
     constexpr bool BIAS = F & kBias, CAP = F & kCap, DOCUMENTS = F & kDocuments;
     extern __shared__ __align__(256) char lds[];
     __shared__ uint64_t live[4];
@@ -338,7 +352,7 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
 #pragma unroll
     for (int ft = 0; ft < DP / 32; ++ft) dk[ft] = Acc{}, dv[ft] = Acc{};
     ColumnScale<T, DP> fit;
-    const float inverse_cap = CAP && p.cap != 0.0f ? 1.0f / p.cap : 0.0f, scale = p.scale;
+    const float cap = OCTAVES ? p.cap_out : p.cap, inverse_cap = CAP && cap != 0.0f ? 1.0f / cap : 0.0f, scale = OCTAVES ? p.scale2 : p.scale;
     constexpr float kWeight = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;  // p <= 1 (to rounding) into float16's upper octaves
     TileWalk<DOCUMENTS> walk{row_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> qs, ds;
@@ -353,8 +367,6 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
         const int first_tile = from_tile + (int)max(share_begin - (int64_t)g * each, (int64_t)0);
         walk.tiles = from_tile + (int)min(share_end - (int64_t)g * each, (int64_t)each);
         __syncthreads();
-        WaveBias bias;
-        if (BIAS) bias = begin_bias<false>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
         const float *lse = p.lse + ((int64_t)b * p.H + h) * p.N, *delta = p.delta + ((int64_t)b * p.H + h) * p.N;
         qs.begin(rows_of<T>(p.q, p.q_stride, b, h), p.loaded, thread);
         ds.begin(rows_of<T>(p.dout, p.dout_stride, b, h), p.loaded, thread);
@@ -365,12 +377,14 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                 const int i = t * kKeys + thread, d = i >= end ? -1 : row_document ? row_document[i] : 0;
                 const float x = d >= 0 ? lse[i] : -INFINITY;
                 row_doc[buffer][thread] = d;
-                row_lse[buffer][thread] = x == -INFINITY ? INFINITY : x;
+                row_lse[buffer][thread] = x == -INFINITY ? INFINITY : OCTAVES ? x * kLog2e : x;
                 row_delta[buffer][thread] = d >= 0 ? delta[i] : 0.0f;
             }
         };
         int t = walk.next(first_tile), buffer = 0;
         if (t < walk.tiles) fetch(t, 0);
+        WaveBias bias;
+        if (BIAS) bias = begin_bias(p, rule, OCTAVES ? kLog2e : 1.0f, lds + 4 * kTile, h, wave, 4, thread, 256);
         while (t < walk.tiles) {
             const int first = t * kKeys, now = buffer;
             char *const qtile = lds + buffer * kTile, *const dtile = lds + (2 + buffer) * kTile;
@@ -391,29 +405,23 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, F & kCap && DP == 96 ? 128 
                 if (i0 + 32 <= mine || i0 >= end || !any) continue;
                 bool open = sight.limit(i0) >= min(first_key + 32, sight.keys);
                 if (DOCUMENTS) open = open && low == high && __all(row_doc[now][sub * 32 + c] == low);
-                Acc s = along_features<T, DP>(qt, k, lane);
-                Acc capped;
+                const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
+                Acc s = along_features<T, DP>(qt, k, lane), dp, capped;
+                if (kEarly<DP>) dp = along_features<T, DP>(dt, v, lane);
                 if (CAP) {
-                    if (p.cap != 0.0f) cap_scores(s, p.cap_in, p.cap);
+                    if (cap != 0.0f) cap_scores(s, p.cap_in, cap);
                     else s *= scale;
                     capped = s;
                 }
-                const float *at_lse = row_lse[now] + sub * 32 + 4 * half, *at_delta = row_delta[now] + sub * 32 + 4 * half;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = CAP ? s[r] - at_lse[tile_row(r, 0)] : fmaf(s[r], scale, -at_lse[tile_row(r, 0)]);
                 if (BIAS) {
                     bias.look(rule, first_key - (i0 + 31) - sight.offset, lane);
-                    if (bias.same) {
-                        s += bias.one;
-                    } else {
-                        const float *at = bias.at + 31 + c - 4 * half;
-#pragma unroll
-                        for (int r = 0; r < 16; ++r) s[r] += at[-tile_row(r, 0)];
-                    }
+                    bias.add_to_keys(s, lane);
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * kLog2e);
-                Acc dp = along_features<T, DP>(dt, v, lane);
+                for (int r = 0; r < 16; ++r) s[r] = exp2_fast(OCTAVES ? s[r] : s[r] * kLog2e);
+                if (!kEarly<DP>) dp = along_features<T, DP>(dt, v, lane);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - at_delta[tile_row(r, 0)]);
                 if (CAP) through_cap(dp, capped, inverse_cap);

@@ -81,8 +81,6 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     const int h = place.unit % p.H, b = place.unit / p.H, hk = h / (p.H / p.Hk);
     const Sight sight(p, b);
     const int32_t *col_document = DOCUMENTS && p.col_document ? p.col_document + (int64_t)b * p.M : nullptr;
-    WaveBias bias;
-    if (BIAS) bias = begin_bias<true>(p, rule, lds + 4 * kTile, h, wave, 4, thread, 256);
 
     const int first_row = rt * 128 + wave * 32, i = first_row + c;
     bool valid = i < sight.rows;
@@ -107,13 +105,12 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     for (int w = 0; w < 4; ++w) end = max(end, shared[w][0]), lowest = min(lowest, shared[w][1]), highest = max(highest, shared[w][2]);
     end = __builtin_amdgcn_readfirstlane(end);
 
-    Running<DP> run;
-    run.clear();
     TileWalk<DOCUMENTS> walk{col_document, end, (end + kKeys - 1) / kKeys, lowest, highest, -1, live};
     Stage<T, DP, kKeys, 256> ks, vs;
     ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, thread);
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, thread);
     const float scale2 = p.scale2, cap_out = p.cap_out;
+    const bool fold = !CAP || cap_out == 0.0f;  // the bias comes in with the products
     const int base = first_row + 31 + sight.offset;  // j less this: the lowest diagonal of the wavefront's rows
     auto fetch = [&](int t, int buffer) {
         ks.copy(lds + buffer * kTile, t * kKeys, end, thread);
@@ -123,6 +120,10 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
     };
     int t = walk.next(0), buffer = 0;
     if (t < walk.tiles) fetch(t, 0);
+    WaveBias bias;  // (laid out while the first tile is on its way)
+    if (BIAS) bias = begin_bias(p, rule, fold ? p.unscale : kLog2e, lds + 4 * kTile, h, wave, 4, thread, 256);
+    Running<DP> run;
+    run.clear();
     while (t < walk.tiles) {
         const int j0 = t * kKeys;
         char *const ktile = lds + buffer * kTile, *const vtile = lds + (2 + buffer) * kTile;
@@ -139,35 +140,40 @@ __global__ __launch_bounds__(256, (kForwardWaves<T, DP, F>)) void attention_forw
         if (t < walk.tiles) fetch(t, buffer);
         if (j0 < to) {
             Acc s[SUBS];
-#pragma unroll
-            for (int x = 0; x < SUBS; ++x) s[x] = along_features<T, DP>(ktile + Shape::bytes(x * 32), col, lane);
             bool open = j0 + kKeys <= from;
             if (DOCUMENTS) open = open && low == high && __all(document[lane] == low);
-            // The scores are the products times a number, plus a number: or made so, by 1 and 0.
+            // The scores are the products times a number, plus a number; or made so, by 1 and 0.
             float factor = scale2, add = 0.0f;
-            const bool plain = open && (!CAP || cap_out == 0.0f) && (!BIAS || bias.far(rule, j0 - base, j0 - base + 94));
-            if (plain) {
-                if (BIAS) add = bias.one;
+            if (BIAS && fold && !bias.far(rule, j0 - base, j0 - base + 94)) {
+#pragma unroll
+                for (int x = 0; x < SUBS; ++x) {
+                    bias.look(rule, j0 + 32 * x - base, lane);
+                    s[x] = bias.of_rows(lane);
+                }
             } else {
+#pragma unroll
+                for (int x = 0; x < SUBS; ++x) s[x] = Acc{};
+                if (BIAS && fold) add = bias.one * scale2;
+            }
+#pragma unroll
+            for (int x = 0; x < SUBS; ++x) s[x] = along_features<T, DP>(ktile + Shape::bytes(x * 32), col, lane, s[x]);
+            if (CAP && !fold) {
                 factor = 1.0f;
 #pragma unroll
                 for (int x = 0; x < SUBS; ++x) {
-                    scale_scores<CAP>(s[x], p);
+                    cap_scores(s[x], p.cap_in, cap_out);
                     if (BIAS) {
                         bias.look(rule, j0 + 32 * x - base, lane);
-                        if (bias.same) {
-                            s[x] += bias.one;
-                        } else {
-                            const float *at = bias.at + 31 - c + 4 * half;
-#pragma unroll
-                            for (int r = 0; r < 16; ++r) s[x][r] += at[tile_row(r, 0)];
-                        }
+                        bias.add_to_rows(s[x], lane);
                     }
-                    if (!open) {
-                        const Seen<DOCUMENTS> seen(lim - j0 - 32 * x - 4 * half, document + 32 * x, doc, half);
+                }
+            }
+            if (!open) {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) s[x][r] = seen.at[r] ? s[x][r] : -INFINITY;
-                    }
+                for (int x = 0; x < SUBS; ++x) {
+                    const Seen<DOCUMENTS> seen(lim - j0 - 32 * x - 4 * half, document + 32 * x, doc, half);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[x][r] = seen.at[r] ? s[x][r] : -INFINITY;
                 }
             }
             run.take(s, factor, add);
@@ -231,20 +237,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
         const Rows<T> q = rows_of<T>(p.q, p.q_stride, b, valid ? h : 0);
         col.load(q.base + (valid ? i : 0) * q.row, p.loaded, valid, half);
     }
-    // the entries of every head that is here, and the rule's starts
-    float *values = reinterpret_cast<float *>(lds + few_rows_bytes<T, DP>());
-    int32_t *starts = reinterpret_cast<int32_t *>(values + min(G, 32) * p.buckets);
-    const int first_head = G <= 32 ? 0 : rt * 32 % G;  // (the heads of 32 rows of a larger group follow each other, round its end)
-    if (BIAS) {
-        for (int u = thread; u < min(G, 32) * p.buckets; u += 256) {
-            const int head = hk * G + (first_head + u / p.buckets) % G;
-            values[u] = entry_of<true>(load_typed(p.table, head * p.table_stride[0] + u % p.buckets * p.table_stride[1], p.table_type));
-        }
-        for (int u = thread; u <= rule.m; u += 256) starts[u] = rule.start[u];
-        __syncthreads();
-    }
-    const float *mine = values + ((row % G - first_head + G) % G) * p.buckets;
-
     // the workgroup's tiles of 128 keys
     const int tiles = (to + 127) / 128, each = (tiles + p.splits - 1) / p.splits;
     const int begin = min(tiles, split * each), end = min(tiles, begin + each);
@@ -259,6 +251,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     auto fetch_values = [&](int t) { if (t < end && t * 128 + wave * 32 < to) vs.copy(vtile, t * 128 + wave * 32, to, lane); };
     fetch_keys(begin);
     fetch_values(begin);
+    // the entries of every head that is here, and the rule's starts
+    float *values = reinterpret_cast<float *>(lds + few_rows_bytes<T, DP>());
+    int32_t *starts = reinterpret_cast<int32_t *>(values + min(G, 32) * p.buckets);
+    const int first_head = G <= 32 ? 0 : rt * 32 % G;  // (the heads of 32 rows of a larger group follow each other, round its end)
+    if (BIAS) {
+        for (int u = thread; u < min(G, 32) * p.buckets; u += 256) {
+            const int head = hk * G + (first_head + u / p.buckets) % G;
+            values[u] = entry_of(load_typed(p.table, head * p.table_stride[0] + u % p.buckets * p.table_stride[1], p.table_type), kLog2e);
+        }
+        for (int u = thread; u <= rule.m; u += 256) starts[u] = rule.start[u];
+        __syncthreads();
+    }
+    const float *mine = values + ((row % G - first_head + G) % G) * p.buckets;
+
     for (int t = begin; t < end; ++t) {
         const int j0 = t * 128 + wave * 32;
         if (j0 >= to) break;
@@ -279,7 +285,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
         Acc &s = scores[0];
         reads_done();
         fetch_keys(t + 1);
-        scale_scores<CAP>(s, p);
+        if (CAP && p.cap_out != 0.0f) cap_scores(s, p.cap_in, p.cap_out);
+        else s *= p.scale2;
         if (BIAS) {
             const int near = j0 - i - sight.offset;
             const int u0 = rule.bucket(near, starts), u1 = rule.bucket(near + 31, starts);

@@ -66,7 +66,7 @@ inline int attention_check(const sdtw_attention_desc *d, BucketRule *rule)
     if (!d || d->B < 0 || d->H < 0 || d->Hk < 1 || d->N < 0 || d->M < 0 || d->D < 1) return SDTW_ERR_INVALID_ARG;
     if (d->H % d->Hk != 0 || d->N > 1 << 28 || d->M > 1 << 28) return SDTW_ERR_INVALID_ARG;
     if (!attention_type_ok(d->type) || d->flags != 0 || (d->causal != 0 && d->causal != 1)) return SDTW_ERR_INVALID_ARG;
-    if (!(d->scale > 0.0f) || !std::isfinite(d->scale * kLog2e)) return SDTW_ERR_INVALID_ARG;
+    if (!(d->scale > 0.0f) || !std::isfinite(d->scale * kLog2e) || !std::isfinite(1.0f / d->scale)) return SDTW_ERR_INVALID_ARG;
     if (!(d->cap >= 0.0f) || !std::isfinite(d->cap * kLog2e) || (d->cap > 0.0f && !std::isfinite(d->scale / d->cap))) return SDTW_ERR_INVALID_ARG;
     if (d->offset >= (int64_t)1 << 62 || d->offset <= -((int64_t)1 << 62)) return SDTW_ERR_INVALID_ARG;
     if (d->prefix < 0 || (d->prefix > 0 && !d->causal)) return SDTW_ERR_INVALID_ARG;
@@ -99,6 +99,7 @@ inline AttentionParams attention_params(const sdtw_attention_desc *d, const sdtw
     p.prefix = (int32_t)std::min<int64_t>(d->prefix, 1 << 29);
     p.scale = d->scale;
     p.scale2 = d->scale * kLog2e;
+    p.unscale = 1.0f / d->scale;
     p.cap = d->cap;
     if (d->cap > 0.0f) p.cap_in = d->scale / d->cap, p.cap_out = d->cap * kLog2e;
     if (lists) {

@@ -82,6 +82,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const void *base, uint3
 typedef __attribute__((address_space(3))) char LdsByte;
 __device__ __forceinline__ uint32_t lds_address(const char *p) { return (uint32_t)reinterpret_cast<uintptr_t>((LdsByte *)p); }
 
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t address, int offset)
+{
+    typedef __attribute__((address_space(3))) const char Byte;
+    typedef __attribute__((address_space(3))) const V Value;
+    return *(Value *)((Byte *)(uintptr_t)address + offset);
+}
+
 // 16 bytes a lane from the window straight into LDS, lane after lane from `lds` on.  Written out because the compiler, which cannot tell the
 // tile that is being filled from the one that is being read, would wait for it before every read.
 __device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t at, uint32_t lds)
@@ -178,20 +185,12 @@ template <typename T> __device__ __forceinline__ void mma(Acc &acc, const Bits4 
     }
 }
 
-template <typename V> __device__ __forceinline__ V lds_read(uint32_t address, int offset)
-{
-    typedef __attribute__((address_space(3))) const char Byte;
-    typedef __attribute__((address_space(3))) const V Value;
-    return *(Value *)((Byte *)(uintptr_t)address + offset);
-}
-
-// S = X R for the 32 rows of `tile`
-template <typename T, int DP> __device__ __forceinline__ Acc along_features(const char *tile, const Column<T, DP> &col, int lane)
+// S = X R for the 32 rows of `tile`, and what `acc` holds
+template <typename T, int DP> __device__ __forceinline__ Acc along_features(const char *tile, const Column<T, DP> &col, int lane, Acc acc = Acc{})
 {
     using Shape = TileShape<T, DP>;
     const int row = lane & 31;
     const uint32_t at = lds_address(tile) + (uint32_t)(row * Shape::kStride + ((lane >> 5) ^ Shape::turn(row)) * 16);  // chunk 2 s + half
-    Acc acc = {};
 #pragma unroll
     for (int s = 0; s < Column<T, DP>::kSteps; ++s)
         mma<T>(acc, lds_read<Bits4>(at ^ (uint32_t)(2 * s & Shape::kMask) * 16, (2 * s & ~Shape::kMask) * 16), col.v[s]);
@@ -313,7 +312,7 @@ struct AttentionParams {
     int32_t loaded;             // D rounded up to whole chunks, where D does not fill them
     int32_t buckets, table_type, causal;
     int32_t offset, prefix;
-    float scale, scale2;        // of the products; times log2(e)
+    float scale, scale2, unscale;  // of the products; times log2(e); 1 over it
     float cap, cap_in, cap_out; // 0: no cap; scale / cap; cap log2(e)
     const void *q, *k, *v, *table, *dout;
     void *out, *dq, *dk, *dv;
@@ -405,52 +404,87 @@ __device__ __forceinline__ void cap_scores(Acc &s, float in, float out)
     }
 }
 
-// An entry below -1e30 forbids its cells, as -inf does.
-template <bool OCTAVES> __device__ __forceinline__ float entry_of(float v) { return v < -1e30f ? -INFINITY : OCTAVES ? v * kLog2e : v; }
+// An entry times `unit`; one below -1e30 forbids its cells, as -inf does.
+__device__ __forceinline__ float entry_of(float v, float unit) { return v < -1e30f ? -INFINITY : v * unit; }
 
 // Diagonals kept on each side of those that are not all in one bucket: a tile of 64 x 32 cells that touches these reaches over by 94.
 constexpr int kBiasMargin = 95;
 
 // The bias of tiles of 32 x 32 cells.  Far from the diagonal it is one number.  Near it, cells take it from `at`, by their diagonal: of the
-// whole neighbourhood, which is laid out once where that is small, else of the tile's 63 diagonals.
+// whole neighbourhood, which is laid out once where that is small, else of the tile's 63 diagonals.  All of it by LDS addresses: a
+// pointer that may be one of two would be read as memory, and wait for the tiles that are being copied.
 struct WaveBias {
-    const float *values;     // LDS: the head's entries
-    const int32_t *starts;   // LDS
-    const float *near;       // LDS: the entry of j - i - offset = 0, and of its neighbours around it; nullptr where there are too many
-    const uint8_t *near_bucket;
-    float *diagonal;         // LDS, 64 of the wavefront's own
-    uint8_t *bucket;         // LDS, 64 of the wavefront's own
-    int last;                // first distance of a side's last bucket
-    float one;               // the bias of all cells, where it is the same
+    uint32_t values;       // the head's entries
+    const int32_t *starts;
+    uint32_t near;         // the entry of j - i - offset = 0, and of its neighbours around it
+    uint32_t near_bucket;
+    bool have_near;
+    float *diagonal;       // 64 of the wavefront's own
+    uint8_t *bucket;       // 64 of the wavefront's own
+    int last;              // first distance of a side's last bucket
+    float one;             // the bias of all cells, where it is the same
     int one_bucket;
     bool same;
-    const float *at;         // else: of the tile's lowest diagonal and those above it
-    const uint8_t *at_bucket;
+    uint32_t at;           // else: of the tile's lowest diagonal and those above it
+    uint32_t at_bucket;
     // whether all cells with lowest <= j - i - offset <= highest are in the last bucket of their side (or in the one of all later keys)
     __device__ __forceinline__ bool far(const BucketRule &rule, int lowest, int highest)
     {
         const int before = highest <= -last ? rule.n - 1 : -1, behind = rule.two_sided ? (lowest >= last ? 2 * rule.n - 1 : -1) : lowest >= 0 ? 0 : -1;
         one_bucket = max(before, behind);
         same = one_bucket >= 0;
-        if (same) one = values[one_bucket];
+        if (same) one = lds_read<float>(values + 4 * (uint32_t)one_bucket, 0);
         return same;
     }
     // `lowest`: j - i - offset on the lowest of the diagonals
     __device__ __forceinline__ void look(const BucketRule &rule, int lowest, int lane)
     {
         if (far(rule, lowest, lowest + 62)) return;
-        if (near) {
-            at = near + lowest;
-            at_bucket = near_bucket + lowest;
+        if (have_near) {
+            at = near + 4 * (uint32_t)lowest;
+            at_bucket = near_bucket + (uint32_t)lowest;
             return;
         }
-        at = diagonal;
-        at_bucket = bucket;
+        at = lds_address(reinterpret_cast<char *>(diagonal));
+        at_bucket = lds_address(reinterpret_cast<char *>(bucket));
         const int u = rule.bucket(lowest + min(lane, 62), starts);
         wavefront_order();
-        diagonal[lane] = values[u];
+        diagonal[lane] = lds_read<float>(values + 4 * (uint32_t)u, 0);
         bucket[lane] = (uint8_t)u;
         wavefront_order();
+    }
+    // The bias of 32 keys (registers) and 32 rows (columns).
+    __device__ __forceinline__ Acc of_rows(int lane) const
+    {
+        if (same) return Acc{} + one;
+        const uint32_t from = at + 4 * (uint32_t)(31 - (lane & 31) + 4 * (lane >> 5));
+        Acc s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = lds_read<float>(from, 4 * tile_row(r, 0));
+        return s;
+    }
+    // Adds it ...
+    __device__ __forceinline__ void add_to_rows(Acc &s, int lane) const
+    {
+        if (same) {
+            s += one;
+            return;
+        }
+        const uint32_t from = at + 4 * (uint32_t)(31 - (lane & 31) + 4 * (lane >> 5));
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] += lds_read<float>(from, 4 * tile_row(r, 0));
+    }
+    // ... or that of 32 rows (registers) and 32 keys (columns).
+    __device__ __forceinline__ void add_to_keys(Acc &s, int lane) const
+    {
+        if (same) {
+            s += one;
+            return;
+        }
+        constexpr int kMost = tile_row(15, 0);
+        const uint32_t from = at + 4 * (uint32_t)(31 + (lane & 31) - 4 * (lane >> 5) - kMost);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] += lds_read<float>(from, 4 * (kMost - tile_row(r, 0)));
     }
 };
 
@@ -458,10 +492,11 @@ struct WaveBias {
 constexpr int kBiasStarts = (kMaxBuckets / 2 + 1 + 3) / 4 * 4;
 constexpr int bias_bytes(int waves, int near) { return kMaxBuckets * 4 + kBiasStarts * 4 + waves * 64 * 5 + (near + 3) / 4 * 4 * 5; }
 
-// Lays the bias's part of LDS out and fills it; a barrier has to follow.  OCTAVES: the entries times log2(e).
-template <bool OCTAVES>
-__device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const BucketRule &rule, char *lds, int h, int wave, int waves, int thread,
-                                               int threads)
+// Lays the bias's part of LDS out and fills it with the entries times `unit`; a barrier has to follow.  The forward pass's
+// products, unless they are capped, begin with the bias over the scale: in the matrix cores' accumulator it costs nothing more (68 to 62 us
+// at 4 x 16 x 2048 x 2048 x 64 bfloat16 causal; the gradients' are slower so, 118 to 130).
+__device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const BucketRule &rule, float unit, char *lds, int h, int wave, int waves,
+                                               int thread, int threads)
 {
     float *values = reinterpret_cast<float *>(lds);
     int32_t *starts = reinterpret_cast<int32_t *>(values + kMaxBuckets);
@@ -472,7 +507,7 @@ __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const B
     const int last = rule.first(rule.n - 1);
     if (p.buckets) {
         for (int u = thread; u < p.buckets; u += threads)
-            values[u] = entry_of<OCTAVES>(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type));
+            values[u] = entry_of(load_typed(p.table, h * p.table_stride[0] + u * p.table_stride[1], p.table_type), unit);
         for (int k = thread; k <= rule.m; k += threads) starts[k] = rule.start[k];
         if (p.near) {
             __syncthreads();
@@ -484,10 +519,11 @@ __device__ __forceinline__ WaveBias begin_bias(const AttentionParams &p, const B
         }
     }
     WaveBias b{};
-    b.values = values;
+    b.values = __builtin_amdgcn_readfirstlane(lds_address(reinterpret_cast<char *>(values)));
     b.starts = starts;
-    b.near = p.near ? near + last + kBiasMargin : nullptr;
-    b.near_bucket = near_bucket + last + kBiasMargin;
+    b.have_near = p.near != 0;
+    b.near = __builtin_amdgcn_readfirstlane(lds_address(reinterpret_cast<char *>(near + last + kBiasMargin)));
+    b.near_bucket = __builtin_amdgcn_readfirstlane(lds_address(reinterpret_cast<char *>(near_bucket + last + kBiasMargin)));
     b.diagonal = diagonal + 64 * wave;
     b.bucket = bucket + 64 * wave;
     b.last = last;
@@ -547,15 +583,6 @@ template <bool DOCUMENTS> struct TileWalk {
         return tiles;
     }
 };
-
-// Products into scores, in octaves.
-template <bool CAP> __device__ __forceinline__ void scale_scores(Acc &s, const AttentionParams &p)
-{
-    if (CAP && p.cap_out != 0.0f)
-        cap_scores(s, p.cap_in, p.cap_out);
-    else
-        s *= p.scale2;
-}
 
 struct PackParams {
     const void *in;
