@@ -10,6 +10,7 @@ import contextlib
 import ctypes
 import functools
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libsdtw_hip.so")
@@ -204,13 +205,13 @@ def load_library():
     lib.sdtw_forward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sdtw_backward_biased.restype = i32
     lib.sdtw_backward_biased.argtypes = [pdesc, pb, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-    pa, pl = ctypes.POINTER(AttentionDesc), ctypes.POINTER(AttentionLists)
+    # (descriptors and lists as structures by reference, or as their bytes)
     for name in ("sdtw_attention_forward_workspace_bytes", "sdtw_attention_backward_workspace_bytes"):
-        getattr(lib, name).restype, getattr(lib, name).argtypes = sz, [pa]
+        getattr(lib, name).restype, getattr(lib, name).argtypes = sz, [vp]
     lib.sdtw_attention_forward.restype = i32
-    lib.sdtw_attention_forward.argtypes = [pa, vp, vp, vp, vp, pl, vp, vp, vp, sz, vp]
+    lib.sdtw_attention_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sdtw_attention_backward.restype = i32
-    lib.sdtw_attention_backward.argtypes = [pa, vp, vp, vp, vp, pl, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.sdtw_attention_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.sdtw_gradient_clip_workspace_bytes.restype = sz
     lib.sdtw_gradient_clip_workspace_bytes.argtypes = [vp, i32]
     lib.sdtw_gradient_clip.restype = i32
@@ -1030,9 +1031,15 @@ def _positions_ptr(t, B, n, device, name):
     return t.data_ptr()
 
 
+# struct sdtw_attention_desc and sdtw_attention_lists, put together at once: field by field takes several times as long
+_attention_desc = struct.Struct("=12i2fI4x2q32q2q").pack
+_attention_lists = struct.Struct("=6Q").pack
+_NO_STRIDES = (0, 0, 0, 0)
+
+
 def _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len, row_document,
-                    col_document):
-    """(descriptor without outputs, lists, pointers of q, k, v, table)"""
+                    col_document, out=_NO_STRIDES, dout=_NO_STRIDES, dq=_NO_STRIDES, dk=_NO_STRIDES, dv=_NO_STRIDES):
+    """(descriptor, lists or None, pointers of q, k, v, table); `out` and on: the strides of the tensors that a call has beside them"""
     import torch
 
     if q.dim() != 4 or k.dim() != 4 or not q.is_cuda:
@@ -1042,43 +1049,60 @@ def _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided,
         raise ValueError("k and v must be [B, Hk, M, D] with q's B and D, on its device and of its type")
     if Hk < 1 or H % Hk:
         raise ValueError("the number of q's heads must be a multiple of that of k's")
-    desc = AttentionDesc(B, H, Hk, N, M, D, _type_of(q, "q"), 0, 0, 0, 0, 1 if causal else 0, D ** -0.5 if scale is None else scale, cap)
-    desc.q_stride[:], desc.k_stride[:], desc.v_stride[:] = q.stride(), k.stride(), v.stride()
-    tp = None
+    if max(B, H, N, M, D) >= _I32:
+        raise ValueError("a dimension is too large")
+    table_type = buckets = 0
+    tp, table_strides = None, (0, 0)
     if table is not None:
         if table.dim() != 2 or table.shape[0] != H or table.device != dev:
             raise ValueError("table must be [%d, buckets] on %s" % (H, dev))
-        if table.shape[1] < 1:
+        buckets = table.shape[1]
+        if not 1 <= buckets < _I32:
             raise ValueError("table must have buckets")
-        desc.table_type, desc.buckets = _type_of(table, "table"), table.shape[1]
-        desc.max_distance, desc.two_sided = _whole(max_distance, _I32, "max_distance"), 1 if two_sided else 0
-        desc.table_stride[:] = table.stride()
-        tp = table.data_ptr()
-    lists = AttentionLists()
-    if torch.is_tensor(offset):
-        lists.offsets = _vector_ptr(offset, B, dev, torch.int32, "offset")
+        table_type, table_strides, tp = _type_of(table, "table"), table.stride(), table.data_ptr()
+        max_distance = _whole(max_distance, _I32, "max_distance")
     else:
-        desc.offset = _whole(offset, _I64, "offset")
-    if prefix is not None:
+        max_distance = two_sided = 0
+    lists = [0, 0, 0, 0, 0, 0]
+    if torch.is_tensor(offset):
+        lists[0] = _vector_ptr(offset, B, dev, torch.int32, "offset")
+        offset = 0
+    else:
+        offset = _whole(offset, _I64, "offset")
+    if prefix is None:
+        prefix = 0
+    else:
         if not causal:
             raise ValueError("a prefix belongs to a causal mask")
         if torch.is_tensor(prefix):
-            lists.prefixes = _vector_ptr(prefix, B, dev, torch.int32, "prefix")
+            lists[1] = _vector_ptr(prefix, B, dev, torch.int32, "prefix")
+            prefix = 0
         else:
-            desc.prefix = _whole(prefix, _I64, "prefix")
-    lists.row_len = _vector_ptr(row_len, B, dev, torch.int32, "row_len")
-    lists.col_len = _vector_ptr(col_len, B, dev, torch.int32, "col_len")
+            prefix = _whole(prefix, _I64, "prefix")
+    if row_len is not None:
+        lists[2] = _vector_ptr(row_len, B, dev, torch.int32, "row_len")
+    if col_len is not None:
+        lists[3] = _vector_ptr(col_len, B, dev, torch.int32, "col_len")
     if (row_document is None) != (col_document is None):
         raise ValueError("row_document and col_document go together")
-    lists.row_document = _positions_ptr(row_document, B, N, dev, "row_document")
-    lists.col_document = _positions_ptr(col_document, B, M, dev, "col_document")
-    return desc, lists, (q.data_ptr(), k.data_ptr(), v.data_ptr(), tp)
+    if row_document is not None:
+        lists[4] = _positions_ptr(row_document, B, N, dev, "row_document")
+        lists[5] = _positions_ptr(col_document, B, M, dev, "col_document")
+    try:
+        desc = _attention_desc(B, H, Hk, N, M, D, _type_of(q, "q"), table_type, buckets, max_distance, 1 if two_sided else 0, 1 if causal else 0,
+                               D ** -0.5 if scale is None else scale, cap, 0, offset, prefix, *q.stride(), *k.stride(), *v.stride(), *out, *dout,
+                               *dq, *dk, *dv, *table_strides)
+    except OverflowError:
+        raise ValueError("scale and cap must be float32 numbers") from None
+    return desc, _attention_lists(*lists) if any(lists) else None, (q.data_ptr(), k.data_ptr(), v.data_ptr(), tp)
 
 
 def _like(given, like, name):
     """(a tensor as ``like``, with contiguous features)"""
     import torch
 
+    if like.dim() != 4:
+        raise ValueError("q [B, H, N, D] and k, v [B, Hk, M, D] must be device tensors")
     if given is None:
         given = torch.empty_like(like)  # (the same order of dimensions in memory)
         return given if given.shape[3] <= 1 or given.stride(3) == 1 else torch.empty(like.shape, dtype=like.dtype, device=like.device)
@@ -1100,19 +1124,17 @@ def sdtw_attention_forward(q, k, v, table=None, scale=None, cap=0.0, causal=Fals
     import torch
 
     lib = load_library()
-    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
-                                        row_document, col_document)
     dev = q.device
     out = _like(out, q, "out")
-    desc.out_stride[:] = out.stride()
-    ref = ctypes.byref(desc)
-    keep, wp, wn = _operator_workspace(lib.sdtw_attention_forward_workspace_bytes(ref), workspace, dev, "sdtw_attention_forward")
+    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
+                                        row_document, col_document, out.stride())
+    keep, wp, wn = _operator_workspace(lib.sdtw_attention_forward_workspace_bytes(desc), workspace, dev, "sdtw_attention_forward")
     if lse is None:
-        lse = torch.empty((desc.B, desc.H, desc.N), dtype=torch.float32, device=dev)
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev)
         lp = lse.data_ptr()
     else:
-        lp = _ptr(lse, torch.float32, (desc.B, desc.H, desc.N), "lse")
-    rc = lib.sdtw_attention_forward(ref, *args, ctypes.byref(lists), out.data_ptr(), lp, wp, wn, _stream_of(dev))
+        lp = _ptr(lse, torch.float32, q.shape[:3], "lse")
+    rc = lib.sdtw_attention_forward(desc, *args, lists, out.data_ptr(), lp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_attention_forward")
     return out, lse
@@ -1128,27 +1150,24 @@ def sdtw_attention_backward(q, k, v, out, lse, dout, table=None, scale=None, cap
     import torch
 
     lib = load_library()
-    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
-                                        row_document, col_document)
     dev = q.device
     for t, name in ((out, "out"), (dout, "dout")):
         if t.shape != q.shape or t.dtype != q.dtype or t.device != dev:
             raise ValueError("%s must be %s of %s on %s" % (name, tuple(q.shape), q.dtype, dev))
     dq, dk, dv = _like(dq, q, "dq"), _like(dk, k, "dk"), _like(dv, v, "dv")
-    desc.out_stride[:], desc.dout_stride[:] = out.stride(), dout.stride()
-    desc.dq_stride[:], desc.dk_stride[:], desc.dv_stride[:] = dq.stride(), dk.stride(), dv.stride()
+    desc, lists, args = _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided, offset, prefix, row_len, col_len,
+                                        row_document, col_document, out.stride(), dout.stride(), dq.stride(), dk.stride(), dv.stride())
     dp = None
     if table is None or not want_dtable:
         dtable = None
     elif dtable is None:
-        dtable = torch.empty((desc.H, desc.buckets), dtype=torch.float32, device=dev)
+        dtable = torch.empty(table.shape, dtype=torch.float32, device=dev)
         dp = dtable.data_ptr()
     else:
-        dp = _ptr(dtable, torch.float32, (desc.H, desc.buckets), "dtable")
-    ref = ctypes.byref(desc)
-    keep, wp, wn = _operator_workspace(lib.sdtw_attention_backward_workspace_bytes(ref), workspace, dev, "sdtw_attention_backward")
-    rc = lib.sdtw_attention_backward(ref, *args, ctypes.byref(lists), out.data_ptr(), _ptr(lse, torch.float32, (desc.B, desc.H, desc.N), "lse"),
-                                     dout.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dp, wp, wn, _stream_of(dev))
+        dp = _ptr(dtable, torch.float32, table.shape, "dtable")
+    keep, wp, wn = _operator_workspace(lib.sdtw_attention_backward_workspace_bytes(desc), workspace, dev, "sdtw_attention_backward")
+    rc = lib.sdtw_attention_backward(desc, *args, lists, out.data_ptr(), _ptr(lse, torch.float32, q.shape[:3], "lse"), dout.data_ptr(),
+                                     dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_attention_backward")
     return dq, dk, dv, dtable

@@ -16,7 +16,7 @@ size_t few_rows_lds(const sdtw_attention_desc *d)
 {
     size_t bytes = 0;
     with_shape(d->type, d->D, [&](auto t, auto features) { bytes = (size_t)few_rows_bytes<decltype(t), decltype(features)::value>(); });
-    return bytes + (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 : 0);
+    return bytes + (d->buckets ? ((size_t)std::min(32, d->H / d->Hk) * d->buckets + kBiasStarts) * 4 + 2048 : 0);
 }
 
 ForwardPlan split_forward(const sdtw_attention_desc *d)
@@ -35,8 +35,10 @@ ForwardPlan split_forward(const sdtw_attention_desc *d)
     }
     P.row_tiles = ((int64_t)d->N * G + 31) / 32;
     const int64_t units = (int64_t)d->B * d->Hk * P.row_tiles;
-    P.splits = std::min<int64_t>(std::min<int64_t>((512 + units - 1) / units, (d->M + 127) / 128), 1024);
-    P.splits = std::max<int64_t>(P.splits, 1);
+    // Two workgroups for each compute unit, of two tiles of 128 keys at least; up to four tiles are walked through without a split, which
+    // would take a second launch.
+    const int64_t key_tiles = ((int64_t)d->M + 127) / 128;
+    P.splits = key_tiles <= 4 ? 1 : std::max<int64_t>(1, std::min<int64_t>({(512 + units - 1) / units, key_tiles / 2, 1024}));
     P.workgroups = units * P.splits;
     P.fits = attention_grid_ok(P.workgroups) && attention_grid_ok((int64_t)d->B * d->H * d->N);
     if (P.splits > 1) P.off_packed = align_up((size_t)d->B * d->H * d->N * P.splits * (d->D + 2) * sizeof(float), 256);

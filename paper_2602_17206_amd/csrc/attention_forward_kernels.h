@@ -254,6 +254,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     // the entries of every head that is here, and the rule's starts
     float *values = reinterpret_cast<float *>(lds + few_rows_bytes<T, DP>());
     int32_t *starts = reinterpret_cast<int32_t *>(values + min(G, 32) * p.buckets);
+    uint8_t *near = reinterpret_cast<uint8_t *>(starts + kBiasStarts);  // the buckets of the diagonals around 0
+    const int last = rule.first(rule.n - 1);
     const int first_head = G <= 32 ? 0 : rt * 32 % G;  // (the heads of 32 rows of a larger group follow each other, round its end)
     if (BIAS) {
         for (int u = thread; u < min(G, 32) * p.buckets; u += 256) {
@@ -262,8 +264,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
         }
         for (int u = thread; u <= rule.m; u += 256) starts[u] = rule.start[u];
         __syncthreads();
+        for (int d = thread; d < p.near; d += 256) near[d] = (uint8_t)rule.bucket(d - last - kBiasMargin, starts);
+        if (p.near) __syncthreads();
     }
-    const float *mine = values + ((row % G - first_head + G) % G) * p.buckets;
+    const float *const mine = values + ((row % G - first_head + G) % G) * p.buckets;
+    // (beyond the neighbourhood all is as on its edge)
+    auto bucket = [&](int r) { return p.near ? (int)near[min(max(r + last + kBiasMargin, 0), p.near - 1)] : rule.bucket(r, starts); };
 
     for (int t = begin; t < end; ++t) {
         const int j0 = t * 128 + wave * 32;
@@ -288,13 +294,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
         if (CAP && p.cap_out != 0.0f) cap_scores(s, p.cap_in, p.cap_out);
         else s *= p.scale2;
         if (BIAS) {
-            const int near = j0 - i - sight.offset;
-            const int u0 = rule.bucket(near, starts), u1 = rule.bucket(near + 31, starts);
-            if (__all(u0 == u1 && (near > 0 || near + 31 <= 0))) {
+            const int first = j0 - i - sight.offset, u0 = bucket(first), u1 = bucket(first + 31);
+            if (__all(u0 == u1 && (first > 0 || first + 31 <= 0))) {
                 s += mine[u0];
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] += mine[rule.bucket(near + tile_row(r, half), starts)];
+                for (int r = 0; r < 16; ++r) s[r] += mine[bucket(first + tile_row(r, half))];
             }
         }
         if (DOCUMENTS || j0 + 32 > from) {

@@ -105,6 +105,17 @@ int sdtw_gradient_clip(const sdtw_gradient *gradients, int32_t count, float max_
         return writes;
     };
     ClipList list;
+    if (launches == 1) {
+        (void)fill(list, 0);
+        int64_t elements = 0;
+        for (int32_t i = 0; i < count; ++i) elements += gradients[i].count;
+        if (list.first[list.tensors] <= 64 && elements <= 1 << 16) {
+            p.norm = norm;
+            ProfScope ps("clip_small", st);
+            clip_small_kernel<<<1, 1024, 0, st>>>(list, p);
+            return hip_ok();
+        }
+    }
     for (int l = 0; l < launches; ++l) {
         (void)fill(list, l);
         const int grid = std::min(list.first[list.tensors], most);
