@@ -98,6 +98,10 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
         pack(desc, p.k, p.k_stride, desc->Hk, desc->M, room, st);
         pack(desc, p.v, p.v_stride, desc->Hk, desc->M, room, st);
     }
+    // delta from the rounded outputs is good enough where they are averages over many keys.  Over few of them - a row of one key has no gradient
+    // at all - it is not: float16 gradients of 68 rows and keys were twice as far from 64 bits as those of a chain in 32 bits.
+    p.close = desc->type != SDTW_TYPE_F32 && desc->M <= 512;
+    const bool close_delta = dtable || p.close;
     with_shape(desc->type, desc->D, [&](auto t, auto features) {
         using T = decltype(t);
         constexpr int DP = decltype(features)::value;
@@ -105,12 +109,12 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
             constexpr int F = decltype(variant)::value;
             const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4, p.near);
             const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
+            if (rows && close_delta) {
+                ProfScope ps("attention_delta", st);
+                attention_rows_gradient_kernel<T, DP, F, kRowsDelta><<<grid, 256, bytes, st>>>(p, rule);
+            }
             if (rows && dtable) {
                 if constexpr ((F & kBias) != 0) {
-                    {
-                        ProfScope ps("attention_delta", st);
-                        attention_rows_gradient_kernel<T, DP, F, kRowsDelta><<<grid, 256, bytes, st>>>(p, rule);
-                    }
                     ProfScope ps("attention_rows_gradient", st);
                     p.table_columns = 32;
                     const size_t tiles = TileShape<T, DP>::bytes(kKeys) >= 16384 ? 2 * TileShape<T, DP>::bytes(kKeys) : 0;  // (one buffer, see there)
@@ -118,6 +122,9 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
                     while (need() + 2048 > kLdsBytes) p.table_columns /= 2;
                     attention_rows_gradient_kernel<T, DP, F, kRowsTable><<<grid, 256, need(), st>>>(p, rule);
                 }
+            } else if (rows && close_delta) {
+                ProfScope ps("attention_rows_gradient", st);
+                attention_rows_gradient_kernel<T, DP, F, kRowsGiven><<<grid, 256, bytes, st>>>(p, rule);
             } else if (rows) {
                 ProfScope ps("attention_rows_gradient", st);
                 attention_rows_gradient_kernel<T, DP, F, kRowsPlain><<<grid, 256, bytes, st>>>(p, rule);

@@ -107,9 +107,9 @@ template <typename T, int DP> constexpr int kDeltaWaves = sizeof(T) == 4 ? (DP <
 template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : DP <= 96 || !MORE ? 2 : 1;
 
 // 4 wavefronts of 32 rows each, one head of one sequence.  delta comes from the rows' outputs - sum_j p dp = <dout, out> - unless the table's
-// gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals would show the rounding of a 16-bit `out`; then
-// the keys are walked over once more beforehand, for delta alone.
-enum { kRowsPlain, kRowsDelta, kRowsTable };
+// gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals would show the rounding of a 16-bit `out`; then, and for
+// 16-bit gradients over few keys, the keys are walked over once more beforehand, for delta alone.
+enum { kRowsPlain, kRowsDelta, kRowsTable, kRowsGiven };
 template <typename T, int DP, int F, int WORK>
 __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBackwardWaves<T, DP, false>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)
 {
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
     constexpr int kTile = Shape::bytes(kKeys);
     constexpr int kBuffers = TABLE && kTile >= 16384 ? 1 : 2;  // (with one, two workgroups still fit into LDS beside the table's sums)
     // (16-bit results take exponents in octaves as they are; 32-bit ones want them rounded as late as can be)
-    constexpr bool OCTAVES = sizeof(T) == 2 && WORK == kRowsPlain;
+    constexpr bool OCTAVES = sizeof(T) == 2 && (WORK == kRowsPlain || WORK == kRowsGiven);
     const int thread = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(thread / 64), lane = thread % 64, c = lane % 32, half = lane / 32;
     const Place at_work(p.B * p.H);
     const int rt = p.row_tiles - 1 - at_work.tile;  // (the last rows see the most keys of a causal sequence)
@@ -159,7 +159,9 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
         dout.load(y.base + i * y.row, p.loaded, valid, half);
     }
     float delta = 0.0f;
-    if (TABLE && valid) delta = p.delta[place];
+    // With the delta that there is, a row's ds add up to what delta is off by: the kernel for the keys gets the better one.
+    float rest = 0.0f;
+    if ((TABLE || WORK == kRowsGiven) && valid) delta = p.delta[place];
     if (WORK == kRowsPlain) {
         const Rows<T> x = rows_of<T>(p.out, p.out_stride, b, h);
         Column<T, DP> out;
@@ -169,7 +171,6 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
 #pragma unroll
             for (int e = 0; e < Elem<T>::kWidth; ++e) delta = fmaf(Elem<T>::at(dout.v[s], e), Elem<T>::at(out.v[s], e), delta);
         delta = both_sum(delta);
-        if (half == 0 && i < p.N) p.delta[place] = delta;
     }
     if (lane == 0) shared[wave][0] = to, shared[wave][1] = low, shared[wave][2] = high;
     __syncthreads();
@@ -238,29 +239,32 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
                 bias.add_to_rows(s, lane);
             }
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = exp2_fast(OCTAVES ? s[r] : s[r] * kLog2e);
+            for (int r = 0; r < 16; ++r) s[r] = OCTAVES ? exp2_fast(s[r]) : exp2_fast(s[r] * kLog2e);
             if (!open) {
                 const Seen<DOCUMENTS> seen(lim - j0 - 4 * half, document + sub * 32, doc, half);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
             }
             if (!kEarly<DP>) dp = along_features<T, DP>(vt, dout, lane);
-            if (WORK == kRowsDelta) {
+            if (WORK == kRowsDelta) {  // (a tile's sum first: hundreds of additions to one number would show)
+                float sum = s[0] * dp[0];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) delta = fmaf(s[r], dp[r], delta);
+                for (int r = 1; r < 16; ++r) sum = fmaf(s[r], dp[r], sum);
+                delta += sum;
                 continue;
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= dp[r] - delta;
+            float sum = s[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) sum += s[r];
+            if (WORK == kRowsPlain) rest += sum;
             if (TABLE) {
                 if (bias.same) {
                     if (bias.one_bucket != table.bucket) {
                         table.flush(lane);
                         table.bucket = bias.one_bucket;
                     }
-                    float sum = s[0];
-#pragma unroll
-                    for (int r = 1; r < 16; ++r) sum += s[r];
                     table.running += sum;
                 } else {
                     table.by_diagonals(s, lane, bias.at_bucket);
@@ -275,6 +279,10 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
         delta = both_sum(delta);
         if (half == 0 && i < p.N) p.delta[place] = delta;
         return;
+    }
+    if (WORK == kRowsPlain) {
+        rest = both_sum(rest);
+        if (half == 0 && i < p.N) p.delta[place] = delta + rest;
     }
     if (i < p.N) {
         if (!valid) {
@@ -439,7 +447,8 @@ __global__ __launch_bounds__(256, (kBackwardWaves<T, DP, (F & kCap) != 0>)) void
                 if (kWeight != 1.0f) s *= kWeight;
                 along_rows<T, DP>(dv, dt, Weights<T>(s), lane);
                 fit.fit(dp, dk);
-                along_rows<T, DP>(dk, qt, Weights<T>(dp), lane);
+                if (DP <= 96 && p.close) along_rows_twice<T, DP>(dk, qt, dp, lane);
+                else along_rows<T, DP>(dk, qt, Weights<T>(dp), lane);
             }
         }
     }
