@@ -406,11 +406,14 @@ int sdtw_position_bias_backward(const sdtw_bias_desc *desc, const void *grad, co
  *   causal: j <= i + offset_b, or j < prefix_b;
  *   row_document[b,i] == col_document[b,j] >= 0, where there are documents (any order; negative: in none).
  * A row that sees no key, that is not below row_len[b], or all of whose scores are -inf: out 0, lse -inf, gradients 0.
- *   - The bucket of a distance is that of sdtw_bias_desc.  A table entry below -1e30 forbids its cells as -inf does.
+ *   - The bucket of a distance is that of sdtw_bias_desc.  A table entry below -1e30 forbids its cells as -inf does; one above 2^100
+ *     counts as 2^100.
  *   - Keys and rows behind their length and in no document, and keys behind all that a causal row of the sequence sees, may hold
  *     anything, NaN too.  Of other keys and rows, infinities and NaN may reach every row or key of their sequence.
  *   - Scores, softmax and sums are carried in 32 bits.  For 16-bit types the softmax's numerators and the scores' gradients are rounded
- *     to the type for the matrix cores, in float16 under a scale that keeps small ones.
+ *     to the type for the matrix cores, in float16 under a scale that keeps small ones; those of dq to twice its digits.
+ *   - The backward call takes exp(s - lse) anew: weights are off by about |s| 2^-21 of themselves, so that gradients want scores far below 2^20.
+ *   - Tensors whose rows are no whole 16-byte chunks, or whose features are not side by side, are packed into the workspace first.
  *   - The same inputs give the same bits, forward and backward.
  */
 typedef struct sdtw_attention_desc {
@@ -421,7 +424,7 @@ typedef struct sdtw_attention_desc {
     int32_t max_distance;
     int32_t two_sided;
     int32_t causal;              /* 0 or 1 */
-    float scale;                 /* > 0, finite */
+    float scale;                 /* from 2^-26 to 2^26 */
     float cap;                   /* 0: none; else > 0, finite, and scale / cap finite */
     uint32_t flags;              /* 0 */
     int64_t offset;              /* offset_b of every sequence, |offset| < 2^62; not used with `offsets` */
@@ -449,7 +452,8 @@ size_t sdtw_attention_backward_workspace_bytes(const sdtw_attention_desc *desc);
 
 /*
  *   table [H, buckets]: device, read only; NULL exactly without buckets.  lists: host, or NULL.
- *   out [B,H,N,D], lse [B,H,N] (float32, contiguous): device, out.  They overlap no input.
+ *   out [B,H,N,D], lse [B,H,N] (float32, contiguous): device, out.  They overlap no input; one that begins where an input does is
+ *   refused (SDTW_ERR_INVALID_ARG).
  */
 int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
                            const sdtw_attention_lists *lists, void *out, float *lse, void *workspace, size_t workspace_bytes,
@@ -457,8 +461,10 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
 
 /*
  * out, lse: as the forward call with the same inputs left them.
- *   dq [B,H,N,D], dk, dv [B,Hk,M,D]: device, out.  dtable [H, buckets]: device, float32, contiguous, out; NULL if it is not wanted
- *   (the walk over the keys that serves it is then left out) and without buckets.
+ *   dq [B,H,N,D], dk, dv [B,Hk,M,D]: device, out; they overlap no input and not each other (views of one tensor side by side do
+ *   not overlap), and are refused where they begin at the same place.
+ *   dtable [H, buckets]: device, float32, contiguous, out; NULL if it is not wanted (what only it needs is then left out) and
+ *   without buckets.
  */
 int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
                             const sdtw_attention_lists *lists, const void *out, const float *lse, const void *dout, void *dq,

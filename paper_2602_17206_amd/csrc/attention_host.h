@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "attention_tiles.h"
 #include "host_common.h"
@@ -65,8 +66,11 @@ inline int attention_check(const sdtw_attention_desc *d, BucketRule *rule)
 {
     if (!d || d->B < 0 || d->H < 0 || d->Hk < 1 || d->N < 0 || d->M < 0 || d->D < 1) return SDTW_ERR_INVALID_ARG;
     if (d->H % d->Hk != 0 || d->N > 1 << 28 || d->M > 1 << 28) return SDTW_ERR_INVALID_ARG;
+    // (what follows stays within 64 bits)
+    const int64_t heads = (int64_t)d->B * d->H, key_heads = (int64_t)d->B * d->Hk, most = (int64_t)1 << 48;
+    if (heads > 0x7fffffff || key_heads > 0x7fffffff || heads * d->N > most || key_heads * d->M > most) return SDTW_ERR_INVALID_ARG;
     if (!attention_type_ok(d->type) || d->flags != 0 || (d->causal != 0 && d->causal != 1)) return SDTW_ERR_INVALID_ARG;
-    if (!(d->scale > 0.0f) || !std::isfinite(d->scale * kLog2e) || !std::isfinite(1.0f / d->scale)) return SDTW_ERR_INVALID_ARG;
+    if (!(d->scale >= 0x1p-26f && d->scale <= 0x1p26f)) return SDTW_ERR_INVALID_ARG;
     if (!(d->cap >= 0.0f) || !std::isfinite(d->cap * kLog2e) || (d->cap > 0.0f && !std::isfinite(d->scale / d->cap))) return SDTW_ERR_INVALID_ARG;
     if (d->offset >= (int64_t)1 << 62 || d->offset <= -((int64_t)1 << 62)) return SDTW_ERR_INVALID_ARG;
     if (d->prefix < 0 || (d->prefix > 0 && !d->causal)) return SDTW_ERR_INVALID_ARG;
@@ -87,6 +91,14 @@ inline bool lists_ok(const sdtw_attention_desc *d, const sdtw_attention_lists *l
 {
     if (!lists) return true;
     return (!lists->prefixes || d->causal) && !lists->row_document == !lists->col_document;
+}
+
+// Whether an output is none of the inputs (a kernel behind the one that writes it may still read them).  Empty tensors have no place.
+inline bool apart(const void *out, std::initializer_list<const void *> others)
+{
+    for (const void *x : others)
+        if (out && out == x) return false;
+    return true;
 }
 
 inline AttentionParams attention_params(const sdtw_attention_desc *d, const sdtw_attention_lists *lists)

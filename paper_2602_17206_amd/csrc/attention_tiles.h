@@ -405,8 +405,9 @@ __device__ __forceinline__ void cap_scores(Acc &s, float in, float out)
     }
 }
 
-// An entry times `unit`; one below -1e30 forbids its cells, as -inf does.
-__device__ __forceinline__ float entry_of(float v, float unit) { return v < -1e30f ? -INFINITY : v * unit; }
+// An entry times `unit`, which is at most 2^26; one below -1e30 forbids its cells, as -inf does, and one above 2^100 counts as that, so
+// that the product stays finite.  NaN stays NaN.
+__device__ __forceinline__ float entry_of(float v, float unit) { return v < -1e30f ? -INFINITY : (v > 0x1p100f ? 0x1p100f : v) * unit; }
 
 // Diagonals kept on each side of those that are not all in one bucket: a tile of 64 x 32 cells that touches these reaches over by 94.
 constexpr int kBiasMargin = 95;

@@ -7,7 +7,7 @@ import pytest
 import paper_2602_17206_amd as pkg
 from paper_2602_17206_amd import binding
 
-FAKE, OTHER = ctypes.c_void_p(0x10000), ctypes.c_void_p(0x20000)  # never dereferenced
+FAKE, OTHER, THIRD, FOURTH = (ctypes.c_void_p(0x10000 * n) for n in (1, 2, 3, 4))  # never dereferenced
 INVALID, UNSUPPORTED, WORKSPACE, OK = binding.STATUS_INVALID_ARG, binding.STATUS_UNSUPPORTED, binding.STATUS_WORKSPACE, binding.STATUS_OK
 
 
@@ -30,7 +30,7 @@ def forward(d, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lists=None, out=OTHER, lse=OT
     return pkg.load_library().sdtw_attention_forward(ctypes.byref(d) if d else None, q, k, v, table, lists, out, lse, ws, nbytes, None)
 
 
-def backward(d, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lists=None, out=FAKE, lse=FAKE, dout=FAKE, dq=OTHER, dk=OTHER, dv=OTHER, dtable=OTHER, ws=FAKE,
+def backward(d, q=FAKE, k=FAKE, v=FAKE, table=FAKE, lists=None, out=FAKE, lse=FAKE, dout=FAKE, dq=OTHER, dk=THIRD, dv=FOURTH, dtable=OTHER, ws=FAKE,
              nbytes=1 << 40):
     return pkg.load_library().sdtw_attention_backward(ctypes.byref(d) if d else None, q, k, v, table, lists, out, lse, dout, dq, dk, dv, dtable, ws,
                                                       nbytes, None)
@@ -48,7 +48,7 @@ def test_struct_sizes_match_the_header_layout():
 
 @pytest.mark.parametrize("kw", [
     dict(B=-1), dict(H=-1), dict(Hk=0), dict(Hk=3), dict(N=-1), dict(M=-1), dict(N=(1 << 28) + 1), dict(M=(1 << 28) + 1), dict(D=0), dict(type=3),
-    dict(type=-1), dict(flags=1), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38),
+    dict(type=-1), dict(flags=1), dict(causal=2), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(scale=2.0 ** -27), dict(scale=2.0 ** 27),
     dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")), dict(cap=1e-45), dict(offset=1 << 62), dict(offset=-(1 << 62)), dict(prefix=-1, causal=1),
     dict(prefix=1), dict(buckets=-1), dict(buckets=3), dict(buckets=258), dict(buckets=1, two_sided=0), dict(max_distance=8), dict(max_distance=1 << 25),
     dict(two_sided=2), dict(table_type=5), dict(table_stride=(-1, 1)), dict(q_stride=(-1, 64, 16, 1)), dict(k_stride=(224, 112, 16, -1)),
@@ -90,6 +90,17 @@ def test_attention_pointers_strides_and_workspace():
         assert backward(desc(dv_stride=stride)) == INVALID, stride
 
 
+def test_outputs_in_the_place_of_inputs_are_refused():
+    fifth = ctypes.c_void_p(0x50000)
+    for name in ("q", "k", "v", "table"):
+        assert forward(desc(), **{name: OTHER}) == INVALID, name
+    for out in ("dq", "dk", "dv"):
+        for name in ("q", "k", "v", "table", "out", "dout"):
+            assert backward(desc(), **{name: fifth, out: fifth}) == INVALID, (out, name)
+    for a, b in (("dq", "dk"), ("dq", "dv"), ("dk", "dv")):
+        assert backward(desc(), **{a: fifth, b: fifth}) == INVALID, (a, b)
+
+
 def test_attention_lists():
     lists = binding.AttentionLists()
     d, ref = desc(), ctypes.byref(lists)
@@ -111,7 +122,8 @@ def test_nothing_to_do():
 
 def test_problems_that_need_more_workgroups_than_there_are():
     most = (1 << 31) - 1
-    for kw in (dict(B=1 << 20, H=1 << 20, Hk=1 << 20), dict(B=most, H=most, Hk=1, N=1 << 28, M=1 << 28), dict(B=1 << 12, H=1 << 12, Hk=1, N=1 << 20)):
+    for kw in (dict(B=1 << 20, H=1 << 20, Hk=1 << 20), dict(B=most, H=most, Hk=most, N=1 << 28, M=1 << 28),
+               dict(B=1 << 20, H=1, Hk=1, M=1 << 28, N=1 << 28), dict(B=most, H=most, Hk=1, N=1 << 28, M=1 << 28), dict(B=1 << 12, H=1 << 12, Hk=1, N=1 << 20)):
         d = desc(**{**kw, **{s: (0, 0, 0, 1) for s in ("q_stride", "k_stride", "v_stride", "dout_stride")}})
         assert sizes(d)[0] == 0 or sizes(d)[1] == 0
         assert forward(d) == INVALID and backward(d) == INVALID

@@ -265,6 +265,25 @@ def test_forbidden_distances(N, M, low, kind):
         check(1, 2, 1, N, M, 32, kind, table=table)
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("scale", [2.0 ** -26, 0.25, 2.0 ** 26])
+@pytest.mark.parametrize("N", [1, 40])
+def test_entries_that_outweigh_all_scores(N, scale, kind):
+    # at distance 3 an entry of 2^100 or more: a row sees that key alone, which 2^100 stands out from all scores for, and lse is the entry
+    (q, k, v, _), _ = problem(1, 2, 2, N, 40, 32, kind, seed=3)
+    table = some_table(2, 16).clone()
+    table[0, 3], table[1, 3] = 2.0 ** 100, 3e38
+    options = dict(scale=scale, causal=True, two_sided=False, max_distance=50, offset=40 - N)
+    out, lse = pkg.sdtw_attention_forward(q, k, v, table, **options)
+    rows = torch.arange(N, device="cuda") + 40 - N
+    those = rows >= 3
+    # the weight and the sum are both 1: out is v, rounded not at all
+    assert torch.equal(out[:, :, those], v[:, :, rows[those] - 3])
+    # the entry by 1 / scale (a power of two, or 4), by scale times log2(e) and by ln(2), each rounded: 4 roundings
+    assert ((lse[:, :, those].double() / 2.0 ** 100 - 1).abs() <= 4 * EPS).all()
+    assert torch.isfinite(out).all() and torch.isfinite(lse).all()
+
+
 def test_bias_without_its_gradient():
     check(2, 2, 1, 200, 300, 64, "bf16", table=some_table(2, 32), want_dtable=False)
 
