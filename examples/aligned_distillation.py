@@ -3,7 +3,7 @@
 Nobody says which frame of the teacher a frame of the student answers to.  Soft-DTW aligns their features, with a learned
 penalty on how far apart two frames' positions are; the alignment names a teacher's row for every row of the student's logits;
 and the student's logits are drawn towards the teacher's top logits there.  The student attends over its frames under a learned
-bias on relative positions.
+bias on relative positions, and its gradients are clipped to a largest norm.
 
     python examples/aligned_distillation.py [steps]
 """
@@ -16,21 +16,23 @@ sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."
 import paper_2602_17206_amd as sdtw  # noqa: E402
 
 RULE = dict(max_distance=64, two_sided=True)
-BUCKETS, HEADS, GAMMA, TEMPERATURE = 16, 2, 0.1, 2.0
+BUCKETS, HEADS, GAMMA, TEMPERATURE, MAX_NORM = 16, 2, 0.1, 2.0, 1.0
 
 
-class PositionBias(torch.autograd.Function):
-    """scores [B, H, N, N] + table [H, buckets] by the distance of their positions"""
+class Attention(torch.autograd.Function):
+    """q, k, v [B, H, N, D] to [B, H, N, D], with a bias table [H, buckets] by distance, each sequence within its length"""
 
     @staticmethod
-    def forward(ctx, scores, table, lengths):
-        ctx.lengths, ctx.buckets = lengths, table.shape[1]
-        return sdtw.sdtw_position_bias_forward(table, scores, row_len=lengths, col_len=lengths, **RULE)
+    def forward(ctx, q, k, v, table, lengths):
+        out, lse = sdtw.sdtw_attention_forward(q, k, v, table, row_len=lengths, col_len=lengths, **RULE)
+        ctx.save_for_backward(q, k, v, table, lengths, out, lse)
+        return out
 
     @staticmethod
     def backward(ctx, grad):
-        # (scores outside a sequence's length pass through unbiased and so does their gradient)
-        return grad, sdtw.sdtw_position_bias_backward(grad, ctx.buckets, row_len=ctx.lengths, col_len=ctx.lengths, **RULE), None
+        q, k, v, table, lengths, out, lse = ctx.saved_tensors
+        dq, dk, dv, dtable = sdtw.sdtw_attention_backward(q, k, v, out, lse, grad, table, row_len=lengths, col_len=lengths, **RULE)
+        return dq, dk, dv, dtable.to(table.dtype), None
 
 
 class Student(torch.nn.Module):
@@ -47,10 +49,8 @@ class Student(torch.nn.Module):
         """(features [B, N, width], logits [B * N, vocab] bfloat16)"""
         B, N, _ = x.shape
         h = torch.tanh(x @ self.embed)
-        q, k, v = (h @ self.qkv).view(B, N, 3, HEADS, -1).permute(2, 0, 3, 1, 4).contiguous()
-        scores = PositionBias.apply(q @ k.transpose(2, 3).contiguous() / q.shape[-1] ** 0.5, self.bias, lengths)
-        beyond = torch.arange(N, device="cuda") >= lengths[:, None]
-        mixed = scores.masked_fill(beyond[:, None, None, :], float("-inf")).softmax(-1) @ v
+        q, k, v = (h @ self.qkv).view(B, N, 3, HEADS, -1).permute(2, 0, 3, 1, 4)
+        mixed = Attention.apply(q, k, v, self.bias, lengths)
         h = h + mixed.permute(0, 2, 1, 3).reshape(B, N, -1) @ self.out
         return h, (h.reshape(B * N, -1) @ self.head).bfloat16()
 
@@ -83,7 +83,8 @@ def train(steps=60, seed=0):
     student = Student(inputs, width, vocab, torch.Generator(device="cuda").manual_seed(seed + 1))
     # the penalty on cells off the diagonal: 0 nearby, more with each bucket of distance
     penalty = torch.nn.Parameter(0.02 * (torch.arange(BUCKETS, device="cuda") % (BUCKETS // 2)).float()[None])
-    optimizer = torch.optim.Adam([*student.parameters(), penalty], lr=0.01)
+    parameters = [*student.parameters(), penalty]
+    optimizer = torch.optim.Adam(parameters, lr=0.01)
     inside = torch.arange(N, device="cuda") < x_len[:, None]
     row_weight = (inside / inside.sum()).reshape(-1).float()
     # every student with its own teacher, and with its neighbour's
@@ -108,6 +109,7 @@ def train(steps=60, seed=0):
                                                 teacher_row=teacher_row)
         torch.autograd.backward([both_x, logits], [d_pairs, d_logits])
         penalty.grad = d_penalty
+        sdtw.sdtw_gradient_clip([p.grad for p in parameters], MAX_NORM)
         optimizer.step()
         history.append((float((loss * row_weight).sum()), float(margin.mean())))
     return history
