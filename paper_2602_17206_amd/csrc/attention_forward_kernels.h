@@ -15,10 +15,12 @@ namespace sdtw {
 template <int DP> struct Running {
     static constexpr float kAhead = 8.0f;
     float m, l;
+    bool far;  // some reference of the wavefront's is so large that its rounding would show in an exponent
     Acc o[DP / 32];
     __device__ __forceinline__ void clear()
     {
         m = -INFINITY;
+        far = false;
         l = 0.0f;
 #pragma unroll
         for (int ft = 0; ft < DP / 32; ++ft) o[ft] = Acc{};
@@ -30,6 +32,7 @@ template <int DP> struct Running {
             const float to = fmaxf(m, top);
             const float factor = m == to ? 1.0f : exp2_fast(m - to);
             m = to;
+            far = far || __any(fabsf(m) > 65536.0f && fabsf(m) < INFINITY);
             l *= factor;
 #pragma unroll
             for (int ft = 0; ft < DP / 32; ++ft) o[ft] *= factor;
@@ -46,6 +49,14 @@ template <int DP> struct Running {
             for (int r = 2; r < 16; r += 2) top[x] = fmaxf(fmaxf(s[x][r], s[x][r + 1]), top[x]);
         }
         raise(fmaf(both_max(SUBS == 2 ? fmaxf(top[0], top[SUBS - 1]) : top[0]), factor, add));
+        if (far) {  // then scores are rounded as their maximum was, before it is subtracted
+#pragma unroll
+            for (int x = 0; x < SUBS; ++x)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[x][r] = fmaf(s[x][r], factor, add);
+            factor = 1.0f;
+            add = 0.0f;
+        }
         const float from = add - (m == -INFINITY ? 0.0f : m);
         float sum[2] = {};
 #pragma unroll

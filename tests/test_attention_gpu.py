@@ -284,6 +284,26 @@ def test_entries_that_outweigh_all_scores(N, scale, kind):
     assert torch.isfinite(out).all() and torch.isfinite(lse).all()
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("with_table", [False, True])
+@pytest.mark.parametrize("N,M", [(3, 70), (40, 40), (100, 300), (1000, 1030)])
+def test_scores_of_any_size(N, M, with_table, kind):
+    # Every key's product with every row is a whole number below 2^11 times 2^e, keys M - 1 to M / 2 have the most, all alike: a row's answer is
+    # the mean of their values whatever the size of the scores.  Weights 1 are exact, their sum too; the values' sum has M roundings.
+    gen = torch.Generator(device="cuda").manual_seed(N + M)
+    D, H, e = 32, 3, {"f16": 12, "bf16": 50, "f32": 50}[kind]
+    q, k = (torch.zeros((1, H, n, D), device="cuda") for n in (N, M))
+    q[..., 0] = 2.0 ** e
+    k[..., 0] = torch.where(torch.arange(M, device="cuda") < M // 2, 5.0, 7.0) * 2.0 ** (e if kind == "f16" else 40)
+    v = values((1, H, M, D), kind, gen)
+    out, lse = pkg.sdtw_attention_forward(q.to(TYPES[kind]), k.to(TYPES[kind]), v, some_table(H, 16) * 0.0 if with_table else None, scale=3.0)
+    mean = v[:, :, M // 2:].double().mean(2, keepdim=True)
+    size = v[:, :, M // 2:].double().abs().mean(2, keepdim=True)
+    assert ((out - mean).abs() <= 1.01 * HALF_ULP[kind] * mean.abs() + (M + 4) * EPS * size + LEAST[kind]).all()
+    score = 3.0 * q[0, 0, 0, 0].double() * k[0, 0, -1, 0].double()
+    assert ((lse.double() / score - 1).abs() <= 8 * EPS).all()
+
+
 def test_bias_without_its_gradient():
     check(2, 2, 1, 200, 300, 64, "bf16", table=some_table(2, 32), want_dtable=False)
 
