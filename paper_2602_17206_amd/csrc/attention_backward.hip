@@ -17,9 +17,18 @@ BackwardPlan backward_plan(const sdtw_attention_desc *d)
     BackwardPlan P{};
     P.row_tiles = ((int64_t)d->N + 127) / 128;
     P.key_tiles = ((int64_t)d->M + 127) / 128;
-    // The keys' kernel is split over the rows until there are about four workgroups for each compute unit, of four tiles of rows at least.
+    // The keys' kernel is split over the rows, of which it walks `steps` tiles, until there are two workgroups for each compute unit, or
+    // four where they still have 32 tiles each; with at least 8 tiles (4 where units are very few).  What it costs is parts in 32 bits and the
+    // launch that adds them up.  bfloat16, us with and without a split:
+    //   1 x 8 heads in groups of 4, 2048 x 64: 47 (8 parts) and 267; 32 parts 57   1 x 8 x 1024 x 64: 31 (4) and 40
+    //   1 x 16 x 2048 x 64: 69 (2) and 74; 4 parts 79   2 x 16 heads in groups of 4, 4096 x 128, causal: 331 (4) and 772; 2 parts 458
+    //   4 x 16 x 1024 x 64 (512 units): 82 (2) and 54   5 x 16 x 512 x 64 (8 tiles): 49 (2) and 33
     const int64_t units = (int64_t)d->B * d->Hk * P.key_tiles, steps = (int64_t)(d->H / d->Hk) * (((int64_t)d->N + 63) / 64);
-    P.parts = units > 0 && units < (1 << 20) ? std::max<int64_t>(1, std::min<int64_t>((1024 + units - 1) / units, steps / 4)) : 1;
+    P.parts = 1;
+    if (units > 0 && units < 512) {
+        const int64_t two = (511 + units) / units, four = (1023 + units) / units;
+        P.parts = steps >= 32 * four ? four : std::max<int64_t>(1, std::min(two, steps / (units < 128 ? 4 : 8)));
+    }
     P.fits = (int64_t)d->B * d->H <= 0x7fffffff && attention_grid_ok((int64_t)d->B * d->H * std::max<int64_t>(1, P.row_tiles)) &&
              (int64_t)d->B * d->Hk <= 0x7fffffff &&
              attention_grid_ok((int64_t)d->B * d->Hk * std::max<int64_t>(1, P.key_tiles) * P.parts) && attention_grid_ok((int64_t)d->H * d->buckets);

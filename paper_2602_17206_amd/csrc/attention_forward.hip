@@ -26,7 +26,14 @@ ForwardPlan split_forward(const sdtw_attention_desc *d)
     P.splits = 1;
     if (d->B == 0 || d->H == 0 || d->N == 0) return P;
     const int64_t tiles = (d->N + 127) / 128, G = d->H / d->Hk;
-    P.few = (d->N * G <= 64 || (int64_t)d->B * d->H * tiles < 256) && few_rows_lds(d) + 4096 <= kLdsBytes;
+    // The kernel for few rows, where there are no 1024 wavefronts of 32 rows for the other one (the matrix cores have as many), or a group's
+    // rows fill no more than two of its tiles; over few keys its joins cost more than they give.  bfloat16 (float32), D 64, one head a group, us
+    // with it and with the other:
+    //   64 rows of 16 x 16 heads, 8192 keys: 141 and 207; 128 rows: 228 and 198   4 x 1000 x 1000: 21 and 21 (29 and 78); 256: 116 and 59
+    //   32 x 512 x 512: 14 and 14 (31 and 44)   32 x 256 x 256: 11 and 10 (15 and 25)   256 x 192 x 192: 23 and 12 (50 and 33)
+    //   4 x 64 x 64: 10 and 8 (13 and 11)   8 x 4 groups of 8 heads, 32 rows, 8192 keys: 55 and 147
+    const int64_t waves = (int64_t)d->B * d->H * ((d->N + 31) / 32);
+    P.few = (d->N * G <= 64 || waves < 1024) && d->M > (d->type == SDTW_TYPE_F32 ? 64 : 256) && few_rows_lds(d) + 4096 <= kLdsBytes;
     if (!P.few) {
         P.row_tiles = tiles;
         P.workgroups = (int64_t)d->B * d->H * tiles;
