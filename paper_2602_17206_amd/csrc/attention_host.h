@@ -159,8 +159,9 @@ inline void pack(const sdtw_attention_desc *d, const void *&x, int64_t (&stride)
     stride[3] = 1; stride[2] = loaded; stride[1] = loaded * rows; stride[0] = loaded * rows * heads;
 }
 
-// Diagonals from the last bucket's first distance on either side, and a margin; 0 beyond 2048 of them (10 KB of LDS), which take longer to lay
-// out than to look up tile by tile.
+// Diagonals from the last bucket's first distance on either side, and a margin; 0 beyond 2048 of them (10 KB of LDS).  Laid out once they save
+// looking them up tile by tile: 4 x 16 x 2048 x 2048 x 64 bfloat16 causal, last distance 1024: forward 66 us and 68 without, delta 59 and 65, rows
+// 229 and 242, keys 124 and 135; beyond 2048 there is nothing left to gain (4096: 69, 69, 255 and 126 either way).
 inline int near_diagonals(const sdtw_attention_desc *d, const BucketRule &rule)
 {
     if (!d->buckets) return 0;

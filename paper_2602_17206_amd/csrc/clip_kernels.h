@@ -5,6 +5,9 @@
 // up in 64 bits by workgroups; then every workgroup adds those sums up itself, in one order, and scales its share.
 // Both read all of the gradients.  The second walks from the end to the beginning: what was read last is still in
 // the memory-side cache.
+// What bounds it: reading twice and writing once, 386 us for 400 tensors of 430 MB bfloat16 that leave in float32 (1.7 GB, 4.5 TB/s); one
+// read cannot be saved, as no element may be written before the norm is known and they do not fit on the chip.  Small lists wait
+// for the launch: 13 tensors of 10000 elements, 8.3 us in one kernel.
 #pragma once
 #include "vector_io.h"
 
