@@ -1090,9 +1090,9 @@ def _attention_args(q, k, v, table, scale, cap, causal, max_distance, two_sided,
         lists[5] = _positions_ptr(col_document, B, M, dev, "col_document")
     try:
         desc = _attention_desc(B, H, Hk, N, M, D, _type_of(q, "q"), table_type, buckets, max_distance, 1 if two_sided else 0, 1 if causal else 0,
-                               D ** -0.5 if scale is None else scale, cap, 0, offset, prefix, *q.stride(), *k.stride(), *v.stride(), *out, *dout,
+                               max(D, 1) ** -0.5 if scale is None else scale, cap, 0, offset, prefix, *q.stride(), *k.stride(), *v.stride(), *out, *dout,
                                *dq, *dk, *dv, *table_strides)
-    except OverflowError:
+    except (OverflowError, struct.error):
         raise ValueError("scale and cap must be float32 numbers") from None
     return desc, _attention_lists(*lists) if any(lists) else None, (q.data_ptr(), k.data_ptr(), v.data_ptr(), tp)
 

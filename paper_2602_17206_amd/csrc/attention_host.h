@@ -90,7 +90,9 @@ inline int attention_check(const sdtw_attention_desc *d, BucketRule *rule)
 inline bool lists_ok(const sdtw_attention_desc *d, const sdtw_attention_lists *lists)
 {
     if (!lists) return true;
-    return (!lists->prefixes || d->causal) && !lists->row_document == !lists->col_document;
+    if (lists->prefixes && !d->causal) return false;
+    // (an empty list may have no place)
+    return !lists->row_document == !lists->col_document || d->B == 0 || d->N == 0 || d->M == 0;
 }
 
 // Whether an output is none of the inputs (a kernel behind the one that writes it may still read them).  Empty tensors have no place.

@@ -112,6 +112,13 @@ def test_attention_lists():
     assert forward(d, lists=ref) == INVALID and backward(d, lists=ref) == INVALID
 
 
+def test_an_empty_list_of_documents_has_no_place():
+    lists = binding.AttentionLists()
+    lists.col_document = FAKE
+    assert forward(desc(), lists=ctypes.byref(lists)) == INVALID and backward(desc(), lists=ctypes.byref(lists)) == INVALID
+    assert forward(desc(N=0), lists=ctypes.byref(lists)) == OK and backward(desc(N=0, M=0), lists=ctypes.byref(lists), dtable=None) == OK
+
+
 def test_nothing_to_do():
     for kw in (dict(B=0), dict(H=0), dict(N=0)):
         assert forward(desc(**kw), q=None, k=None, v=None, table=None, out=None, lse=None, ws=None, nbytes=0) == OK

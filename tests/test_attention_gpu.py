@@ -421,6 +421,17 @@ def test_empty_problems():
     assert out.shape == (2, 4, 0, 8) and lse.shape == (2, 4, 0)
     dq, dk, dv, dt = pkg.sdtw_attention_backward(q[:, :, :0], k, k, out, lse, out, table)
     assert dq.shape == (2, 4, 0, 8) and (dk == 0).all() and (dv == 0).all() and (dt == 0).all()
+    for cap in (0.0, 3.0):
+        for n, m in ((3, 0), (0, 5)):
+            rows, keys = q[:, :, :n], k[:, :, :m]
+            documents = dict(cap=cap, row_document=torch.zeros((2, n), dtype=torch.int32, device="cuda"),
+                             col_document=torch.zeros((2, m), dtype=torch.int32, device="cuda"))
+            out, lse = pkg.sdtw_attention_forward(rows, keys, keys, table, **documents)
+            assert (out == 0).all() and (lse == -INF).all()
+            dq, dk, dv, dt = pkg.sdtw_attention_backward(rows, keys, keys, out, lse, rows, table, **documents)
+            assert all((x == 0).all() for x in (dq, dk, dv, dt))
+    with pytest.raises(pkg.SdtwError):
+        pkg.sdtw_attention_forward(q[..., :0], k[..., :0], k[..., :0])
     out, lse = pkg.sdtw_attention_forward(q[:0], k[:0], k[:0], table)
     dq, dk, dv, dt = pkg.sdtw_attention_backward(q[:0], k[:0], k[:0], out, lse, out, table)
     assert dq.shape == (0, 4, 3, 8) and (dt == 0).all()
@@ -593,7 +604,7 @@ def test_refusals_of_the_binding():
         dict(row_len=i32(3)), dict(col_len=i32(2).float()), dict(row_document=i32(2, 6)), dict(col_document=i32(2, 7)),
         dict(row_document=i32(2, 7), col_document=i32(2, 7)), dict(row_document=i32(2, 12)[:, ::2], col_document=i32(2, 7)),
         dict(out=torch.empty_like(out)[:, :, :5]), dict(out=torch.empty_like(out).float()), dict(lse=lse[:1]), dict(lse=lse.double()),
-        dict(max_distance=1 << 40), dict(max_distance=2.5),
+        dict(max_distance=1 << 40), dict(max_distance=2.5), dict(scale="1"), dict(scale=1e300), dict(cap=None),
     ]
     for kw in bad:
         a = {"q": q, "k": k, "v": v, "table": table, **kw}
