@@ -120,7 +120,11 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
             constexpr int F = decltype(variant)::value;
             const size_t bytes = 4 * TileShape<T, DP>::bytes(kKeys) + bias_bytes(4, p.near);
             const unsigned grid = (unsigned)((int64_t)p.B * p.H * p.row_tiles);
-            if (rows && close_delta) {
+            // Few keys and workgroups: delta in the same kernel saves a launch; with more, its own one has more wavefronts on a SIMD.  us in
+            // one kernel and in two, with the table's gradient: 4 x 2 x 96 x 96 x 16 float32 27 and 33; 4 x 16 x 256 x 256 x 64 bfloat16 34 and
+            // 40; 8 x 16 x 512 x 512 67 and 72; 16 x 16 x 512 x 512 126 and 127; 2 x 16 x 2048 x 2048 141 and 136.
+            p.together = kTogether<DP> && grid <= 512 && p.M <= 512;
+            if (rows && close_delta && !p.together) {
                 ProfScope ps("attention_delta", st);
                 attention_rows_gradient_kernel<T, DP, F, kRowsDelta><<<grid, 256, bytes, st>>>(p, rule);
             }

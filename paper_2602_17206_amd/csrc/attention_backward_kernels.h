@@ -7,7 +7,7 @@
 // Two kernels, each the sole writer of what it sums: no atomics on memory, the same bits from the same inputs.
 //   rows   wavefronts own queries and walk over the keys: delta, dq, dtable
 //   keys   wavefronts own keys and walk over the queries of all heads of the group: dk, dv
-// The products are made twice, which is 14 D operations a cell for the formula's 10; one kernel that made them once would have to add dq up in
+// The products are made twice, which is 14 D operations a cell for the formula's 10 (18 D with delta's walk); one kernel that made them once would have to add dq up in
 // memory, by atomics or by 32-bit parts of all keys.
 // What bounds them: matrix cores and vector units in turn, at two wavefronts a SIMD, which is what registers leave.  4 x 16 x 2048 x 2048 x 64
 // bfloat16 causal with bias and its table: delta 57 us, rows 143, keys 130; 2 x 16 heads in groups of 4, 4096 x 4096 x 128 causal with
@@ -107,6 +107,9 @@ struct TableSum {
 // Both products of a tile before anything else, where there are registers for it: the matrix cores go on while the scores are worked on.
 template <int DP> constexpr bool kEarly = DP < 128;
 
+// Whether the rows' kernel can sum delta up itself (beyond that there are no registers for it).
+template <int DP> constexpr bool kTogether = DP <= 96;
+
 // Wavefronts on a SIMD that registers are kept for.
 template <typename T, int DP> constexpr int kDeltaWaves = sizeof(T) == 4 ? (DP <= 32 ? 4 : DP <= 64 ? 2 : 1) : DP <= 64 ? 4 : 3;
 template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T) == 4 ? (DP <= 32 ? 2 : 1) : DP <= 32 ? 3 : DP <= 96 || !MORE ? 2 : 1;
@@ -169,7 +172,9 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
     float delta = 0.0f;
     // With the delta that there is, a row's ds add up to what delta is off by: the kernel for the keys gets the better one.
     float rest = 0.0f;
-    if ((TABLE || WORK == kRowsGiven) && valid) delta = p.delta[place];
+    constexpr bool GIVEN = TABLE || WORK == kRowsGiven, BOTH = GIVEN && kTogether<DP>;
+    bool summing = BOTH && p.together;  // this walk over the keys is for delta
+    if (GIVEN && !summing && valid) delta = p.delta[place];
     if (WORK == kRowsPlain) {
         const Rows<T> x = rows_of<T>(p.out, p.out_stride, b, h);
         Column<T, DP> out;
@@ -221,6 +226,11 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
             __syncthreads();
         }
         t = walk.next(t + 1);
+        const bool for_delta = summing;
+        if (BOTH && summing && t >= walk.tiles) {
+            summing = false;
+            t = walk.next(0);
+        }
         if (kBuffers == 2) {
             buffer ^= 1;
             if (t < walk.tiles) fetch(t, buffer);
@@ -254,7 +264,7 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
                 for (int r = 0; r < 16; ++r) s[r] = seen.at[r] ? s[r] : 0.0f;
             }
             if (!kEarly<DP>) dp = along_features<T, DP>(vt, dout, lane);
-            if (WORK == kRowsDelta) {  // (a tile's sum first: hundreds of additions to one number would show)
+            if (WORK == kRowsDelta || (BOTH && for_delta)) {  // (a tile's sum first: hundreds of additions to one number would show)
                 float sum = s[0] * dp[0];
 #pragma unroll
                 for (int r = 1; r < 16; ++r) sum = fmaf(s[r], dp[r], sum);
@@ -282,7 +292,9 @@ __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBa
             fit.fit(s, dq);
             along_rows_twice<T, DP>(dq, kt, s, lane);
         }
+        if (BOTH && for_delta && !summing) delta = both_sum(delta);
     }
+    if (BOTH && p.together && half == 0 && i < p.N) p.delta[place] = delta;
     if (WORK == kRowsDelta) {
         delta = both_sum(delta);
         if (half == 0 && i < p.N) p.delta[place] = delta;

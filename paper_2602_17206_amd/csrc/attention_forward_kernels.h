@@ -7,7 +7,7 @@
 // Scores and their exponentials never leave registers: 32 rows stand in a wavefront's columns, 64 keys at a time come through LDS, copied
 // there directly, one tile while the other is worked on.
 // What bounds it: the vector units, which take 32 exponents, maxima, sums and conversions a lane for each tile, at D = 64 (4 x 16 x 2048 x 2048
-// bfloat16 causal with bias 55 us, 626 TFLOP/s with the skipped half not counted; without mask and bias 92 us, 733 TFLOP/s); they and the
+// bfloat16 causal with bias 54 us, 638 TFLOP/s with the skipped half not counted; without mask and bias 92 us, 733 TFLOP/s); they and the
 // matrix cores alike at D = 128 (160 us, 859 TFLOP/s, where a large library product reaches 1243).
 // Tried: no maximum taken within a tile (77 us for 62 then: scalar registers spilled); three wavefronts a SIMD instead of four (slower).
 #pragma once

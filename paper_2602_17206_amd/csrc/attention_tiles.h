@@ -322,6 +322,7 @@ struct AttentionParams {
     int64_t table_stride[2];
     // how the work is split
     int32_t row_tiles, key_tiles, splits, parts, table_columns;
+    int32_t together;           // the rows' kernel sums delta up itself, in a walk over the keys before the one for gradients
     int32_t close;              // few keys: their gradients' weights to twice the type's digits
     int32_t near;               // diagonals of the neighbourhood that is laid out; 0: it is too wide
     float *part;                // [B, H, N, splits][D + 2]: unfinished sums, their reference and total
