@@ -7,8 +7,8 @@
 // Two kernels, each the sole writer of what it sums: no atomics on memory, the same bits from the same inputs.
 //   rows   wavefronts own queries and walk over the keys: delta, dq, dtable
 //   keys   wavefronts own keys and walk over the queries of all heads of the group: dk, dv
-// The products are made twice, which is 14 D operations a cell for the formula's 10 (18 D with delta's walk); one kernel that made them once would have to add dq up in
-// memory, by atomics or by 32-bit parts of all keys.
+// The products are made twice, which is 14 D operations a cell for the formula's 10 (18 D with delta's walk); one kernel that made them once
+// would have to add dq up in memory, by atomics or by 32-bit parts of all keys.
 // What bounds them: matrix cores and vector units in turn, at two wavefronts a SIMD, which is what registers leave.  4 x 16 x 2048 x 2048 x 64
 // bfloat16 causal with bias and its table: delta 57 us, rows 143, keys 130; 2 x 16 heads in groups of 4, 4096 x 4096 x 128 causal with
 // prefixes: rows 353 (matrix cores busy 55 % of the time), keys 404 (45 %), their parts added up 24.
