@@ -90,12 +90,19 @@ template <typename V> __device__ __forceinline__ V lds_read(uint32_t address, in
 }
 
 // 16 bytes a lane from the window straight into LDS, lane after lane from `lds` on.  Written out because the compiler, which cannot tell the
-// tile that is being filled from the one that is being read, would wait for it before every read.
+// tile that is being filled from the one that is being read, would wait for it before every read.  It does not look into what is written
+// out, so the wait states that the hardware does not see to are here: one between m0's write and the copy that reads it, and five after a vector
+// instruction that wrote a scalar register - the window comes from readfirstlane, or from lanes that scalar registers were spilled to -
+// of which m0's write is one and s_nop 3 are four.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is reserved, so that naming it is warned of; it is not to be kept here)
 __device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint32_t at, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from), "s"(__builtin_amdgcn_readfirstlane(lds))
-                 : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from),
+                 "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 // All that the wavefront asked for is there, and what it read from LDS has left it.
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
