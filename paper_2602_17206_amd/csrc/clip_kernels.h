@@ -109,7 +109,25 @@ template <> struct Piece<8> {
     typedef Bits Any __attribute__((aligned(2)));
 };
 
-template <typename T, typename U> __device__ __forceinline__ void clip_scale(const T *in, U *out, int n, float factor, int who, int threads)
+// What the gradients are multiplied by, as `by` 2^octaves: octaves is 0, but for factors below the normal numbers, which would have
+// few digits or none.
+struct ClipFactor {
+    float by;
+    int octaves;
+    bool scaled;
+    __device__ __forceinline__ ClipFactor(double norm, float max_norm) : octaves(0), scaled(norm > (double)max_norm && norm < INFINITY)
+    {
+        double factor = scaled ? (double)max_norm / norm : 1.0;  // (a NaN is not scaled)
+        if (factor < 0x1p-126) {
+            octaves = __builtin_amdgcn_frexp_exp(factor);
+            factor = __builtin_amdgcn_frexp_mant(factor);
+        }
+        by = (float)factor;
+    }
+    __device__ __forceinline__ float times(float x) const { return __builtin_amdgcn_ldexpf(x * by, octaves); }
+};
+
+template <typename T, typename U> __device__ __forceinline__ void clip_scale(const T *in, U *out, int n, const ClipFactor &factor, int who, int threads)
 {
     constexpr int W = 16 / (sizeof(T) > sizeof(U) ? (int)sizeof(T) : (int)sizeof(U)), kSteps = 8;
     typedef Piece<W * (int)sizeof(T)> In;
@@ -120,7 +138,7 @@ template <typename T, typename U> __device__ __forceinline__ void clip_scale(con
         for (int e = 0; e < (int)sizeof(v) / 4; ++e) b[e] = v[e];
         float x[Elem<U>::kWidth] = {};
 #pragma unroll
-        for (int e = 0; e < W; ++e) x[e] = Elem<T>::at(b, e) * factor;
+        for (int e = 0; e < W; ++e) x[e] = factor.times(Elem<T>::at(b, e));
         const Bits4 y = Elem<U>::pack(x);
         typename Out::Bits z;
         for (int e = 0; e < (int)sizeof(z) / 4; ++e) z[e] = y[e];
@@ -135,7 +153,7 @@ template <typename T, typename U> __device__ __forceinline__ void clip_scale(con
         for (int s = 0; s < kSteps; ++s) store(i + s * threads * W, v[s]);
     }
     for (; i + W <= n; i += threads * W) store(i, load(i));
-    for (; i < n; ++i) out[i] = Elem<U>::down(Elem<T>::up(in[i]) * factor);  // (one thread's at most, fewer than a piece)
+    for (; i < n; ++i) out[i] = Elem<U>::down(factor.times(Elem<T>::up(in[i])));  // (one thread's at most, fewer than a piece)
 }
 
 // Calls f with the element that SDTW_TYPE_* `type` stands for.
@@ -166,10 +184,9 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipList list, ClipPara
     for (int k = threadIdx.x; k < p.all_parts; k += 256) sum += p.parts[k];
     const double norm = sqrt(workgroup_sum_f64(sum, lds));
     if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
-    const bool scaled = norm > (double)p.max_norm && norm < INFINITY;  // (false for a NaN)
-    const float factor = scaled ? (float)((double)p.max_norm / norm) : 1.0f;
+    const ClipFactor factor(norm, p.max_norm);
     clip_chunks<true>(list, [&](int tensor, int64_t at, int n) {
-        if (!scaled && list.out[tensor] == list.data[tensor]) return;
+        if (!factor.scaled && list.out[tensor] == list.data[tensor]) return;
         const uint64_t types = list.count_types[tensor];
         clip_typed((int)(types >> 56 & 15), [&](auto t) {
             clip_typed((int)(types >> 60), [&](auto u) {
@@ -206,10 +223,9 @@ __global__ __launch_bounds__(1024) void clip_small_kernel(ClipList list, ClipPar
     for (int w = 0; w < 16; ++w) sum += sums[w];
     const double norm = sqrt(sum);
     if (threadIdx.x == 0) *p.norm = (float)norm;
-    const bool scaled = norm > (double)p.max_norm && norm < INFINITY;
-    const float factor = scaled ? (float)((double)p.max_norm / norm) : 1.0f;
+    const ClipFactor factor(norm, p.max_norm);
     each([&](int tensor, int64_t at, int n) {
-        if (!scaled && list.out[tensor] == list.data[tensor]) return;
+        if (!factor.scaled && list.out[tensor] == list.data[tensor]) return;
         const uint64_t types = list.count_types[tensor];
         clip_typed((int)(types >> 56 & 15), [&](auto t) {
             clip_typed((int)(types >> 60), [&](auto u) {

@@ -99,6 +99,12 @@ def test_gradients_of_any_size(size):
     check(grads, 100.0 * size)
 
 
+@pytest.mark.parametrize("max_norm", [1e-9, 1e-30])
+def test_factors_below_the_normal_numbers(max_norm):
+    grads = some([5000, 77], ["f32", "bf16"], size=1e32)
+    check(grads, max_norm)
+
+
 @pytest.mark.parametrize("bad", [INF, -INF, NAN])
 @pytest.mark.parametrize("kind", sorted(TYPES))
 def test_a_norm_that_is_not_finite_leaves_the_gradients(kind, bad):
