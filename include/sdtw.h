@@ -475,6 +475,7 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
  * out = gradient * min(1, max_norm / norm).  Squares are summed in 64 bits: no gradient is too large or too small.  The factor is rounded
  * to 24 digits, however small it is, the product to float32, and that to out_type.
  * If the norm is not finite (an element is NaN or infinite) the gradients go to `out` as they are, for the caller to see by `norm`.
+ * A norm of finite elements that is beyond float32's largest number is returned as that number; they are scaled by the norm itself.
  * Elements are taken in the order of memory: a tensor and its `out` lie there alike, without gaps.
  */
 typedef struct sdtw_gradient {

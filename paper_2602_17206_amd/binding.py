@@ -1196,7 +1196,7 @@ def sdtw_gradient_clip(grads, max_norm, out=None, norm=None, workspace=None):
     together have a 2-norm of at most ``max_norm``, in place or into the tensors ``out``: as many elements each, of any of the types.
     If the norm is not finite they stay as they are.  A tensor's elements fill its memory; one that does so in another order
     than its shape's goes with an ``out`` of its strides.  No tensor may stand in the list twice.
-    Returns the norm before, a float32 scalar on the device: nothing waits for it."""
+    Returns the norm before, a float32 scalar on the device: nothing waits for it.  It is not finite only if an element is not."""
     import torch
 
     lib = load_library()

@@ -109,6 +109,9 @@ template <> struct Piece<8> {
     typedef Bits Any __attribute__((aligned(2)));
 };
 
+// The norm as it is returned: not finite only where an element is not, so that it says whether the gradients were left as they are.
+__device__ __forceinline__ float clip_norm(double norm) { return norm < INFINITY ? (float)fmin(norm, 0x1.fffffep127) : (float)norm; }
+
 // What the gradients are multiplied by, as `by` 2^octaves: octaves is 0, but for factors below the normal numbers, which would have
 // few digits or none.
 struct ClipFactor {
@@ -183,7 +186,7 @@ __global__ __launch_bounds__(256) void clip_scale_kernel(ClipList list, ClipPara
     double sum = 0.0;
     for (int k = threadIdx.x; k < p.all_parts; k += 256) sum += p.parts[k];
     const double norm = sqrt(workgroup_sum_f64(sum, lds));
-    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+    if (p.norm && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = clip_norm(norm);
     const ClipFactor factor(norm, p.max_norm);
     clip_chunks<true>(list, [&](int tensor, int64_t at, int n) {
         if (!factor.scaled && list.out[tensor] == list.data[tensor]) return;
@@ -222,7 +225,7 @@ __global__ __launch_bounds__(1024) void clip_small_kernel(ClipList list, ClipPar
     sum = 0.0;
     for (int w = 0; w < 16; ++w) sum += sums[w];
     const double norm = sqrt(sum);
-    if (threadIdx.x == 0) *p.norm = (float)norm;
+    if (threadIdx.x == 0) *p.norm = clip_norm(norm);
     const ClipFactor factor(norm, p.max_norm);
     each([&](int tensor, int64_t at, int n) {
         if (!factor.scaled && list.out[tensor] == list.data[tensor]) return;

@@ -99,10 +99,48 @@ def test_gradients_of_any_size(size):
     check(grads, 100.0 * size)
 
 
+@pytest.mark.parametrize("sizes", [[2], [60000, 500]])
+@pytest.mark.parametrize("out", sorted(TYPES))
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e-10, 2.0 ** -100, 1e20])
+def test_norms_beyond_float32(max_norm, out, sizes):
+    """Every element is finite, their norm is above float32's largest number: that is what is returned, and they are clipped by the norm itself.
+    Where the factor is below 2^-126 it has a power of two of its own, so that it keeps its digits.  Bars as above; float16's results may
+    be beyond its largest number."""
+    grads = [(3e38 * torch.sign(t)).float() for t in some(sizes, ["f32"])]
+    want = norm_of(grads)
+    assert want > torch.finfo(torch.float32).max
+    outs = [torch.empty(g.shape, dtype=TYPES[out], device="cuda") for g in grads]
+    norm = pkg.sdtw_gradient_clip(grads, max_norm, out=outs)
+    assert float(norm) == torch.finfo(torch.float32).max
+    assert float(pkg.sdtw_gradient_norm(grads)) == torch.finfo(torch.float32).max
+    for g, o in zip(grads, outs):
+        x = g.double() * (max_norm / want)
+        bar = (2.1 * 2.0 ** -24 + 1.001 * HALF_ULP[o.dtype]) * x.abs() + LEAST[o.dtype]
+        beyond = x.abs() > torch.finfo(o.dtype).max
+        assert torch.equal(o[beyond].double(), INF * torch.sign(x[beyond]))
+        assert ((o.double() - x).abs() <= bar)[~beyond].all()
+
+
 @pytest.mark.parametrize("max_norm", [1e-9, 1e-30])
 def test_factors_below_the_normal_numbers(max_norm):
     grads = some([5000, 77], ["f32", "bf16"], size=1e32)
     check(grads, max_norm)
+
+
+@pytest.mark.parametrize("bad", [INF, -INF, NAN])
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("n", [3000, 90000])
+def test_what_is_not_finite_is_passed_on(n, kind, bad):
+    grads = some([n, 50], [kind])
+    grads[0][n // 2:n // 2 + 3] = bad
+    before = [g.clone() for g in grads]
+    outs = [torch.zeros_like(g) for g in grads]
+    norms = [pkg.sdtw_gradient_clip(grads, 1.0, out=outs), pkg.sdtw_gradient_clip(grads, 1.0)]
+    for norm in norms:
+        assert torch.isnan(norm) if bad != bad else float(norm) == INF
+    for b, g, o in zip(before, grads, outs):
+        for after in (g, o):
+            assert torch.equal(torch.isnan(after), torch.isnan(b)) and torch.equal(after[~torch.isnan(b)], b[~torch.isnan(b)])
 
 
 @pytest.mark.parametrize("bad", [INF, -INF, NAN])
