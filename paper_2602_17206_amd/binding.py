@@ -249,12 +249,14 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
-def _ptr(t, dtype=None, shape=None, name="tensor"):
+def _ptr(t, dtype=None, shape=None, name="tensor", device=None):
     """Device pointer of a contiguous CUDA tensor (None -> NULL)."""
     if t is None:
         return ctypes.c_void_p(0)
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError("%s must be a contiguous device tensor" % name)
+    if device is not None and t.device != device:
+        raise ValueError("%s must be on %s" % (name, device))
     if dtype is not None and t.dtype != dtype:
         raise ValueError("%s must have dtype %s" % (name, dtype))
     if shape is not None and tuple(t.shape) != tuple(shape):
@@ -775,6 +777,8 @@ def _operator_workspace(nbytes, workspace, device, where):
     import torch
 
     if workspace is not None:
+        if workspace.buffer.device != device:
+            raise ValueError("workspace must be on %s" % device)
         return workspace, workspace.ptr, workspace.nbytes
     if nbytes == 0:
         raise SdtwError(STATUS_INVALID_ARG, where)
@@ -1133,7 +1137,7 @@ def sdtw_attention_forward(q, k, v, table=None, scale=None, cap=0.0, causal=Fals
         lse = torch.empty(q.shape[:3], dtype=torch.float32, device=dev)
         lp = lse.data_ptr()
     else:
-        lp = _ptr(lse, torch.float32, q.shape[:3], "lse")
+        lp = _ptr(lse, torch.float32, q.shape[:3], "lse", dev)
     rc = lib.sdtw_attention_forward(desc, *args, lists, out.data_ptr(), lp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_attention_forward")
@@ -1164,9 +1168,9 @@ def sdtw_attention_backward(q, k, v, out, lse, dout, table=None, scale=None, cap
         dtable = torch.empty(table.shape, dtype=torch.float32, device=dev)
         dp = dtable.data_ptr()
     else:
-        dp = _ptr(dtable, torch.float32, table.shape, "dtable")
+        dp = _ptr(dtable, torch.float32, table.shape, "dtable", dev)
     keep, wp, wn = _operator_workspace(lib.sdtw_attention_backward_workspace_bytes(desc), workspace, dev, "sdtw_attention_backward")
-    rc = lib.sdtw_attention_backward(desc, *args, lists, out.data_ptr(), _ptr(lse, torch.float32, q.shape[:3], "lse"), dout.data_ptr(),
+    rc = lib.sdtw_attention_backward(desc, *args, lists, out.data_ptr(), _ptr(lse, torch.float32, q.shape[:3], "lse", dev), dout.data_ptr(),
                                      dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), dp, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_attention_backward")
@@ -1231,7 +1235,7 @@ def sdtw_gradient_clip(grads, max_norm, out=None, norm=None, workspace=None):
     keep, wp, wn = _operator_workspace(lib.sdtw_gradient_clip_workspace_bytes(ptr, n), workspace, dev, "sdtw_gradient_clip")
     if norm is None:
         norm = torch.empty((), dtype=torch.float32, device=dev)
-    np = _ptr(norm, torch.float32, (), "norm")
+    np = _ptr(norm, torch.float32, (), "norm", dev)
     rc = lib.sdtw_gradient_clip(ptr, n, max_norm, np, wp, wn, _stream_of(dev))
     if rc != 0:
         raise SdtwError(rc, "sdtw_gradient_clip")

@@ -184,3 +184,26 @@ def test_clip_arguments():
 def test_outputs_that_overlap_are_refused(entries):
     assert clip(entries) == INVALID
     assert clip(entries[::-1]) == INVALID
+
+
+@pytest.mark.filterwarnings("ignore::UserWarning")
+def test_tensors_on_another_device_are_refused():
+    """What a call is given beside its inputs lies on their device too.  (Tensors without memory, so that this needs no device.)"""
+    torch = pytest.importorskip("torch")
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    with FakeTensorMode():
+        make = lambda *s, at=0: torch.empty(s, device="cuda:%d" % at)  # noqa: E731
+        q, out, lse, table = make(1, 2, 3, 16), make(1, 2, 3, 16), make(1, 2, 3), make(2, 16)
+        workspace = pkg.Workspace.__new__(pkg.Workspace)
+        workspace.nbytes, workspace.buffer = 1 << 20, torch.empty(1 << 20, dtype=torch.uint8, device="cuda:1")
+        for kw in (dict(lse=make(1, 2, 3, at=1)), dict(workspace=workspace)):
+            with pytest.raises(ValueError, match="must be on cuda:0"):
+                pkg.sdtw_attention_forward(q, q, q, table, **kw)
+        for kw in (dict(lse=make(1, 2, 3, at=1)), dict(dtable=make(2, 16, at=1)), dict(workspace=workspace)):
+            a = {"lse": lse, **kw}
+            with pytest.raises(ValueError, match="must be on cuda:0"):
+                pkg.sdtw_attention_backward(q, q, q, out, a.pop("lse"), out, table, **a)
+        for kw in (dict(norm=make(at=1)), dict(workspace=workspace)):
+            with pytest.raises(ValueError, match="must be on cuda:0"):
+                pkg.sdtw_gradient_clip([make(0)], 1.0, **kw)
