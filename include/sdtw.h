@@ -452,8 +452,8 @@ size_t sdtw_attention_backward_workspace_bytes(const sdtw_attention_desc *desc);
 
 /*
  *   table [H, buckets]: device, read only; NULL exactly without buckets.  lists: host, or NULL.
- *   out [B,H,N,D], lse [B,H,N] (float32, contiguous): device, out.  They overlap no input; one that begins where an input does is
- *   refused (SDTW_ERR_INVALID_ARG).
+ *   out [B,H,N,D], lse [B,H,N] (float32, contiguous): device, out.  They overlap no input and not each other; one that begins where an
+ *   input or the other does is refused (SDTW_ERR_INVALID_ARG).
  */
 int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
                            const sdtw_attention_lists *lists, void *out, float *lse, void *workspace, size_t workspace_bytes,
@@ -463,8 +463,8 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
  * out, lse: as the forward call with the same inputs left them.
  *   dq [B,H,N,D], dk, dv [B,Hk,M,D]: device, out; they overlap no input and not each other (views of one tensor side by side do
  *   not overlap), and are refused where they begin at the same place.
- *   dtable [H, buckets]: device, float32, contiguous, out; NULL if it is not wanted (what only it needs is then left out) and
- *   without buckets.
+ *   dtable [H, buckets]: device, float32, contiguous, out, apart from dq, dk and dv; NULL if it is not wanted (what only it needs is
+ *   then left out) and without buckets.
  */
 int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, const void *k, const void *v, const void *table,
                             const sdtw_attention_lists *lists, const void *out, const float *lse, const void *dout, void *dq,

@@ -76,11 +76,13 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
         (keys && (!places_differ(desc->dk_stride, desc->B, desc->Hk, desc->M, desc->D) ||
                   !places_differ(desc->dv_stride, desc->B, desc->Hk, desc->M, desc->D))))
         return SDTW_ERR_INVALID_ARG;
-    if (!apart(dq, {q, k, v, table, out, dout, dk, dv}) || !apart(dk, {q, k, v, table, out, dout, dv}) || !apart(dv, {q, k, v, table, out, dout}))
+    if (!apart(dq, {q, k, v, table, out, lse, dout, dk, dv}) || !apart(dk, {q, k, v, table, out, lse, dout, dv}) ||
+        !apart(dv, {q, k, v, table, out, lse, dout}))
         return SDTW_ERR_INVALID_ARG;
     const BackwardPlan P = backward_plan(desc);
     if (!P.fits) return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    if (!apart(dtable, {dq, dk, dv})) return SDTW_ERR_INVALID_ARG;
     (void)hipGetLastError();
     AttentionParams p = attention_params(desc, lists);
     p.q = q; p.k = k; p.v = v; p.table = table;

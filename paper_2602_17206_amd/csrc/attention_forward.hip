@@ -84,10 +84,11 @@ int sdtw_attention_forward(const sdtw_attention_desc *desc, const void *q, const
     if (!strides_ok(desc->out_stride, desc->B, desc->H, desc->N, desc->D) ||
         !places_differ(desc->out_stride, desc->B, desc->H, desc->N, desc->D))
         return SDTW_ERR_INVALID_ARG;
-    if (!apart(out, {q, k, v, table})) return SDTW_ERR_INVALID_ARG;
+    if (!apart(out, {q, k, v, table}) || !apart(lse, {q, k, v, table})) return SDTW_ERR_INVALID_ARG;
     const ForwardPlan P = forward_plan(desc);
     if (!P.fits) return SDTW_ERR_INVALID_ARG;
     if (int rc = check_ws(workspace, workspace_bytes, P.total)) return rc;
+    if (!apart(lse, {out})) return SDTW_ERR_INVALID_ARG;
     (void)hipGetLastError();
     AttentionParams p = attention_params(desc, lists);
     p.q = q; p.k = k; p.v = v; p.table = table;

@@ -207,3 +207,13 @@ def test_tensors_on_another_device_are_refused():
         for kw in (dict(norm=make(at=1)), dict(workspace=workspace)):
             with pytest.raises(ValueError, match="must be on cuda:0"):
                 pkg.sdtw_gradient_clip([make(0)], 1.0, **kw)
+
+
+def test_statistics_in_the_place_of_inputs_and_outputs_are_refused():
+    fifth = ctypes.c_void_p(0x50000)
+    for name in ("q", "k", "v", "table"):
+        assert forward(desc(), **{name: fifth, "lse": fifth}) == INVALID, name
+    assert forward(desc(), out=fifth, lse=fifth) == INVALID
+    for out in ("dq", "dk", "dv"):
+        assert backward(desc(), **{"lse": fifth, out: fifth}) == INVALID, out
+        assert backward(desc(), **{"dtable": fifth, out: fifth}) == INVALID, out
