@@ -491,7 +491,7 @@ size_t sdtw_gradient_clip_workspace_bytes(const sdtw_gradient *gradients, int32_
 /*
  *   gradients [count]: HOST, read before the call returns.  Outputs may not overlap each other: a tensor stands in the list once.
  *   max_norm: >= 0; +inf: nothing is scaled (and nothing written where `out` is `data`).
- *   norm [1]: device, float32, out.
+ *   norm [1]: device, float32, out; in no tensor's memory.
  */
 int sdtw_gradient_clip(const sdtw_gradient *gradients, int32_t count, float max_norm, float *norm, void *workspace,
                        size_t workspace_bytes, void *stream);

@@ -34,12 +34,14 @@ bool gradients_ok(const sdtw_gradient *g, int32_t count)
 }
 
 // Whether what is written overlaps nothing else: SDTW_OK, SDTW_ERR_INVALID_ARG, or SDTW_ERR_WORKSPACE without host memory for it.
-int check_overlap(const sdtw_gradient *g, int32_t count)
+int check_overlap(const sdtw_gradient *g, int32_t count, const float *norm)
 {
     struct Span { uintptr_t begin, end; bool written; };
-    Span *span = new (std::nothrow) Span[2 * (size_t)count + 1];
+    Span *span = new (std::nothrow) Span[2 * (size_t)count + 1];  // (the tensors', and the norm's)
     if (!span) return SDTW_ERR_WORKSPACE;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(norm);
     size_t n = 0;
+    span[n++] = Span{at, at + sizeof(float), true};
     for (int32_t i = 0; i < count; ++i) {
         if (g[i].count == 0) continue;
         const uintptr_t in = reinterpret_cast<uintptr_t>(g[i].data), out = reinterpret_cast<uintptr_t>(g[i].out);
@@ -78,7 +80,7 @@ int sdtw_gradient_clip(const sdtw_gradient *gradients, int32_t count, float max_
                        size_t workspace_bytes, void *stream)
 {
     if (!gradients_ok(gradients, count) || !norm || !(max_norm >= 0.0f)) return SDTW_ERR_INVALID_ARG;
-    if (int rc = check_overlap(gradients, count)) return rc;
+    if (int rc = check_overlap(gradients, count, norm)) return rc;
     const int launches = launches_of(count), most = most_workgroups(launches);
     if (int rc = check_ws(workspace, workspace_bytes, (size_t)launches * most * sizeof(double))) return rc;
     (void)hipGetLastError();

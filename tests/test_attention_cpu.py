@@ -217,3 +217,11 @@ def test_statistics_in_the_place_of_inputs_and_outputs_are_refused():
     for out in ("dq", "dk", "dv"):
         assert backward(desc(), **{"lse": fifth, out: fifth}) == INVALID, out
         assert backward(desc(), **{"dtable": fifth, out: fifth}) == INVALID, out
+
+
+def test_a_norm_within_a_gradient_is_refused():
+    for at in (0x1000, 0x118c, 0x2000, 0x218c):
+        assert clip([(0x1000, 0x2000, 100, 0, 0)], norm=ctypes.c_void_p(at)) == INVALID, hex(at)
+        assert clip([(0x9000, 0x9000, 3, 0, 0), (0x1000, 0x2000, 100, 0, 0)], max_norm=float("inf"), norm=ctypes.c_void_p(at)) == INVALID, hex(at)
+    for at in (0x0ffc, 0x1190, 0x1ffc, 0x2190):
+        assert clip([(0x1000, 0x2000, 100, 0, 0)], norm=ctypes.c_void_p(at), ws=None) == WORKSPACE, hex(at)
