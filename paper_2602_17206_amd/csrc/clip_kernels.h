@@ -132,7 +132,9 @@ struct ClipFactor {
 
 template <typename T, typename U> __device__ __forceinline__ void clip_scale(const T *in, U *out, int n, const ClipFactor &factor, int who, int threads)
 {
-    constexpr int W = 16 / (sizeof(T) > sizeof(U) ? (int)sizeof(T) : (int)sizeof(U)), kSteps = 8;
+    // (a workgroup's whole chunk at once: 8 steps, or 4 between 16-bit types)
+    constexpr int W = 16 / (sizeof(T) > sizeof(U) ? (int)sizeof(T) : (int)sizeof(U)), kSteps = kClipChunk / 256 / W;
+    static_assert(kSteps * 256 * W == kClipChunk, "a chunk is dealt out evenly");
     typedef Piece<W * (int)sizeof(T)> In;
     typedef Piece<W * (int)sizeof(U)> Out;
     auto load = [&](int i) { return *reinterpret_cast<const typename In::Any *>(in + i); };
