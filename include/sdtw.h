@@ -425,7 +425,7 @@ typedef struct sdtw_attention_desc {
     int32_t two_sided;
     int32_t causal;              /* 0 or 1 */
     float scale;                 /* from 2^-26 to 2^26 */
-    float cap;                   /* 0: none; else > 0, finite, and scale / cap finite */
+    float cap;                   /* 0: none; else from 2^-126 to 2^127, and scale / cap from 2^-126 on and finite */
     uint32_t flags;              /* 0 */
     int64_t offset;              /* offset_b of every sequence, |offset| < 2^62; not used with `offsets` */
     int64_t prefix;              /* prefix_b of every sequence; 0 unless causal; not used with `prefixes` */

@@ -71,7 +71,9 @@ inline int attention_check(const sdtw_attention_desc *d, BucketRule *rule)
     if (heads > 0x7fffffff || key_heads > 0x7fffffff || heads * d->N > most || key_heads * d->M > most) return SDTW_ERR_INVALID_ARG;
     if (!attention_type_ok(d->type) || d->flags != 0 || (d->causal != 0 && d->causal != 1)) return SDTW_ERR_INVALID_ARG;
     if (!(d->scale >= 0x1p-26f && d->scale <= 0x1p26f)) return SDTW_ERR_INVALID_ARG;
-    if (!(d->cap >= 0.0f) || !std::isfinite(d->cap * kLog2e) || (d->cap > 0.0f && !std::isfinite(d->scale / d->cap))) return SDTW_ERR_INVALID_ARG;
+    // (the kernels multiply by the cap, by 1 over it and by the scale over it: numbers below the normal ones would have few digits or none)
+    if (!(d->cap >= 0.0f) || !std::isfinite(d->cap * kLog2e)) return SDTW_ERR_INVALID_ARG;
+    if (d->cap != 0.0f && !(std::isnormal(d->cap) && std::isnormal(d->scale / d->cap))) return SDTW_ERR_INVALID_ARG;
     if (d->offset >= (int64_t)1 << 62 || d->offset <= -((int64_t)1 << 62)) return SDTW_ERR_INVALID_ARG;
     if (d->prefix < 0 || (d->prefix > 0 && !d->causal)) return SDTW_ERR_INVALID_ARG;
     if (!strides_ok(d->q_stride, d->B, d->H, d->N, d->D) || !strides_ok(d->k_stride, d->B, d->Hk, d->M, d->D) ||

@@ -225,3 +225,14 @@ def test_a_norm_within_a_gradient_is_refused():
         assert clip([(0x9000, 0x9000, 3, 0, 0), (0x1000, 0x2000, 100, 0, 0)], max_norm=float("inf"), norm=ctypes.c_void_p(at)) == INVALID, hex(at)
     for at in (0x0ffc, 0x1190, 0x1ffc, 0x2190):
         assert clip([(0x1000, 0x2000, 100, 0, 0)], norm=ctypes.c_void_p(at), ws=None) == WORKSPACE, hex(at)
+
+
+@pytest.mark.parametrize("scale,cap,fine", [
+    (2.0 ** -26, 2e38, False), (0.25, 2e38, False), (0.25, 2.0 ** 124, True), (0.25, 2.0 ** 125, False), (2.0 ** 26, 2.0 ** 127, True), (2.0 ** -26, 1e-40, False),
+    (2.0 ** -26, 2.0 ** -126, True), (0.25, 2.0 ** -126, True), (2.0, 2.0 ** -126, True), (4.0, 2.0 ** -126, False),
+])
+def test_caps_that_float32_cannot_divide_by_or_into(scale, cap, fine):
+    # scale / cap would be a subnormal number or 0 (scores lose their digits, or are all 0), or 1 / cap infinite (gradients NaN)
+    d = desc(scale=scale, cap=cap)
+    assert (sizes(d)[0] > 0) == (sizes(d)[1] > 0) == fine
+    assert forward(d, ws=None) == backward(d, ws=None) == (WORKSPACE if fine else INVALID)

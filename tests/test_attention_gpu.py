@@ -235,6 +235,13 @@ def test_flat_and_decided_rows(kind, size):
     check(2, 3, 1, 150, 333, 64, kind, size=size, cap=20.0)
 
 
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("cap", [2.0 ** 124, 2.0 ** 60, 2.0 ** -60, 2.0 ** -126])
+@pytest.mark.parametrize("N,M", [(3, 300), (1100, 130)])
+def test_the_largest_and_smallest_caps(N, M, cap, kind):
+    check(1, 32, 32, N, M, 32, kind, cap=cap, scale=0.25)
+
+
 # ---------------------------------------------------------------- bias
 
 @pytest.mark.parametrize("kind", sorted(TYPES))
