@@ -9,9 +9,12 @@
 //   keys   wavefronts own keys and walk over the queries of all heads of the group: dk, dv
 // The products are made twice, which is 14 D operations a cell for the formula's 10 (18 D with delta's walk); one kernel that made them once
 // would have to add dq up in memory, by atomics or by 32-bit parts of all keys.
-// What bounds them: matrix cores and vector units in turn, at two wavefronts a SIMD, which is what registers leave.  4 x 16 x 2048 x 2048 x 64
-// bfloat16 causal with bias and its table: delta 57 us, rows 143, keys 130; 2 x 16 heads in groups of 4, 4096 x 4096 x 128 causal with
-// prefixes: rows 353 (matrix cores busy 55 % of the time), keys 404 (45 %), their parts added up 24.
+// What bounds them: matrix cores and vector units in turn, at two wavefronts a SIMD, which is what registers leave, and in the keys' kernel
+// the wait for tiles: the rows' lse and delta are read behind a tile's copies, and so waited for with them.  4 x 16 x 2048 x 2048 x 64
+// bfloat16 causal with bias and its table: delta 58 us, rows 141 to 152, keys 120 to 128; 2 x 16 heads in groups of 4, 4096 x 4096 x 128
+// causal with prefixes: rows 315 to 361 (matrix cores busy 55 % of the time), keys 348 to 421 (44 %), their parts added up 25.
+// In float32 the kernels for rows and keys stand at one wavefront a SIMD: the first of these 352, 641 and 759 us, 49 of a library
+// product's 153 TFLOP/s.
 #pragma once
 #include "attention_tiles.h"
 
@@ -119,7 +122,8 @@ template <typename T, int DP, bool MORE> constexpr int kBackwardWaves = sizeof(T
 //
 // 4 wavefronts of 32 rows each, one head of one sequence.  delta comes from the rows' outputs - sum_j p dp = <dout, out> - unless the table's
 // gradient is wanted: that is kept in 32 bits, and its sums over whole diagonals would show the rounding of a 16-bit `out`; then, and for
-// 16-bit gradients over few keys, the keys are walked over once more beforehand, for delta alone.
+// 16-bit gradients over few keys, the keys are walked over once more beforehand, for delta alone.  (So is float32, whose `out` is not rounded:
+// its table's gradient from <dout, out> has not been held against 64 bits.)
 enum { kRowsPlain, kRowsDelta, kRowsTable, kRowsGiven };
 template <typename T, int DP, int F, int WORK>
 __global__ __launch_bounds__(256, (WORK == kRowsDelta ? kDeltaWaves<T, DP> : kBackwardWaves<T, DP, false>)) void attention_rows_gradient_kernel(AttentionParams p, BucketRule rule)

@@ -32,6 +32,10 @@ ForwardPlan split_forward(const sdtw_attention_desc *d)
     //   64 rows of 16 x 16 heads, 8192 keys: 141 and 207; 128 rows: 228 and 198   4 x 1000 x 1000: 21 and 21 (29 and 78); 256: 116 and 59
     //   32 x 512 x 512: 14 and 14 (31 and 44)   32 x 256 x 256: 11 and 10 (15 and 25)   256 x 192 x 192: 23 and 12 (50 and 33)
     //   4 x 64 x 64: 10 and 8 (13 and 11)   8 x 4 groups of 8 heads, 32 rows, 8192 keys: 55 and 147
+    // ... at D 128, and just below the 1024 wavefronts:
+    //   64 rows of 16 x 16 heads, 8192 keys: 236 and 327 (739 and 1276)   8 heads, 512 x 8192: 50 and 219 (192 and 1179)
+    //   4 x 16 heads, 480 x 4096: 129 and 131 (683 and 640); D 64: 77 and 85 (323 and 333)   480 x 480 causal: 37 and 21 (102 and 82)
+    //   16 heads, 1984 x 1984 causal: 65 and 56 (238 and 293); D 64: 33 and 38 (129 and 150)   1000 x 1000 causal: 27 and 32 (92 and 148)
     const int64_t waves = (int64_t)d->B * d->H * ((d->N + 31) / 32);
     P.few = (d->N * G <= 64 || waves < 1024) && d->M > (d->type == SDTW_TYPE_F32 ? 64 : 256) && few_rows_lds(d) + 4096 <= kLdsBytes;
     if (!P.few) {

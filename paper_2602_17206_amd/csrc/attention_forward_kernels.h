@@ -5,10 +5,12 @@
 // in one pass over the keys: a running reference m, total l and unfinished sum o per row; with exponents in octaves
 //   m' = max(m, max_j s),  l' = l 2^(m - m') + sum_j 2^(s_j - m'),  o' = o 2^(m - m') + sum_j 2^(s_j - m') v_j.
 // Scores and their exponentials never leave registers: 32 rows stand in a wavefront's columns, 64 keys at a time come through LDS, copied
-// there directly, one tile while the other is worked on.
-// What bounds it: the vector units, which take 32 exponents, maxima, sums and conversions a lane for each tile, at D = 64 (4 x 16 x 2048 x 2048
-// bfloat16 causal with bias 54 us, 638 TFLOP/s with the skipped half not counted; without mask and bias 92 us, 733 TFLOP/s); they and the
-// matrix cores alike at D = 128 (160 us, 859 TFLOP/s, where a large library product reaches 1243).
+// there directly; the next tile is asked for before this one is worked on, and waited for before its first product (see copies_done).
+// What bounds it: at D = 64 the vector units, which take 32 exponents, maxima, sums and conversions a lane for each tile and are busy 77 % of the
+// time (4 x 16 x 2048 x 2048 bfloat16 causal with bias 55 to 60 us, 573 to 625 TFLOP/s with the skipped half not counted; without mask and bias 89
+// us, 775 TFLOP/s); at D = 128 they and the matrix cores in turn, and the wait for tiles (152 us, 902 TFLOP/s, where a large library product
+// reaches 1250; capped, with documents, vector units 51 % and matrix cores 21 %).  float32: the matrix cores (332 us at D = 64, 104
+// TFLOP/s of a library product's 153).
 // Tried: no maximum taken within a tile (77 us for 62 then: scalar registers spilled); three wavefronts a SIMD instead of four (slower).
 #pragma once
 #include "attention_tiles.h"
@@ -219,8 +221,9 @@ template <typename T, int DP> constexpr int few_rows_bytes()
 // A few rows against many keys.  The rows of a group of heads that share their keys stand in one wavefront's columns together: row t is
 // query t / G of head t % G of the group.  Each of 4 wavefronts takes every fourth 32 keys of the workgroup's share, on its own; then
 // they are joined in LDS, and the workgroups of a row by attention_join_kernel.
-// What bounds it: reading the keys and values.  32 x 16 heads in groups of 4, one row each, 4097 keys of 128 bfloat16: 165 MB in 34 us, 4.9 TB/s,
-// where a copy of 1 GiB reaches 5.1 both ways; 131072 float16 keys, 4 capped rows: 202 MB in 45 us, half of it the capping's vector work.
+// What bounds it: reading the keys and values.  32 x 16 heads in groups of 4, one row each, 4097 keys of 128 bfloat16: 165 MB in 33 us, 4.9 TB/s,
+// where a copy of 1 GiB reaches 5.1 both ways; in float32 336 MB in 129, 2.6 TB/s, at one wavefront a SIMD.  131072 float16 keys, 4 rows: 268 MB
+// in 54 us capped and 52 as they are.
 template <typename T, int DP, int F>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_rows_kernel(AttentionParams p, BucketRule rule)
 {
@@ -264,8 +267,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void attention_few_row
     Stage<T, DP, 32, 64> ks, vs;
     ks.begin(rows_of<T>(p.k, p.k_stride, b, hk), p.loaded, lane);
     vs.begin(rows_of<T>(p.v, p.v_stride, b, hk), p.loaded, lane);
-    // The next keys are asked for as soon as the products with these are done, the next values likewise: half of a wavefront's share of LDS
-    // is always on its way.
+    // The next keys are asked for as soon as the products with these are done, the next values likewise.  (Before the first product with keys
+    // all that was asked for is waited for, see copies_done: from there to the next request nothing is on its way.)
     auto fetch_keys = [&](int t) { if (t < end && t * 128 + wave * 32 < to) ks.copy(ktile, t * 128 + wave * 32, to, lane); };
     auto fetch_values = [&](int t) { if (t < end && t * 128 + wave * 32 < to) vs.copy(vtile, t * 128 + wave * 32, to, lane); };
     fetch_keys(begin);

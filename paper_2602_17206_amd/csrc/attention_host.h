@@ -177,7 +177,7 @@ inline int near_diagonals(const sdtw_attention_desc *d, const BucketRule &rule)
 // Calls f with a value of the element type and, as a type, the features rounded up to 32, 64, 96 or 128.
 template <int DP> struct Features { static constexpr int value = DP; };
 template <int F> struct Variant { static constexpr int value = F; };
-// ... and what the kernel has to be compiled for.
+// ... and what the kernel has to be compiled for.  (A cap and documents are one variant: either pays for the other's tests.)
 template <typename F> void with_variant(const sdtw_attention_desc *d, const sdtw_attention_lists *lists, F f)
 {
     const bool more = d->cap > 0.0f || (lists && lists->row_document);

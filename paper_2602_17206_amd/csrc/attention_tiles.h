@@ -103,7 +103,9 @@ __device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint32_
                  : "memory", "m0");
 }
 #pragma clang diagnostic pop
-// All that the wavefront asked for is there, and what it read from LDS has left it.
+// All that the wavefront asked for is there, and what it read from LDS has left it.  (The compiler does not reckon with this wait: what it
+// loaded itself before a loop - a column's features - it waits for inside once more, before the first product.  Memory answers in order, so
+// that the copies asked for in between are waited for as well: the next tile is on its way during what comes before that product only.)
 __device__ __forceinline__ void copies_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); }
 
 // All but the last N copies that the wavefront asked for are there.
@@ -204,7 +206,8 @@ template <typename T, int DP> __device__ __forceinline__ Acc along_features(cons
     return acc;
 }
 
-// P [32 rows][column] as the matrix cores take it: rounded to T, except for float32
+// P [32 rows][column] as the matrix cores take it: rounded to T, except for float32.  Numbers of more digits would be two products for one, as
+// in along_rows_twice; rounded once, they put out, dv and dk 1.1 to 1.45 times as far from 64 bits as the result's own rounding does.
 template <typename T> struct Weights {
     Bits4 v[2];
     __device__ __forceinline__ explicit Weights(const Acc &p)
