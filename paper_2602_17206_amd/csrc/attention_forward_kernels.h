@@ -7,7 +7,7 @@
 // Scores and their exponentials never leave registers: 32 rows stand in a wavefront's columns, 64 keys at a time come through LDS, copied
 // there directly; the next tile is asked for before this one is worked on, and waited for before its first product (see copies_done).
 // What bounds it: at D = 64 the vector units, which take 32 exponents, maxima, sums and conversions a lane for each tile and are busy 77 % of the
-// time (4 x 16 x 2048 x 2048 bfloat16 causal with bias 55 to 60 us, 573 to 625 TFLOP/s with the skipped half not counted; without mask and bias 89
+// time (4 x 16 x 2048 x 2048 bfloat16 causal with bias 54 to 60 us, 573 to 638 TFLOP/s with the skipped half not counted; without mask and bias 89
 // us, 775 TFLOP/s); at D = 128 they and the matrix cores in turn, and the wait for tiles (152 us, 902 TFLOP/s, where a large library product
 // reaches 1250; capped, with documents, vector units 51 % and matrix cores 21 %).  float32: the matrix cores (332 us at D = 64, 104
 // TFLOP/s of a library product's 153).
