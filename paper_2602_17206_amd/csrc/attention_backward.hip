@@ -12,6 +12,10 @@ struct BackwardPlan {
     size_t off_table, off_keys, off_packed, total;
 };
 
+// delta from the rounded outputs is good enough where they are averages over many keys.  Over few of them - a row of one key has no gradient
+// at all - it is not: float16 gradients of 68 rows and keys were twice as far from 64 bits as those of a chain in 32 bits.
+bool few_keys(const sdtw_attention_desc *d) { return d->type != SDTW_TYPE_F32 && d->M <= 512; }
+
 BackwardPlan backward_plan(const sdtw_attention_desc *d)
 {
     BackwardPlan P{};
@@ -38,7 +42,8 @@ BackwardPlan backward_plan(const sdtw_attention_desc *d)
     P.off_packed = P.off_keys + (P.parts > 1 ? align_up((size_t)P.parts * 2 * d->B * d->Hk * d->M * d->D * sizeof(float), 256) : 0);
     if (P.parts > 1) P.fits = attention_grid_ok(((int64_t)2 * d->B * d->Hk * d->M * d->D + 255) / 256);
     P.total = P.off_packed;
-    for (const auto *stride : {&d->q_stride, &d->out_stride, &d->dout_stride}) P.total += packed_bytes(d, *stride, d->H, d->N);
+    for (const auto *stride : {&d->q_stride, &d->dout_stride}) P.total += packed_bytes(d, *stride, d->H, d->N);
+    if (!few_keys(d)) P.total += packed_bytes(d, d->out_stride, d->H, d->N);
     for (const auto *stride : {&d->k_stride, &d->v_stride}) P.total += packed_bytes(d, *stride, d->Hk, d->M);
     P.total = std::max<size_t>(256, P.total);
     return P;
@@ -101,20 +106,18 @@ int sdtw_attention_backward(const sdtw_attention_desc *desc, const void *q, cons
     hipStream_t st = static_cast<hipStream_t>(stream);
     char *room = static_cast<char *>(workspace) + P.off_packed;
     const void *packed_out = p.out;
+    p.close = few_keys(desc);
+    const bool close_delta = dtable || p.close;  // (nothing reads the outputs then)
     if (rows) {
         pack(desc, p.q, p.q_stride, desc->H, desc->N, room, st);
         pack(desc, p.dout, p.dout_stride, desc->H, desc->N, room, st);
-        if (!dtable) pack(desc, packed_out, p.out_stride, desc->H, desc->N, room, st);
+        if (!close_delta) pack(desc, packed_out, p.out_stride, desc->H, desc->N, room, st);
     }
     p.out = const_cast<void *>(packed_out);
     if (keys) {
         pack(desc, p.k, p.k_stride, desc->Hk, desc->M, room, st);
         pack(desc, p.v, p.v_stride, desc->Hk, desc->M, room, st);
     }
-    // delta from the rounded outputs is good enough where they are averages over many keys.  Over few of them - a row of one key has no gradient
-    // at all - it is not: float16 gradients of 68 rows and keys were twice as far from 64 bits as those of a chain in 32 bits.
-    p.close = desc->type != SDTW_TYPE_F32 && desc->M <= 512;
-    const bool close_delta = dtable || p.close;
     with_shape(desc->type, desc->D, [&](auto t, auto features) {
         using T = decltype(t);
         constexpr int DP = decltype(features)::value;

@@ -236,3 +236,13 @@ def test_caps_that_float32_cannot_divide_by_or_into(scale, cap, fine):
     d = desc(scale=scale, cap=cap)
     assert (sizes(d)[0] > 0) == (sizes(d)[1] > 0) == fine
     assert forward(d, ws=None) == backward(d, ws=None) == (WORKSPACE if fine else INVALID)
+
+
+@pytest.mark.parametrize("kind,M,read", [(0, 300, True), (1, 300, False), (2, 512, False), (1, 513, True)])
+def test_workspaces_hold_no_copy_that_nothing_reads(kind, M, read):
+    # outputs whose rows are far apart are packed where delta comes from them; 16-bit gradients over few keys take it from the keys
+    B, H, N, D = 2, 4, 64, 24
+    rows, keys = (N * H * D, N * D, D, 1), (M * 2 * D, M * D, D, 1)
+    near, far = (sizes(desc(N=N, M=M, D=D, type=kind, buckets=0, q_stride=rows, dout_stride=rows, dq_stride=rows, k_stride=keys, v_stride=keys, dk_stride=keys,
+                            dv_stride=keys, out_stride=out))[1] for out in (rows, (N * H << 22, N << 22, 1 << 22, 1)))
+    assert far - near == (B * H * N * D * (4 if kind == 0 else 2) if read else 0)

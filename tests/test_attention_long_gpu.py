@@ -78,3 +78,13 @@ def test_references_that_rise(size, kind):
 @pytest.mark.parametrize("kind", sorted(TYPES))
 def test_a_training_step_of_2048_positions(kind):
     long_check(1, 16, 16, 2048, 2048, 64, kind, causal=True, table=some_table(16, 32), two_sided=False)
+
+
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("M", [300, 600])
+def test_outputs_are_packed_where_they_are_read(M, kind):
+    (q, k, v, dout), _ = problem(2, 4, 2, 70, M, 21, kind)
+    out, lse = pkg.sdtw_attention_forward(q, k, v)
+    few = M <= 512 and kind != "f32"
+    assert kernels_of(lambda: pkg.sdtw_attention_backward(q, k, v, out, lse, dout)).count("attention_pack") == (4 if few else 5)
+    check(2, 4, 2, 70, M, 21, kind)
